@@ -357,6 +357,122 @@ art_status art_build_block_list_padded(const art_decode_shape* shape, const art_
                                        int32_t* block_list_len, double* block_scores,
                                        void* workspace, size_t workspace_bytes, hipStream_t stream);
 
+/*
+ * A cache held in 8 bits.  The K and V pools hold one byte a value, laid out
+ * like the bf16 pools (page, head and token strides, now in bytes), and a
+ * fp32 scale belongs to every run of `scale_tokens` slots of a page and KV
+ * head: a token's values are code * scale.  art_quant_append writes such a
+ * cache, art_quant_read brings tokens back as rows, and
+ * art_decode_attention_quant attends to it.
+ *
+ *   ART_QUANT_E4M3  codes are 8-bit floats of 4 exponent and 3 mantissa bits
+ *                   (largest 448, no infinities, NaN 0x7f and 0xff)
+ *   ART_QUANT_INT8  codes are two's complement integers; art_quant_append
+ *                   writes -127..127
+ *
+ * The scale of slot `s` of page `p` of KV head `h` is
+ * k_scale[p*k_scale_stride_page + h*k_scale_stride_head + s/scale_tokens], and
+ * the same for V.  scale_tokens is a power of two of at least 16 and at most
+ * page_size (at most 256 for art_quant_append).  Scale strides are in floats
+ * (>= 0).  The pools' own strides (art_decode_shape) are multiples of 16 bytes,
+ * their token strides less than 16 MiB, and the pools 16-byte aligned.
+ * Anything else returns ART_ERR_UNSUPPORTED.
+ */
+typedef enum { ART_QUANT_E4M3 = 0, ART_QUANT_INT8 = 1 } art_quant_format;
+typedef enum { ART_ROWS_BF16 = 0, ART_ROWS_F16 = 1, ART_ROWS_F32 = 2 } art_rows_dtype;
+
+typedef struct {
+    int32_t format;                /* art_quant_format */
+    int32_t scale_tokens;          /* slots that share a scale */
+    int64_t k_scale_stride_page, k_scale_stride_head;
+    int64_t v_scale_stride_page, v_scale_stride_head;
+} art_quant_cache;
+
+/*
+ * art_decode_attention over a cache held in 8 bits: the definition at the top
+ * of this header with k = code * k_scale and v = code * v_scale.  Scales are
+ * any finite fp32 values (art_quant_append writes powers of two).  All
+ * options, the workspace (art_decode_workspace_bytes of the same shape and
+ * options), lists, outputs and restrictions are those of
+ * art_decode_attention.  k_cache and v_cache are the code pools.  Codes and
+ * scales of slots past a sequence's length are never used.
+ */
+art_status art_decode_attention_quant(const art_decode_shape* shape, const art_decode_opts* opts,
+                                      const art_quant_cache* cache,
+                                      const void* q, const void* k_cache, const void* v_cache,
+                                      const float* k_scale, const float* v_scale,
+                                      const int32_t* page_table, const int32_t* seq_lens,
+                                      const int32_t* block_list, const int32_t* block_list_len,
+                                      void* out, float* lse, int32_t* stop_block,
+                                      void* workspace, size_t workspace_bytes,
+                                      hipStream_t stream);
+
+/*
+ * Rows.  art_quant_append takes, and art_quant_read gives, K and V of the
+ * tokens of several sequences as packed rows [rows][num_kv_heads][128] of
+ * rows_dtype: rows row_offsets[b] .. row_offsets[b+1]-1 belong to sequence b,
+ * in order, and are its tokens positions[b], positions[b]+1, ...
+ *   row_offsets  int32 [batch + 1], non-decreasing, in 0 .. rows; NULL when
+ *                every sequence has rows / batch of them (rows is then a
+ *                multiple of batch).
+ *   positions    int32 [batch]; NULL for all zeros.
+ * Rows outside row_offsets[0] .. row_offsets[batch]-1 belong to no sequence;
+ * rows of a sequence with a negative position, of tokens at or past
+ * max_pages_per_seq * page_size, and of tokens whose page id is not in
+ * 0 .. num_pages-1 are passed over.  (All of this is checked on the device:
+ * no malformed index makes a call read or write outside the arrays.  A
+ * negative position marks an unused row of a padded batch.)
+ *
+ * Row and head strides are in elements of rows_dtype, multiples of 16 bytes
+ * (>= 0), and the arrays 16-byte aligned; head_dim is contiguous; rows is less
+ * than 2^24.
+ *
+ * Shape fields used: batch, num_kv_heads, head_dim (128), page_size,
+ * num_pages, max_pages_per_seq and the K and V strides.  No workspace; calls
+ * are asynchronous on `stream`, keep nothing, and may be captured in a HIP
+ * graph and replayed.
+ */
+typedef struct {
+    int32_t rows_dtype;            /* art_rows_dtype */
+    int32_t rows;
+    int64_t k_stride_row, k_stride_head, v_stride_row, v_stride_head;
+} art_quant_rows;
+
+/*
+ * Quantise rows into the cache.  For every run of scale_tokens slots that
+ * gets a row (per sequence, KV head, and K and V apart):
+ *   a     = the largest finite magnitude of its new rows
+ *   need  = the smallest 2^e, e >= -120, with a <= 448 * 2^e (127 for int8)
+ *   scale = need, if the run begins at or after positions[b]; otherwise, as
+ *           it holds older tokens, max(its scale, need)
+ *   new codes: x / scale rounded to the nearest code, ties to even; infinities
+ *           become the largest code of their sign, NaN stays NaN (e4m3) or
+ *           becomes 0 (int8)
+ *   old codes of the run, where its scale grew: code * (old scale / scale),
+ *           rounded the same way
+ * A scale that is a power of two costs e4m3 codes nothing but their smallest
+ * values and int8 codes less than one bit, and when a run's scale grows its
+ * old codes lose nothing (e4m3) or half a step of the new scale (int8).  Results depend on no
+ * order of execution.  Slots that no row or old token of a touched run occupies
+ * keep their bytes.  Tokens that two sequences share must not lie in a run
+ * that either of them appends to, and no run may get rows twice in a call
+ * (positions that overlap): the result for such input is unspecified.
+ */
+art_status art_quant_append(const art_decode_shape* shape, const art_quant_cache* cache,
+                            const art_quant_rows* rows, const void* k_rows, const void* v_rows,
+                            const int32_t* row_offsets, const int32_t* positions,
+                            const int32_t* page_table, void* k_cache, void* v_cache,
+                            float* k_scale, float* v_scale, hipStream_t stream);
+
+/* The rows' values, code * scale rounded once to rows_dtype, ties to even.
+ * Rows that are passed over keep their bytes. */
+art_status art_quant_read(const art_decode_shape* shape, const art_quant_cache* cache,
+                          const art_quant_rows* rows, const void* k_cache, const void* v_cache,
+                          const float* k_scale, const float* v_scale,
+                          const int32_t* row_offsets, const int32_t* positions,
+                          const int32_t* page_table, void* k_rows, void* v_rows,
+                          hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

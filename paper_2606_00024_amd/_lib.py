@@ -26,13 +26,20 @@ OUT_BF16 = 1
 EXPORTS = ("art_abi_version", "art_status_str", "art_decode_workspace_bytes",
            "art_workspace_init", "art_decode_attention", "art_validate_inputs",
            "art_workspace_status", "art_block_list_workspace_bytes", "art_build_block_list",
-           "art_decode_attention_static", "art_build_block_list_padded")
+           "art_decode_attention_static", "art_build_block_list_padded",
+           "art_decode_attention_quant", "art_quant_append", "art_quant_read")
 STATIC_SCRATCH_BYTES = 64 << 20   # ART_STATIC_SCRATCH_BYTES
 
 LIST_IMPORTANCE = 0
 LIST_STREAMING = 1
 SCORE_KEY_NORM = 0
 SCORE_QUERY_BOUND = 1
+
+QUANT_E4M3 = 0
+QUANT_INT8 = 1
+ROWS_BF16 = 0
+ROWS_F16 = 1
+ROWS_F32 = 2
 
 
 class DecodeShape(ctypes.Structure):
@@ -61,6 +68,20 @@ class DecodeOpts(ctypes.Structure):
 class ListOpts(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in (
         "policy", "score_kind", "budget", "sink_blocks", "keep_last")]
+
+
+class QuantCacheSpec(ctypes.Structure):
+    """art_quant_cache"""
+    _fields_ = [("format", ctypes.c_int32), ("scale_tokens", ctypes.c_int32)] + [
+        (n, ctypes.c_int64) for n in ("k_scale_stride_page", "k_scale_stride_head",
+                                      "v_scale_stride_page", "v_scale_stride_head")]
+
+
+class QuantRows(ctypes.Structure):
+    """art_quant_rows"""
+    _fields_ = [("rows_dtype", ctypes.c_int32), ("rows", ctypes.c_int32)] + [
+        (n, ctypes.c_int64) for n in ("k_stride_row", "k_stride_head", "v_stride_row",
+                                      "v_stride_head")]
 
 
 class ArtError(RuntimeError):
@@ -124,6 +145,16 @@ def load_variant(path: str) -> ctypes.CDLL:
         build.restype = ctypes.c_int
         build.argtypes = [ctypes.POINTER(DecodeShape), ctypes.POINTER(ListOpts), vp, vp, vp, vp, vp,
                           vp, vp, vp, ctypes.c_size_t, vp]
+    quant = getattr(lib, "art_decode_attention_quant", None)
+    if quant is not None:   # (as above: earlier builds lack the calls on 8-bit caches)
+        spec = ctypes.POINTER(QuantCacheSpec)
+        quant.restype = ctypes.c_int
+        quant.argtypes = [ctypes.POINTER(DecodeShape), ctypes.POINTER(DecodeOpts), spec,
+                          vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+        for call in (lib.art_quant_append, lib.art_quant_read):
+            call.restype = ctypes.c_int
+            call.argtypes = [ctypes.POINTER(DecodeShape), spec, ctypes.POINTER(QuantRows),
+                             vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
     got = int(lib.art_abi_version())
     if got != ABI_VERSION:
         raise RuntimeError(f"{path} has ABI version {got}, this binding needs "
@@ -189,6 +220,33 @@ def decode_attention_static(shape, opts, q, k, v, page_table, seq_lens, block_li
     return int(load().art_decode_attention_static(
         ctypes.byref(shape), ctypes.byref(opts), q, k, v, page_table, seq_lens,
         block_list or None, block_list_len or None, out, lse, stop_block, stream or None))
+
+
+def decode_attention_quant(shape, opts, cache, q, k, v, k_scale, v_scale, page_table, seq_lens,
+                           block_list, block_list_len, out, lse, stop_block, workspace,
+                           workspace_bytes, stream) -> int:
+    """Raw call over an 8-bit cache; pointers are ints (0 for NULL).  Returns
+    the status."""
+    return int(load().art_decode_attention_quant(
+        ctypes.byref(shape), ctypes.byref(opts), ctypes.byref(cache), q, k, v, k_scale, v_scale,
+        page_table, seq_lens, block_list or None, block_list_len or None, out, lse, stop_block,
+        workspace or None, workspace_bytes, stream or None))
+
+
+def quant_append(shape, cache, rows, k_rows, v_rows, row_offsets, positions, page_table, k, v,
+                 k_scale, v_scale, stream) -> int:
+    """Raw call; pointers are ints (0 for NULL).  Returns the status."""
+    return int(load().art_quant_append(
+        ctypes.byref(shape), ctypes.byref(cache), ctypes.byref(rows), k_rows, v_rows,
+        row_offsets or None, positions or None, page_table, k, v, k_scale, v_scale, stream or None))
+
+
+def quant_read(shape, cache, rows, k, v, k_scale, v_scale, row_offsets, positions, page_table,
+               k_rows, v_rows, stream) -> int:
+    """Raw call; pointers are ints (0 for NULL).  Returns the status."""
+    return int(load().art_quant_read(
+        ctypes.byref(shape), ctypes.byref(cache), ctypes.byref(rows), k, v, k_scale, v_scale,
+        row_offsets or None, positions or None, page_table, k_rows, v_rows, stream or None))
 
 
 def validate_inputs(shape, opts, page_table, seq_lens, block_list, block_list_len, stream):

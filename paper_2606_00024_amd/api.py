@@ -8,7 +8,7 @@ from __future__ import annotations
 
 import math
 import threading
-from typing import Optional
+from typing import NamedTuple, Optional
 
 import torch
 
@@ -244,3 +244,230 @@ def build_block_list(q: torch.Tensor, k_cache: torch.Tensor, page_table: torch.T
     if st != _lib.OK:
         raise ArtError(st, "art_build_block_list")
     return (bl, bll, scores) if return_scores else (bl, bll)
+
+
+# ---- a cache held in 8 bits -----------------------------------------------------
+
+_QUANT_FORMATS = {torch.float8_e4m3fn: _lib.QUANT_E4M3, torch.int8: _lib.QUANT_INT8}
+_ROWS_TYPES = {torch.bfloat16: _lib.ROWS_BF16, torch.float16: _lib.ROWS_F16,
+               torch.float32: _lib.ROWS_F32}
+
+
+class QuantCache(NamedTuple):
+    """A paged K/V cache of 8-bit codes: ``k`` and ``v`` [P][Hkv][Ps][D],
+    float8_e4m3fn or int8 (any strides with a unit head-dim stride), and a fp32
+    scale for every run of slots, ``k_scale`` and ``v_scale`` [P][Hkv][Ps / run]
+    (unit stride of the last dimension).  A token's values are code * scale.
+    """
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: torch.Tensor
+    v_scale: torch.Tensor
+
+    @property
+    def scale_tokens(self) -> int:
+        """Slots that share a scale."""
+        return self.k.shape[2] // max(1, self.k_scale.shape[2])
+
+
+def new_quant_cache(num_pages: int, num_kv_heads: int, page_size: int, *,
+                    dtype=torch.float8_e4m3fn, scale_tokens: Optional[int] = None,
+                    head_dim: int = 128, device="cuda") -> QuantCache:
+    """An empty 8-bit cache (codes and scales zero) with a scale for every
+    ``scale_tokens`` slots (default: the whole page, at most 64)."""
+    if dtype not in _QUANT_FORMATS:
+        raise ValueError("dtype must be float8_e4m3fn or int8")
+    run = min(page_size, 64) if scale_tokens is None else int(scale_tokens)
+    if run < 1 or page_size % run:
+        raise ValueError("scale_tokens must divide page_size")
+    pool = lambda: torch.zeros((num_pages, num_kv_heads, page_size, head_dim),  # noqa: E731
+                               dtype=torch.uint8, device=device).view(dtype)
+    scale = lambda: torch.zeros((num_pages, num_kv_heads, page_size // run),  # noqa: E731
+                                dtype=torch.float32, device=device)
+    return QuantCache(pool(), pool(), scale(), scale())
+
+
+def _quant_spec(cache: QuantCache) -> _lib.QuantCacheSpec:
+    k, v, ks, vs = cache
+    fmt = _QUANT_FORMATS.get(k.dtype)
+    if fmt is None or v.dtype != k.dtype:
+        raise ValueError("the cache must be float8_e4m3fn or int8")
+    for t, name in ((k, "k"), (v, "v")):
+        _require_cuda(t, name)
+    for t, name in ((ks, "k_scale"), (vs, "v_scale")):
+        _require_cuda(t, name, torch.float32)
+    P, H, Ps, _ = k.shape
+    runs = ks.shape[-1] if ks.dim() == 3 else 0
+    if (tuple(ks.shape) != (P, H, runs) or tuple(vs.shape) != tuple(ks.shape) or not runs
+            or Ps % runs):
+        raise ValueError("k_scale/v_scale must both be [pages][kv_heads][page_size / run]")
+    a, b = ks.stride(), vs.stride()
+    if runs > 1 and (a[2] != 1 or b[2] != 1):
+        raise ValueError("the runs of a page must be the scales' innermost (unit-stride) dimension")
+    return _lib.QuantCacheSpec(format=fmt, scale_tokens=Ps // runs,
+                               k_scale_stride_page=a[0], k_scale_stride_head=a[1],
+                               v_scale_stride_page=b[0], v_scale_stride_head=b[1])
+
+
+def _same_device(dev, *tensors):
+    for t in tensors:
+        if t is not None and t.device != dev:
+            raise ValueError(f"all tensors must be on one device ({dev}), got {t.device}")
+
+
+def decode_attention_quant(q: torch.Tensor, cache: QuantCache, page_table: torch.Tensor,
+                           seq_lens: torch.Tensor, *, block_size: int, tau: float, phi: float,
+                           patience: int, softmax_scale: Optional[float] = None,
+                           dense_order: int = 0, block_list: Optional[torch.Tensor] = None,
+                           block_list_len: Optional[torch.Tensor] = None,
+                           list_per_head: bool = True, out_dtype=torch.float32,
+                           chunk_blocks: int = 0, probe_stride: int = 1,
+                           scale_of_accumulator: bool = False, no_detector: bool = False,
+                           max_wait_polls: int = 0, per_head_stop: bool = False,
+                           max_ahead_chunks: int = 0, workspace: Optional[torch.Tensor] = None,
+                           out: Optional[torch.Tensor] = None,
+                           lse: Optional[torch.Tensor] = None,
+                           stop_block: Optional[torch.Tensor] = None):
+    """``decode_attention`` over a cache held in 8 bits: K and V are the
+    cache's code * scale; everything else (options, lists, workspace, results)
+    is as there."""
+    _require_cuda(q, "q", torch.bfloat16)
+    _require_cuda(page_table, "page_table", torch.int32)
+    _require_cuda(seq_lens, "seq_lens", torch.int32)
+    if not q.is_contiguous() or not page_table.is_contiguous() or not seq_lens.is_contiguous():
+        raise ValueError("q, page_table and seq_lens must be contiguous")
+    if (block_list is None) != (block_list_len is None):
+        raise ValueError("block_list and block_list_len go together")
+    if block_list is not None:
+        _require_cuda(block_list, "block_list", torch.int32)
+        _require_cuda(block_list_len, "block_list_len", torch.int32)
+        if not block_list.is_contiguous() or not block_list_len.is_contiguous():
+            raise ValueError("block_list and block_list_len must be contiguous")
+    spec = _quant_spec(cache)
+    B, Hq, D = q.shape
+    Hkv = cache.k.shape[1]
+    if page_table.dim() != 2 or page_table.shape[0] != B or tuple(seq_lens.shape) != (B,):
+        raise ValueError("page_table must be [batch][max_pages] and seq_lens [batch]")
+    dev = q.device
+    heads = Hq if per_head_stop and not no_detector else Hkv
+    _same_device(dev, *cache, page_table, seq_lens, block_list, block_list_len, workspace, out, lse,
+                 stop_block)
+    if softmax_scale is None:
+        softmax_scale = 1.0 / math.sqrt(D)
+    shape = make_shape(q, cache.k, cache.v, page_table, block_size=block_size,
+                       block_list=block_list, list_per_head=list_per_head)
+    opts = make_opts(softmax_scale=softmax_scale, tau=tau, phi=phi, patience=patience,
+                     dense_order=dense_order, out_dtype=out_dtype, chunk_blocks=chunk_blocks,
+                     probe_stride=probe_stride, scale_of_accumulator=scale_of_accumulator,
+                     no_detector=no_detector, max_wait_polls=max_wait_polls,
+                     per_head_stop=per_head_stop, max_ahead_chunks=max_ahead_chunks)
+    if out is None:
+        out = torch.empty((B, Hq, D), dtype=out_dtype, device=dev)
+    if lse is None:
+        lse = torch.empty((B, Hq), dtype=torch.float32, device=dev)
+    if stop_block is None:
+        stop_block = torch.empty((B, heads), dtype=torch.int32, device=dev)
+    need = workspace_bytes(shape, opts)
+    with torch.cuda.device(dev):
+        stream = torch.cuda.current_stream(dev).cuda_stream
+        ws = workspace if workspace is not None else _cached_workspace(need, dev, stream)
+        st = _lib.decode_attention_quant(
+            shape, opts, spec, _ptr(q), _ptr(cache.k), _ptr(cache.v), _ptr(cache.k_scale),
+            _ptr(cache.v_scale), _ptr(page_table), _ptr(seq_lens), _ptr(block_list),
+            _ptr(block_list_len), _ptr(out), _ptr(lse), _ptr(stop_block), _ptr(ws), ws.numel(),
+            stream)
+    if st != _lib.OK:
+        raise ArtError(st, "art_decode_attention_quant")
+    return out, lse, stop_block
+
+
+def _quant_rows_call(cache, k_rows, v_rows, page_table, positions, token_offsets):
+    """(shape, spec, rows) of an append or a read, its tensors checked."""
+    spec = _quant_spec(cache)
+    P, H, Ps, D = cache.k.shape
+    if tuple(cache.v.shape) != (P, H, Ps, D) or cache.k.stride(3) != 1 or cache.v.stride(3) != 1:
+        raise ValueError("the cache's k and v must both be [pages][kv_heads][page_size][head_dim], "
+                         "head_dim innermost")
+    kind = _ROWS_TYPES.get(k_rows.dtype)
+    if kind is None:
+        raise ValueError("rows must be bfloat16, float16 or float32")
+    for t, name in ((k_rows, "k"), (v_rows, "v")):
+        _require_cuda(t, name, k_rows.dtype)
+        if t.dim() != 3 or tuple(t.shape) != (k_rows.shape[0], H, D):
+            raise ValueError(f"{name} must be [rows][{H}][{D}]")
+        if t.stride(2) != 1:
+            raise ValueError("head_dim must be the innermost (unit-stride) dimension")
+    _require_cuda(page_table, "page_table", torch.int32)
+    if page_table.dim() != 2 or not page_table.is_contiguous():
+        raise ValueError("page_table must be a contiguous [batch][max_pages]")
+    B = page_table.shape[0]
+    for t, name, n in ((positions, "positions", B), (token_offsets, "token_offsets", B + 1)):
+        if t is not None:
+            _require_cuda(t, name, torch.int32)
+            if tuple(t.shape) != (n,) or not t.is_contiguous():
+                raise ValueError(f"{name} must be a contiguous [{n}]")
+    _same_device(cache.k.device, *cache, k_rows, v_rows, page_table, positions, token_offsets)
+    ks, vs = cache.k.stride(), cache.v.stride()
+    shape = DecodeShape(batch=B, num_q_heads=H, num_kv_heads=H, head_dim=D, block_size=64,
+                        page_size=Ps, num_pages=P, max_pages_per_seq=int(page_table.shape[1]),
+                        max_blocks_per_list=0, list_per_head=1,
+                        k_stride_page=ks[0], k_stride_head=ks[1], k_stride_token=ks[2],
+                        v_stride_page=vs[0], v_stride_head=vs[1], v_stride_token=vs[2])
+    a, b = k_rows.stride(), v_rows.stride()
+    rows = _lib.QuantRows(rows_dtype=kind, rows=k_rows.shape[0], k_stride_row=a[0],
+                          k_stride_head=a[1], v_stride_row=b[0], v_stride_head=b[1])
+    return shape, spec, rows
+
+
+def quant_append(cache: QuantCache, k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor,
+                 positions: Optional[torch.Tensor], *,
+                 token_offsets: Optional[torch.Tensor] = None) -> None:
+    """Quantise new tokens into the cache, on the current stream.
+
+    ``k`` and ``v`` [rows][Hkv][D] (bf16, fp16 or fp32) hold the new tokens of
+    all sequences, packed: rows token_offsets[b] .. token_offsets[b + 1] - 1 are
+    sequence b's tokens positions[b], positions[b] + 1, ... (``token_offsets``
+    int32 [B + 1]; without it every sequence has rows / B of them).
+    ``positions`` int32 [B]: the tokens that each sequence holds already (None:
+    none; negative: an unused row of a padded batch).  A run of slots gets the
+    smallest power-of-two scale that holds its tokens; one that holds older
+    tokens keeps its scale unless it has to grow, and its old codes are then
+    rounded anew.  ``seq_lens`` stays the caller's to advance.
+    """
+    shape, spec, rows = _quant_rows_call(cache, k, v, page_table, positions, token_offsets)
+    with torch.cuda.device(k.device):
+        st = _lib.quant_append(shape, spec, rows, _ptr(k), _ptr(v), _ptr(token_offsets),
+                               _ptr(positions), _ptr(page_table), _ptr(cache.k), _ptr(cache.v),
+                               _ptr(cache.k_scale), _ptr(cache.v_scale),
+                               torch.cuda.current_stream(k.device).cuda_stream)
+    if st != _lib.OK:
+        raise ArtError(st, "art_quant_append")
+
+
+def quant_read(cache: QuantCache, page_table: torch.Tensor, positions: Optional[torch.Tensor], *,
+               token_offsets: Optional[torch.Tensor] = None, rows: Optional[int] = None,
+               dtype=torch.bfloat16, k: Optional[torch.Tensor] = None,
+               v: Optional[torch.Tensor] = None):
+    """Bring stored tokens back as packed rows, on the current stream.
+
+    Rows token_offsets[b] .. token_offsets[b + 1] - 1 receive sequence b's
+    tokens positions[b], positions[b] + 1, ... (as in ``quant_append``).
+    Returns (k, v) [rows][Hkv][D] in ``dtype`` (bf16, fp16 or fp32; code * scale
+    rounded once); ``rows`` sizes them where they are not given.  Rows of no
+    token are left as they were (not initialised, where they are not given).
+    """
+    if k is None or v is None:
+        if rows is None:
+            raise ValueError("rows is needed where k and v are not given")
+        size = (int(rows), cache.k.shape[1], cache.k.shape[3])
+        k = torch.empty(size, dtype=dtype, device=cache.k.device) if k is None else k
+        v = torch.empty(size, dtype=dtype, device=cache.k.device) if v is None else v
+    shape, spec, packed = _quant_rows_call(cache, k, v, page_table, positions, token_offsets)
+    with torch.cuda.device(k.device):
+        st = _lib.quant_read(shape, spec, packed, _ptr(cache.k), _ptr(cache.v),
+                             _ptr(cache.k_scale), _ptr(cache.v_scale), _ptr(token_offsets),
+                             _ptr(positions), _ptr(page_table), _ptr(k), _ptr(v),
+                             torch.cuda.current_stream(k.device).cuda_stream)
+    if st != _lib.OK:
+        raise ArtError(st, "art_quant_read")
+    return k, v

@@ -38,7 +38,9 @@ ASAN_LIB = os.path.join(HERE, "libart_asan.so")
 ARCH = os.environ.get("ART_OFFLOAD_ARCH", "gfx950")
 ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 
-DEVICE_SOURCES = ["art_kernels.hip", "art_lists.hip", "art_static.hip"]
+DEVICE_SOURCES = ["art_kernels.hip", "art_lists.hip", "art_static.hip", "art_quant.hip"]
+# the decode kernels once more for each kind of 8-bit cache
+KV_FORMATS = {"art_kernels_e4m3": "-DART_KV_FORMAT=1", "art_kernels_int8": "-DART_KV_FORMAT=2"}
 HOST_SOURCE = "art_api.cpp"
 SOURCES = DEVICE_SOURCES + [HOST_SOURCE]
 
@@ -102,6 +104,9 @@ def build(verbose: bool = False, extra=()) -> str:
     cc = hipcc()
     src = lambda s: os.path.join(CSRC, s)
     jobs = [(s, [cc, *flags(extra), "-c", "-o", _obj(s), src(s)]) for s in SOURCES]
+    for name, define in KV_FORMATS.items():
+        jobs.append((f"art_kernels.hip ({name})", [cc, *flags(extra), define, "-c", "-o", _obj(name),
+                                                   src("art_kernels.hip")]))
     jobs.append(("art_kernels.hip (stress)", [cc, *flags(extra), "-DART_RACE_STRESS", "-c",
                                               "-o", _obj("art_kernels_stress"), src("art_kernels.hip")]))
     jobs.append(("art_read_peak.hip", [cc, *flags(extra), "-c", "-o", _obj("art_read_peak.hip"),
@@ -109,7 +114,7 @@ def build(verbose: bool = False, extra=()) -> str:
     jobs.append(("art_api.cpp (asan)", [*_asan_host_flags(), "-c", "-o", _obj("art_api_asan"),
                                         src(HOST_SOURCE)]))
     _run_all(jobs, verbose)
-    dev = [_obj(s) for s in DEVICE_SOURCES]
+    dev = [_obj(s) for s in DEVICE_SOURCES] + [_obj(name) for name in KV_FORMATS]
     links = {
         LIB: dev + [_obj(HOST_SOURCE)],
         STRESS_LIB: [_obj("art_kernels_stress")] + dev[1:] + [_obj(HOST_SOURCE)],

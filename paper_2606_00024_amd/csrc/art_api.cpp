@@ -290,6 +290,13 @@ art_status check_decode_call(const art_decode_shape* shape, const art_decode_opt
     return fit_plan(shape, opts, bytes, plan);
 }
 
+// What a call over an 8-bit cache adds (nullptr for bf16 pools).
+struct QuantArgs {
+    const art_quant_cache* cache;
+    const float* k_scale;
+    const float* v_scale;
+};
+
 // Kernel parameters of a checked call over the workspace at `workspace`,
 // then the launch.
 art_status enqueue_decode(const Plan& plan, const art_decode_shape* shape,
@@ -297,7 +304,8 @@ art_status enqueue_decode(const Plan& plan, const art_decode_shape* shape,
                           const void* v_cache, const int32_t* page_table,
                           const int32_t* seq_lens, const int32_t* block_list,
                           const int32_t* block_list_len, void* out, float* lse,
-                          int32_t* stop_block, void* workspace, hipStream_t stream) {
+                          int32_t* stop_block, void* workspace, hipStream_t stream,
+                          const QuantArgs* quant = nullptr) {
     KernelParams k;
     memset(&k, 0, sizeof k);
     k.batch = shape->batch;
@@ -365,7 +373,17 @@ art_status enqueue_decode(const Plan& plan, const art_decode_shape* shape,
     k.spin_limit = opts->max_wait_polls > 0 ? (uint32_t)opts->max_wait_polls : kSpinLimit;
     k.max_ahead = opts->max_ahead_chunks;
     if (k.epoch >= (uint64_t(1) << 40)) return ART_ERR_UNSUPPORTED;
-    return art::launch_decode(plan, k, stream) == (int)hipSuccess ? ART_OK : ART_ERR_HIP;
+    if (!quant) return art::launch_decode(plan, k, stream) == (int)hipSuccess ? ART_OK : ART_ERR_HIP;
+    k.k_scale = quant->k_scale;
+    k.v_scale = quant->v_scale;
+    k.ksc_page = quant->cache->k_scale_stride_page;
+    k.ksc_head = quant->cache->k_scale_stride_head;
+    k.vsc_page = quant->cache->v_scale_stride_page;
+    k.vsc_head = quant->cache->v_scale_stride_head;
+    k.scale_shift = ilog2(quant->cache->scale_tokens);
+    const int e = quant->cache->format == ART_QUANT_E4M3 ? art::launch_decode_e4m3(plan, k, stream)
+                                                         : art::launch_decode_int8(plan, k, stream);
+    return e == (int)hipSuccess ? ART_OK : ART_ERR_HIP;
 }
 
 }  // namespace
@@ -416,6 +434,26 @@ art_status art_decode_attention(const art_decode_shape* shape, const art_decode_
     if ((uintptr_t)workspace % 8) return ART_ERR_INVALID_ARG;
     return enqueue_decode(plan, shape, opts, q, k_cache, v_cache, page_table, seq_lens,
                           block_list, block_list_len, out, lse, stop_block, workspace, stream);
+}
+
+art_status art_decode_attention_quant(const art_decode_shape* shape, const art_decode_opts* opts,
+                                      const art_quant_cache* cache, const void* q, const void* k_cache,
+                                      const void* v_cache, const float* k_scale, const float* v_scale,
+                                      const int32_t* page_table, const int32_t* seq_lens,
+                                      const int32_t* block_list, const int32_t* block_list_len,
+                                      void* out, float* lse, int32_t* stop_block,
+                                      void* workspace, size_t workspace_bytes, hipStream_t stream) {
+    art_status st = art::check_quant(shape, cache);
+    if (st != ART_OK) return st;
+    Plan plan;
+    st = check_decode_call(shape, opts, q, k_cache, v_cache, page_table, seq_lens, block_list,
+                           block_list_len, out, lse, stop_block, workspace ? workspace_bytes : 0, &plan);
+    if (st != ART_OK || shape->batch == 0) return st;
+    if (!k_scale || !v_scale || (uintptr_t)workspace % 8 || ((uintptr_t)k_scale | (uintptr_t)v_scale) % 4)
+        return ART_ERR_INVALID_ARG;
+    const QuantArgs quant{cache, k_scale, v_scale};
+    return enqueue_decode(plan, shape, opts, q, k_cache, v_cache, page_table, seq_lens, block_list,
+                          block_list_len, out, lse, stop_block, workspace, stream, &quant);
 }
 
 art_status art_decode_attention_static(const art_decode_shape* shape, const art_decode_opts* opts,

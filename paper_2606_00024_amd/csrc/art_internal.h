@@ -7,6 +7,8 @@
 
 #include <hip/hip_runtime_api.h>
 
+#include "art.h"
+
 namespace art {
 
 constexpr int kHeadDim = 128;   // dims per head (the only supported value)
@@ -111,14 +113,24 @@ struct KernelParams {
     uint64_t epoch;          // unique per call; tags every flag it writes
     uint32_t spin_limit;     // polls before a wait gives up
     int32_t max_ahead;       // 0, or chunks a load may run ahead of the last tested chunk
+    // 8-bit pools (k and v then point at codes, their strides are in bytes)
+    const float* k_scale;
+    const float* v_scale;
+    int64_t ksc_page, ksc_head, vsc_page, vsc_head;
+    int32_t scale_shift;     // log2 of the slots that share a scale
 };
 
 // Launchers (art_kernels.hip).  Return a hipError_t.
 int launch_decode(const Plan& plan, const KernelParams& params, hipStream_t stream);
+int launch_decode_e4m3(const Plan& plan, const KernelParams& params, hipStream_t stream);
+int launch_decode_int8(const Plan& plan, const KernelParams& params, hipStream_t stream);
 int launch_fill_zero(void* ptr, size_t bytes, hipStream_t stream);
 // Device address of the library's static scratch on the current device
 // (art_static.hip); set up (address taken, zero-filled on `stream`) on the
 // first call per device.  Returns a hipError_t.
 int static_scratch(hipStream_t stream, void** ptr);
+// Host checks of an 8-bit cache's layout: the shape's page and stride fields
+// and the scales' (art_quant.hip).
+art_status check_quant(const art_decode_shape* shape, const art_quant_cache* cache);
 
 }  // namespace art

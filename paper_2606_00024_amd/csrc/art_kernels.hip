@@ -56,8 +56,17 @@
 
 #include "art_internal.h"
 
+// This source builds once for each kind of cache (ART_KV_FORMAT): 0, bf16
+// pools; 1 and 2, pools of 8-bit codes (e4m3, int8) with a scale for every run
+// of slots, whose kernels differ in how a tile is loaded (load_tile below).
+#ifndef ART_KV_FORMAT
+#define ART_KV_FORMAT 0
+#endif
+
 namespace art {
 namespace {
+
+constexpr int kFormat = ART_KV_FORMAT;
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -522,7 +531,10 @@ __device__ __forceinline__ void load_q(Params& P, int b, int kvh, int lane, bf16
 #pragma unroll
   for (int s = 0; s < 4; ++s) {
     if (h < G) {
-      const uint16_t* src = P.q + ((int64_t)b * P.num_q_heads + kvh * G + h) * kD + (4 * s + (lane >> 4)) * 8;
+      // dims of K-step s as the K loads hold them: 32s + 8g .. +7 of lane
+      // group g, or, of codes, 64(s/2) + 16g + 8(s%2) .. +7
+      const int dim = kFormat == 0 ? (4 * s + (lane >> 4)) * 8 : 64 * (s >> 1) + 16 * (lane >> 4) + 8 * (s & 1);
+      const uint16_t* src = P.q + ((int64_t)b * P.num_q_heads + kvh * G + h) * kD + dim;
       const u32x4 w = *reinterpret_cast<const u32x4*>(src);
       qa[s] = __builtin_bit_cast(bf16x8, w);
     } else {
@@ -567,6 +579,83 @@ __device__ __forceinline__ int vstage_off(int row, int piece) {
   return row * kVRow + ((piece ^ (2 * (row & 3))) << 3);
 }
 
+// ---- a tile of 8-bit codes --------------------------------------------------
+// Codes convert to bf16 exactly (e4m3 holds 4 significant bits, int8 8), so
+// the products run on the bf16 matrix instruction and lose nothing.  A scale
+// belongs to a run of at least 16 slots, so it multiplies the scores of a
+// 16-token group (K) and its probabilities (V), never a single value.
+//
+// K: for 16-token group n, lane (lo, g) holds token 16n + lo, bytes
+// 64j + 16g .. +15 (load_q's order of the dims).  V: lane 8r + c holds token
+// 8i + r, dims 16c .. 16c + 15.
+struct QuantTile {
+  u32x4 k[4][2];
+  u32x4 v[8];
+};
+
+__device__ __forceinline__ void load_codes(Params& P, int kvh, int L, int tok0, const int (&pg)[4], int lane,
+                                           QuantTile& t) {
+  const int lo = lane & 15, g = lane >> 4;
+  const int psz_mask = (1 << P.page_shift) - 1;
+  const uint8_t* const kc = reinterpret_cast<const uint8_t*>(P.k);
+  const uint8_t* const vc = reinterpret_cast<const uint8_t*>(P.v);
+#pragma unroll
+  for (int n = 0; n < 4; ++n) {
+    const int t0 = min(tok0 + 16 * n, L - 1);
+    const uint8_t* kb = kc + (int64_t)pg[n] * P.ks_page + (int64_t)kvh * P.ks_head + (int64_t)(t0 & psz_mask) * P.ks_tok;
+    const uint32_t ko = __umul24(min(lo, L - 1 - t0), (uint32_t)P.ks_tok) + 16u * g;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) t.k[n][j] = *reinterpret_cast<const u32x4*>(kb + (ko + 64u * j));
+  }
+#pragma unroll
+  for (int n = 0; n < 4; ++n) {
+    const int t0 = min(tok0 + 16 * n, L - 1);
+    const uint8_t* vb = vc + (int64_t)pg[n] * P.vs_page + (int64_t)kvh * P.vs_head + (int64_t)(t0 & psz_mask) * P.vs_tok;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const uint32_t vo = __umul24(min(8 * j + (lane >> 3), L - 1 - t0), (uint32_t)P.vs_tok) + 16u * (lane & 7);
+      t.v[2 * n + j] = *reinterpret_cast<const u32x4*>(vb + vo);
+    }
+  }
+}
+
+__device__ __forceinline__ void load_scales(Params& P, int kvh, int L, int tok0, const int (&pg)[4], float (&ksc)[4],
+                                            float (&vsc)[4]) {
+  const int psz_mask = (1 << P.page_shift) - 1;
+#pragma unroll
+  for (int n = 0; n < 4; ++n) {
+    const int run = (min(tok0 + 16 * n, L - 1) & psz_mask) >> P.scale_shift;
+    ksc[n] = P.k_scale[(int64_t)pg[n] * P.ksc_page + (int64_t)kvh * P.ksc_head + run];
+    vsc[n] = P.v_scale[(int64_t)pg[n] * P.vsc_page + (int64_t)kvh * P.vsc_head + run];
+  }
+}
+
+// Eight codes of a lane's sixteen (the lower or the upper half) as bf16.
+__device__ __forceinline__ u32x4 codes_bf16(const u32x4& w, int half) {
+  u32x4 r;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const uint32_t x = w[2 * half + i];
+    if constexpr (kFormat == 1) {
+      r[2 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.0f, false));
+      r[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.0f, true));
+    } else {
+      r[2 * i] = pack_bf16((float)(int8_t)x, (float)(int8_t)(x >> 8));
+      r[2 * i + 1] = pack_bf16((float)(int8_t)(x >> 16), (float)((int32_t)x >> 24));
+    }
+  }
+  return r;
+}
+
+// The scale of group REP i + u, which a lane of copy u works on.
+template <int REP>
+__device__ __forceinline__ float own_scale(float s0, float s1, float s2, float s3, int i, int u) {
+  if constexpr (REP == 1) return i == 0 ? s0 : i == 1 ? s1 : i == 2 ? s2 : s3;
+  if constexpr (REP == 2) return i == 0 ? (u ? s1 : s0) : (u ? s3 : s2);
+  const float a = (u & 1) ? s1 : s0, b = (u & 1) ? s3 : s2;
+  return (u & 2) ? b : a;
+}
+
 // The first tile of a block writes the block record; each later tile of
 // the block (accumulate) is folded into it: both parts rescaled to the
 // larger running max and the combined mass, in tile order.
@@ -600,7 +689,12 @@ __device__ void compute_tile(Params& P, int kvh, int L, int tok0, const int (&pg
   // 64-bit multiplies per lane (36 of them) kept a tile's first loads waiting.
   u32x4 kr[4][4];
   u32x4 vr[16];
-  if constexpr (!WIDE) {
+  QuantTile qt;
+  float ksc[4], vsc[4];   // scales of the 16-token groups
+  if constexpr (kFormat != 0) {
+    load_codes(P, kvh, L, tok0, pg, lane, qt);
+    load_scales(P, kvh, L, tok0, pg, ksc, vsc);
+  } else if constexpr (!WIDE) {
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
       const int t = min(tok0 + 16 * n, L - 1);
@@ -654,8 +748,12 @@ __device__ void compute_tile(Params& P, int kvh, int L, int tok0, const int (&pg
   for (int n = 0; n < 4; ++n) {
     St[n] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int s = 0; s < 4; ++s)
-      St[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[n][s]), qa[s], St[n], 0, 0, 0);
+    for (int s = 0; s < 4; ++s) {
+      u32x4 kf;
+      if constexpr (kFormat == 0) kf = kr[n][s];
+      else kf = codes_bf16(qt.k[n][s >> 1], s & 1);
+      St[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf), qa[s], St[n], 0, 0, 0);
+    }
   }
   // softmax of the lane's head over the tile: the lane's own tokens, the
   // other copies (lanes lo ^ 8, then lo +- 4 of the row), then the four rows
@@ -674,7 +772,8 @@ __device__ void compute_tile(Params& P, int kvh, int L, int tok0, const int (&pg
         const float y = (u & 1) ? St[1][r] : x, z = (u & 1) ? St[3][r] : St[2][r];
         x = (u & 2) ? z : y;
       }
-      sc[i][r] = x * P.scale_log2;
+      if constexpr (kFormat == 0) sc[i][r] = x * P.scale_log2;
+      else sc[i][r] = x * (own_scale<REP>(ksc[0], ksc[1], ksc[2], ksc[3], i, u) * P.scale_log2);
     }
   if (tok0 + kTile > L) {
 #pragma unroll
@@ -724,6 +823,11 @@ __device__ void compute_tile(Params& P, int kvh, int L, int tok0, const int (&pg
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
       float a0 = sc[i][2 * e], a1 = sc[i][2 * e + 1];
+      if constexpr (kFormat != 0) {   // V's scale belongs to the token: into P, not into V
+        const float vs = own_scale<REP>(vsc[0], vsc[1], vsc[2], vsc[3], i, u);
+        a0 *= vs;
+        a1 *= vs;
+      }
 #pragma unroll
       for (int j = 0; j < 3; ++j) {
         const uint32_t w = pack_bf16(a0, a1);
@@ -779,9 +883,18 @@ __device__ void compute_tile(Params& P, int kvh, int L, int tok0, const int (&pg
       v4i16 r0[8];
 #pragma unroll
       for (int qh = 0; qh < 2; ++qh) {
+        if constexpr (kFormat == 0) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          *reinterpret_cast<u32x4*>(vbuf + vstage_off(4 * i + g, lo)) = vr[8 * c + 4 * qh + i];
+          for (int i = 0; i < 4; ++i)
+            *reinterpret_cast<u32x4*>(vbuf + vstage_off(4 * i + g, lo)) = vr[8 * c + 4 * qh + i];
+        } else {
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+              *reinterpret_cast<u32x4*>(vbuf + vstage_off(8 * i + (lane >> 3), 2 * (lane & 7) + e)) =
+                  codes_bf16(qt.v[4 * c + 2 * qh + i], e);
+        }
         wave_lds_order();
 #pragma unroll
         for (int d = 0; d < 8; ++d) {
@@ -804,9 +917,18 @@ __device__ void compute_tile(Params& P, int kvh, int L, int tok0, const int (&pg
     // of a group on 32 distinct banks
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
+      if constexpr (kFormat == 0) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        *reinterpret_cast<u32x4*>(vbuf + (4 * i + g) * kVPitch + 8 * lo) = vr[8 * c + i];
+        for (int i = 0; i < 8; ++i)
+          *reinterpret_cast<u32x4*>(vbuf + (4 * i + g) * kVPitch + 8 * lo) = vr[8 * c + i];
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+            *reinterpret_cast<u32x4*>(vbuf + (8 * i + (lane >> 3)) * kVPitch + 16 * (lane & 7) + 8 * e) =
+                codes_bf16(qt.v[4 * c + i], e);
+      }
       wave_lds_order();
 #pragma unroll
       for (int d = 0; d < 8; ++d) {
@@ -2124,12 +2246,19 @@ int launch_w(const Plan& plan, const KernelParams& params, hipStream_t stream) {
 
 template <int G, bool PH>
 int launch_g(const Plan& plan, const KernelParams& params, hipStream_t stream) {
-  return params.wide ? launch_w<G, PH, true>(plan, params, stream) : launch_w<G, PH, false>(plan, params, stream);
+  if constexpr (kFormat != 0) return launch_w<G, PH, false>(plan, params, stream);
+  else return params.wide ? launch_w<G, PH, true>(plan, params, stream) : launch_w<G, PH, false>(plan, params, stream);
 }
 
 }  // namespace
 
+#if ART_KV_FORMAT == 0
 int launch_decode(const Plan& plan, const KernelParams& params, hipStream_t stream) {
+#elif ART_KV_FORMAT == 1
+int launch_decode_e4m3(const Plan& plan, const KernelParams& params, hipStream_t stream) {
+#else
+int launch_decode_int8(const Plan& plan, const KernelParams& params, hipStream_t stream) {
+#endif
   switch (plan.group) {
     case 1: return params.per_head ? launch_g<1, true>(plan, params, stream) : launch_g<1, false>(plan, params, stream);
     case 2: return params.per_head ? launch_g<2, true>(plan, params, stream) : launch_g<2, false>(plan, params, stream);
@@ -2140,6 +2269,7 @@ int launch_decode(const Plan& plan, const KernelParams& params, hipStream_t stre
   }
 }
 
+#if ART_KV_FORMAT == 0
 int launch_fill_zero(void* ptr, size_t bytes, hipStream_t stream) {
   const size_t words = bytes / 4;
   if (words == 0) return (int)hipSuccess;
@@ -2149,5 +2279,7 @@ int launch_fill_zero(void* ptr, size_t bytes, hipStream_t stream) {
                      static_cast<uint32_t*>(ptr), words);
   return (int)hipGetLastError();
 }
+
+#endif
 
 }  // namespace art
