@@ -38,7 +38,8 @@ ASAN_LIB = os.path.join(HERE, "libart_asan.so")
 ARCH = os.environ.get("ART_OFFLOAD_ARCH", "gfx950")
 ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 
-DEVICE_SOURCES = ["art_kernels.hip", "art_lists.hip", "art_static.hip", "art_quant.hip"]
+DEVICE_SOURCES = ["art_kernels.hip", "art_lists.hip", "art_static.hip", "art_quant.hip",
+                  "art_quant_full.hip"]
 # the decode kernels once more for each kind of 8-bit cache
 KV_FORMATS = {"art_kernels_e4m3": "-DART_KV_FORMAT=1", "art_kernels_int8": "-DART_KV_FORMAT=2"}
 HOST_SOURCE = "art_api.cpp"

@@ -381,8 +381,9 @@ art_status enqueue_decode(const Plan& plan, const art_decode_shape* shape,
     k.vsc_page = quant->cache->v_scale_stride_page;
     k.vsc_head = quant->cache->v_scale_stride_head;
     k.scale_shift = ilog2(quant->cache->scale_tokens);
-    const int e = quant->cache->format == ART_QUANT_E4M3 ? art::launch_decode_e4m3(plan, k, stream)
-                                                         : art::launch_decode_int8(plan, k, stream);
+    const int e = k.no_detector                                ? art::launch_quant_full(plan, k, quant->cache->format, stream)
+                  : quant->cache->format == ART_QUANT_E4M3 ? art::launch_decode_e4m3(plan, k, stream)
+                                                           : art::launch_decode_int8(plan, k, stream);
     return e == (int)hipSuccess ? ART_OK : ART_ERR_HIP;
 }
 

@@ -124,6 +124,8 @@ struct KernelParams {
 int launch_decode(const Plan& plan, const KernelParams& params, hipStream_t stream);
 int launch_decode_e4m3(const Plan& plan, const KernelParams& params, hipStream_t stream);
 int launch_decode_int8(const Plan& plan, const KernelParams& params, hipStream_t stream);
+// Full attention over an 8-bit cache (art_quant_full.hip).
+int launch_quant_full(const Plan& plan, const KernelParams& params, int format, hipStream_t stream);
 int launch_fill_zero(void* ptr, size_t bytes, hipStream_t stream);
 // Device address of the library's static scratch on the current device
 // (art_static.hip); set up (address taken, zero-filled on `stream`) on the

@@ -55,6 +55,7 @@
 #include <stdint.h>
 
 #include "art_internal.h"
+#include "art_wave.h"
 
 // This source builds once for each kind of cache (ART_KV_FORMAT): 0, bf16
 // pools; 1 and 2, pools of 8-bit codes (e4m3, int8) with a scale for every run
@@ -67,13 +68,6 @@ namespace art {
 namespace {
 
 constexpr int kFormat = ART_KV_FORMAT;
-
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-
-constexpr float kNegInf = -__builtin_inff();
 
 // The kernel's parameters, read where they are used from the kernel argument
 // segment through the scalar cache.  fresh() hides the pointer's origin from
@@ -88,107 +82,6 @@ __device__ __forceinline__ Params* fresh(Params* p) {
   return p;
 }
 constexpr int kD = kHeadDim;
-
-__device__ __forceinline__ float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
-__device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
-
-// two floats to two bf16 (round to nearest even), one v_cvt_pk_bf16_f32
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
-}
-
-__device__ __forceinline__ uint32_t f32_to_bf16_bits(float f) {
-  uint32_t u = __float_as_uint(f);
-  if ((u & 0x7fffffffu) > 0x7f800000u) return 0x7fc0u;  // NaN
-  u += 0x7fffu + ((u >> 16) & 1u);                       // round to nearest even
-  return u >> 16;
-}
-
-// ---- wavefront reductions over the 16 lanes of a DPP row -------------------
-template <int CTRL>
-__device__ __forceinline__ float dpp_f(float x) {
-  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, false));
-}
-constexpr int kQuadXor1 = 0xB1;       // quad_perm [1,0,3,2]
-constexpr int kQuadXor2 = 0x4E;       // quad_perm [2,3,0,1]
-constexpr int kRowHalfMirror = 0x141; // lane i <- lane 7-i within each 8
-constexpr int kRowMirror = 0x140;     // lane i <- lane 15-i within each 16
-constexpr int kRowRor4 = 0x124;       // lane i <- lane i-4 of its row of 16 (= i+12)
-constexpr int kRowRor8 = 0x128;       // lane i <- lane i-8 (= i+8)
-
-// Every lane of the row ends with the same bits (each step adds the same two
-// partial sums, only in swapped operand order).
-__device__ __forceinline__ float row_sum(float x) {
-  x = x + dpp_f<kQuadXor1>(x);
-  x = x + dpp_f<kQuadXor2>(x);
-  x = x + dpp_f<kRowHalfMirror>(x);
-  x = x + dpp_f<kRowMirror>(x);
-  return x;
-}
-__device__ __forceinline__ float row_max(float x) {
-  x = fmaxf(x, dpp_f<kQuadXor1>(x));
-  x = fmaxf(x, dpp_f<kQuadXor2>(x));
-  x = fmaxf(x, dpp_f<kRowHalfMirror>(x));
-  x = fmaxf(x, dpp_f<kRowMirror>(x));
-  return x;
-}
-
-__device__ __forceinline__ float read_lane(float x, int lane) {
-  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), lane));
-}
-// Maximum and sum over the four rows of 16 lanes (lanes l, l ^ 16, l ^ 32,
-// l ^ 48), by gfx950's half swaps: each swap hands every lane both operands
-// in the same order, so all four lanes end with the same bits.
-__device__ __forceinline__ void swap_rows16(float x, float& a, float& b) {
-  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_int(x), __float_as_int(x), false, false);
-  a = __int_as_float(r[0]);
-  b = __int_as_float(r[1]);
-}
-__device__ __forceinline__ void swap_rows32(float x, float& a, float& b) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_int(x), __float_as_int(x), false, false);
-  a = __int_as_float(r[0]);
-  b = __int_as_float(r[1]);
-}
-__device__ __forceinline__ float rows_max(float x) {
-  float a, b;
-  swap_rows16(x, a, b);
-  swap_rows32(fmaxf(a, b), a, b);
-  return fmaxf(a, b);
-}
-__device__ __forceinline__ float rows_sum(float x) {
-  float a, b;
-  swap_rows16(x, a, b);
-  swap_rows32(a + b, a, b);
-  return a + b;
-}
-
-// LDS written by some lanes of this wave, read by others.  LDS operations of
-// one wavefront complete in order; this waits for them and keeps the
-// compiler from moving memory operations across.
-__device__ __forceinline__ void wave_lds_sync() {
-  __asm__ __volatile__("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
-  __builtin_amdgcn_wave_barrier();
-  __asm__ __volatile__("" ::: "memory");
-}
-
-// The same ordering without the wait, where only this wave touches the
-// memory: the LDS unit executes one wavefront's operations in the order they
-// were issued, so a read issued after a write of any lane of the wave sees
-// it, and a write issued after a read cannot overtake it.  Only the compiler
-// has to be kept from reordering them.
-__device__ __forceinline__ void wave_lds_order() {
-  __asm__ __volatile__("" ::: "memory");
-  __builtin_amdgcn_wave_barrier();
-  __asm__ __volatile__("" ::: "memory");
-}
-
-__device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
-// single hardware instructions (about 1 ulp): the same bits wherever used
-__device__ __forceinline__ float fast_rcp(float x) { return __builtin_amdgcn_rcpf(x); }
-__device__ __forceinline__ float fast_sqrt(float x) { return __builtin_amdgcn_sqrtf(x); }
 
 // ---- workspace: cross-workgroup data ---------------------------------------
 // Everything one workgroup hands to another (flags, softmax records,
@@ -630,32 +523,6 @@ __device__ __forceinline__ void load_scales(Params& P, int kvh, int L, int tok0,
   }
 }
 
-// Eight codes of a lane's sixteen (the lower or the upper half) as bf16.
-__device__ __forceinline__ u32x4 codes_bf16(const u32x4& w, int half) {
-  u32x4 r;
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const uint32_t x = w[2 * half + i];
-    if constexpr (kFormat == 1) {
-      r[2 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.0f, false));
-      r[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.0f, true));
-    } else {
-      r[2 * i] = pack_bf16((float)(int8_t)x, (float)(int8_t)(x >> 8));
-      r[2 * i + 1] = pack_bf16((float)(int8_t)(x >> 16), (float)((int32_t)x >> 24));
-    }
-  }
-  return r;
-}
-
-// The scale of group REP i + u, which a lane of copy u works on.
-template <int REP>
-__device__ __forceinline__ float own_scale(float s0, float s1, float s2, float s3, int i, int u) {
-  if constexpr (REP == 1) return i == 0 ? s0 : i == 1 ? s1 : i == 2 ? s2 : s3;
-  if constexpr (REP == 2) return i == 0 ? (u ? s1 : s0) : (u ? s3 : s2);
-  const float a = (u & 1) ? s1 : s0, b = (u & 1) ? s3 : s2;
-  return (u & 2) ? b : a;
-}
-
 // The first tile of a block writes the block record; each later tile of
 // the block (accumulate) is folded into it: both parts rescaled to the
 // larger running max and the combined mass, in tile order.
@@ -751,7 +618,7 @@ __device__ void compute_tile(Params& P, int kvh, int L, int tok0, const int (&pg
     for (int s = 0; s < 4; ++s) {
       u32x4 kf;
       if constexpr (kFormat == 0) kf = kr[n][s];
-      else kf = codes_bf16(qt.k[n][s >> 1], s & 1);
+      else kf = codes_bf16<kFormat - 1>(qt.k[n][s >> 1], s & 1);
       St[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf), qa[s], St[n], 0, 0, 0);
     }
   }
@@ -893,7 +760,7 @@ __device__ void compute_tile(Params& P, int kvh, int L, int tok0, const int (&pg
 #pragma unroll
             for (int e = 0; e < 2; ++e)
               *reinterpret_cast<u32x4*>(vbuf + vstage_off(8 * i + (lane >> 3), 2 * (lane & 7) + e)) =
-                  codes_bf16(qt.v[4 * c + 2 * qh + i], e);
+                  codes_bf16<kFormat - 1>(qt.v[4 * c + 2 * qh + i], e);
         }
         wave_lds_order();
 #pragma unroll
@@ -927,7 +794,7 @@ __device__ void compute_tile(Params& P, int kvh, int L, int tok0, const int (&pg
 #pragma unroll
           for (int e = 0; e < 2; ++e)
             *reinterpret_cast<u32x4*>(vbuf + (8 * i + (lane >> 3)) * kVPitch + 16 * (lane & 7) + 8 * e) =
-                codes_bf16(qt.v[4 * c + i], e);
+                codes_bf16<kFormat - 1>(qt.v[4 * c + i], e);
       }
       wave_lds_order();
 #pragma unroll

@@ -1,0 +1,663 @@
+// Full attention (no stability test) over a cache held in 8 bits.
+//
+// Without the test nothing has to be decided block by block, so the work is
+// cut for the memory system alone.  The 64-token tiles of all (sequence, KV
+// head) groups form one line, and every workgroup takes an equal, contiguous
+// part of it, however ragged the batch is; the part of a group in a
+// workgroup's range is a segment.  The four wavefronts of a workgroup take a
+// segment's tiles in turn, each with its own running maximum, mass and output
+// sums in registers, and join at its end through LDS.  A group that lies in
+// one workgroup is written out there; of the others each segment leaves a
+// record (m, L, o) in the workspace and a second, small launch joins them.
+//
+//   s_j = scale * (ks_j (q . ck_j)),  p_j = 2^(s_j log2 e - m),
+//   out = sum_j p_j vs_j cv_j / sum_j p_j
+//
+// with one scale for every 16 tokens, at least (see art_wave.h).
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "art_internal.h"
+#include "art_wave.h"
+
+namespace art {
+namespace {
+
+constexpr int kD = kHeadDim;
+
+template <int G>
+struct Full {
+  static constexpr int REP = G > 8 ? 1 : G > 4 ? 2 : 4;  // copies of the heads over the 16 score columns
+  static constexpr int COLS = 16 / REP;
+  static constexpr int NS = 4 / REP;                     // 16-token groups of a tile that a lane works on
+  static constexpr int NP = G > 8 ? 3 : G > 4 ? 2 : 1;   // P operands of a K-step
+  static constexpr int ND = G > 8 ? 8 : G > 4 ? 4 : 2;   // dims a lane holds in the end
+  static constexpr int REC = G * kD + 2 * G;             // floats of a record: o, m, L
+  // a wavefront's LDS: V's codes (8 KiB) and P's parts (up to 24 rows of 128
+  // bytes); its record at a segment's end takes their place
+  static constexpr int PARTS = G > 8 ? 0 : 24 * 128;
+  static constexpr int WAVE_BYTES = 8192 + PARTS > REC * 4 ? 8192 + PARTS : REC * 4;
+};
+
+// The line of tiles.  A unit is what shares a length: a sequence (all its KV
+// heads), or with a list per head one group.
+struct Unit {
+  int tiles;    // of each of its groups
+  int heads;    // groups
+};
+
+__device__ __forceinline__ int seq_len(const KernelParams& P, int b) {
+  const int64_t cap = (int64_t)P.max_pages << P.page_shift;
+  const int L = P.seq_lens[b];
+  return L < 0 ? 0 : (int)min((int64_t)L, cap);
+}
+__device__ __forceinline__ bool per_group_units(const KernelParams& P) { return P.block_list && P.list_per_head; }
+__device__ __forceinline__ int unit_count(const KernelParams& P) {
+  return per_group_units(P) ? P.batch * P.num_kv_heads : P.batch;
+}
+// blocks of a unit's traversal
+__device__ __forceinline__ int unit_blocks(const KernelParams& P, int u, int L) {
+  if (L == 0) return 0;
+  if (!P.block_list) return (L + P.block_size - 1) / P.block_size;
+  const int T = P.block_list_len[u];
+  return T < 0 ? 0 : min(T, P.max_list);
+}
+__device__ __forceinline__ int unit_tiles(const KernelParams& P, int u) {
+  const int L = seq_len(P, per_group_units(P) ? u / P.num_kv_heads : u);
+  return P.block_list ? unit_blocks(P, u, L) * P.tiles_per_block : (L + kTile - 1) / kTile;
+}
+__device__ __forceinline__ int unit_heads(const KernelParams& P) { return per_group_units(P) ? 1 : P.num_kv_heads; }
+
+// Workgroups that share `total` tiles: every wavefront gets one, at least.
+__device__ __forceinline__ int64_t workers_of(int64_t total, int64_t most) {
+  return max((int64_t)1, min(most, (total + kWaves - 1) / kWaves));
+}
+
+__device__ __forceinline__ int64_t wave_sum(int64_t x) {
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) x += __shfl_xor((long long)x, o);
+  return x;
+}
+
+// ---- a tile's operands -------------------------------------------------------
+// K: for 16-token group n, lane (lo, g) holds token 16n + lo, bytes 64j + 16g
+// .. +15 (the query is read in the same order of the dims).  V: lane 8r + c
+// holds token 8i + r, dims 16c .. 16c + 15.  Tokens past the sequence's end
+// are redirected to its last one.
+struct Tile {
+  u32x4 k[4][2];
+  u32x4 v[8];
+};
+struct TileAt {
+  int tok0;
+  int pg[4];
+};
+
+__device__ __forceinline__ const uint8_t* rows_at(const uint16_t* pool, int64_t sp, int64_t sh, int64_t st, int pg,
+                                                  int kvh, int slot) {
+  return reinterpret_cast<const uint8_t*>(pool) + (int64_t)pg * sp + (int64_t)kvh * sh + (int64_t)slot * st;
+}
+__device__ __forceinline__ void load_k(const KernelParams& P, int kvh, int L, const TileAt& at, int lane, Tile& t) {
+  const int lo = lane & 15, g = lane >> 4, mask = (1 << P.page_shift) - 1;
+#pragma unroll
+  for (int n = 0; n < 4; ++n) {
+    const int t0 = min(at.tok0 + 16 * n, L - 1);
+    const uint8_t* b = rows_at(P.k, P.ks_page, P.ks_head, P.ks_tok, at.pg[n], kvh, t0 & mask);
+    const uint32_t o = __umul24(min(lo, L - 1 - t0), (uint32_t)P.ks_tok) + 16u * g;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) t.k[n][j] = *reinterpret_cast<const u32x4*>(b + (o + 64u * j));
+  }
+}
+__device__ __forceinline__ void load_v(const KernelParams& P, int kvh, int L, const TileAt& at, int lane, Tile& t) {
+  const int mask = (1 << P.page_shift) - 1;
+#pragma unroll
+  for (int n = 0; n < 4; ++n) {
+    const int t0 = min(at.tok0 + 16 * n, L - 1);
+    const uint8_t* b = rows_at(P.v, P.vs_page, P.vs_head, P.vs_tok, at.pg[n], kvh, t0 & mask);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const uint32_t o = __umul24(min(8 * j + (lane >> 3), L - 1 - t0), (uint32_t)P.vs_tok) + 16u * (lane & 7);
+      t.v[2 * n + j] = *reinterpret_cast<const u32x4*>(b + o);
+    }
+  }
+}
+
+// V's stage: token r's 16-byte piece j sits at piece j ^ swizzle(r), so that
+// the eight rows a transposing read touches (tokens 4g .. 4g + 3 and 16 more
+// of each, for two lane groups at once) fall on distinct banks.
+__device__ __forceinline__ int stage_off(int r, int j) {
+  return r * 128 + ((j ^ (((r >> 1) & 1) | ((r >> 4) & 1) << 1 | ((r >> 2) & 1) << 2)) << 4);
+}
+
+// What a wavefront reads ahead for 16 of its tiles: lane 4m + n holds the page
+// and the scales of group n of tile m.
+struct Ahead {
+  int tok0, page;
+  float ks, vs;
+};
+
+struct Segment {
+  int b, kvh, L, T;      // T: blocks of the traversal
+  int t0, n;             // its tiles of the group: t0 .. t0 + n - 1
+  const int32_t* list;
+};
+
+__device__ __forceinline__ void ahead_pages(const KernelParams& P, const Segment& s, int wave, int first, int n_mine,
+                                            int lane, Ahead& a) {
+  const int m = first + (lane >> 2);
+  a.tok0 = 0;
+  a.page = 0;
+  if (m < n_mine) {
+    const int tile = s.t0 + wave + kWaves * m;
+    if (s.list) {
+      const int i = tile / P.tiles_per_block, nblk = (s.L + P.block_size - 1) / P.block_size;
+      int blk = s.list[i];
+      blk = blk < 0 ? 0 : (blk >= nblk ? nblk - 1 : blk);
+      a.tok0 = blk * P.block_size + (tile - i * P.tiles_per_block) * kTile;
+    } else {
+      a.tok0 = tile * kTile;
+    }
+    const int tok = min(a.tok0 + 16 * (lane & 3), s.L - 1);
+    int pg = P.page_table[(int64_t)s.b * P.max_pages + (tok >> P.page_shift)];
+    pg = pg < 0 ? 0 : pg;
+    a.page = pg >= P.num_pages ? P.num_pages - 1 : pg;
+  }
+}
+__device__ __forceinline__ void ahead_scales(const KernelParams& P, const Segment& s, int lane, Ahead& a) {
+  const int tok = min(a.tok0 + 16 * (lane & 3), s.L - 1);
+  const int run = (tok & ((1 << P.page_shift) - 1)) >> P.scale_shift;
+  a.ks = P.k_scale[(int64_t)a.page * P.ksc_page + (int64_t)s.kvh * P.ksc_head + run];
+  a.vs = P.v_scale[(int64_t)a.page * P.vsc_page + (int64_t)s.kvh * P.vsc_head + run];
+}
+__device__ __forceinline__ TileAt tile_at(const Ahead& a, int m) {
+  TileAt t;
+  t.tok0 = __builtin_amdgcn_readlane(a.tok0, 4 * m);
+#pragma unroll
+  for (int n = 0; n < 4; ++n) t.pg[n] = __builtin_amdgcn_readlane(a.page, 4 * m + n);
+  return t;
+}
+
+// A wavefront's running state: the output sums in the accumulators of the
+// P.V products (row 4g + r of A, dim 16d + lo), the maximum of the lane's
+// head (base 2) and the lane's share of its mass.  The maximum is a reference
+// that is moved only where a score passes it by more than 2^8 (and by the
+// first score): the sums keep their relative precision either way, and a tile
+// needs no reduction over the lanes, only a vote.
+struct State {
+  f32x4 acc[8];
+  float m, l;
+};
+
+template <int G, int FMT>
+__device__ __forceinline__ void walk_tiles(const KernelParams& P, const Segment& s, int wave, int lane,
+                                           const bf16x8 (&qa)[4], uint8_t* stage, uint16_t* parts, State& st) {
+  using C = Full<G>;
+  constexpr int REP = C::REP, COLS = C::COLS, NS = C::NS, NP = C::NP;
+  const int lo = lane & 15, g = lane >> 4, u = lo / COLS;
+  const int n_mine = s.n > wave ? (s.n - wave + kWaves - 1) / kWaves : 0;
+  if (n_mine == 0) return;
+  Ahead cur, nxt;
+  ahead_pages(P, s, wave, 0, n_mine, lane, cur);
+  nxt = cur;
+  TileAt at = tile_at(cur, 0);
+  Tile t;
+  load_k(P, s.kvh, s.L, at, lane, t);
+  load_v(P, s.kvh, s.L, at, lane, t);
+  ahead_scales(P, s, lane, cur);
+
+#pragma unroll 1
+  for (int i = 0; i < n_mine; ++i) {
+    const int m = i & 15;
+    // the next 16 tiles' pages and, half-way, their scales
+    if (m == 0) ahead_pages(P, s, wave, i + 16, n_mine, lane, nxt);
+    if (m == 8) ahead_scales(P, s, lane, nxt);
+    const int tok0 = at.tok0;
+    at = i + 1 < n_mine ? (m == 15 ? tile_at(nxt, 0) : tile_at(cur, m + 1)) : at;
+    float ks[4], vs[4];
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      ks[n] = read_lane(cur.ks, 4 * m + n);
+      vs[n] = read_lane(cur.vs, 4 * m + n);
+    }
+
+    // scores, transposed: St[n][r] is token 16n + 4g + r, head lo mod COLS
+    f32x4 St[4];
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      St[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        St[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+            __builtin_bit_cast(bf16x8, codes_bf16<FMT>(t.k[n][k >> 1], k & 1)), qa[k], St[n], 0, 0, 0);
+    }
+    // K's registers are free: the next tile's K is on its way while this one
+    // goes through the softmax and P.V (at the end the last tile once more)
+    load_k(P, s.kvh, s.L, at, lane, t);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      *reinterpret_cast<u32x4*>(stage + stage_off(8 * j + (lane >> 3), lane & 7)) = t.v[j];
+    load_v(P, s.kvh, s.L, at, lane, t);
+    __builtin_amdgcn_sched_barrier(0);
+
+    float sc[NS][4];
+    float top = kNegInf;
+#pragma unroll
+    for (int j = 0; j < NS; ++j) {
+      const float c = own_scale<REP>(ks[0], ks[1], ks[2], ks[3], j, u) * P.scale_log2;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        float x = St[REP * j][r];
+        if constexpr (REP == 2) {
+          x = u ? St[2 * j + 1][r] : x;
+        } else if constexpr (REP == 4) {
+          const float y = (u & 1) ? St[1][r] : x, z = (u & 1) ? St[3][r] : St[2][r];
+          x = (u & 2) ? z : y;
+        }
+        sc[j][r] = x * c;
+      }
+    }
+    if (tok0 + kTile > s.L) {
+#pragma unroll
+      for (int j = 0; j < NS; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (tok0 + 16 * (REP * j + u) + 4 * g + r >= s.L) sc[j][r] = kNegInf;
+    }
+#pragma unroll
+    for (int j = 0; j < NS; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) top = fmaxf(top, sc[j][r]);
+    if (__any(top > st.m + 8.0f)) {
+      if constexpr (REP >= 2) top = fmaxf(top, dpp_f<kRowRor8>(top));
+      if constexpr (REP == 4) top = fmaxf(top, dpp_f<kRowRor4>(top));
+      const float mn = fmaxf(st.m, rows_max(top));
+      const float a = st.m == kNegInf ? 0.f : fast_exp2(st.m - mn);
+      st.m = mn;
+      st.l *= a;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        // the factor of row 4g + r's head
+        float f = read_lane(a, r);
+        if constexpr (COLS >= 8) f = (g & 1) ? read_lane(a, 4 + r) : f;
+        if constexpr (COLS == 16) f = g == 2 ? read_lane(a, 8 + r) : g == 3 ? read_lane(a, 12 + r) : f;
+#pragma unroll
+        for (int d = 0; d < 8; ++d) st.acc[d][r] *= f;
+      }
+    }
+    const float ref = st.m == kNegInf ? 0.f : st.m;
+#pragma unroll
+    for (int j = 0; j < NS; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        sc[j][r] = fast_exp2(sc[j][r] - ref);
+        st.l += sc[j][r];
+      }
+
+    // P times V's scales, in three bf16 parts (24 significant bits); the
+    // parts' rows of A are laid out as in the decode kernel: up to four heads
+    // have all of them in one operand, eight in two
+    uint32_t own[NS][3][2];
+#pragma unroll
+    for (int j = 0; j < NS; ++j) {
+      const float c = own_scale<REP>(vs[0], vs[1], vs[2], vs[3], j, u);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        float a0 = sc[j][2 * e] * c, a1 = sc[j][2 * e + 1] * c;
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+          const uint32_t w = pack_bf16(a0, a1);
+          own[j][k][e] = w;
+          a0 = a0 - bf_lo(w);
+          a1 = a1 - bf_hi(w);
+          if (G <= 8 && k == 1) {
+            a0 = 0.5f * a0;
+            a1 = 0.5f * a1;
+          }
+        }
+      }
+    }
+    bf16x8 a[2][NP];
+    if constexpr (G > 8) {
+#pragma unroll
+      for (int k = 0; k < 3; ++k)
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+          a[c][k] = __builtin_bit_cast(
+              bf16x8, u32x4{own[2 * c][k][0], own[2 * c][k][1], own[2 * c + 1][k][0], own[2 * c + 1][k][1]});
+    } else {
+      const int h = lo & (COLS - 1);
+#pragma unroll
+      for (int k = 0; k < (G > 4 ? 3 : 4); ++k)
+#pragma unroll
+        for (int j = 0; j < NS; ++j)
+          *reinterpret_cast<u32x2*>(parts + (COLS * k + h) * 64 + g * 16 + 4 * (REP * j + u)) =
+              u32x2{own[j][k < 3 ? k : 2][0], own[j][k < 3 ? k : 2][1]};
+      wave_lds_order();
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        a[c][0] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(parts + lo * 64 + g * 16 + 8 * c));
+        if constexpr (NP == 2)
+          a[c][1] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(parts + (16 + h) * 64 + g * 16 + 8 * c));
+      }
+    }
+    wave_lds_order();
+
+    // P.V: element e of lane (lo, g) of K-step c is token 16(2c + e/4) + 4g +
+    // e%4, dim 16d + lo.  Source lane 2k + h of a group of 16 points a
+    // transposing read at bytes 8h .. +7 of row k's 16.
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const int k = lo >> 1, row = 16 * (2 * c + (k >> 2)) + 4 * g + (k & 3);
+#pragma unroll
+      for (int d = 0; d < 8; ++d) {
+        const u32x2 w = __builtin_bit_cast(
+            u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+                       (__attribute__((address_space(3))) v2i32*)(stage + stage_off(row, d) + 8 * (lo & 1))));
+        const bf16x8 b = __builtin_bit_cast(bf16x8, codes_bf16<FMT>(w[0], w[1]));
+#pragma unroll
+        for (int j = 0; j < NP; ++j)
+          st.acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[c][j], b, st.acc[d], 0, 0, 0);
+      }
+    }
+    wave_lds_order();   // these reads come before the next tile's writes
+    if (m == 15) cur = nxt;
+  }
+}
+
+// The wavefront's record into LDS: o (sums relative to m), m, L.
+template <int G>
+__device__ __forceinline__ void leave_record(State& st, float* rec, int lane) {
+  using C = Full<G>;
+  constexpr int ND = C::ND;
+  const int lo = lane & 15, g = lane >> 4;
+  float l = st.l;
+  if constexpr (C::REP >= 2) l = l + dpp_f<kRowRor8>(l);
+  if constexpr (C::REP == 4) l = l + dpp_f<kRowRor4>(l);
+  l = rows_sum(l);
+  // the parts' rows are added by swapping halves (then rows) of accumulators
+  f32x4 sum[ND];
+  if constexpr (G > 8) {
+#pragma unroll
+    for (int d = 0; d < ND; ++d) sum[d] = st.acc[d];
+  } else {
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const auto x = __builtin_amdgcn_permlane32_swap(__float_as_int(st.acc[d][r]), __float_as_int(st.acc[d + 4][r]), false, false);
+        st.acc[d][r] = __int_as_float(x[0]) + __int_as_float(x[1]);
+      }
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        if constexpr (G > 4) {
+          sum[d][r] = st.acc[d][r];
+        } else {
+          const auto x = __builtin_amdgcn_permlane16_swap(__float_as_int(st.acc[d][r]), __float_as_int(st.acc[d + 2][r]), false, false);
+          sum[d][r] = __int_as_float(x[0]) + __int_as_float(x[1]);
+        }
+      }
+  }
+  const int h0 = G > 8 ? 4 * g : G > 4 ? 4 * (g & 1) : 0;
+  float* const to = rec + h0 * kD + 16 * (G > 8 ? 0 : G > 4 ? 4 * (g >> 1) : 2 * g) + lo;
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+    if (r < G) {
+#pragma unroll
+      for (int d = 0; d < ND; ++d) to[r * kD + 16 * d] = sum[d][r];
+    }
+  if (g == 0 && lo < G) {
+    rec[G * kD + lo] = st.m;
+    rec[G * kD + G + lo] = l;
+  }
+}
+
+__device__ __forceinline__ void write_out(const KernelParams& P, int64_t i, float x) {
+  if (P.out_bf16) static_cast<uint16_t*>(P.out)[i] = (uint16_t)f32_to_bf16_bits(x);
+  else static_cast<float*>(P.out)[i] = x;
+}
+__device__ __forceinline__ float ln_of(float m, float L) { return (m + __log2f(L)) * 0.69314718055994531f; }
+
+// Joins `n` records (base 2 maxima): `rec(i)` points at the i-th one's floats.
+// Called by all threads for value (h, d).
+__device__ __forceinline__ float factor(float m, float top) { return m == kNegInf ? 0.f : fast_exp2(m - top); }
+
+template <int G, int FMT>
+__global__ void __launch_bounds__(kThreads, 2) full_kernel(const KernelParams P, const int most) {
+  using C = Full<G>;
+  extern __shared__ __align__(16) uint8_t lds[];
+  __shared__ int64_t s_wave[kWaves];
+  __shared__ int64_t s_base;
+  __shared__ int s_unit;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  const int units = unit_count(P), heads = unit_heads(P);
+
+  // this workgroup's part of the line
+  const int per = (units + kThreads - 1) / kThreads;
+  int64_t own = 0;
+  for (int u = tid * per; u < min(units, (tid + 1) * per); ++u) own += unit_tiles(P, u);
+  int64_t before = own;   // inclusive scan over the wavefront, then the workgroup
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int64_t x = __shfl_up((long long)before, o);
+    if (lane >= o) before += x;
+  }
+  if (lane == 63) s_wave[wave] = before;
+  __syncthreads();
+  int64_t total = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    if (w < wave) before += s_wave[w];
+    total += s_wave[w];
+  }
+  before -= own;
+  total *= heads;
+  const int64_t workers = workers_of(total, most), me = blockIdx.x;
+  if (me >= workers) return;
+  const int64_t begin = me * total / workers, end = (me + 1) * total / workers;
+  if (begin >= end) return;
+  if (before * heads <= begin && begin < (before + own) * heads) {
+    // (one thread) the unit that holds the first tile
+    int u = tid * per;
+    int64_t base = before * heads;
+    for (int64_t n; base + (n = (int64_t)unit_tiles(P, u) * heads) <= begin; ++u) base += n;
+    s_unit = u;
+    s_base = base;
+  }
+  __syncthreads();
+  int u = s_unit;
+  int64_t base = s_base;
+
+  float* const rec = reinterpret_cast<float*>(lds + wave * C::WAVE_BYTES);
+  uint8_t* const stage = lds + wave * C::WAVE_BYTES;
+  uint16_t* const parts = reinterpret_cast<uint16_t*>(stage + 8192);
+  for (int64_t x = begin; x < end;) {
+    int tiles = unit_tiles(P, u);
+    while (x >= base + (int64_t)tiles * heads) {
+      base += (int64_t)tiles * heads;
+      tiles = unit_tiles(P, ++u);
+    }
+    const int h = (int)((x - base) / tiles);
+    const int64_t start = base + (int64_t)h * tiles;   // of the group
+    Segment s;
+    s.b = per_group_units(P) ? u / P.num_kv_heads : u;
+    s.kvh = per_group_units(P) ? u % P.num_kv_heads : h;
+    s.L = seq_len(P, s.b);
+    s.t0 = (int)(x - start);
+    s.n = (int)(min(end, start + tiles) - x);
+    s.list = P.block_list ? P.block_list + (int64_t)u * P.max_list : nullptr;
+
+    bf16x8 qa[4];
+    {
+      const int head = (lane & 15) & (C::COLS - 1);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        u32x4 w{0u, 0u, 0u, 0u};
+        if (head < G)
+          w = *reinterpret_cast<const u32x4*>(P.q + ((int64_t)s.b * P.num_q_heads + s.kvh * G + head) * kD +
+                                              64 * (k >> 1) + 16 * (lane >> 4) + 8 * (k & 1));
+        qa[k] = __builtin_bit_cast(bf16x8, w);
+      }
+    }
+    State st;
+    st.m = kNegInf;
+    st.l = 0.f;
+#pragma unroll
+    for (int d = 0; d < 8; ++d) st.acc[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+    walk_tiles<G, FMT>(P, s, wave, lane, qa, stage, parts, st);
+    leave_record<G>(st, rec, lane);
+    __syncthreads();
+
+    // the wavefronts' records joined: thread tid takes values tid, tid + 256 ..
+    const bool whole = s.n == tiles;
+    // a group that began in an earlier workgroup leaves its record in this
+    // one's first place, one that began here and goes on in its second
+    float* const to = P.records + (2 * me + (s.t0 == 0 ? 1 : 0)) * P.record_floats;
+    const int64_t row0 = (int64_t)s.b * P.num_q_heads + s.kvh * G;
+#pragma unroll 1
+    for (int i = tid; i < G * kD; i += kThreads) {
+      const int h2 = i / kD;
+      float m[kWaves], top = kNegInf;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        m[w] = reinterpret_cast<const float*>(lds + w * C::WAVE_BYTES)[G * kD + h2];
+        top = fmaxf(top, m[w]);
+      }
+      float o = 0.f, L = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        const float* r = reinterpret_cast<const float*>(lds + w * C::WAVE_BYTES);
+        const float f = factor(m[w], top);
+        o += r[i] * f;
+        L += r[G * kD + G + h2] * f;
+      }
+      if (whole) {
+        write_out(P, row0 * kD + i, o / L);
+        if (i % kD == 0) P.lse[row0 + h2] = ln_of(top, L);
+      } else {
+        to[i] = o;
+        if (i % kD == 0) {
+          to[G * kD + h2] = top;
+          to[G * kD + G + h2] = L;
+        }
+      }
+    }
+    __syncthreads();   // the records are read before the next segment's tiles
+    x += s.n;
+  }
+}
+
+// The second launch: one workgroup for every query head.  Groups in several
+// workgroups are joined from their records, in the order of the line; empty
+// ones are written; every group's stop_block is its number of blocks.
+template <int G>
+__global__ void __launch_bounds__(kThreads) join_kernel(const KernelParams P, const int most) {
+  __shared__ int64_t s_sum[2][kWaves];
+  __shared__ float s_o[kThreads], s_l[kThreads];
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  const int gidx = blockIdx.x / G, hq = blockIdx.x % G;
+  const int b = gidx / P.num_kv_heads, kvh = gidx % P.num_kv_heads;
+  const int units = unit_count(P), heads = unit_heads(P);
+  const int unit = per_group_units(P) ? gidx : b;
+  int64_t before = 0, total = 0;
+  for (int u = tid; u < units; u += kThreads) {
+    const int n = unit_tiles(P, u);
+    total += n;
+    before += u < unit ? n : 0;
+  }
+  before = wave_sum(before);
+  total = wave_sum(total);
+  if (lane == 0) {
+    s_sum[0][wave] = before;
+    s_sum[1][wave] = total;
+  }
+  __syncthreads();
+  before = total = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    before += s_sum[0][w];
+    total += s_sum[1][w];
+  }
+  total *= heads;
+  const int64_t row = (int64_t)b * P.num_q_heads + kvh * G + hq;
+  const int L = seq_len(P, b), tiles = unit_tiles(P, unit);
+  if (hq == 0 && tid == 0) P.stop_block[gidx] = unit_blocks(P, unit, L);
+  if (tiles == 0) {
+    if (tid < kD) write_out(P, row * kD + tid, 0.f);
+    if (tid == 0) P.lse[row] = kNegInf;
+    return;
+  }
+  const int64_t workers = workers_of(total, most);
+  const int64_t start = before * heads + (per_group_units(P) ? 0 : (int64_t)kvh * tiles);
+  // the workgroup that holds tile x of the line: the last w with w total / workers <= x
+  const int64_t first = ((start + 1) * workers - 1) / total;
+  const int64_t last = ((start + tiles) * workers - 1) / total;
+  if (first == last) return;   // written by that workgroup
+  const int n = (int)(last - first + 1);
+  auto record = [&](int i) { return P.records + (2 * (first + i) + (i == 0 ? 1 : 0)) * P.record_floats; };
+  float top = kNegInf;
+  for (int i = lane; i < n; i += 64) top = fmaxf(top, record(i)[G * kD + hq]);
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+  float o = 0.f, l = 0.f;
+  const int d = tid & (kD - 1);
+#pragma unroll 4
+  for (int i = tid / kD; i < n; i += kThreads / kD) {
+    const float* r = record(i);
+    const float f = factor(r[G * kD + hq], top);
+    o += r[hq * kD + d] * f;
+    l += r[G * kD + G + hq] * f;
+  }
+  s_o[tid] = o;
+  s_l[tid] = l;
+  __syncthreads();
+  if (tid < kD) {
+    const float os = s_o[tid] + s_o[tid + kD], ls = s_l[tid] + s_l[tid + kD];
+    write_out(P, row * kD + tid, os / ls);
+    if (tid == 0) P.lse[row] = ln_of(top, ls);
+  }
+}
+
+template <int G, int FMT>
+int launch(const Plan& plan, const KernelParams& params, hipStream_t stream) {
+  int dev = 0, cus = 0, per_cu = 0;
+  const size_t bytes = (size_t)kWaves * Full<G>::WAVE_BYTES;
+  hipError_t e = hipGetDevice(&dev);
+  if (e == hipSuccess) e = hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev);
+  if (e == hipSuccess) e = hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, full_kernel<G, FMT>, kThreads, bytes);
+  if (e != hipSuccess) return (int)e;
+  // as many workgroups as the chip holds, two records for each in the plan's
+  // area, and no more than the longest sequences could use
+  const int64_t cap = (int64_t)params.max_pages << params.page_shift;
+  const int64_t tiles = (int64_t)plan.n_groups * max((cap + kTile - 1) / kTile, (int64_t)params.max_list * params.tiles_per_block);
+  const int64_t most = min(min((int64_t)cus * max(per_cu, 1), (int64_t)plan.n_groups * plan.max_chunks),
+                           max((int64_t)1, (tiles + kWaves - 1) / kWaves));
+  hipLaunchKernelGGL((full_kernel<G, FMT>), dim3((unsigned)most), dim3(kThreads), bytes, stream, params, (int)most);
+  e = hipGetLastError();
+  if (e != hipSuccess) return (int)e;
+  hipLaunchKernelGGL(join_kernel<G>, dim3((unsigned)(plan.n_groups * G)), dim3(kThreads), 0, stream, params, (int)most);
+  return (int)hipGetLastError();
+}
+
+template <int FMT>
+int launch_group(const Plan& plan, const KernelParams& params, hipStream_t stream) {
+  switch (plan.group) {
+    case 1: return launch<1, FMT>(plan, params, stream);
+    case 2: return launch<2, FMT>(plan, params, stream);
+    case 4: return launch<4, FMT>(plan, params, stream);
+    case 8: return launch<8, FMT>(plan, params, stream);
+    case 16: return launch<16, FMT>(plan, params, stream);
+    default: return (int)hipErrorInvalidValue;
+  }
+}
+
+}  // namespace
+
+int launch_quant_full(const Plan& plan, const KernelParams& params, int format, hipStream_t stream) {
+  return format == ART_QUANT_E4M3 ? launch_group<ART_QUANT_E4M3>(plan, params, stream)
+                                  : launch_group<ART_QUANT_INT8>(plan, params, stream);
+}
+
+}  // namespace art

@@ -97,6 +97,72 @@ def test_random_shape_against_the_oracle(i):
     assert rep.ok(), f"case {i} {c}: {rep}"
 
 
+@pytest.mark.parametrize("i", range(40))
+def test_full_attention_random_shape(i):
+    """no_detector: the same shapes and lists, against the oracle that never
+    stops."""
+    c = _draw(i)
+    _say(f"  full {i}: {c}")
+    wl = small_workload(c["seed"], batch=c["batch"], kv_heads=c["hkv"], group=c["g"],
+                        seq_len=c["lens"], block_size=c["bk"], page_size=c["ps"],
+                        dense_order=c["order"], needles=2)
+    if i % 3 == 0:
+        wl.block_list, wl.block_list_len = random_lists(wl, c["seed"], fraction=c["fraction"])
+    cache, plain = R.quantised(wl, c["form"], c["run"])
+    host = _on_gpu(plain)
+    gpu = _call(plain, R.to_device(cache, DEV), tau=1.0, phi=1.0, patience=1, no_detector=True,
+                per_head_stop=i % 2 == 0)
+    torch.cuda.synchronize()
+    rep = compare_workload(plain, gpu, tau=0.0, phi=0.0, patience=1, host=host, name="quant_full")
+    assert rep.ok(), f"case {i} {c}: {rep}"
+
+
+@pytest.mark.parametrize("g,lens", [
+    (4, [1 + 37 * (i % 9) for i in range(700)]),        # more sequences than threads
+    (8, [0, 0, 5, 0, 40000, 0, 1, 0, 0, 64, 129, 0]),   # empty ones between, one in many parts
+    (1, [90000]), (16, [30000, 17]), (2, [0] * 300 + [4000] + [0] * 300),
+])
+def test_full_attention_ragged(g, lens):
+    rng = np.random.default_rng(len(lens))
+    H, Ps, run = 1, 64, 32
+    width = -(-max(lens) // Ps)
+    P = sum(-(-n // Ps) for n in lens)
+    cache = _random_cache(rng, R.FORMATS[g % 2], P, H, Ps, run, spread=2.0)
+    order = rng.permutation(P).astype(np.int32)
+    table = np.full((len(lens), width), -5, dtype=np.int32)
+    at = 0
+    for b, n in enumerate(lens):
+        m = -(-n // Ps)
+        table[b, :m] = order[at: at + m]
+        at += m
+    q = torch.from_numpy(rng.standard_normal((len(lens), H * g, 128)).astype(np.float32)).to(DEV).bfloat16()
+    got = api.decode_attention_quant(
+        q, cache, torch.from_numpy(table).to(DEV), torch.tensor(lens, dtype=torch.int32, device=DEV),
+        block_size=64, tau=0.0, phi=0.0, patience=1, softmax_scale=0.1, no_detector=True)
+    _check_full(cache, q, table, lens, got, float(np.float32(0.1)))
+    assert got[2][:, 0].cpu().tolist() == [-(-n // 64) for n in lens]
+
+
+def test_full_attention_scores_that_rise_and_fall():
+    """Scores from -2000 to 2000 over the sequence: the running maximum moves
+    by more than any factor of fp32 holds, up and down."""
+    rng = np.random.default_rng(8)
+    Ps, n = 64, 6400
+    P = n // Ps
+    for rising in (True, False):
+        cache = _random_cache(rng, "e4m3", P, 1, Ps, 64)
+        k = cache.k.view(torch.uint8)
+        k.fill_(0x38)                                              # 1.0
+        ramp = torch.linspace(-20, 20, P, device=DEV)
+        cache.k_scale.copy_((ramp if rising else -ramp).view(P, 1, 1))
+        table = np.arange(P, dtype=np.int32).reshape(1, P)
+        q = torch.ones((1, 8, 128), dtype=torch.bfloat16, device=DEV)
+        got = api.decode_attention_quant(
+            q, cache, torch.from_numpy(table).to(DEV), torch.tensor([n], dtype=torch.int32, device=DEV),
+            block_size=64, tau=0.0, phi=0.0, patience=1, softmax_scale=1.0, no_detector=True)
+        _check_full(cache, q, table, [n], got, 1.0)
+
+
 def _bytes_on_gpu(x):
     return torch.from_numpy(np.ascontiguousarray(x)).to(DEV)
 
@@ -137,17 +203,22 @@ def test_every_code(form, g):
     assert torch.all(stop == 1)
 
 
-def _dequantised(cache, table, length, h):
+def _host(cache):
+    """The cache's arrays in numpy."""
+    return [t.view(torch.uint8).cpu().numpy() for t in cache[:2]] + [t.cpu().numpy().astype(np.float64) for t in cache[2:]]
+
+
+def _dequantised(cache, table, length, h, host=None):
     """fp64 K and V [length][D] of one sequence and head."""
     out = []
     form = "e4m3" if cache.k.dtype == torch.float8_e4m3fn else "int8"
-    for codes, scale in ((cache.k, cache.k_scale), (cache.v, cache.v_scale)):
+    k, v, ks, vs = host or _host(cache)
+    for codes, scale in ((k, ks), (v, vs)):
         Ps = codes.shape[2]
         run = Ps // scale.shape[2]
         t = np.arange(length)
         pages, slots = table[t // Ps], t % Ps
-        c = codes.view(torch.uint8).cpu().numpy()[pages, h, slots]
-        out.append(R.table(form)[c] * scale.cpu().numpy().astype(np.float64)[pages, h, slots // run][:, None])
+        out.append(R.table(form)[codes[pages, h, slots]] * scale[pages, h, slots // run][:, None])
     return out
 
 
@@ -155,14 +226,14 @@ def _check_full(cache, q, table, lens, got, softmax_scale, out_eps=0.0):
     out, lse, _ = (x.float().cpu().numpy().astype(np.float64) for x in got)
     H = cache.k.shape[1]
     g = q.shape[1] // H
-    qd = q.double().cpu().numpy()
+    qd, host = q.double().cpu().numpy(), _host(cache)
     for b, n in enumerate(lens):
         for h in range(H):
             rows = slice(h * g, (h + 1) * g)
             if n == 0:
                 assert not out[b, rows].any() and np.all(np.isneginf(lse[b, rows]))
                 continue
-            k, v = _dequantised(cache, table[b], n, h)
+            k, v = _dequantised(cache, table[b], n, h, host)
             o, l, ds = R.full_attention(qd[b, rows], k, v, softmax_scale)
             # a score off by ds moves a weight by at most a factor e^ds either way,
             # an output by 2 ds of the largest |v|; exp2, the sums over n tokens
