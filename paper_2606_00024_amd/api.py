@@ -287,32 +287,53 @@ def new_quant_cache(num_pages: int, num_kv_heads: int, page_size: int, *,
     return QuantCache(pool(), pool(), scale(), scale())
 
 
-def _quant_spec(cache: QuantCache) -> _lib.QuantCacheSpec:
+# These calls may serve single tokens, where a call's host side is most of its
+# time: every tensor is looked at once, and the structures are filled by
+# position.
+
+def _check(t, name, dtype, dev, shape):
+    """A contiguous index or output array of ``shape`` on GPU ``dev``."""
+    if t.dtype is not dtype or t.get_device() != dev:
+        _require_cuda(t, name, dtype)
+        raise ValueError(f"{name} must be on the cache's device (cuda:{dev}), got {t.device}")
+    if t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {list(shape)}")
+
+
+def _quant_spec(cache: QuantCache):
+    """(device index, pool shape, pool strides of K and V, art_quant_cache) of a
+    cache, its tensors checked."""
     k, v, ks, vs = cache
-    fmt = _QUANT_FORMATS.get(k.dtype)
-    if fmt is None or v.dtype != k.dtype:
+    dev, fmt = k.get_device(), _QUANT_FORMATS.get(k.dtype)
+    if fmt is None or v.dtype is not k.dtype:
         raise ValueError("the cache must be float8_e4m3fn or int8")
-    for t, name in ((k, "k"), (v, "v")):
-        _require_cuda(t, name)
-    for t, name in ((ks, "k_scale"), (vs, "v_scale")):
-        _require_cuda(t, name, torch.float32)
-    P, H, Ps, _ = k.shape
-    runs = ks.shape[-1] if ks.dim() == 3 else 0
-    if (tuple(ks.shape) != (P, H, runs) or tuple(vs.shape) != tuple(ks.shape) or not runs
-            or Ps % runs):
+    if dev < 0 or v.get_device() != dev or ks.get_device() != dev or vs.get_device() != dev:
+        for t, name in ((k, "k"), (v, "v"), (ks, "k_scale"), (vs, "v_scale")):
+            _require_cuda(t, name)
+        raise ValueError("the cache's tensors must be on one device")
+    if ks.dtype is not torch.float32 or vs.dtype is not torch.float32:
+        raise ValueError("k_scale and v_scale must be float32")
+    if k.dim() != 4 or v.shape != k.shape:
+        raise ValueError("k/v must both be [pages][kv_heads][page_size][head_dim]")
+    pool, a, b = k.shape, k.stride(), v.stride()
+    if a[3] != 1 or b[3] != 1:
+        raise ValueError("head_dim must be the innermost (unit-stride) dimension")
+    runs = ks.shape[2] if ks.dim() == 3 else 0
+    if not runs or ks.shape != (pool[0], pool[1], runs) or vs.shape != ks.shape or pool[2] % runs:
         raise ValueError("k_scale/v_scale must both be [pages][kv_heads][page_size / run]")
-    a, b = ks.stride(), vs.stride()
-    if runs > 1 and (a[2] != 1 or b[2] != 1):
+    c, d = ks.stride(), vs.stride()
+    if runs > 1 and (c[2] != 1 or d[2] != 1):
         raise ValueError("the runs of a page must be the scales' innermost (unit-stride) dimension")
-    return _lib.QuantCacheSpec(format=fmt, scale_tokens=Ps // runs,
-                               k_scale_stride_page=a[0], k_scale_stride_head=a[1],
-                               v_scale_stride_page=b[0], v_scale_stride_head=b[1])
+    return dev, pool, a, b, _lib.QuantCacheSpec(fmt, pool[2] // runs, c[0], c[1], d[0], d[1])
 
 
-def _same_device(dev, *tensors):
-    for t in tensors:
-        if t is not None and t.device != dev:
-            raise ValueError(f"all tensors must be on one device ({dev}), got {t.device}")
+def _on_device(dev, call, *args) -> int:
+    """call(*args, the current stream of GPU ``dev``) with that GPU current."""
+    stream = torch._C._cuda_getCurrentRawStream(dev)
+    if torch.cuda.current_device() == dev:
+        return call(*args, stream)
+    with torch.cuda.device(dev):
+        return call(*args, stream)
 
 
 def decode_attention_quant(q: torch.Tensor, cache: QuantCache, page_table: torch.Tensor,
@@ -331,92 +352,89 @@ def decode_attention_quant(q: torch.Tensor, cache: QuantCache, page_table: torch
     """``decode_attention`` over a cache held in 8 bits: K and V are the
     cache's code * scale; everything else (options, lists, workspace, results)
     is as there."""
-    _require_cuda(q, "q", torch.bfloat16)
-    _require_cuda(page_table, "page_table", torch.int32)
-    _require_cuda(seq_lens, "seq_lens", torch.int32)
-    if not q.is_contiguous() or not page_table.is_contiguous() or not seq_lens.is_contiguous():
-        raise ValueError("q, page_table and seq_lens must be contiguous")
+    dev, (P, Hkv, Ps, D), a, b, spec = _quant_spec(cache)
+    if q.dim() != 3 or page_table.dim() != 2:
+        raise ValueError("q must be [batch][q_heads][head_dim], page_table [batch][max_pages]")
+    B, Hq, _ = q.shape
+    _check(q, "q", torch.bfloat16, dev, (B, Hq, D))
+    _check(page_table, "page_table", torch.int32, dev, (B, page_table.shape[1]))
+    _check(seq_lens, "seq_lens", torch.int32, dev, (B,))
     if (block_list is None) != (block_list_len is None):
         raise ValueError("block_list and block_list_len go together")
+    max_list = 0
     if block_list is not None:
-        _require_cuda(block_list, "block_list", torch.int32)
-        _require_cuda(block_list_len, "block_list_len", torch.int32)
-        if not block_list.is_contiguous() or not block_list_len.is_contiguous():
-            raise ValueError("block_list and block_list_len must be contiguous")
-    spec = _quant_spec(cache)
-    B, Hq, D = q.shape
-    Hkv = cache.k.shape[1]
-    if page_table.dim() != 2 or page_table.shape[0] != B or tuple(seq_lens.shape) != (B,):
-        raise ValueError("page_table must be [batch][max_pages] and seq_lens [batch]")
-    dev = q.device
-    heads = Hq if per_head_stop and not no_detector else Hkv
-    _same_device(dev, *cache, page_table, seq_lens, block_list, block_list_len, workspace, out, lse,
-                 stop_block)
+        rows, max_list = ((B, Hkv) if list_per_head else (B,)), block_list.shape[-1]
+        _check(block_list, "block_list", torch.int32, dev, (*rows, max_list))
+        if block_list_len.numel() != math.prod(rows):
+            raise ValueError(f"block_list_len must hold {math.prod(rows)} lengths")
+        _check(block_list_len, "block_list_len", torch.int32, dev, block_list_len.shape)
     if softmax_scale is None:
         softmax_scale = 1.0 / math.sqrt(D)
-    shape = make_shape(q, cache.k, cache.v, page_table, block_size=block_size,
-                       block_list=block_list, list_per_head=list_per_head)
+    shape = DecodeShape(B, Hq, Hkv, D, int(block_size), Ps, P, page_table.shape[1], max_list,
+                        1 if list_per_head else 0, a[0], a[1], a[2], b[0], b[1], b[2])
     opts = make_opts(softmax_scale=softmax_scale, tau=tau, phi=phi, patience=patience,
                      dense_order=dense_order, out_dtype=out_dtype, chunk_blocks=chunk_blocks,
                      probe_stride=probe_stride, scale_of_accumulator=scale_of_accumulator,
                      no_detector=no_detector, max_wait_polls=max_wait_polls,
                      per_head_stop=per_head_stop, max_ahead_chunks=max_ahead_chunks)
+    heads = Hq if per_head_stop and not no_detector else Hkv
     if out is None:
-        out = torch.empty((B, Hq, D), dtype=out_dtype, device=dev)
+        out = torch.empty((B, Hq, D), dtype=out_dtype, device=q.device)
+    else:
+        _check(out, "out", out_dtype, dev, (B, Hq, D))
     if lse is None:
-        lse = torch.empty((B, Hq), dtype=torch.float32, device=dev)
+        lse = torch.empty((B, Hq), dtype=torch.float32, device=q.device)
+    else:
+        _check(lse, "lse", torch.float32, dev, (B, Hq))
     if stop_block is None:
-        stop_block = torch.empty((B, heads), dtype=torch.int32, device=dev)
-    need = workspace_bytes(shape, opts)
-    with torch.cuda.device(dev):
-        stream = torch.cuda.current_stream(dev).cuda_stream
-        ws = workspace if workspace is not None else _cached_workspace(need, dev, stream)
-        st = _lib.decode_attention_quant(
-            shape, opts, spec, _ptr(q), _ptr(cache.k), _ptr(cache.v), _ptr(cache.k_scale),
-            _ptr(cache.v_scale), _ptr(page_table), _ptr(seq_lens), _ptr(block_list),
-            _ptr(block_list_len), _ptr(out), _ptr(lse), _ptr(stop_block), _ptr(ws), ws.numel(),
-            stream)
+        stop_block = torch.empty((B, heads), dtype=torch.int32, device=q.device)
+    else:
+        _check(stop_block, "stop_block", torch.int32, dev, (B, heads))
+    need = _lib.workspace_bytes(shape, opts)
+    ws = workspace
+    if ws is None:
+        ws = _ws_cache.get((dev, torch._C._cuda_getCurrentRawStream(dev)))
+        if ws is None or ws.numel() < need:
+            with torch.cuda.device(dev):
+                ws = _cached_workspace(need, q.device, torch.cuda.current_stream(dev).cuda_stream)
+    elif ws.get_device() != dev or not ws.is_contiguous():
+        raise ValueError("workspace must be contiguous and on the cache's device")
+    st = _on_device(dev, _lib.decode_attention_quant, shape, opts, spec, q.data_ptr(),
+                    cache.k.data_ptr(), cache.v.data_ptr(), cache.k_scale.data_ptr(),
+                    cache.v_scale.data_ptr(), page_table.data_ptr(), seq_lens.data_ptr(),
+                    _ptr(block_list), _ptr(block_list_len), out.data_ptr(), lse.data_ptr(),
+                    stop_block.data_ptr(), ws.data_ptr(), ws.numel() * ws.element_size())
     if st != _lib.OK:
         raise ArtError(st, "art_decode_attention_quant")
     return out, lse, stop_block
 
 
 def _quant_rows_call(cache, k_rows, v_rows, page_table, positions, token_offsets):
-    """(shape, spec, rows) of an append or a read, its tensors checked."""
-    spec = _quant_spec(cache)
-    P, H, Ps, D = cache.k.shape
-    if tuple(cache.v.shape) != (P, H, Ps, D) or cache.k.stride(3) != 1 or cache.v.stride(3) != 1:
-        raise ValueError("the cache's k and v must both be [pages][kv_heads][page_size][head_dim], "
-                         "head_dim innermost")
+    """(device index, shape, spec, rows) of an append or a read, its tensors
+    checked."""
+    dev, (P, H, Ps, D), a, b, spec = _quant_spec(cache)
     kind = _ROWS_TYPES.get(k_rows.dtype)
     if kind is None:
         raise ValueError("rows must be bfloat16, float16 or float32")
-    for t, name in ((k_rows, "k"), (v_rows, "v")):
-        _require_cuda(t, name, k_rows.dtype)
-        if t.dim() != 3 or tuple(t.shape) != (k_rows.shape[0], H, D):
-            raise ValueError(f"{name} must be [rows][{H}][{D}]")
-        if t.stride(2) != 1:
-            raise ValueError("head_dim must be the innermost (unit-stride) dimension")
-    _require_cuda(page_table, "page_table", torch.int32)
-    if page_table.dim() != 2 or not page_table.is_contiguous():
-        raise ValueError("page_table must be a contiguous [batch][max_pages]")
-    B = page_table.shape[0]
-    for t, name, n in ((positions, "positions", B), (token_offsets, "token_offsets", B + 1)):
-        if t is not None:
-            _require_cuda(t, name, torch.int32)
-            if tuple(t.shape) != (n,) or not t.is_contiguous():
-                raise ValueError(f"{name} must be a contiguous [{n}]")
-    _same_device(cache.k.device, *cache, k_rows, v_rows, page_table, positions, token_offsets)
-    ks, vs = cache.k.stride(), cache.v.stride()
-    shape = DecodeShape(batch=B, num_q_heads=H, num_kv_heads=H, head_dim=D, block_size=64,
-                        page_size=Ps, num_pages=P, max_pages_per_seq=int(page_table.shape[1]),
-                        max_blocks_per_list=0, list_per_head=1,
-                        k_stride_page=ks[0], k_stride_head=ks[1], k_stride_token=ks[2],
-                        v_stride_page=vs[0], v_stride_head=vs[1], v_stride_token=vs[2])
-    a, b = k_rows.stride(), v_rows.stride()
-    rows = _lib.QuantRows(rows_dtype=kind, rows=k_rows.shape[0], k_stride_row=a[0],
-                          k_stride_head=a[1], v_stride_row=b[0], v_stride_head=b[1])
-    return shape, spec, rows
+    if k_rows.get_device() != dev or v_rows.get_device() != dev or v_rows.dtype is not k_rows.dtype:
+        for t, name in ((k_rows, "k"), (v_rows, "v")):
+            _require_cuda(t, name, k_rows.dtype)
+        raise ValueError("k and v must be on the cache's device")
+    if k_rows.dim() != 3 or k_rows.shape[1:] != (H, D) or v_rows.shape != k_rows.shape:
+        raise ValueError(f"k and v must both be [rows][{H}][{D}]")
+    c, d = k_rows.stride(), v_rows.stride()
+    if c[2] != 1 or d[2] != 1:
+        raise ValueError("head_dim must be the innermost (unit-stride) dimension")
+    if page_table.dim() != 2:
+        raise ValueError("page_table must be [batch][max_pages]")
+    B, width = page_table.shape
+    _check(page_table, "page_table", torch.int32, dev, (B, width))
+    if positions is not None:
+        _check(positions, "positions", torch.int32, dev, (B,))
+    if token_offsets is not None:
+        _check(token_offsets, "token_offsets", torch.int32, dev, (B + 1,))
+    shape = DecodeShape(B, H, H, D, 64, Ps, P, width, 0, 1, a[0], a[1], a[2], b[0], b[1], b[2])
+    return dev, shape, spec, _lib.QuantRows(kind, k_rows.shape[0], c[0], c[1], d[0], d[1])
 
 
 def quant_append(cache: QuantCache, k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor,
@@ -434,12 +452,11 @@ def quant_append(cache: QuantCache, k: torch.Tensor, v: torch.Tensor, page_table
     tokens keeps its scale unless it has to grow, and its old codes are then
     rounded anew.  ``seq_lens`` stays the caller's to advance.
     """
-    shape, spec, rows = _quant_rows_call(cache, k, v, page_table, positions, token_offsets)
-    with torch.cuda.device(k.device):
-        st = _lib.quant_append(shape, spec, rows, _ptr(k), _ptr(v), _ptr(token_offsets),
-                               _ptr(positions), _ptr(page_table), _ptr(cache.k), _ptr(cache.v),
-                               _ptr(cache.k_scale), _ptr(cache.v_scale),
-                               torch.cuda.current_stream(k.device).cuda_stream)
+    dev, shape, spec, rows = _quant_rows_call(cache, k, v, page_table, positions, token_offsets)
+    st = _on_device(dev, _lib.quant_append, shape, spec, rows, k.data_ptr(), v.data_ptr(),
+                    _ptr(token_offsets), _ptr(positions), page_table.data_ptr(),
+                    cache.k.data_ptr(), cache.v.data_ptr(), cache.k_scale.data_ptr(),
+                    cache.v_scale.data_ptr())
     if st != _lib.OK:
         raise ArtError(st, "art_quant_append")
 
@@ -459,15 +476,14 @@ def quant_read(cache: QuantCache, page_table: torch.Tensor, positions: Optional[
     if k is None or v is None:
         if rows is None:
             raise ValueError("rows is needed where k and v are not given")
-        size = (int(rows), cache.k.shape[1], cache.k.shape[3])
-        k = torch.empty(size, dtype=dtype, device=cache.k.device) if k is None else k
-        v = torch.empty(size, dtype=dtype, device=cache.k.device) if v is None else v
-    shape, spec, packed = _quant_rows_call(cache, k, v, page_table, positions, token_offsets)
-    with torch.cuda.device(k.device):
-        st = _lib.quant_read(shape, spec, packed, _ptr(cache.k), _ptr(cache.v),
-                             _ptr(cache.k_scale), _ptr(cache.v_scale), _ptr(token_offsets),
-                             _ptr(positions), _ptr(page_table), _ptr(k), _ptr(v),
-                             torch.cuda.current_stream(k.device).cuda_stream)
+        size, on = (int(rows), cache.k.shape[1], cache.k.shape[3]), cache.k.device
+        k = torch.empty(size, dtype=dtype, device=on) if k is None else k
+        v = torch.empty(size, dtype=dtype, device=on) if v is None else v
+    dev, shape, spec, packed = _quant_rows_call(cache, k, v, page_table, positions, token_offsets)
+    st = _on_device(dev, _lib.quant_read, shape, spec, packed, cache.k.data_ptr(),
+                    cache.v.data_ptr(), cache.k_scale.data_ptr(), cache.v_scale.data_ptr(),
+                    _ptr(token_offsets), _ptr(positions), page_table.data_ptr(), k.data_ptr(),
+                    v.data_ptr())
     if st != _lib.OK:
         raise ArtError(st, "art_quant_read")
     return k, v

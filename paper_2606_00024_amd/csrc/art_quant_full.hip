@@ -17,6 +17,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "art_internal.h"
 #include "art_wave.h"
 
@@ -620,19 +622,37 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const KernelParams P, co
   }
 }
 
+// Workgroups of full_kernel that the current device holds at once (asked of
+// the runtime once per device: the two queries cost about a microsecond).
+template <int G, int FMT>
+hipError_t resident(int* n) {
+  constexpr int kDevices = 64;
+  static std::atomic<int> known[kDevices];
+  int dev = 0, cus = 0, per_cu = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return e;
+  *n = dev < kDevices ? known[dev].load(std::memory_order_relaxed) : 0;
+  if (*n > 0) return hipSuccess;
+  e = hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev);
+  if (e == hipSuccess)
+    e = hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, full_kernel<G, FMT>, kThreads,
+                                                     (size_t)kWaves * Full<G>::WAVE_BYTES);
+  *n = cus * max(per_cu, 1);
+  if (e == hipSuccess && dev < kDevices) known[dev].store(*n, std::memory_order_relaxed);
+  return e;
+}
+
 template <int G, int FMT>
 int launch(const Plan& plan, const KernelParams& params, hipStream_t stream) {
-  int dev = 0, cus = 0, per_cu = 0;
   const size_t bytes = (size_t)kWaves * Full<G>::WAVE_BYTES;
-  hipError_t e = hipGetDevice(&dev);
-  if (e == hipSuccess) e = hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev);
-  if (e == hipSuccess) e = hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, full_kernel<G, FMT>, kThreads, bytes);
+  int held = 0;
+  hipError_t e = resident<G, FMT>(&held);
   if (e != hipSuccess) return (int)e;
   // as many workgroups as the chip holds, two records for each in the plan's
   // area, and no more than the longest sequences could use
   const int64_t cap = (int64_t)params.max_pages << params.page_shift;
   const int64_t tiles = (int64_t)plan.n_groups * max((cap + kTile - 1) / kTile, (int64_t)params.max_list * params.tiles_per_block);
-  const int64_t most = min(min((int64_t)cus * max(per_cu, 1), (int64_t)plan.n_groups * plan.max_chunks),
+  const int64_t most = min(min((int64_t)held, (int64_t)plan.n_groups * plan.max_chunks),
                            max((int64_t)1, (tiles + kWaves - 1) / kWaves));
   hipLaunchKernelGGL((full_kernel<G, FMT>), dim3((unsigned)most), dim3(kThreads), bytes, stream, params, (int)most);
   e = hipGetLastError();
