@@ -485,6 +485,12 @@ struct QuantTile {
   u32x4 k[4][2];
   u32x4 v[8];
 };
+// The scales of the loader's tiles: lane 4m + n holds those of 16-token group
+// n of tile m, read only after the tile's own loads have been issued.
+struct QuantScales {
+  float k, v;
+  int m;
+};
 
 __device__ __forceinline__ void load_codes(Params& P, int kvh, int L, int tok0, const int (&pg)[4], int lane,
                                            QuantTile& t) {
@@ -512,24 +518,13 @@ __device__ __forceinline__ void load_codes(Params& P, int kvh, int L, int tok0, 
   }
 }
 
-__device__ __forceinline__ void load_scales(Params& P, int kvh, int L, int tok0, const int (&pg)[4], float (&ksc)[4],
-                                            float (&vsc)[4]) {
-  const int psz_mask = (1 << P.page_shift) - 1;
-#pragma unroll
-  for (int n = 0; n < 4; ++n) {
-    const int run = (min(tok0 + 16 * n, L - 1) & psz_mask) >> P.scale_shift;
-    ksc[n] = P.k_scale[(int64_t)pg[n] * P.ksc_page + (int64_t)kvh * P.ksc_head + run];
-    vsc[n] = P.v_scale[(int64_t)pg[n] * P.vsc_page + (int64_t)kvh * P.vsc_head + run];
-  }
-}
-
 // The first tile of a block writes the block record; each later tile of
 // the block (accumulate) is folded into it: both parts rescaled to the
 // larger running max and the combined mass, in tile order.
 template <int G, bool WIDE>
 __device__ void compute_tile(Params& P, int kvh, int L, int tok0, const int (&pg)[4],
                              const bf16x8 (&qa)[4], uint16_t* __restrict__ vbuf,
-                             float* __restrict__ rec, bool accumulate) {
+                             float* __restrict__ rec, bool accumulate, const QuantScales& scales) {
   const int lane = threadIdx.x & 63;
   const int lo = lane & 15, g = lane >> 4;
   const int psz_mask = (1 << P.page_shift) - 1;
@@ -556,11 +551,9 @@ __device__ void compute_tile(Params& P, int kvh, int L, int tok0, const int (&pg
   // 64-bit multiplies per lane (36 of them) kept a tile's first loads waiting.
   u32x4 kr[4][4];
   u32x4 vr[16];
-  QuantTile qt;
-  float ksc[4], vsc[4];   // scales of the 16-token groups
+  QuantTile codes;
   if constexpr (kFormat != 0) {
-    load_codes(P, kvh, L, tok0, pg, lane, qt);
-    load_scales(P, kvh, L, tok0, pg, ksc, vsc);
+    load_codes(P, kvh, L, tok0, pg, lane, codes);
   } else if constexpr (!WIDE) {
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
@@ -618,8 +611,16 @@ __device__ void compute_tile(Params& P, int kvh, int L, int tok0, const int (&pg
     for (int s = 0; s < 4; ++s) {
       u32x4 kf;
       if constexpr (kFormat == 0) kf = kr[n][s];
-      else kf = codes_bf16<kFormat - 1>(qt.k[n][s >> 1], s & 1);
+      else kf = codes_bf16<kFormat - 1>(codes.k[n][s >> 1], s & 1);
       St[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf), qa[s], St[n], 0, 0, 0);
+    }
+  }
+  float ksc[4], vsc[4];
+  if constexpr (kFormat != 0) {
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      ksc[n] = read_lane(scales.k, 4 * scales.m + n);
+      vsc[n] = read_lane(scales.v, 4 * scales.m + n);
     }
   }
   // softmax of the lane's head over the tile: the lane's own tokens, the
@@ -742,7 +743,26 @@ __device__ void compute_tile(Params& P, int kvh, int L, int tok0, const int (&pg
 #pragma unroll
   for (int d = 0; d < 8; ++d) acc[d] = f32x4{0.f, 0.f, 0.f, 0.f};
   const int rk = lo >> 2, cq = lo & 3;
-  if constexpr (G >= 8) {
+  if constexpr (kFormat != 0) {
+    // codes: half a tile (4 KiB) at a time, transposed as bytes and converted
+    // in the operand's registers
+    uint8_t* const stage = reinterpret_cast<uint8_t*>(vbuf);
+    const int k = lo >> 1, row = 16 * (k >> 2) + 4 * g + (k & 3);
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<u32x4*>(stage + code_stage_off(8 * i + (lane >> 3), lane & 7)) = codes.v[4 * c + i];
+      wave_lds_order();
+#pragma unroll
+      for (int d = 0; d < 8; ++d) {
+        const bf16x8 b = codes_tr<kFormat - 1>(stage, row, d, lo);
+#pragma unroll
+        for (int j = 0; j < NP; ++j) acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[c][j], b, acc[d], 0, 0, 0);
+      }
+      wave_lds_order();  // the reads of this half come before the next half's writes
+    }
+  } else if constexpr (G >= 8) {
     // a quarter at a time, the first quarter's B parts (elements 0..3) kept
     // in registers until the second's are read
 #pragma unroll
@@ -750,18 +770,9 @@ __device__ void compute_tile(Params& P, int kvh, int L, int tok0, const int (&pg
       v4i16 r0[8];
 #pragma unroll
       for (int qh = 0; qh < 2; ++qh) {
-        if constexpr (kFormat == 0) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            *reinterpret_cast<u32x4*>(vbuf + vstage_off(4 * i + g, lo)) = vr[8 * c + 4 * qh + i];
-        } else {
-#pragma unroll
-          for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int e = 0; e < 2; ++e)
-              *reinterpret_cast<u32x4*>(vbuf + vstage_off(8 * i + (lane >> 3), 2 * (lane & 7) + e)) =
-                  codes_bf16<kFormat - 1>(qt.v[4 * c + 2 * qh + i], e);
-        }
+        for (int i = 0; i < 4; ++i)
+          *reinterpret_cast<u32x4*>(vbuf + vstage_off(4 * i + g, lo)) = vr[8 * c + 4 * qh + i];
         wave_lds_order();
 #pragma unroll
         for (int d = 0; d < 8; ++d) {
@@ -784,18 +795,9 @@ __device__ void compute_tile(Params& P, int kvh, int L, int tok0, const int (&pg
     // of a group on 32 distinct banks
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
-      if constexpr (kFormat == 0) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          *reinterpret_cast<u32x4*>(vbuf + (4 * i + g) * kVPitch + 8 * lo) = vr[8 * c + i];
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int e = 0; e < 2; ++e)
-            *reinterpret_cast<u32x4*>(vbuf + (8 * i + (lane >> 3)) * kVPitch + 16 * (lane & 7) + 8 * e) =
-                codes_bf16<kFormat - 1>(qt.v[4 * c + i], e);
-      }
+      for (int i = 0; i < 8; ++i)
+        *reinterpret_cast<u32x4*>(vbuf + (4 * i + g) * kVPitch + 8 * lo) = vr[8 * c + i];
       wave_lds_order();
 #pragma unroll
       for (int d = 0; d < 8; ++d) {
@@ -1219,6 +1221,13 @@ __device__ void write_empty_wave(Params& P, int b, int kvh, int lane) {
 }
 
 constexpr int kLoaders = kWaves - 1;   // wavefronts 1..3 stream tiles
+// Workgroups that share a CU (a wavefront of each on every SIMD).  A tile of
+// codes is half the bytes of a bf16 tile and waits as long for them, so groups
+// of up to 4 heads, whose chunk buffers leave the LDS for it, have three where
+// the registers allow (168): 8 x 32K tokens, int8, the test never passing, 143
+// us with two and 135 with three, thresholds of 1e-2 77 and 69.
+template <int G>
+constexpr int kWorkgroupsPerCu = kFormat != 0 && G <= 4 ? 3 : 2;
 constexpr int kSlots = kChunkSlots;    // chunk buffers in LDS
 constexpr int kLenCache = 256;         // sequence lengths kept in LDS
 enum SlotState : int { kSlotFree = 0, kSlotLoading = 1, kSlotReady = 2, kSlotEnd = 3 };
@@ -1815,7 +1824,7 @@ __device__ void resolve_chunk(Params& P, int gidx, int k, const GroupInfo& gi,
 // only once a buffer is free, and every wait targets a chunk claimed
 // earlier, so the launch always makes progress.
 template <int G, bool PH, bool WIDE>
-__global__ void __launch_bounds__(kThreads, 2) art_decode_kernel(const KernelParams) {
+__global__ void __launch_bounds__(kThreads, kWorkgroupsPerCu<G>) art_decode_kernel(const KernelParams) {
   Params* const args = (Params*)__builtin_amdgcn_kernarg_segment_ptr();
   // the dynamic buffers must start 16-byte aligned (128-bit LDS accesses):
   // the static block below is a multiple of 16 bytes
@@ -1862,12 +1871,13 @@ __global__ void __launch_bounds__(kThreads, 2) art_decode_kernel(const KernelPar
   }
 
   // ---------------- loaders ----------------
-  const int lw = wave - 1;
+  // (of codes, in a scalar register: what follows from it is then scalar too)
+  const int lw = kFormat != 0 ? __builtin_amdgcn_readfirstlane(wave - 1) : wave - 1;
   // (a loader's own staging buffer after the chunk buffers, 16-byte aligned:
   // a half tile, or a quarter tile for 8 or more heads; unused when V is
   // staged in the records)
   uint16_t* vbuf = reinterpret_cast<uint16_t*>(smem + ((kSlots * slot_floats + 3) & ~3)) +
-                   lw * (G >= 8 ? 16 * kVRow : kVBufU16);
+                   lw * (kFormat != 0 ? kCodeStage / 2 : G >= 8 ? 16 * kVRow : kVBufU16);
   // leader: the queue it claims from (its own first, as many workgroups to
   // each as it has groups, then the others in turn once its own is used up),
   // the queues that may still hold work (those past
@@ -2040,6 +2050,16 @@ __global__ void __launch_bounds__(kThreads, 2) art_decode_kernel(const KernelPar
           if (my_tok0 < gi.L) my_page = clamp_page(P, gi.b, min(my_tok0 + 16 * n, gi.L - 1));
         }
       }
+      // the scales of the same 16-token groups
+      float my_ks = 0.f, my_vs = 0.f;
+      if constexpr (kFormat != 0) {
+        if (my_tok0 < gi.L) {
+          const int tok = min(my_tok0 + 16 * (lane & 3), gi.L - 1);
+          const int run = (tok & ((1 << P.page_shift) - 1)) >> P.scale_shift;
+          my_ks = P.k_scale[(int64_t)my_page * P.ksc_page + (int64_t)gi.kvh * P.ksc_head + run];
+          my_vs = P.v_scale[(int64_t)my_page * P.vsc_page + (int64_t)gi.kvh * P.vsc_head + run];
+        }
+      }
       if (stop_word_before(sw0, P.epoch, k)) {
         aborted = true;
         // (with one group per queue the claims of its last chunks keep its
@@ -2054,9 +2074,10 @@ __global__ void __launch_bounds__(kThreads, 2) art_decode_kernel(const KernelPar
         const int tok0 = __builtin_amdgcn_readlane(my_tok0, 4 * m);
         const int pg[4] = {__builtin_amdgcn_readlane(my_page, 4 * m), __builtin_amdgcn_readlane(my_page, 4 * m + 1),
                            __builtin_amdgcn_readlane(my_page, 4 * m + 2), __builtin_amdgcn_readlane(my_page, 4 * m + 3)};
+        const QuantScales scales{my_ks, my_vs, m};
         compute_tile<G, WIDE>(*fresh(args), gi.kvh, gi.L, tok0, pg, qa,
                         P.v_in_record ? reinterpret_cast<uint16_t*>(blocks + i * REC) : vbuf,
-                        blocks + i * REC, j > 0);
+                        blocks + i * REC, j > 0, scales);
         if (stop_word_before(sw, P.epoch, k)) {
           aborted = true;
           break;
@@ -2087,15 +2108,23 @@ int launch_w(const Plan& plan, const KernelParams& params, hipStream_t stream) {
   const int64_t work = (int64_t)plan.n_groups * plan.max_chunks;
   if (work <= 0) return (int)hipSuccess;
   int dev = 0, cus = 0, per_cu = 0;
+  // (the plan counts the staging buffers of bf16 tiles)
+  size_t lds = plan.lds_bytes;
+  if (kFormat != 0)
+    lds = (size_t)kChunkSlots * plan.chunk_blocks * Cfg<G>::REC * 4 +
+          (plan.v_in_record ? 0 : (size_t)kLoaders * kCodeStage + 16);
   hipError_t e = hipGetDevice(&dev);
   if (e == hipSuccess) e = hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev);
   if (e == hipSuccess)
-    e = hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, art_decode_kernel<G, PH, WIDE>, kThreads, plan.lds_bytes);
+    e = hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, art_decode_kernel<G, PH, WIDE>, kThreads, lds);
   if (e != hipSuccess) return (int)e;
   if (per_cu < 1) per_cu = 1;
   // As many workgroups as the chip holds, but no more than the plan allows
   // per group (and never fewer than one per CU).
-  const int64_t per_groups = max((int64_t)cus, (int64_t)plan.group_workgroups * plan.n_groups);
+  // (Two per CU over codes, whose chunks take half as long: 512K tokens, int8,
+  // the test never passing, 323 us with one and 271 with two, three no better;
+  // thresholds of 1e-2 80, 70 and 91.)
+  const int64_t per_groups = max((int64_t)(kFormat != 0 ? 2 : 1) * cus, (int64_t)plan.group_workgroups * plan.n_groups);
   const int64_t grid = min(work, min((int64_t)cus * per_cu, per_groups));
   // Chunks of one group in flight at once: about the launch's chunk buffers
   // over the groups.  Up to 8 (many groups), a chunk of a group of 8 or
@@ -2107,7 +2136,7 @@ int launch_w(const Plan& plan, const KernelParams& params, hipStream_t stream) {
   p.look_first = grid * kChunkSlots <= (int64_t)8 * plan.n_groups ? 1 : 0;
   auto kernel = art_decode_kernel<G, PH, WIDE>;
   hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(kThreads),
-                     plan.lds_bytes, stream, p);
+                     lds, stream, p);
   return (int)hipGetLastError();
 }
 

@@ -75,6 +75,10 @@ __device__ __forceinline__ int64_t workers_of(int64_t total, int64_t most) {
   return max((int64_t)1, min(most, (total + kWaves - 1) / kWaves));
 }
 
+__device__ __forceinline__ int64_t uniform(int64_t x) {
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((int)x), hi = __builtin_amdgcn_readfirstlane((int)(x >> 32));
+  return (int64_t)((uint64_t)hi << 32 | lo);
+}
 __device__ __forceinline__ int64_t wave_sum(int64_t x) {
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) x += __shfl_xor((long long)x, o);
@@ -122,13 +126,6 @@ __device__ __forceinline__ void load_v(const KernelParams& P, int kvh, int L, co
       t.v[2 * n + j] = *reinterpret_cast<const u32x4*>(b + o);
     }
   }
-}
-
-// V's stage: token r's 16-byte piece j sits at piece j ^ swizzle(r), so that
-// the eight rows a transposing read touches (tokens 4g .. 4g + 3 and 16 more
-// of each, for two lane groups at once) fall on distinct banks.
-__device__ __forceinline__ int stage_off(int r, int j) {
-  return r * 128 + ((j ^ (((r >> 1) & 1) | ((r >> 4) & 1) << 1 | ((r >> 2) & 1) << 2)) << 4);
 }
 
 // What a wavefront reads ahead for 16 of its tiles: lane 4m + n holds the page
@@ -198,23 +195,30 @@ __device__ __forceinline__ void walk_tiles(const KernelParams& P, const Segment&
   const int lo = lane & 15, g = lane >> 4, u = lo / COLS;
   const int n_mine = s.n > wave ? (s.n - wave + kWaves - 1) / kWaves : 0;
   if (n_mine == 0) return;
-  Ahead cur, nxt;
+  // Pages are fetched two sets of 16 tiles ahead and scales one, before the
+  // loads of a set's first tile: no wait for them then holds up for the tiles
+  // in flight behind them.
+  Ahead cur, nxt, far;
   ahead_pages(P, s, wave, 0, n_mine, lane, cur);
-  nxt = cur;
+  ahead_pages(P, s, wave, 16, n_mine, lane, nxt);
+  ahead_scales(P, s, lane, cur);
   TileAt at = tile_at(cur, 0);
   Tile t;
   load_k(P, s.kvh, s.L, at, lane, t);
   load_v(P, s.kvh, s.L, at, lane, t);
-  ahead_scales(P, s, lane, cur);
 
 #pragma unroll 1
-  for (int i = 0; i < n_mine; ++i) {
-    const int m = i & 15;
-    // the next 16 tiles' pages and, half-way, their scales
-    if (m == 0) ahead_pages(P, s, wave, i + 16, n_mine, lane, nxt);
-    if (m == 8) ahead_scales(P, s, lane, nxt);
+  for (int first = 0; first < n_mine; first += 16) {
+  const int n_set = min(16, n_mine - first);
+  const TileAt over = tile_at(nxt, 0);
+  ahead_scales(P, s, lane, nxt);
+  ahead_pages(P, s, wave, first + 32, n_mine, lane, far);
+#pragma unroll 1
+  for (int m = 0; m < n_set; ++m) {
     const int tok0 = at.tok0;
-    at = i + 1 < n_mine ? (m == 15 ? tile_at(nxt, 0) : tile_at(cur, m + 1)) : at;
+    // (behind the last tile, that tile once more)
+    if (m + 1 < n_set) at = tile_at(cur, m + 1);
+    else if (first + 16 < n_mine) at = over;
     float ks[4], vs[4];
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
@@ -238,7 +242,7 @@ __device__ __forceinline__ void walk_tiles(const KernelParams& P, const Segment&
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int j = 0; j < 8; ++j)
-      *reinterpret_cast<u32x4*>(stage + stage_off(8 * j + (lane >> 3), lane & 7)) = t.v[j];
+      *reinterpret_cast<u32x4*>(stage + code_stage_off(8 * j + (lane >> 3), lane & 7)) = t.v[j];
     load_v(P, s.kvh, s.L, at, lane, t);
     __builtin_amdgcn_sched_barrier(0);
 
@@ -346,24 +350,22 @@ __device__ __forceinline__ void walk_tiles(const KernelParams& P, const Segment&
     wave_lds_order();
 
     // P.V: element e of lane (lo, g) of K-step c is token 16(2c + e/4) + 4g +
-    // e%4, dim 16d + lo.  Source lane 2k + h of a group of 16 points a
-    // transposing read at bytes 8h .. +7 of row k's 16.
+    // e%4, dim 16d + lo
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
       const int k = lo >> 1, row = 16 * (2 * c + (k >> 2)) + 4 * g + (k & 3);
 #pragma unroll
       for (int d = 0; d < 8; ++d) {
-        const u32x2 w = __builtin_bit_cast(
-            u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32(
-                       (__attribute__((address_space(3))) v2i32*)(stage + stage_off(row, d) + 8 * (lo & 1))));
-        const bf16x8 b = __builtin_bit_cast(bf16x8, codes_bf16<FMT>(w[0], w[1]));
+        const bf16x8 b = codes_tr<FMT>(stage, row, d, lo);
 #pragma unroll
         for (int j = 0; j < NP; ++j)
           st.acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[c][j], b, st.acc[d], 0, 0, 0);
       }
     }
     wave_lds_order();   // these reads come before the next tile's writes
-    if (m == 15) cur = nxt;
+  }
+  cur = nxt;
+  nxt = far;
   }
 }
 
@@ -433,7 +435,9 @@ __global__ void __launch_bounds__(kThreads, 2) full_kernel(const KernelParams P,
   __shared__ int64_t s_wave[kWaves];
   __shared__ int64_t s_base;
   __shared__ int s_unit;
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  // (the wavefront's number in a scalar register: everything that follows from
+  // it, page addresses above all, then stays there too)
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int units = unit_count(P), heads = unit_heads(P);
 
   // this workgroup's part of the line
@@ -455,10 +459,10 @@ __global__ void __launch_bounds__(kThreads, 2) full_kernel(const KernelParams P,
     total += s_wave[w];
   }
   before -= own;
-  total *= heads;
+  total = uniform(total * heads);
   const int64_t workers = workers_of(total, most), me = blockIdx.x;
   if (me >= workers) return;
-  const int64_t begin = me * total / workers, end = (me + 1) * total / workers;
+  const int64_t begin = uniform(me * total / workers), end = uniform((me + 1) * total / workers);
   if (begin >= end) return;
   if (before * heads <= begin && begin < (before + own) * heads) {
     // (one thread) the unit that holds the first tile
@@ -469,24 +473,24 @@ __global__ void __launch_bounds__(kThreads, 2) full_kernel(const KernelParams P,
     s_base = base;
   }
   __syncthreads();
-  int u = s_unit;
-  int64_t base = s_base;
+  int u = __builtin_amdgcn_readfirstlane(s_unit);
+  int64_t base = uniform(s_base);
 
   float* const rec = reinterpret_cast<float*>(lds + wave * C::WAVE_BYTES);
   uint8_t* const stage = lds + wave * C::WAVE_BYTES;
   uint16_t* const parts = reinterpret_cast<uint16_t*>(stage + 8192);
   for (int64_t x = begin; x < end;) {
-    int tiles = unit_tiles(P, u);
+    int tiles = __builtin_amdgcn_readfirstlane(unit_tiles(P, u));
     while (x >= base + (int64_t)tiles * heads) {
       base += (int64_t)tiles * heads;
-      tiles = unit_tiles(P, ++u);
+      tiles = __builtin_amdgcn_readfirstlane(unit_tiles(P, ++u));
     }
-    const int h = (int)((x - base) / tiles);
+    const int h = __builtin_amdgcn_readfirstlane((int)((x - base) / tiles));
     const int64_t start = base + (int64_t)h * tiles;   // of the group
     Segment s;
     s.b = per_group_units(P) ? u / P.num_kv_heads : u;
     s.kvh = per_group_units(P) ? u % P.num_kv_heads : h;
-    s.L = seq_len(P, s.b);
+    s.L = __builtin_amdgcn_readfirstlane(seq_len(P, s.b));
     s.t0 = (int)(x - start);
     s.n = (int)(min(end, start + tiles) - x);
     s.list = P.block_list ? P.block_list + (int64_t)u * P.max_list : nullptr;

@@ -144,6 +144,24 @@ __device__ __forceinline__ u32x4 codes_bf16(const u32x4& w, int half) {
   return codes_bf16<FMT>(w[2 * half], w[2 * half + 1]);
 }
 
+// V's codes in LDS, 128 bytes a token: token r's 16-byte piece j sits at piece
+// j ^ swizzle(r), so that the eight rows that a transposing read touches
+// (tokens 4g .. 4g + 3 and 16 more of each, for two lane groups at once) fall
+// on distinct banks.  Half a tile takes kCodeStage bytes.
+constexpr int kCodeStage = 32 * 128;
+__device__ __forceinline__ int code_stage_off(int r, int j) {
+  return r * 128 + ((j ^ (((r >> 1) & 1) | ((r >> 4) & 1) << 1 | ((r >> 2) & 1) << 2)) << 4);
+}
+// The B operand of a P.V product (32 tokens x dims 16d .. 16d + 15): source
+// lane 2k + h of each 16 points the transposing read at bytes 8h .. +7 of the
+// 16 that row k has there, and lane i receives byte i of all eight rows.
+template <int FMT>
+__device__ __forceinline__ bf16x8 codes_tr(uint8_t* stage, int row, int d, int lo) {
+  const v2i32 w = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+      (__attribute__((address_space(3))) v2i32*)(stage + code_stage_off(row, d) + 8 * (lo & 1)));
+  return __builtin_bit_cast(bf16x8, codes_bf16<FMT>((uint32_t)w[0], (uint32_t)w[1]));
+}
+
 // Scores are computed in REP copies over the 16 columns of the matrix
 // instruction, and copy u keeps those of the 16-token groups REP i + u: the
 // scale of such a group out of those of the tile's four.
