@@ -4,7 +4,9 @@
 // cut for the memory system alone.  The 64-token tiles of all (sequence, KV
 // head) groups form one line, and every workgroup takes an equal, contiguous
 // part of it, however ragged the batch is; the part of a group in a
-// workgroup's range is a segment.  The four wavefronts of a workgroup take a
+// workgroup's range is a segment.  (Where that leaves a workgroup few tiles, a
+// second segment costs more than an uneven share: groups are then cut into
+// equal parts, a workgroup to each.)  The four wavefronts of a workgroup take a
 // segment's tiles in turn, each with its own running maximum, mass and output
 // sums in registers, and join at its end through LDS.  A group that lies in
 // one workgroup is written out there; of the others each segment leaves a
@@ -70,10 +72,24 @@ __device__ __forceinline__ int unit_tiles(const KernelParams& P, int u) {
 }
 __device__ __forceinline__ int unit_heads(const KernelParams& P) { return per_group_units(P) ? 1 : P.num_kv_heads; }
 
-// Workgroups that share `total` tiles: every wavefront gets one, at least.
-__device__ __forceinline__ int64_t workers_of(int64_t total, int64_t most) {
-  return max((int64_t)1, min(most, (total + kWaves - 1) / kWaves));
+// How `total` tiles are cut for at most `most` workgroups; every wavefront gets
+// a tile, at least.  part == 0: the line in `workers` equal ranges.  part > 0:
+// every group in parts of that many tiles (of which there are no more than
+// `most`), where a range would hold 16 tiles or fewer.
+struct Cut {
+  int64_t workers;
+  int part;
+};
+__device__ __forceinline__ Cut cut_of(const KernelParams& P, int64_t total, int64_t most) {
+  const int64_t groups = (int64_t)P.batch * P.num_kv_heads;
+  Cut c{max((int64_t)1, min(most, (total + kWaves - 1) / kWaves)), 0};
+  if (2 * groups <= most && total <= 16 * most) {
+    const int64_t room = most - groups;
+    c.part = max((int)((total + room - 1) / room), kWaves);
+  }
+  return c;
 }
+__device__ __forceinline__ int parts_of(int tiles, int part) { return (tiles + part - 1) / part; }
 
 __device__ __forceinline__ int64_t uniform(int64_t x) {
   const uint32_t lo = __builtin_amdgcn_readfirstlane((int)x), hi = __builtin_amdgcn_readfirstlane((int)(x >> 32));
@@ -432,7 +448,7 @@ template <int G, int FMT>
 __global__ void __launch_bounds__(kThreads, 2) full_kernel(const KernelParams P, const int most) {
   using C = Full<G>;
   extern __shared__ __align__(16) uint8_t lds[];
-  __shared__ int64_t s_wave[kWaves];
+  __shared__ int64_t s_wave[2][kWaves];
   __shared__ int64_t s_base;
   __shared__ int s_unit;
   // (the wavefront's number in a scalar register: everything that follows from
@@ -440,35 +456,55 @@ __global__ void __launch_bounds__(kThreads, 2) full_kernel(const KernelParams P,
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int units = unit_count(P), heads = unit_heads(P);
 
-  // this workgroup's part of the line
+  // this workgroup's part of the line: a sum over the units, then a scan of
+  // their tiles (or parts) that finds the unit where it begins
   const int per = (units + kThreads - 1) / kThreads;
+  const int u0 = tid * per, u1 = min(units, u0 + per);
   int64_t own = 0;
-  for (int u = tid * per; u < min(units, (tid + 1) * per); ++u) own += unit_tiles(P, u);
+  for (int u = u0; u < u1; ++u) own += unit_tiles(P, u);
+  int64_t total = wave_sum(own);
+  if (lane == 0) s_wave[0][wave] = total;
+  __syncthreads();
+  total = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) total += s_wave[0][w];
+  total = uniform(total * heads);
+  const Cut cut = cut_of(P, total, most);
+  auto weight = [&](int u) {
+    const int n = unit_tiles(P, u);
+    return (int64_t)heads * (cut.part ? parts_of(n, cut.part) : n);
+  };
+  own *= heads;
+  if (cut.part) {
+    own = 0;
+    for (int u = u0; u < u1; ++u) own += weight(u);
+  }
   int64_t before = own;   // inclusive scan over the wavefront, then the workgroup
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
     const int64_t x = __shfl_up((long long)before, o);
     if (lane >= o) before += x;
   }
-  if (lane == 63) s_wave[wave] = before;
+  if (lane == 63) s_wave[1][wave] = before;
   __syncthreads();
-  int64_t total = 0;
+  int64_t line = 0;
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) {
-    if (w < wave) before += s_wave[w];
-    total += s_wave[w];
+    if (w < wave) before += s_wave[1][w];
+    line += s_wave[1][w];
   }
   before -= own;
-  total = uniform(total * heads);
-  const int64_t workers = workers_of(total, most), me = blockIdx.x;
+  line = uniform(line);   // tiles of the line, or parts
+  const int64_t workers = cut.part ? line : cut.workers, me = blockIdx.x;
   if (me >= workers) return;
-  const int64_t begin = uniform(me * total / workers), end = uniform((me + 1) * total / workers);
+  const int64_t begin = cut.part ? me : uniform(me * line / workers);
+  const int64_t end = cut.part ? me + 1 : uniform((me + 1) * line / workers);
   if (begin >= end) return;
-  if (before * heads <= begin && begin < (before + own) * heads) {
+  if (before <= begin && begin < before + own) {
     // (one thread) the unit that holds the first tile
-    int u = tid * per;
-    int64_t base = before * heads;
-    for (int64_t n; base + (n = (int64_t)unit_tiles(P, u) * heads) <= begin; ++u) base += n;
+    int u = u0;
+    int64_t base = before;
+    for (int64_t n; base + (n = weight(u)) <= begin; ++u) base += n;
     s_unit = u;
     s_base = base;
   }
@@ -481,18 +517,20 @@ __global__ void __launch_bounds__(kThreads, 2) full_kernel(const KernelParams P,
   uint16_t* const parts = reinterpret_cast<uint16_t*>(stage + 8192);
   for (int64_t x = begin; x < end;) {
     int tiles = __builtin_amdgcn_readfirstlane(unit_tiles(P, u));
-    while (x >= base + (int64_t)tiles * heads) {
+    while (!cut.part && x >= base + (int64_t)tiles * heads) {
       base += (int64_t)tiles * heads;
       tiles = __builtin_amdgcn_readfirstlane(unit_tiles(P, ++u));
     }
-    const int h = __builtin_amdgcn_readfirstlane((int)((x - base) / tiles));
-    const int64_t start = base + (int64_t)h * tiles;   // of the group
+    // in parts: part x - base - h * parts of head h
+    const int each = cut.part ? parts_of(tiles, cut.part) : tiles;
+    const int h = __builtin_amdgcn_readfirstlane((int)((x - base) / each));
+    const int64_t start = base + (int64_t)h * each;   // of the group
     Segment s;
     s.b = per_group_units(P) ? u / P.num_kv_heads : u;
     s.kvh = per_group_units(P) ? u % P.num_kv_heads : h;
     s.L = __builtin_amdgcn_readfirstlane(seq_len(P, s.b));
-    s.t0 = (int)(x - start);
-    s.n = (int)(min(end, start + tiles) - x);
+    s.t0 = (int)(x - start) * (cut.part ? cut.part : 1);
+    s.n = cut.part ? min(cut.part, tiles - s.t0) : (int)(min(end, start + tiles) - x);
     s.list = P.block_list ? P.block_list + (int64_t)u * P.max_list : nullptr;
 
     bf16x8 qa[4];
@@ -518,9 +556,9 @@ __global__ void __launch_bounds__(kThreads, 2) full_kernel(const KernelParams P,
 
     // the wavefronts' records joined: thread tid takes values tid, tid + 256 ..
     const bool whole = s.n == tiles;
-    // a group that began in an earlier workgroup leaves its record in this
-    // one's first place, one that began here and goes on in its second
-    float* const to = P.records + (2 * me + (s.t0 == 0 ? 1 : 0)) * P.record_floats;
+    // (of the line) a group that began in an earlier workgroup leaves its record in
+    // this one's first place, one that began here and goes on in its second
+    float* const to = P.records + (cut.part ? me : 2 * me + (s.t0 == 0 ? 1 : 0)) * P.record_floats;
     const int64_t row0 = (int64_t)s.b * P.num_q_heads + s.kvh * G;
 #pragma unroll 1
     for (int i = tid; i < G * kD; i += kThreads) {
@@ -550,6 +588,7 @@ __global__ void __launch_bounds__(kThreads, 2) full_kernel(const KernelParams P,
         }
       }
     }
+    if (cut.part) return;
     __syncthreads();   // the records are read before the next segment's tiles
     x += s.n;
   }
@@ -587,6 +626,7 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const KernelParams P, co
     total += s_sum[1][w];
   }
   total *= heads;
+  const Cut cut = cut_of(P, total, most);
   const int64_t row = (int64_t)b * P.num_q_heads + kvh * G + hq;
   const int L = seq_len(P, b), tiles = unit_tiles(P, unit);
   if (hq == 0 && tid == 0) P.stop_block[gidx] = unit_blocks(P, unit, L);
@@ -595,14 +635,34 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const KernelParams P, co
     if (tid == 0) P.lse[row] = kNegInf;
     return;
   }
-  const int64_t workers = workers_of(total, most);
-  const int64_t start = before * heads + (per_group_units(P) ? 0 : (int64_t)kvh * tiles);
-  // the workgroup that holds tile x of the line: the last w with w total / workers <= x
-  const int64_t first = ((start + 1) * workers - 1) / total;
-  const int64_t last = ((start + tiles) * workers - 1) / total;
-  if (first == last) return;   // written by that workgroup
+  const int in_unit = per_group_units(P) ? 0 : kvh;
+  int64_t first, last;
+  if (cut.part) {
+    const int each = parts_of(tiles, cut.part);
+    if (each == 1) return;   // written by its workgroup
+    // the parts before this unit's
+    int64_t parts = 0;
+    for (int u = tid; u < unit; u += kThreads) parts += parts_of(unit_tiles(P, u), cut.part);
+    parts = wave_sum(parts);
+    __syncthreads();
+    if (lane == 0) s_sum[0][wave] = parts;
+    __syncthreads();
+    parts = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) parts += s_sum[0][w];
+    first = parts * heads + (int64_t)in_unit * each;
+    last = first + each - 1;
+  } else {
+    // the workgroup that holds tile x of the line: the last w with w total / workers <= x
+    const int64_t start = before * heads + (int64_t)in_unit * tiles;
+    first = ((start + 1) * cut.workers - 1) / total;
+    last = ((start + tiles) * cut.workers - 1) / total;
+    if (first == last) return;   // written by that workgroup
+  }
   const int n = (int)(last - first + 1);
-  auto record = [&](int i) { return P.records + (2 * (first + i) + (i == 0 ? 1 : 0)) * P.record_floats; };
+  auto record = [&](int i) {
+    return P.records + (cut.part ? first + i : 2 * (first + i) + (i == 0 ? 1 : 0)) * P.record_floats;
+  };
   float top = kNegInf;
   for (int i = lane; i < n; i += 64) top = fmaxf(top, record(i)[G * kD + hq]);
 #pragma unroll
@@ -657,7 +717,7 @@ int launch(const Plan& plan, const KernelParams& params, hipStream_t stream) {
   const int64_t cap = (int64_t)params.max_pages << params.page_shift;
   const int64_t tiles = (int64_t)plan.n_groups * max((cap + kTile - 1) / kTile, (int64_t)params.max_list * params.tiles_per_block);
   const int64_t most = min(min((int64_t)held, (int64_t)plan.n_groups * plan.max_chunks),
-                           max((int64_t)1, (tiles + kWaves - 1) / kWaves));
+                           (tiles + kWaves - 1) / kWaves + plan.n_groups);
   hipLaunchKernelGGL((full_kernel<G, FMT>), dim3((unsigned)most), dim3(kThreads), bytes, stream, params, (int)most);
   e = hipGetLastError();
   if (e != hipSuccess) return (int)e;
