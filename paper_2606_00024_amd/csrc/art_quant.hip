@@ -85,48 +85,92 @@ __device__ __forceinline__ int page_of(const QuantParams& P, int b, int64_t t) {
   return pg >= 0 && pg < P.num_pages ? pg : -1;
 }
 
-// Eight values of a row, and the reverse.
+// Sixteen values of a row, as they are loaded: 32 bytes, or 64.
 template <int DT>
-__device__ __forceinline__ void load8(const char* p, float (&x)[8]) {
+struct Raw {
+  static constexpr int N = DT == ART_ROWS_F32 ? 4 : 2;
+  u32x4 w[N];
+};
+template <int DT>
+__device__ __forceinline__ float value(const Raw<DT>& r, int i) {
   if constexpr (DT == ART_ROWS_F32) {
-    const f32x4 a = reinterpret_cast<const f32x4*>(p)[0], b = reinterpret_cast<const f32x4*>(p)[1];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { x[i] = a[i]; x[4 + i] = b[i]; }
+    const uint32_t u = r.w[i >> 2][i & 3];
+    return __uint_as_float(u);
   } else {
-    const u32x4 w = *reinterpret_cast<const u32x4*>(p);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if constexpr (DT == ART_ROWS_BF16) {
-        x[2 * i] = __uint_as_float(w[i] << 16);
-        x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-      } else {
-        const uint32_t u = w[i];   // (a cast of the element itself takes element 0)
-        const f16x2 h = __builtin_bit_cast(f16x2, u);
-        x[2 * i] = (float)h[0];
-        x[2 * i + 1] = (float)h[1];
-      }
+    const uint32_t u = r.w[i >> 3][(i >> 1) & 3];
+    if constexpr (DT == ART_ROWS_BF16) {
+      return __uint_as_float(i & 1 ? u & 0xffff0000u : u << 16);
+    } else {
+      const f16x2 h = __builtin_bit_cast(f16x2, u);
+      return (float)h[i & 1];
     }
   }
 }
+// The largest magnitude, as bits of the rows' type without their sign: two
+// 16-bit values at a time where the rows have them.  Bits of kNotFinite and
+// above are infinities and NaN.
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 template <int DT>
-__device__ __forceinline__ void store8(char* p, const float (&x)[8]) {
+constexpr uint32_t kNotFinite = DT == ART_ROWS_F32 ? 0x7f800000u : DT == ART_ROWS_BF16 ? 0x7f80u : 0x7c00u;
+template <int DT>
+__device__ __forceinline__ uint32_t max_bits(uint32_t a, const Raw<DT>& r) {
   if constexpr (DT == ART_ROWS_F32) {
-    reinterpret_cast<f32x4*>(p)[0] = f32x4{x[0], x[1], x[2], x[3]};
-    reinterpret_cast<f32x4*>(p)[1] = f32x4{x[4], x[5], x[6], x[7]};
+#pragma unroll
+    for (int i = 0; i < 16; ++i) a = max(a, r.w[i >> 2][i & 3] & 0x7fffffffu);
+    return a;
   } else {
-    u32x4 w;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t w = r.w[i >> 2][i & 3] & 0x7fff7fffu;
+      a = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, w)));
+    }
+    return a;
+  }
+}
+template <int DT>
+__device__ __forceinline__ uint32_t as_f32_bits(uint32_t a) {
+  if constexpr (DT == ART_ROWS_F32) return a;
+  else if constexpr (DT == ART_ROWS_BF16) return a << 16;
+  else return __float_as_uint((float)__builtin_bit_cast(_Float16, (uint16_t)a));
+}
+// ... of the finite values only, in fp32 bits
+template <int DT>
+__device__ __forceinline__ uint32_t max_finite_bits(uint32_t a, const Raw<DT>& r) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const uint32_t u = __float_as_uint(value<DT>(r, i)) & 0x7fffffffu;
+    a = max(a, u < 0x7f800000u ? u : 0u);
+  }
+  return a;
+}
+__device__ __forceinline__ uint32_t wave_max(uint32_t a) {
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) a = max(a, (uint32_t)__shfl_xor((int)a, o));
+  return a;
+}
+
+// N values (16 bytes of the rows' type).
+template <int DT, int N>
+__device__ __forceinline__ u32x4 packed(const float (&x)[N]) {
+  u32x4 w;
+  if constexpr (DT == ART_ROWS_F32) {
+    static_assert(N == 4);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(x[i]);
+  } else {
+    static_assert(N == 8);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const f32x2 y{x[2 * i], x[2 * i + 1]};
       w[i] = DT == ART_ROWS_BF16 ? __builtin_bit_cast(uint32_t, __builtin_convertvector(y, bf16x2))
                                  : __builtin_bit_cast(uint32_t, __builtin_convertvector(y, f16x2));
     }
-    *reinterpret_cast<u32x4*>(p) = w;
   }
+  return w;
 }
 
 // Four codes in a word, and the reverse.  Rounding is to the nearest code,
-// ties to even; |x| beyond the largest code (infinities only) is clamped.
+// ties to even.  WILD: the values may lie beyond the largest code or be NaN.
 template <int FMT>
 __device__ __forceinline__ void decode4(uint32_t w, float* x) {
   if constexpr (FMT == ART_QUANT_E4M3) {
@@ -139,22 +183,25 @@ __device__ __forceinline__ void decode4(uint32_t w, float* x) {
     x[3] = (float)(int8_t)(w >> 24);
   }
 }
-template <int FMT>
+template <int FMT, bool WILD>
 __device__ __forceinline__ uint32_t encode4(const float* x) {
   float y[4];
   if constexpr (FMT == ART_QUANT_E4M3) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) y[i] = x[i] != x[i] ? x[i] : fminf(fmaxf(x[i], -448.f), 448.f);
+    for (int i = 0; i < 4; ++i) y[i] = !WILD || x[i] != x[i] ? x[i] : fminf(fmaxf(x[i], -448.f), 448.f);
     int w = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], w, true);
   } else {
-    uint32_t w = 0;
+    // |y| <= 127: adding 1.5 * 2^23 rounds to the nearest integer, ties to
+    // even, whose two's complement then is the sum's low byte
+    uint32_t u[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      y[i] = x[i] != x[i] ? 0.f : fminf(fmaxf(x[i], -127.f), 127.f);
-      w |= ((uint32_t)(int)rintf(y[i]) & 0xffu) << (8 * i);
+      y[i] = !WILD ? x[i] : x[i] != x[i] ? 0.f : fminf(fmaxf(x[i], -127.f), 127.f);
+      u[i] = __float_as_uint(__fadd_rn(y[i], 12582912.f));
     }
-    return w;
+    const uint32_t lo = __builtin_amdgcn_perm(u[1], u[0], 0x0c0c0400u), hi = __builtin_amdgcn_perm(u[3], u[2], 0x0c0c0400u);
+    return lo | hi << 16;
   }
 }
 
@@ -171,71 +218,130 @@ __device__ __forceinline__ uint32_t needed_scale(uint32_t a) {
   return (uint32_t)(e + 127) << 23;
 }
 
-// Append.  One wavefront quantises one run of slots of one head's K or V: 16
-// lanes hold a row (8 values each), four rows at a time.  The first pass over
-// the new rows takes their largest magnitude, the second rounds them.  A run
-// that a sequence has begun before keeps its scale unless it has to grow;
-// only then are its old codes read and rounded anew.
+// Append.  One wavefront quantises one run of slots of one head's K or V: 8
+// lanes hold a row (16 values each), eight rows a step, and up to 64 rows (32
+// of 32-bit values) stay in registers between the pass that takes their
+// largest magnitude and the one that rounds them (of longer runs the second
+// pass reads them again, from the L2).  A run that a sequence has begun before
+// keeps its scale unless it has to grow; only then are its old codes read and
+// rounded anew.
+template <int DT>
+constexpr int kSlab = DT == ART_ROWS_F32 ? 4 : 8;   // steps in registers
+
+template <int DT>
+__device__ __forceinline__ void load_slab(const char* src, int64_t stride, int n, int r8, Raw<DT> (&raw)[kSlab<DT>]) {
+#pragma unroll
+  for (int k = 0; k < kSlab<DT>; ++k) {
+    if (8 * k >= n) break;
+#pragma unroll
+    for (int i = 0; i < Raw<DT>::N; ++i) raw[k].w[i] = u32x4{0u, 0u, 0u, 0u};
+    if (8 * k + r8 < n) {
+      const u32x4* p = reinterpret_cast<const u32x4*>(src + (int64_t)(8 * k + r8) * stride);
+#pragma unroll
+      for (int i = 0; i < Raw<DT>::N; ++i) raw[k].w[i] = p[i];
+    }
+  }
+}
+template <int FMT, int DT>
+__device__ __forceinline__ void store_slab(uint8_t* dst, int64_t stride, int n, int r8, float inv, const Raw<DT> (&raw)[kSlab<DT>]) {
+#pragma unroll
+  for (int k = 0; k < kSlab<DT>; ++k) {
+    if (8 * k >= n) break;
+    float x[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = value<DT>(raw[k], i) * inv;
+    if (8 * k + r8 < n)
+      *reinterpret_cast<u32x4*>(dst + (int64_t)(8 * k + r8) * stride) =
+          u32x4{encode4<FMT, false>(x), encode4<FMT, false>(x + 4), encode4<FMT, false>(x + 8), encode4<FMT, false>(x + 12)};
+  }
+}
+
 template <int FMT, int DT>
 __device__ void append_run(const QuantParams& P, const Side& S, int head, int b, int64_t t, int row, int n, int old,
                            int lane) {
-  constexpr int kSize = DT == ART_ROWS_F32 ? 4 : 2;
+  constexpr int kSize = DT == ART_ROWS_F32 ? 4 : 2, kRows = 8 * kSlab<DT>;
   const int pg = page_of(P, b, t);
   if (pg < 0) return;
   const int slot = (int)(t & ((1 << P.page_shift) - 1));
   float* sp = S.scale + pg * S.scp + head * S.sch + (slot >> P.run_shift);
-  const int r4 = lane >> 4, c = lane & 15;
-  const char* src = S.rows + (int64_t)row * S.row + head * S.head + c * (8 * kSize);
-  uint8_t* dst = S.codes + pg * S.sp + head * S.sh + c * 8;
+  const int r8 = lane >> 3, c = lane & 7;
+  const char* src = S.rows + (int64_t)row * S.row + head * S.head + c * (16 * kSize);
+  uint8_t* dst = S.codes + pg * S.sp + head * S.sh + slot * S.st + c * 16;
   const float old_scale = old > 0 ? *sp : 0.f;
 
-  uint32_t a = 0;
-  for (int i = r4; i < n; i += 4) {
-    float x[8];
-    load8<DT>(src + i * S.row, x);
+  // the run's scale from its new rows' largest finite magnitude (fp32 bits);
+  // old codes follow it where it grows.  Returns 1 / scale.
+  auto settle = [&](uint32_t top) {
+    const float need = __uint_as_float(needed_scale<FMT>(top));
+    const float scale = old > 0 ? fmaxf(need, old_scale) : need;
+    const float inv = 1.0f / scale;
+    if (old > 0 && scale != old_scale) {
+      const float ratio = old_scale * inv;
+      for (int i = r8; i < old; i += 8) {
+        u32x4* p = reinterpret_cast<u32x4*>(dst + (int64_t)(i - old) * S.st);
+        u32x4 w = *p;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const uint32_t u = __float_as_uint(x[j]) & 0x7fffffffu;
-      a = max(a, u < 0x7f800000u ? u : 0u);
+        for (int q = 0; q < 4; ++q) {
+          float x[4];
+          decode4<FMT>(w[q], x);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) x[j] *= ratio;
+          w[q] = encode4<FMT, true>(x);
+        }
+        *p = w;
+      }
     }
-  }
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) a = max(a, (uint32_t)__shfl_xor((int)a, o));
-  const float need = __uint_as_float(needed_scale<FMT>(a));
-  const float scale = old > 0 ? fmaxf(need, old_scale) : need;
-  const float inv = 1.0f / scale;
+    if (lane == 0 && (old == 0 || scale != old_scale)) *sp = scale;
+    return inv;
+  };
 
-  if (old > 0 && scale != old_scale) {
-    const float ratio = old_scale * inv;
-    for (int i = r4; i < old; i += 4) {
-      u32x2* p = reinterpret_cast<u32x2*>(dst + (int64_t)(slot - old + i) * S.st);
-      u32x2 w = *p;
-      float x[8];
-      decode4<FMT>(w[0], x);
-      decode4<FMT>(w[1], x + 4);
+  if (n <= kRows) {
+    Raw<DT> raw[kSlab<DT>];
+    load_slab<DT>(src, S.row, n, r8, raw);
+    uint32_t a = 0;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] *= ratio;
-      *p = u32x2{encode4<FMT>(x), encode4<FMT>(x + 4)};
+    for (int k = 0; k < kSlab<DT>; ++k) {
+      if (8 * k >= n) break;
+      a = max_bits<DT>(a, raw[k]);
+    }
+    if constexpr (DT != ART_ROWS_F32) a = max(a & 0xffffu, a >> 16);
+    a = wave_max(a);
+    if (a < kNotFinite<DT>) {
+      store_slab<FMT, DT>(dst, S.st, n, r8, settle(as_f32_bits<DT>(a)), raw);
+      return;
     }
   }
-  for (int i = r4; i < n; i += 4) {
-    float x[8];
-    load8<DT>(src + i * S.row, x);
+  // more rows than the registers hold, or infinities or NaN among them: the
+  // largest finite magnitude, then codes with clamps, from the rows once more
+  auto row_of = [&](int i) {
+    Raw<DT> r;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] *= inv;
-    *reinterpret_cast<u32x2*>(dst + (int64_t)(slot + i) * S.st) = u32x2{encode4<FMT>(x), encode4<FMT>(x + 4)};
+    for (int q = 0; q < Raw<DT>::N; ++q) r.w[q] = reinterpret_cast<const u32x4*>(src + (int64_t)i * S.row)[q];
+    return r;
+  };
+  uint32_t a = 0;
+#pragma unroll 4
+  for (int i = r8; i < n; i += 8) a = max_finite_bits<DT>(a, row_of(i));
+  const float inv = settle(wave_max(a));
+#pragma unroll 4
+  for (int i = r8; i < n; i += 8) {
+    const Raw<DT> r = row_of(i);
+    float x[16];
+#pragma unroll
+    for (int q = 0; q < 16; ++q) x[q] = value<DT>(r, q) * inv;
+    *reinterpret_cast<u32x4*>(dst + (int64_t)i * S.st) =
+        u32x4{encode4<FMT, true>(x), encode4<FMT, true>(x + 4), encode4<FMT, true>(x + 8), encode4<FMT, true>(x + 12)};
   }
-  if (lane == 0 && (old == 0 || scale != old_scale)) *sp = scale;
 }
 
 // A wavefront takes the runs whose first new row lies in its window of rows.
 template <int FMT, int DT>
-__global__ void __launch_bounds__(kThreads) append_kernel(const QuantParams P) {
+__global__ void __launch_bounds__(kThreads, 3) append_kernel(const QuantParams P) {
   const int lane = threadIdx.x & 63;
-  const int u = blockIdx.y * kWaves + (threadIdx.x >> 6);
+  const int u = blockIdx.y * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (u >= 2 * P.heads) return;
-  const Side& S = P.side[u & 1];
-  const int head = u >> 1;
+  const Side& S = P.side[u >= P.heads ? 1 : 0];
+  const int head = u >= P.heads ? u - P.heads : u;
   const int run = 1 << P.run_shift;
   const int64_t cap = (int64_t)P.max_pages << P.page_shift;
   int row = blockIdx.x * P.window;
@@ -253,49 +359,91 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const QuantParams P) {
   }
 }
 
-// Read.  A wavefront brings back eight rows of one head's K or V, eight lanes
-// and 16 codes a lane to a row.
-template <int FMT, int DT>
+// Read.  A wavefront brings back STEPS rows (of 32 bits) or 8 * STEPS rows (of
+// 16) of one head's K or V: the page lookups of all of them, then their scales
+// and codes, are in flight together.  A lane takes 16 codes of a row of 16-bit
+// values, whose two stores fill 32 bytes, and of 32-bit values only the four
+// that one store holds, so that a store instruction writes whole rows (16 codes
+// a lane, whose stores lie 64 bytes apart: 182 us in place of 151 for 134K rows
+// of 8 heads).  The wavefronts of a workgroup take neighbouring heads,
+// whose parts of a row lie side by side.
+template <int DT>
+struct ReadCfg {
+  static constexpr int CODES = DT == ART_ROWS_F32 ? 4 : 16;  // codes of a lane
+  static constexpr int LANES = kHeadDim / CODES;             // lanes of a row
+  static constexpr int ROWS = 64 / LANES;                    // rows of a step
+  static constexpr int STEPS = DT == ART_ROWS_F32 ? 8 : 4;   // steps of a long read
+};
+
+template <int FMT, int DT, int STEPS>
 __global__ void __launch_bounds__(kThreads) read_kernel(const QuantParams P) {
+  using C = ReadCfg<DT>;
   constexpr int kSize = DT == ART_ROWS_F32 ? 4 : 2;
   const int lane = threadIdx.x & 63;
-  const int u = blockIdx.y * kWaves + (threadIdx.x >> 6);
+  const int u = blockIdx.y * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (u >= 2 * P.heads) return;
-  const Side& S = P.side[u & 1];
-  const int head = u >> 1, c = lane & 7;
-  const int row = blockIdx.x * 8 + (lane >> 3);
-  Span s = span_of(P, blockIdx.x * 8, lane);
-  // lanes whose row lies behind the span go on to their own
-  while (P.offsets && s.b < P.batch && row >= s.end) {
-    ++s.b;
-    if (s.b < P.batch) {
-      s.first = P.offsets[s.b];
-      s.end = max(s.end, min(P.offsets[s.b + 1], P.rows));
-      s.pos = P.positions ? P.positions[s.b] : 0;
+  const Side& S = P.side[u >= P.heads ? 1 : 0];
+  const int head = u >= P.heads ? u - P.heads : u, c = lane % C::LANES;
+  const int row0 = blockIdx.x * (C::ROWS * STEPS), in_step = lane / C::LANES;
+  const Span s0 = span_of(P, row0, lane);
+  int pg[STEPS], slot[STEPS];
+#pragma unroll
+  for (int k = 0; k < STEPS; ++k) {
+    const int row = row0 + C::ROWS * k + in_step;
+    Span s = s0;
+    if (P.offsets) {
+      // lanes whose row lies behind the span go on to their own
+      while (s.b < P.batch && row >= s.end) {
+        ++s.b;
+        if (s.b < P.batch) {
+          s.first = P.offsets[s.b];
+          s.end = max(s.end, min(P.offsets[s.b + 1], P.rows));
+          s.pos = P.positions ? P.positions[s.b] : 0;
+        }
+      }
+    } else if (row >= s.end) {
+      s.b = row / P.per_seq;
+      s.first = s.b * P.per_seq;
+      s.pos = s.b < P.batch && P.positions ? P.positions[s.b] : 0;
+    }
+    pg[k] = -1;
+    slot[k] = 0;
+    if (row < P.rows && s.b < P.batch && s.pos >= 0 && s.first >= 0 && row >= s.first) {
+      const int64_t t = s.pos + ((int64_t)row - s.first);
+      pg[k] = page_of(P, s.b, t);
+      slot[k] = (int)(t & ((1 << P.page_shift) - 1));
     }
   }
-  if (!P.offsets && P.per_seq > 0) {
-    s.b = row / P.per_seq;
-    s.first = s.b * P.per_seq;
-    s.pos = s.b < P.batch && P.positions ? P.positions[s.b] : 0;
-  }
-  if (row >= P.rows || s.b >= P.batch || s.pos < 0 || s.first < 0 || row < s.first) return;
-  const int64_t t = s.pos + ((int64_t)row - s.first);
-  const int pg = page_of(P, s.b, t);
-  if (pg < 0) return;
-  const int slot = (int)(t & ((1 << P.page_shift) - 1));
-  const float scale = S.scale[pg * S.scp + head * S.sch + (slot >> P.run_shift)];
-  const u32x4 w = *reinterpret_cast<const u32x4*>(S.codes + pg * S.sp + head * S.sh + slot * S.st + c * 16);
-  char* dst = S.rows + (int64_t)row * S.row + head * S.head + c * (16 * kSize);
+  float scale[STEPS];
+  uint32_t w[STEPS][C::CODES / 4];
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    float x[8];
-    decode4<FMT>(w[2 * h], x);
-    decode4<FMT>(w[2 * h + 1], x + 4);
+  for (int k = 0; k < STEPS; ++k)
+    if (pg[k] >= 0) {
+      scale[k] = S.scale[pg[k] * S.scp + head * S.sch + (slot[k] >> P.run_shift)];
+      const uint8_t* src = S.codes + pg[k] * S.sp + head * S.sh + slot[k] * S.st + c * C::CODES;
+      if constexpr (C::CODES == 16) {
+        const u32x4 x = *reinterpret_cast<const u32x4*>(src);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] *= scale;
-    store8<DT>(dst + h * 8 * kSize, x);
-  }
+        for (int q = 0; q < 4; ++q) w[k][q] = x[q];
+      } else {
+        w[k][0] = *reinterpret_cast<const uint32_t*>(src);
+      }
+    }
+#pragma unroll
+  for (int k = 0; k < STEPS; ++k)
+    if (pg[k] >= 0) {
+      constexpr int N = 16 / kSize;   // values of a store
+      char* dst = S.rows + (int64_t)(row0 + C::ROWS * k + in_step) * S.row + head * S.head + c * (C::CODES * kSize);
+#pragma unroll
+      for (int h = 0; h < C::CODES / N; ++h) {
+        float x[N];
+#pragma unroll
+        for (int q = 0; q < N / 4; ++q) decode4<FMT>(w[k][h * (N / 4) + q], x + 4 * q);
+#pragma unroll
+        for (int j = 0; j < N; ++j) x[j] *= scale[k];
+        *reinterpret_cast<u32x4*>(dst + h * 16) = packed<DT, N>(x);
+      }
+    }
 }
 
 int log2_of(int64_t v) {
@@ -377,12 +525,23 @@ void launch_append(const QuantParams& p, int dtype, dim3 grid, hipStream_t strea
                                    : append_kernel<FMT, ART_ROWS_F32>;
   hipLaunchKernelGGL(k, grid, dim3(kThreads), 0, stream, p);
 }
-template <int FMT>
-void launch_read(const QuantParams& p, int dtype, dim3 grid, hipStream_t stream) {
-  auto k = dtype == ART_ROWS_BF16  ? read_kernel<FMT, ART_ROWS_BF16>
-           : dtype == ART_ROWS_F16 ? read_kernel<FMT, ART_ROWS_F16>
-                                   : read_kernel<FMT, ART_ROWS_F32>;
+template <int FMT, int DT>
+void launch_read(const QuantParams& p, hipStream_t stream) {
+  using C = ReadCfg<DT>;
+  // several steps a wavefront where that still leaves the chip 16 wavefronts a
+  // CU, one otherwise (522 rows of 4 heads in 32 bits: 4.6 us with one step)
+  const int64_t slices = (int64_t)2 * p.heads, rows = C::ROWS * C::STEPS;
+  const bool many = (p.rows + rows - 1) / rows * slices >= 16 * 256;
+  const int64_t each = many ? rows : C::ROWS;
+  const dim3 grid((unsigned)((p.rows + each - 1) / each), (unsigned)((slices + kWaves - 1) / kWaves));
+  auto k = many ? read_kernel<FMT, DT, C::STEPS> : read_kernel<FMT, DT, 1>;
   hipLaunchKernelGGL(k, grid, dim3(kThreads), 0, stream, p);
+}
+template <int FMT>
+void launch_read(const QuantParams& p, int dtype, hipStream_t stream) {
+  if (dtype == ART_ROWS_BF16) launch_read<FMT, ART_ROWS_BF16>(p, stream);
+  else if (dtype == ART_ROWS_F16) launch_read<FMT, ART_ROWS_F16>(p, stream);
+  else launch_read<FMT, ART_ROWS_F32>(p, stream);
 }
 
 }  // namespace
@@ -421,11 +580,10 @@ art_status art_quant_read(const art_decode_shape* shape, const art_quant_cache* 
   const art_status st = check_rows(shape, cache, rows, k_rows, v_rows, row_offsets, positions, page_table, k_cache,
                                    v_cache, k_scale, v_scale, false, &p);
   if (st != ART_OK || shape->batch == 0 || rows->rows == 0) return st;
-  const dim3 grid((unsigned)((p.rows + 7) / 8), (unsigned)((2 * p.heads + kWaves - 1) / kWaves));
   if (cache->format == ART_QUANT_E4M3)
-    launch_read<ART_QUANT_E4M3>(p, rows->rows_dtype, grid, stream);
+    launch_read<ART_QUANT_E4M3>(p, rows->rows_dtype, stream);
   else
-    launch_read<ART_QUANT_INT8>(p, rows->rows_dtype, grid, stream);
+    launch_read<ART_QUANT_INT8>(p, rows->rows_dtype, stream);
   return hipGetLastError() == hipSuccess ? ART_OK : ART_ERR_HIP;
 }
 
