@@ -424,8 +424,8 @@ art_status art_decode_attention_quant(const art_decode_shape* shape, const art_d
  * negative position marks an unused row of a padded batch.)
  *
  * Row and head strides are in elements of rows_dtype, multiples of 16 bytes
- * (>= 0), and the arrays 16-byte aligned; head_dim is contiguous; rows is less
- * than 2^24.
+ * (>= 0), row strides less than 256 MiB, and the arrays 16-byte aligned;
+ * head_dim is contiguous; rows * ceil(num_kv_heads / 2) is less than 2^24.
  *
  * Shape fields used: batch, num_kv_heads, head_dim (128), page_size,
  * num_pages, max_pages_per_seq and the K and V strides.  No workspace; calls

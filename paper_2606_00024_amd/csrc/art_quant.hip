@@ -53,14 +53,38 @@ struct Span {
   int64_t pos;
 };
 
-__device__ __forceinline__ Span span_of(const QuantParams& P, int row, int lane) {
+// The offsets and positions of up to 64 sequences, lane i those of sequence i,
+// read once and together (a row's span then costs no further round trip).
+struct SpanTable {
+  int begin, end, pos;
+};
+__device__ __forceinline__ SpanTable span_table(const QuantParams& P, int lane) {
+  SpanTable t{0, 0, 0};
+  if (P.offsets && P.batch <= 64 && lane < P.batch) {
+    t.begin = P.offsets[lane];
+    t.end = P.offsets[lane + 1];
+    t.pos = P.positions ? P.positions[lane] : 0;
+  }
+  return t;
+}
+
+__device__ __forceinline__ Span span_of(const QuantParams& P, const SpanTable& t, int row, int lane) {
   Span s;
+  if (P.offsets && P.batch <= 64) {
+    // the number of sequences that end at or before the row
+    s.b = __popcll(__ballot(lane < P.batch && t.end <= row));
+    const int at = min(s.b, 63);
+    s.first = __builtin_amdgcn_readlane(t.begin, at);
+    s.end = min(__builtin_amdgcn_readlane(t.end, at), P.rows);
+    s.pos = __builtin_amdgcn_readlane(t.pos, at);
+    if (s.b >= P.batch) s.first = s.end = row;
+    return s;
+  }
   if (!P.offsets) {
     s.b = P.per_seq > 0 ? row / P.per_seq : P.batch;
     s.first = s.b * P.per_seq;
     s.end = s.first + P.per_seq;
   } else {
-    // the number of sequences that end at or before the row
     s.b = 0;
     for (int i = 0; i < P.batch; i += 64)
       s.b += __popcll(__ballot(i + lane < P.batch && P.offsets[i + lane + 1] <= row));
@@ -85,19 +109,16 @@ __device__ __forceinline__ int page_of(const QuantParams& P, int b, int64_t t) {
   return pg >= 0 && pg < P.num_pages ? pg : -1;
 }
 
-// Sixteen values of a row, as they are loaded: 32 bytes, or 64.
+// Sixteen bytes of a row: 8 values, or 4.
 template <int DT>
-struct Raw {
-  static constexpr int N = DT == ART_ROWS_F32 ? 4 : 2;
-  u32x4 w[N];
-};
+constexpr int kValues = DT == ART_ROWS_F32 ? 4 : 8;
 template <int DT>
-__device__ __forceinline__ float value(const Raw<DT>& r, int i) {
+__device__ __forceinline__ float value(const u32x4& w, int i) {
   if constexpr (DT == ART_ROWS_F32) {
-    const uint32_t u = r.w[i >> 2][i & 3];
+    const uint32_t u = w[i];
     return __uint_as_float(u);
   } else {
-    const uint32_t u = r.w[i >> 3][(i >> 1) & 3];
+    const uint32_t u = w[i >> 1];   // (a cast of the element itself takes element 0)
     if constexpr (DT == ART_ROWS_BF16) {
       return __uint_as_float(i & 1 ? u & 0xffff0000u : u << 16);
     } else {
@@ -113,19 +134,17 @@ typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 template <int DT>
 constexpr uint32_t kNotFinite = DT == ART_ROWS_F32 ? 0x7f800000u : DT == ART_ROWS_BF16 ? 0x7f80u : 0x7c00u;
 template <int DT>
-__device__ __forceinline__ uint32_t max_bits(uint32_t a, const Raw<DT>& r) {
-  if constexpr (DT == ART_ROWS_F32) {
+__device__ __forceinline__ uint32_t max_bits(uint32_t a, const u32x4& r) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) a = max(a, r.w[i >> 2][i & 3] & 0x7fffffffu);
-    return a;
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const uint32_t w = r.w[i >> 2][i & 3] & 0x7fff7fffu;
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (DT == ART_ROWS_F32) {
+      a = max(a, r[i] & 0x7fffffffu);
+    } else {
+      const uint32_t w = r[i] & 0x7fff7fffu;
       a = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, w)));
     }
-    return a;
   }
+  return a;
 }
 template <int DT>
 __device__ __forceinline__ uint32_t as_f32_bits(uint32_t a) {
@@ -135,9 +154,9 @@ __device__ __forceinline__ uint32_t as_f32_bits(uint32_t a) {
 }
 // ... of the finite values only, in fp32 bits
 template <int DT>
-__device__ __forceinline__ uint32_t max_finite_bits(uint32_t a, const Raw<DT>& r) {
+__device__ __forceinline__ uint32_t max_finite_bits(uint32_t a, const u32x4& r) {
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
+  for (int i = 0; i < kValues<DT>; ++i) {
     const uint32_t u = __float_as_uint(value<DT>(r, i)) & 0x7fffffffu;
     a = max(a, u < 0x7f800000u ? u : 0u);
   }
@@ -218,55 +237,57 @@ __device__ __forceinline__ uint32_t needed_scale(uint32_t a) {
   return (uint32_t)(e + 127) << 23;
 }
 
-// Append.  One wavefront quantises one run of slots of one head's K or V: 8
-// lanes hold a row (16 values each), eight rows a step, and up to 64 rows (32
-// of 32-bit values) stay in registers between the pass that takes their
-// largest magnitude and the one that rounds them (of longer runs the second
-// pass reads them again, from the L2).  A run that a sequence has begun before
-// keeps its scale unless it has to grow; only then are its old codes read and
-// rounded anew.
+// Append.  One wavefront quantises one run of slots of one head's K or V: 16
+// bytes of a row to a lane, four rows a step (two of 32-bit values), and up to
+// 64 rows (32) stay in registers between the pass that takes their largest
+// magnitude and the one that rounds them (of longer runs the second pass reads
+// them again, from the L2).  A run that a sequence has begun before keeps its
+// scale unless it has to grow; only then are its old codes read and rounded
+// anew.
+constexpr int kSlab = 16;   // steps in registers
 template <int DT>
-constexpr int kSlab = DT == ART_ROWS_F32 ? 4 : 8;   // steps in registers
+struct Step {
+  static constexpr int LANES = kHeadDim / kValues<DT>;   // lanes of a row
+  static constexpr int ROWS = 64 / LANES;                // rows of a step
+};
 
-template <int DT>
-__device__ __forceinline__ void load_slab(const char* src, int64_t stride, int n, int r8, Raw<DT> (&raw)[kSlab<DT>]) {
+template <int FMT, int DT, bool WILD>
+__device__ __forceinline__ void store_codes(uint8_t* p, const u32x4& r, float inv) {
+  float x[kValues<DT>];
 #pragma unroll
-  for (int k = 0; k < kSlab<DT>; ++k) {
-    if (8 * k >= n) break;
-#pragma unroll
-    for (int i = 0; i < Raw<DT>::N; ++i) raw[k].w[i] = u32x4{0u, 0u, 0u, 0u};
-    if (8 * k + r8 < n) {
-      const u32x4* p = reinterpret_cast<const u32x4*>(src + (int64_t)(8 * k + r8) * stride);
-#pragma unroll
-      for (int i = 0; i < Raw<DT>::N; ++i) raw[k].w[i] = p[i];
-    }
-  }
-}
-template <int FMT, int DT>
-__device__ __forceinline__ void store_slab(uint8_t* dst, int64_t stride, int n, int r8, float inv, const Raw<DT> (&raw)[kSlab<DT>]) {
-#pragma unroll
-  for (int k = 0; k < kSlab<DT>; ++k) {
-    if (8 * k >= n) break;
-    float x[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] = value<DT>(raw[k], i) * inv;
-    if (8 * k + r8 < n)
-      *reinterpret_cast<u32x4*>(dst + (int64_t)(8 * k + r8) * stride) =
-          u32x4{encode4<FMT, false>(x), encode4<FMT, false>(x + 4), encode4<FMT, false>(x + 8), encode4<FMT, false>(x + 12)};
-  }
+  for (int i = 0; i < kValues<DT>; ++i) x[i] = value<DT>(r, i) * inv;
+  if constexpr (kValues<DT> == 8)
+    *reinterpret_cast<u32x2*>(p) = u32x2{encode4<FMT, WILD>(x), encode4<FMT, WILD>(x + 4)};
+  else
+    *reinterpret_cast<uint32_t*>(p) = encode4<FMT, WILD>(x);
 }
 
 template <int FMT, int DT>
 __device__ void append_run(const QuantParams& P, const Side& S, int head, int b, int64_t t, int row, int n, int old,
                            int lane) {
-  constexpr int kSize = DT == ART_ROWS_F32 ? 4 : 2, kRows = 8 * kSlab<DT>;
-  const int pg = page_of(P, b, t);
+  constexpr int ROWS = Step<DT>::ROWS, LANES = Step<DT>::LANES;
+  // uniform bases and 32-bit lane offsets; the rows are on their way before
+  // the page is known (they need none)
+  const int r0 = lane / LANES, c = lane % LANES;
+  const char* src = S.rows + (int64_t)row * S.row + head * S.head;
+  const uint32_t from = (uint32_t)(r0 * (int)S.row) + c * 16, to = (uint32_t)(r0 * (int)S.st) + c * kValues<DT>;
+  auto load = [&](int i) { return *reinterpret_cast<const u32x4*>(src + (int64_t)i * S.row + from); };  // row i + r0
+  const int page = page_of(P, b, t);
+  u32x4 raw[kSlab];
+  const bool held = n <= kSlab * ROWS;
+  if (held) {
+#pragma unroll
+    for (int k = 0; k < kSlab; ++k) {
+      raw[k] = u32x4{0u, 0u, 0u, 0u};
+      if (ROWS * k + r0 < n) raw[k] = load(ROWS * k);
+    }
+  }
+  const int pg = __builtin_amdgcn_readfirstlane(page);
   if (pg < 0) return;
   const int slot = (int)(t & ((1 << P.page_shift) - 1));
   float* sp = S.scale + pg * S.scp + head * S.sch + (slot >> P.run_shift);
-  const int r8 = lane >> 3, c = lane & 7;
-  const char* src = S.rows + (int64_t)row * S.row + head * S.head + c * (16 * kSize);
-  uint8_t* dst = S.codes + pg * S.sp + head * S.sh + slot * S.st + c * 16;
+  uint8_t* pool = S.codes + pg * S.sp + head * S.sh + slot * S.st;
+  auto at = [&](int i) { return pool + (int64_t)i * S.st + to; };
   const float old_scale = old > 0 ? *sp : 0.f;
 
   // the run's scale from its new rows' largest finite magnitude (fp32 bits);
@@ -277,8 +298,8 @@ __device__ void append_run(const QuantParams& P, const Side& S, int head, int b,
     const float inv = 1.0f / scale;
     if (old > 0 && scale != old_scale) {
       const float ratio = old_scale * inv;
-      for (int i = r8; i < old; i += 8) {
-        u32x4* p = reinterpret_cast<u32x4*>(dst + (int64_t)(i - old) * S.st);
+      for (int i = lane >> 3; i < old; i += 8) {
+        u32x4* p = reinterpret_cast<u32x4*>(pool + (int64_t)(i - old) * S.st + (lane & 7) * 16);
         u32x4 w = *p;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
@@ -294,60 +315,50 @@ __device__ void append_run(const QuantParams& P, const Side& S, int head, int b,
     if (lane == 0 && (old == 0 || scale != old_scale)) *sp = scale;
     return inv;
   };
-
-  if (n <= kRows) {
-    Raw<DT> raw[kSlab<DT>];
-    load_slab<DT>(src, S.row, n, r8, raw);
+  if (held) {
     uint32_t a = 0;
 #pragma unroll
-    for (int k = 0; k < kSlab<DT>; ++k) {
-      if (8 * k >= n) break;
-      a = max_bits<DT>(a, raw[k]);
-    }
+    for (int k = 0; k < kSlab; ++k) a = max_bits<DT>(a, raw[k]);
     if constexpr (DT != ART_ROWS_F32) a = max(a & 0xffffu, a >> 16);
     a = wave_max(a);
     if (a < kNotFinite<DT>) {
-      store_slab<FMT, DT>(dst, S.st, n, r8, settle(as_f32_bits<DT>(a)), raw);
+      const float inv = settle(as_f32_bits<DT>(a));
+#pragma unroll
+      for (int k = 0; k < kSlab; ++k) {
+        if (ROWS * k + r0 < n) store_codes<FMT, DT, false>(at(ROWS * k), raw[k], inv);
+      }
       return;
     }
   }
   // more rows than the registers hold, or infinities or NaN among them: the
   // largest finite magnitude, then codes with clamps, from the rows once more
-  auto row_of = [&](int i) {
-    Raw<DT> r;
-#pragma unroll
-    for (int q = 0; q < Raw<DT>::N; ++q) r.w[q] = reinterpret_cast<const u32x4*>(src + (int64_t)i * S.row)[q];
-    return r;
-  };
   uint32_t a = 0;
 #pragma unroll 4
-  for (int i = r8; i < n; i += 8) a = max_finite_bits<DT>(a, row_of(i));
+  for (int i = 0; i < n; i += ROWS)
+    if (i + r0 < n) a = max_finite_bits<DT>(a, load(i));
   const float inv = settle(wave_max(a));
 #pragma unroll 4
-  for (int i = r8; i < n; i += 8) {
-    const Raw<DT> r = row_of(i);
-    float x[16];
-#pragma unroll
-    for (int q = 0; q < 16; ++q) x[q] = value<DT>(r, q) * inv;
-    *reinterpret_cast<u32x4*>(dst + (int64_t)i * S.st) =
-        u32x4{encode4<FMT, true>(x), encode4<FMT, true>(x + 4), encode4<FMT, true>(x + 8), encode4<FMT, true>(x + 12)};
-  }
+  for (int i = 0; i < n; i += ROWS)
+    if (i + r0 < n) store_codes<FMT, DT, true>(at(i), load(i), inv);
 }
 
 // A wavefront takes the runs whose first new row lies in its window of rows.
 template <int FMT, int DT>
 __global__ void __launch_bounds__(kThreads, 3) append_kernel(const QuantParams P) {
   const int lane = threadIdx.x & 63;
-  const int u = blockIdx.y * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t slices = (uint32_t)(2 * P.heads + kWaves - 1) / kWaves, part = blockIdx.x / slices;
+  const int u = (blockIdx.x - part * slices) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (u >= 2 * P.heads) return;
   const Side& S = P.side[u >= P.heads ? 1 : 0];
   const int head = u >= P.heads ? u - P.heads : u;
   const int run = 1 << P.run_shift;
   const int64_t cap = (int64_t)P.max_pages << P.page_shift;
-  int row = blockIdx.x * P.window;
+  int row = part * P.window;
   const int stop = min(row + P.window, P.rows);
+  const SpanTable table = span_table(P, lane);
+  Span s{0, 0, 0, 0};
   while (row < stop) {
-    const Span s = span_of(P, row, lane);
+    if (row >= s.end) s = span_of(P, table, row, lane);
     if (s.b >= P.batch) return;                                    // rows behind the last sequence
     if (s.first > row || s.end <= row) { ++row; continue; }        // before the first one (or no offsets)
     const int64_t t = s.pos + ((int64_t)row - s.first);
@@ -380,12 +391,13 @@ __global__ void __launch_bounds__(kThreads) read_kernel(const QuantParams P) {
   using C = ReadCfg<DT>;
   constexpr int kSize = DT == ART_ROWS_F32 ? 4 : 2;
   const int lane = threadIdx.x & 63;
-  const int u = blockIdx.y * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t slices = (uint32_t)(2 * P.heads + kWaves - 1) / kWaves, part = blockIdx.x / slices;
+  const int u = (blockIdx.x - part * slices) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (u >= 2 * P.heads) return;
   const Side& S = P.side[u >= P.heads ? 1 : 0];
   const int head = u >= P.heads ? u - P.heads : u, c = lane % C::LANES;
-  const int row0 = blockIdx.x * (C::ROWS * STEPS), in_step = lane / C::LANES;
-  const Span s0 = span_of(P, row0, lane);
+  const int row0 = part * (C::ROWS * STEPS), in_step = lane / C::LANES;
+  const Span s0 = span_of(P, span_table(P, lane), row0, lane);
   int pg[STEPS], slot[STEPS];
 #pragma unroll
   for (int k = 0; k < STEPS; ++k) {
@@ -489,10 +501,12 @@ art_status check_rows(const art_decode_shape* s, const art_quant_cache* c, const
   if (append && c->scale_tokens > kMaxRun) return ART_ERR_UNSUPPORTED;
   if (!offsets && s->batch > 0 && r->rows % s->batch) return ART_ERR_INVALID_ARG;
   const int64_t size = r->rows_dtype == ART_ROWS_F32 ? 4 : 2;
-  if ((r->k_stride_row | r->k_stride_head | r->v_stride_row | r->v_stride_head) * size % 16) return ART_ERR_UNSUPPORTED;
-  // the grid's dimensions: threads along the first (at most 2^32) and
-  // workgroups along the second
-  if (r->rows >= (1 << 24) || s->num_kv_heads > 65536) return ART_ERR_UNSUPPORTED;
+  if ((r->k_stride_row | r->k_stride_head | r->v_stride_row | r->v_stride_head) * size % 16 ||
+      r->k_stride_row * size >= (1 << 28) || r->v_stride_row * size >= (1 << 28))
+    return ART_ERR_UNSUPPORTED;
+  // a launch has less than 2^32 threads: 256 for every row and four slices
+  if (r->rows >= (1 << 24) || (int64_t)r->rows * ((2 * (int64_t)s->num_kv_heads + kWaves - 1) / kWaves) >= (1 << 24))
+    return ART_ERR_UNSUPPORTED;
   if (s->batch == 0 || r->rows == 0) return ART_OK;
   if (!k_rows || !v_rows || !table || !k_cache || !v_cache || !k_scale || !v_scale) return ART_ERR_INVALID_ARG;
   if (((uintptr_t)k_scale | (uintptr_t)v_scale) % 4) return ART_ERR_INVALID_ARG;
@@ -533,7 +547,7 @@ void launch_read(const QuantParams& p, hipStream_t stream) {
   const int64_t slices = (int64_t)2 * p.heads, rows = C::ROWS * C::STEPS;
   const bool many = (p.rows + rows - 1) / rows * slices >= 16 * 256;
   const int64_t each = many ? rows : C::ROWS;
-  const dim3 grid((unsigned)((p.rows + each - 1) / each), (unsigned)((slices + kWaves - 1) / kWaves));
+  const dim3 grid((unsigned)((p.rows + each - 1) / each * ((slices + kWaves - 1) / kWaves)));
   auto k = many ? read_kernel<FMT, DT, C::STEPS> : read_kernel<FMT, DT, 1>;
   hipLaunchKernelGGL(k, grid, dim3(kThreads), 0, stream, p);
 }
@@ -563,7 +577,7 @@ art_status art_quant_append(const art_decode_shape* shape, const art_quant_cache
   int window = 1;
   while (window < cache->scale_tokens && window * 2 <= p.per_seq) window *= 2;
   p.window = window;
-  const dim3 grid((unsigned)((p.rows + window - 1) / window), (unsigned)((2 * p.heads + kWaves - 1) / kWaves));
+  const dim3 grid((unsigned)((p.rows + window - 1) / window * ((2 * p.heads + kWaves - 1) / kWaves)));
   if (cache->format == ART_QUANT_E4M3)
     launch_append<ART_QUANT_E4M3>(p, rows->rows_dtype, grid, stream);
   else

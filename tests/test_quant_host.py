@@ -118,6 +118,7 @@ def test_specs(kw, status):
     (dict(v_stride_head=4), _lib.ERR_UNSUPPORTED),
     (dict(rows_dtype=_lib.ROWS_F32, v_stride_head=2), _lib.ERR_UNSUPPORTED),
     (dict(rows=1 << 24), _lib.ERR_UNSUPPORTED),
+    (dict(k_stride_row=1 << 27), _lib.ERR_UNSUPPORTED),
 ])
 def test_rows(kw, status):
     assert _append(_shape(), _spec(), _rows(**kw)) == status
