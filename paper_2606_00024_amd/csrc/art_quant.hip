@@ -241,7 +241,8 @@ __device__ __forceinline__ uint32_t needed_scale(uint32_t a) {
 // bytes of a row to a lane, four rows a step (two of 32-bit values), and up to
 // 64 rows (32) stay in registers between the pass that takes their largest
 // magnitude and the one that rounds them (of longer runs the second pass reads
-// them again, from the L2).  A run that a sequence has begun before keeps its
+// them again, from the L2).  They are read past the caches (88 us with plain
+// loads and 65 without, for 54K rows of 8 heads: 5.1 TB/s).  A run that a sequence has begun before keeps its
 // scale unless it has to grow; only then are its old codes read and rounded
 // anew.
 constexpr int kSlab = 16;   // steps in registers
@@ -271,7 +272,7 @@ __device__ void append_run(const QuantParams& P, const Side& S, int head, int b,
   const int r0 = lane / LANES, c = lane % LANES;
   const char* src = S.rows + (int64_t)row * S.row + head * S.head;
   const uint32_t from = (uint32_t)(r0 * (int)S.row) + c * 16, to = (uint32_t)(r0 * (int)S.st) + c * kValues<DT>;
-  auto load = [&](int i) { return *reinterpret_cast<const u32x4*>(src + (int64_t)i * S.row + from); };  // row i + r0
+  auto load = [&](int i) { return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src + (int64_t)i * S.row + from)); };  // row i + r0
   const int page = page_of(P, b, t);
   u32x4 raw[kSlab];
   const bool held = n <= kSlab * ROWS;
@@ -370,26 +371,27 @@ __global__ void __launch_bounds__(kThreads, 3) append_kernel(const QuantParams P
   }
 }
 
-// Read.  A wavefront brings back STEPS rows (of 32 bits) or 8 * STEPS rows (of
-// 16) of one head's K or V: the page lookups of all of them, then their scales
-// and codes, are in flight together.  A lane takes 16 codes of a row of 16-bit
-// values, whose two stores fill 32 bytes, and of 32-bit values only the four
-// that one store holds, so that a store instruction writes whole rows (16 codes
-// a lane, whose stores lie 64 bytes apart: 182 us in place of 151 for 134K rows
-// of 8 heads).  The wavefronts of a workgroup take neighbouring heads,
-// whose parts of a row lie side by side.
+// Read.  A wavefront brings back 8 steps of 4 rows (of 2 rows of 32-bit values)
+// of one head's K or V: the page lookups of all of them, then their scales and
+// codes, are in flight together.  A lane takes the codes that one 16-byte
+// store holds the values of, so that a store instruction writes whole rows
+// (with 16 codes a lane, 54K rows of 8 heads to fp32 took 182 us, not 106, and
+// 103K rows to bf16 132, not 126).  The wavefronts of a workgroup take
+// neighbouring heads, whose parts of a row lie side by side, and neighbouring
+// workgroups the rest of the row: all of a row moves at about the same time
+// and meets every memory channel (with the heads far apart in the launch, fp32
+// 121 us and the append 110, not 88).
 template <int DT>
 struct ReadCfg {
-  static constexpr int CODES = DT == ART_ROWS_F32 ? 4 : 16;  // codes of a lane
-  static constexpr int LANES = kHeadDim / CODES;             // lanes of a row
-  static constexpr int ROWS = 64 / LANES;                    // rows of a step
-  static constexpr int STEPS = DT == ART_ROWS_F32 ? 8 : 4;   // steps of a long read
+  static constexpr int CODES = kValues<DT>;        // codes of a lane
+  static constexpr int LANES = kHeadDim / CODES;   // lanes of a row
+  static constexpr int ROWS = 64 / LANES;          // rows of a step
+  static constexpr int STEPS = 8;                  // steps of a long read
 };
 
 template <int FMT, int DT, int STEPS>
 __global__ void __launch_bounds__(kThreads) read_kernel(const QuantParams P) {
   using C = ReadCfg<DT>;
-  constexpr int kSize = DT == ART_ROWS_F32 ? 4 : 2;
   const int lane = threadIdx.x & 63;
   const uint32_t slices = (uint32_t)(2 * P.heads + kWaves - 1) / kWaves, part = blockIdx.x / slices;
   const int u = (blockIdx.x - part * slices) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -433,28 +435,24 @@ __global__ void __launch_bounds__(kThreads) read_kernel(const QuantParams P) {
     if (pg[k] >= 0) {
       scale[k] = S.scale[pg[k] * S.scp + head * S.sch + (slot[k] >> P.run_shift)];
       const uint8_t* src = S.codes + pg[k] * S.sp + head * S.sh + slot[k] * S.st + c * C::CODES;
-      if constexpr (C::CODES == 16) {
-        const u32x4 x = *reinterpret_cast<const u32x4*>(src);
-#pragma unroll
-        for (int q = 0; q < 4; ++q) w[k][q] = x[q];
+      if constexpr (C::CODES == 8) {
+        const u32x2 x = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(src));
+        w[k][0] = x[0];
+        w[k][1] = x[1];
       } else {
-        w[k][0] = *reinterpret_cast<const uint32_t*>(src);
+        w[k][0] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(src));
       }
     }
 #pragma unroll
   for (int k = 0; k < STEPS; ++k)
     if (pg[k] >= 0) {
-      constexpr int N = 16 / kSize;   // values of a store
-      char* dst = S.rows + (int64_t)(row0 + C::ROWS * k + in_step) * S.row + head * S.head + c * (C::CODES * kSize);
+      float x[C::CODES];
 #pragma unroll
-      for (int h = 0; h < C::CODES / N; ++h) {
-        float x[N];
+      for (int q = 0; q < C::CODES / 4; ++q) decode4<FMT>(w[k][q], x + 4 * q);
 #pragma unroll
-        for (int q = 0; q < N / 4; ++q) decode4<FMT>(w[k][h * (N / 4) + q], x + 4 * q);
-#pragma unroll
-        for (int j = 0; j < N; ++j) x[j] *= scale[k];
-        *reinterpret_cast<u32x4*>(dst + h * 16) = packed<DT, N>(x);
-      }
+      for (int j = 0; j < C::CODES; ++j) x[j] *= scale[k];
+      char* dst = S.rows + (int64_t)(row0 + C::ROWS * k + in_step) * S.row + head * S.head + c * 16;
+      *reinterpret_cast<u32x4*>(dst) = packed<DT, C::CODES>(x);
     }
 }
 
