@@ -327,6 +327,11 @@ def _quant_spec(cache: QuantCache):
     return dev, pool, a, b, _lib.QuantCacheSpec(fmt, pool[2] // runs, c[0], c[1], d[0], d[1])
 
 
+def quant_spec(cache: QuantCache) -> _lib.QuantCacheSpec:
+    """ABI description of a cache (its tensors checked), for raw calls."""
+    return _quant_spec(cache)[4]
+
+
 def _on_device(dev, call, *args) -> int:
     """call(*args, the current stream of GPU ``dev``) with that GPU current."""
     stream = torch._C._cuda_getCurrentRawStream(dev)

@@ -26,7 +26,7 @@ Modes: NODET (full attention, no stability test: the baseline), OFF (test on,
 never stops) and ON (the workload thresholds).  Reported per mode: TPOT, the
 attention's share, and the speedup over NODET.
 
-    python -m paper_2606_00024_amd.tpot --model llama3_8b --batch 8 --seq-len 32768
+    python -m paper_2606_00024_amd.tpot --model llama3_8b --batch 8 --seq-len 32768 [--kv e4m3]
 """
 from __future__ import annotations
 
@@ -83,11 +83,16 @@ class Step:
     """Weights, caches and pre-marshalled attention calls of one model."""
 
     def __init__(self, model: ModelShape, batch: int, seq_len: int, seed: int = 11,
-                 tau: float = 1e-3, phi: float = 1e-4, patience: int = 5):
+                 tau: float = 1e-3, phi: float = 1e-4, patience: int = 5, kv: str = "bf16"):
         import torch
         from . import _lib, api, workloads as W
         self.torch = torch
         self._lib = _lib
+        self.api = api
+        kinds = {"bf16": None, "e4m3": torch.float8_e4m3fn, "int8": torch.int8}
+        if kv not in kinds:
+            raise ValueError(f"kv must be one of {sorted(kinds)}")
+        self.quant = kinds[kv]
         self.model, self.batch, self.seq_len = model, batch, seq_len
         dev = torch.device("cuda", torch.cuda.current_device())
         gen = torch.Generator(device=dev).manual_seed(seed)
@@ -106,7 +111,7 @@ class Step:
                                   tau=tau, phi=phi, patience=patience, seed=1000 * seed + layer)
             wl = W.make_workload(spec, device=dev)
             self.layers.append({
-                "wl": wl,
+                "wl": wl, "cache": self._quantised(wl) if self.quant is not None else None,
                 "w_qkv": weight(m.hidden, (m.q_heads + 2 * m.kv_heads) * d),
                 "w_o": weight(m.q_heads * d, m.hidden),
                 "w_gu": weight(m.hidden, 2 * m.ffn),
@@ -114,6 +119,9 @@ class Step:
             })
         self.w_head = weight(m.hidden, m.vocab)
         self.x0 = torch.empty((batch, m.hidden), dtype=torch.bfloat16, device=dev).normal_(generator=gen)
+        # the step's token: the last of every sequence
+        self.position = torch.full((batch,), seq_len - 1, dtype=torch.int32, device=dev)
+        self.kv0 = torch.empty((batch, 2 * m.kv_heads * d), dtype=torch.bfloat16, device=dev).normal_(generator=gen)
         self.out = torch.empty((batch, m.q_heads, d), dtype=torch.bfloat16, device=dev)
         self.lse = torch.empty((batch, m.q_heads), dtype=torch.float32, device=dev)
         self.stop = [torch.empty((batch, m.kv_heads), dtype=torch.int32, device=dev)
@@ -128,21 +136,44 @@ class Step:
             per_layer = []
             for li, L in enumerate(self.layers):
                 wl = L["wl"]
-                shape = api.make_shape(wl.q, wl.k_cache, wl.v_cache, wl.page_table,
-                                       block_size=wl.spec.block_size)
+                k, v = L["cache"][:2] if L["cache"] else (wl.k_cache, wl.v_cache)
+                shape = api.make_shape(wl.q, k, v, wl.page_table, block_size=wl.spec.block_size)
                 opts = api.make_opts(softmax_scale=wl.spec.softmax_scale, out_dtype=torch.bfloat16,
                                      dense_order=wl.spec.dense_order, **kw)
                 ws_bytes = max(ws_bytes, api.workspace_bytes(shape, opts))
-                per_layer.append((shape, opts, (p(wl.q), p(wl.k_cache), p(wl.v_cache), p(wl.page_table),
-                                                p(wl.seq_lens), 0, 0, p(self.out), p(self.lse),
-                                                p(self.stop[li]))))
+                rest = (p(wl.page_table), p(wl.seq_lens), 0, 0, p(self.out), p(self.lse), p(self.stop[li]))
+                if L["cache"]:
+                    args = (api.quant_spec(L["cache"]), p(wl.q), *(p(t) for t in L["cache"]), *rest)
+                else:
+                    args = (p(wl.q), p(k), p(v), *rest)
+                per_layer.append((shape, opts, args))
             self.calls[mode] = per_layer
         self.ws = api.new_workspace(ws_bytes, dev)
 
+    def _quantised(self, wl):
+        """The workload's cache in 8 bits; its bf16 pools are given up."""
+        torch = self.torch
+        pages, heads, size, d = wl.k_cache.shape
+        cache = self.api.new_quant_cache(pages, heads, size, dtype=self.quant, device=wl.q.device)
+        for b in range(self.batch):   # a sequence at a time: its rows fit beside the pools
+            rows = [pool[wl.page_table[b].long()].transpose(1, 2).reshape(-1, heads, d)[:self.seq_len]
+                    for pool in (wl.k_cache, wl.v_cache)]
+            self.api.quant_append(cache, *rows, wl.page_table[b:b + 1], None)
+        wl.k_cache = wl.v_cache = None
+        torch.cuda.synchronize()
+        return cache
+
+    def append(self, layer: int, kv):
+        """The step's K and V, [batch][2 * kv_heads * 128], into the layer's
+        8-bit cache."""
+        L, width = self.layers[layer], self.model.kv_heads * 128
+        k, v = (kv[:, i * width:(i + 1) * width].unflatten(1, (-1, 128)) for i in (0, 1))
+        self.api.quant_append(L["cache"], k, v, L["wl"].page_table, self.position)
+
     def attention(self, mode: str, layer: int):
         shape, opts, args = self.calls[mode][layer]
-        st = self._lib.decode_attention(shape, opts, *args, int(self.ws.data_ptr()), self.ws.numel(),
-                                        self.stream)
+        call = self._lib.decode_attention if self.quant is None else self._lib.decode_attention_quant
+        st = call(shape, opts, *args, int(self.ws.data_ptr()), self.ws.numel(), self.stream)
         if st != 0:
             raise self._lib.ArtError(st, "art_decode_attention")
         return self.out
@@ -155,10 +186,14 @@ class Step:
         m = self.model
         x = self.x0
         for li, L in enumerate(self.layers):
+            kv = self.kv0
             if dense:
                 h = F.rms_norm(x, (m.hidden,))
-                _ = h @ L["w_qkv"]
+                qkv = h @ L["w_qkv"]
+                kv = qkv[:, m.q_heads * 128:]
             if attention:
+                if self.quant is not None:
+                    self.append(li, kv)
                 a = self.attention(mode, li).view(self.batch, m.q_heads * 128)
             else:
                 a = self.out.view(self.batch, m.q_heads * 128)
@@ -195,10 +230,12 @@ class Step:
         return 100.0 * (1 - consumed / total)
 
 
-def measure(model: ModelShape, batch: int, seq_len: int, steps: int = 10, warmup: int = 3) -> dict:
-    step = Step(model, batch, seq_len)
-    res = {"model": model.name, "batch": batch, "seq_len": seq_len, "layers": model.layers,
-           "weight_gb": model.weight_bytes() / 1e9, "kv_gb": model.kv_bytes(batch, seq_len) / 1e9,
+def measure(model: ModelShape, batch: int, seq_len: int, steps: int = 10, warmup: int = 3,
+            kv: str = "bf16") -> dict:
+    step = Step(model, batch, seq_len, kv=kv)
+    kv_bytes = model.kv_bytes(batch, seq_len) / (1 if kv == "bf16" else 2)
+    res = {"model": model.name, "batch": batch, "seq_len": seq_len, "layers": model.layers, "kv": kv,
+           "weight_gb": model.weight_bytes() / 1e9, "kv_gb": kv_bytes / 1e9,
            "dense_only_ms": float(np.median(step.time_ms("nodet", steps, warmup, attention=False))),
            "modes": {}}
     for mode in ("nodet", "off", "on"):
@@ -219,9 +256,11 @@ def main(argv=None) -> int:
     ap.add_argument("--batch", type=int, default=8)
     ap.add_argument("--seq-len", type=int, default=32768)
     ap.add_argument("--steps", type=int, default=10)
+    ap.add_argument("--kv", default="bf16", choices=("bf16", "e4m3", "int8"),
+                    help="type of the KV cache (8-bit caches are written by the step as well)")
     ap.add_argument("--json", default=None)
     args = ap.parse_args(argv)
-    res = measure(MODELS[args.model], args.batch, args.seq_len, steps=args.steps)
+    res = measure(MODELS[args.model], args.batch, args.seq_len, steps=args.steps, kv=args.kv)
     print(json.dumps(res), flush=True)
     if args.json:
         with open(args.json, "w") as f:
