@@ -69,18 +69,6 @@ namespace {
 
 constexpr int kFormat = ART_KV_FORMAT;
 
-// The kernel's parameters, read where they are used from the kernel argument
-// segment through the scalar cache.  fresh() hides the pointer's origin from
-// the compiler: it then loads a phase's fields in that phase, instead of
-// holding all of them (about 60 registers' worth, with what it derives from
-// them) in scalar registers across the whole kernel.  Held so, 140 of them
-// were spilled to lanes of vector registers, and 1170 of the kernel's 3600
-// instructions (g = 4) were v_readlane to fetch them back.
-typedef const __attribute__((address_space(4))) KernelParams Params;
-__device__ __forceinline__ Params* fresh(Params* p) {
-  __asm__ __volatile__("" : "+s"(p));
-  return p;
-}
 constexpr int kD = kHeadDim;
 
 // ---- workspace: cross-workgroup data ---------------------------------------

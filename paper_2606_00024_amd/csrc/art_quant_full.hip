@@ -6,7 +6,8 @@
 // part of it, however ragged the batch is; the part of a group in a
 // workgroup's range is a segment.  (Where that leaves a workgroup few tiles, a
 // second segment costs more than an uneven share: groups are then cut into
-// equal parts, a workgroup to each.)  The four wavefronts of a workgroup take a
+// equal parts, a workgroup to each, or, where there are many, each is one
+// wavefront's.)  The four wavefronts of a workgroup take a
 // segment's tiles in turn, each with its own running maximum, mass and output
 // sums in registers, and join at its end through LDS.  A group that lies in
 // one workgroup is written out there; of the others each segment leaves a
@@ -45,49 +46,55 @@ struct Full {
 
 // The line of tiles.  A unit is what shares a length: a sequence (all its KV
 // heads), or with a list per head one group.
-struct Unit {
-  int tiles;    // of each of its groups
-  int heads;    // groups
-};
-
-__device__ __forceinline__ int seq_len(const KernelParams& P, int b) {
+__device__ __forceinline__ int seq_len(Params& P, int b) {
   const int64_t cap = (int64_t)P.max_pages << P.page_shift;
   const int L = P.seq_lens[b];
   return L < 0 ? 0 : (int)min((int64_t)L, cap);
 }
-__device__ __forceinline__ bool per_group_units(const KernelParams& P) { return P.block_list && P.list_per_head; }
-__device__ __forceinline__ int unit_count(const KernelParams& P) {
+__device__ __forceinline__ bool per_group_units(Params& P) { return P.block_list && P.list_per_head; }
+__device__ __forceinline__ int unit_count(Params& P) {
   return per_group_units(P) ? P.batch * P.num_kv_heads : P.batch;
 }
 // blocks of a unit's traversal
-__device__ __forceinline__ int unit_blocks(const KernelParams& P, int u, int L) {
+__device__ __forceinline__ int unit_blocks(Params& P, int u, int L) {
   if (L == 0) return 0;
   if (!P.block_list) return (L + P.block_size - 1) / P.block_size;
   const int T = P.block_list_len[u];
   return T < 0 ? 0 : min(T, P.max_list);
 }
-__device__ __forceinline__ int unit_tiles(const KernelParams& P, int u) {
+__device__ __forceinline__ int unit_tiles(Params& P, int u) {
   const int L = seq_len(P, per_group_units(P) ? u / P.num_kv_heads : u);
   return P.block_list ? unit_blocks(P, u, L) * P.tiles_per_block : (L + kTile - 1) / kTile;
 }
-__device__ __forceinline__ int unit_heads(const KernelParams& P) { return per_group_units(P) ? 1 : P.num_kv_heads; }
+__device__ __forceinline__ int unit_heads(Params& P) { return per_group_units(P) ? 1 : P.num_kv_heads; }
 
-// How `total` tiles are cut for at most `most` workgroups; every wavefront gets
-// a tile, at least.  part == 0: the line in `workers` equal ranges.  part > 0:
-// every group in parts of that many tiles (of which there are no more than
-// `most`), where a range would hold 16 tiles or fewer.
+// How the tiles are cut for `most` workgroups.
+//   kLine   the line in `workers` equal ranges (every wavefront gets a tile)
+//   kParts  every group in parts of `part` tiles, of which there are no more
+//           than `most`: where a range would hold 16 tiles or fewer (16 ragged
+//           sequences of up to 2K tokens 26.5 -> 19.3 us)
+//   kWaves1 every group to one wavefront
+// A segment's set-up and end take about as long as three tiles of a wavefront;
+// with that the last takes the rounds of groups times the longest one, and the
+// line a wavefront's share of the tiles and the segments of its workgroup.
+// (4096 sequences of 100 tokens, 8 heads: 783 us by the line.)
+enum CutKind { kLine, kParts, kWaves1 };
 struct Cut {
+  CutKind kind;
   int64_t workers;
   int part;
 };
-__device__ __forceinline__ Cut cut_of(const KernelParams& P, int64_t total, int64_t most) {
-  const int64_t groups = (int64_t)P.batch * P.num_kv_heads;
-  Cut c{max((int64_t)1, min(most, (total + kWaves - 1) / kWaves)), 0};
-  if (2 * groups <= most && total <= 16 * most) {
+__device__ __forceinline__ Cut cut_of(Params& P, int64_t total, int64_t longest, int64_t most) {
+  const int64_t groups = (int64_t)P.batch * P.num_kv_heads, waves = most * kWaves;
+  const Cut line{kLine, max((int64_t)1, min(most, (total + kWaves - 1) / kWaves)), 0};
+  if (2 * groups <= most) {
+    if (total > 16 * most) return line;
     const int64_t room = most - groups;
-    c.part = max((int)((total + room - 1) / room), kWaves);
+    return Cut{kParts, most, max((int)((total + room - 1) / room), kWaves)};
   }
-  return c;
+  if ((groups + waves - 1) / waves * (2 + longest) <= total / waves + 3 * (groups / most + 1))
+    return Cut{kWaves1, most, 0};
+  return line;
 }
 __device__ __forceinline__ int parts_of(int tiles, int part) { return (tiles + part - 1) / part; }
 
@@ -121,7 +128,7 @@ __device__ __forceinline__ const uint8_t* rows_at(const uint16_t* pool, int64_t 
                                                   int kvh, int slot) {
   return reinterpret_cast<const uint8_t*>(pool) + (int64_t)pg * sp + (int64_t)kvh * sh + (int64_t)slot * st;
 }
-__device__ __forceinline__ void load_k(const KernelParams& P, int kvh, int L, const TileAt& at, int lane, Tile& t) {
+__device__ __forceinline__ void load_k(Params& P, int kvh, int L, const TileAt& at, int lane, Tile& t) {
   const int lo = lane & 15, g = lane >> 4, mask = (1 << P.page_shift) - 1;
 #pragma unroll
   for (int n = 0; n < 4; ++n) {
@@ -132,7 +139,7 @@ __device__ __forceinline__ void load_k(const KernelParams& P, int kvh, int L, co
     for (int j = 0; j < 2; ++j) t.k[n][j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(b + (o + 64u * j)));
   }
 }
-__device__ __forceinline__ void load_v(const KernelParams& P, int kvh, int L, const TileAt& at, int lane, Tile& t) {
+__device__ __forceinline__ void load_v(Params& P, int kvh, int L, const TileAt& at, int lane, Tile& t) {
   const int mask = (1 << P.page_shift) - 1;
 #pragma unroll
   for (int n = 0; n < 4; ++n) {
@@ -156,16 +163,17 @@ struct Ahead {
 struct Segment {
   int b, kvh, L, T;      // T: blocks of the traversal
   int t0, n;             // its tiles of the group: t0 .. t0 + n - 1
+  int off, step;         // of which this wavefront takes off, off + step, ...
   const int32_t* list;
 };
 
-__device__ __forceinline__ void ahead_pages(const KernelParams& P, const Segment& s, int wave, int first, int n_mine,
+__device__ __forceinline__ void ahead_pages(Params& P, const Segment& s, int first, int n_mine,
                                             int lane, Ahead& a) {
   const int m = first + (lane >> 2);
   a.tok0 = 0;
   a.page = 0;
   if (m < n_mine) {
-    const int tile = s.t0 + wave + kWaves * m;
+    const int tile = s.t0 + s.off + s.step * m;
     if (s.list) {
       const int i = tile / P.tiles_per_block, nblk = (s.L + P.block_size - 1) / P.block_size;
       int blk = s.list[i];
@@ -180,7 +188,7 @@ __device__ __forceinline__ void ahead_pages(const KernelParams& P, const Segment
     a.page = pg >= P.num_pages ? P.num_pages - 1 : pg;
   }
 }
-__device__ __forceinline__ void ahead_scales(const KernelParams& P, const Segment& s, int lane, Ahead& a) {
+__device__ __forceinline__ void ahead_scales(Params& P, const Segment& s, int lane, Ahead& a) {
   const int tok = min(a.tok0 + 16 * (lane & 3), s.L - 1);
   const int run = (tok & ((1 << P.page_shift) - 1)) >> P.scale_shift;
   a.ks = P.k_scale[(int64_t)a.page * P.ksc_page + (int64_t)s.kvh * P.ksc_head + run];
@@ -206,19 +214,19 @@ struct State {
 };
 
 template <int G, int FMT>
-__device__ __forceinline__ void walk_tiles(const KernelParams& P, const Segment& s, int wave, int lane,
+__device__ __forceinline__ void walk_tiles(Params& P, const Segment& s, int lane,
                                            const bf16x8 (&qa)[4], uint8_t* stage, uint16_t* parts, State& st) {
   using C = Full<G>;
   constexpr int REP = C::REP, COLS = C::COLS, NS = C::NS, NP = C::NP;
   const int lo = lane & 15, g = lane >> 4, u = lo / COLS;
-  const int n_mine = s.n > wave ? (s.n - wave + kWaves - 1) / kWaves : 0;
+  const int n_mine = s.n > s.off ? (s.n - s.off + s.step - 1) / s.step : 0;
   if (n_mine == 0) return;
   // Pages are fetched two sets of 16 tiles ahead and scales one, before the
   // loads of a set's first tile: no wait for them then holds up for the tiles
   // in flight behind them.
   Ahead cur, nxt, far;
-  ahead_pages(P, s, wave, 0, n_mine, lane, cur);
-  ahead_pages(P, s, wave, 16, n_mine, lane, nxt);
+  ahead_pages(P, s, 0, n_mine, lane, cur);
+  ahead_pages(P, s, 16, n_mine, lane, nxt);
   ahead_scales(P, s, lane, cur);
   TileAt at = tile_at(cur, 0);
   Tile t;
@@ -230,7 +238,7 @@ __device__ __forceinline__ void walk_tiles(const KernelParams& P, const Segment&
   const int n_set = min(16, n_mine - first);
   const TileAt over = tile_at(nxt, 0);
   ahead_scales(P, s, lane, nxt);
-  ahead_pages(P, s, wave, first + 32, n_mine, lane, far);
+  ahead_pages(P, s, first + 32, n_mine, lane, far);
 #pragma unroll 1
   for (int m = 0; m < n_set; ++m) {
     const int tok0 = at.tok0;
@@ -436,7 +444,7 @@ __device__ __forceinline__ void leave_record(State& st, float* rec, int lane) {
   }
 }
 
-__device__ __forceinline__ void write_out(const KernelParams& P, int64_t i, float x) {
+__device__ __forceinline__ void write_out(Params& P, int64_t i, float x) {
   if (P.out_bf16) static_cast<uint16_t*>(P.out)[i] = (uint16_t)f32_to_bf16_bits(x);
   else static_cast<float*>(P.out)[i] = x;
 }
@@ -446,41 +454,113 @@ __device__ __forceinline__ float ln_of(float m, float L) { return (m + __log2f(L
 // Called by all threads for value (h, d).
 __device__ __forceinline__ float factor(float m, float top) { return m == kNegInf ? 0.f : fast_exp2(m - top); }
 
+// What the first launch tells the second of a group that holds tiles: the
+// workgroups that hold it (one: it is written) and how it was cut.  (In the
+// workspace's flag words; bits 24 and up stay far below any call's tag there.)
+__device__ __forceinline__ uint64_t split_word(int64_t first, int64_t last, bool in_parts) {
+  return (uint64_t)last << 24 | (in_parts ? 1ull << 23 : 0ull) | (uint64_t)first;
+}
+
 template <int G, int FMT>
-__global__ void __launch_bounds__(kThreads, 2) full_kernel(const KernelParams P, const int most) {
+__global__ void __launch_bounds__(kThreads, 2) full_kernel(const KernelParams, const int most) {
+  Params* const args = (Params*)__builtin_amdgcn_kernarg_segment_ptr();
+  Params& P = *args;
   using C = Full<G>;
   extern __shared__ __align__(16) uint8_t lds[];
   __shared__ int64_t s_wave[2][kWaves];
   __shared__ int64_t s_base;
-  __shared__ int s_unit;
+  __shared__ int s_unit, s_longest[kWaves];
   // (the wavefront's number in a scalar register: everything that follows from
   // it, page addresses above all, then stays there too)
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int units = unit_count(P), heads = unit_heads(P);
 
-  // this workgroup's part of the line: a sum over the units, then a scan of
-  // their tiles (or parts) that finds the unit where it begins
+  // the tiles of all units, and the most that a group has
+  int64_t total = 0;
+  int longest = 0;
+  for (int u = tid; u < units; u += kThreads) {
+    const int n = unit_tiles(P, u);
+    total += n;
+    longest = max(longest, n);
+  }
+  total = wave_sum(total);
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) longest = max(longest, __shfl_xor(longest, o));
+  if (lane == 0) {
+    s_wave[0][wave] = total;
+    s_longest[wave] = longest;
+  }
+  __syncthreads();
+  total = longest = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    total += s_wave[0][w];
+    longest = max(longest, s_longest[w]);
+  }
+  const Cut cut = cut_of(P, uniform(total * heads), __builtin_amdgcn_readfirstlane(longest), most);
+
+  float* const rec = reinterpret_cast<float*>(lds + wave * C::WAVE_BYTES);
+  uint8_t* const stage = lds + wave * C::WAVE_BYTES;
+  uint16_t* const parts = reinterpret_cast<uint16_t*>(stage + 8192);
+  // group (b, kvh)'s query and the state before its first tile
+  bf16x8 qa[4];
+  State st;
+  auto begin_group = [&](const Segment& s) {
+    Params& P = *fresh(args);
+    const int head = (lane & 15) & (C::COLS - 1);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      u32x4 w{0u, 0u, 0u, 0u};
+      if (head < G)
+        w = *reinterpret_cast<const u32x4*>(P.q + ((int64_t)s.b * P.num_q_heads + s.kvh * G + head) * kD +
+                                            64 * (k >> 1) + 16 * (lane >> 4) + 8 * (k & 1));
+      qa[k] = __builtin_bit_cast(bf16x8, w);
+    }
+    st.m = kNegInf;
+    st.l = 0.f;
+#pragma unroll
+    for (int d = 0; d < 8; ++d) st.acc[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+  };
+
+  if (cut.kind == kWaves1) {
+    const int groups = P.batch * P.num_kv_heads;
+    for (int g = blockIdx.x * kWaves + wave; g < groups; g += most * kWaves) {
+      Params& P = *fresh(args);
+      Segment s;
+      s.b = g / P.num_kv_heads;
+      s.kvh = g - s.b * P.num_kv_heads;
+      const int u = per_group_units(P) ? g : s.b;
+      s.L = __builtin_amdgcn_readfirstlane(seq_len(P, s.b));
+      s.n = __builtin_amdgcn_readfirstlane(unit_tiles(P, u));
+      s.t0 = s.off = 0;
+      s.step = 1;
+      s.list = P.block_list ? P.block_list + (int64_t)u * P.max_list : nullptr;
+      if (s.n == 0) continue;   // (the second launch writes empty groups)
+      begin_group(s);
+      walk_tiles<G, FMT>(*fresh(args), s, lane, qa, stage, parts, st);
+      leave_record<G>(st, rec, lane);
+      wave_lds_sync();
+      Params& W = *fresh(args);
+      const int64_t row0 = (int64_t)s.b * W.num_q_heads + s.kvh * G;
+      for (int i = lane; i < G * kD; i += 64) write_out(W, row0 * kD + i, rec[i] / rec[G * kD + G + i / kD]);
+      if (lane < G) W.lse[row0 + lane] = ln_of(rec[G * kD + lane], rec[G * kD + G + lane]);
+      if (lane == 0) W.flags[g] = split_word(0, 0, false);
+      wave_lds_sync();   // the record is read before the next group's tiles
+    }
+    return;
+  }
+
+  // this workgroup's part of the line: a scan of the units' tiles (or parts)
+  // that finds the unit where it begins
+  const bool in_parts = cut.kind == kParts;
+  auto weight = [&](int u) {
+    const int n = unit_tiles(P, u);
+    return (int64_t)heads * (in_parts ? parts_of(n, cut.part) : n);
+  };
   const int per = (units + kThreads - 1) / kThreads;
   const int u0 = tid * per, u1 = min(units, u0 + per);
   int64_t own = 0;
-  for (int u = u0; u < u1; ++u) own += unit_tiles(P, u);
-  int64_t total = wave_sum(own);
-  if (lane == 0) s_wave[0][wave] = total;
-  __syncthreads();
-  total = 0;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) total += s_wave[0][w];
-  total = uniform(total * heads);
-  const Cut cut = cut_of(P, total, most);
-  auto weight = [&](int u) {
-    const int n = unit_tiles(P, u);
-    return (int64_t)heads * (cut.part ? parts_of(n, cut.part) : n);
-  };
-  own *= heads;
-  if (cut.part) {
-    own = 0;
-    for (int u = u0; u < u1; ++u) own += weight(u);
-  }
+  for (int u = u0; u < u1; ++u) own += weight(u);
   int64_t before = own;   // inclusive scan over the wavefront, then the workgroup
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
@@ -497,10 +577,10 @@ __global__ void __launch_bounds__(kThreads, 2) full_kernel(const KernelParams P,
   }
   before -= own;
   line = uniform(line);   // tiles of the line, or parts
-  const int64_t workers = cut.part ? line : cut.workers, me = blockIdx.x;
+  const int64_t workers = in_parts ? line : cut.workers, me = blockIdx.x;
   if (me >= workers) return;
-  const int64_t begin = cut.part ? me : uniform(me * line / workers);
-  const int64_t end = cut.part ? me + 1 : uniform((me + 1) * line / workers);
+  const int64_t begin = in_parts ? me : uniform(me * line / workers);
+  const int64_t end = in_parts ? me + 1 : uniform((me + 1) * line / workers);
   if (begin >= end) return;
   if (before <= begin && begin < before + own) {
     // (one thread) the unit that holds the first tile
@@ -514,54 +594,44 @@ __global__ void __launch_bounds__(kThreads, 2) full_kernel(const KernelParams P,
   int u = __builtin_amdgcn_readfirstlane(s_unit);
   int64_t base = uniform(s_base);
 
-  float* const rec = reinterpret_cast<float*>(lds + wave * C::WAVE_BYTES);
-  uint8_t* const stage = lds + wave * C::WAVE_BYTES;
-  uint16_t* const parts = reinterpret_cast<uint16_t*>(stage + 8192);
   for (int64_t x = begin; x < end;) {
+    Params& P = *fresh(args);
     int tiles = __builtin_amdgcn_readfirstlane(unit_tiles(P, u));
-    while (!cut.part && x >= base + (int64_t)tiles * heads) {
+    while (!in_parts && x >= base + (int64_t)tiles * heads) {
       base += (int64_t)tiles * heads;
       tiles = __builtin_amdgcn_readfirstlane(unit_tiles(P, ++u));
     }
     // in parts: part x - base - h * parts of head h
-    const int each = cut.part ? parts_of(tiles, cut.part) : tiles;
+    const int each = in_parts ? parts_of(tiles, cut.part) : tiles;
     const int h = __builtin_amdgcn_readfirstlane((int)((x - base) / each));
     const int64_t start = base + (int64_t)h * each;   // of the group
     Segment s;
     s.b = per_group_units(P) ? u / P.num_kv_heads : u;
     s.kvh = per_group_units(P) ? u % P.num_kv_heads : h;
     s.L = __builtin_amdgcn_readfirstlane(seq_len(P, s.b));
-    s.t0 = (int)(x - start) * (cut.part ? cut.part : 1);
-    s.n = cut.part ? min(cut.part, tiles - s.t0) : (int)(min(end, start + tiles) - x);
+    s.t0 = (int)(x - start) * (in_parts ? cut.part : 1);
+    s.n = in_parts ? min(cut.part, tiles - s.t0) : (int)(min(end, start + tiles) - x);
+    s.off = wave;
+    s.step = kWaves;
     s.list = P.block_list ? P.block_list + (int64_t)u * P.max_list : nullptr;
 
-    bf16x8 qa[4];
-    {
-      const int head = (lane & 15) & (C::COLS - 1);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        u32x4 w{0u, 0u, 0u, 0u};
-        if (head < G)
-          w = *reinterpret_cast<const u32x4*>(P.q + ((int64_t)s.b * P.num_q_heads + s.kvh * G + head) * kD +
-                                              64 * (k >> 1) + 16 * (lane >> 4) + 8 * (k & 1));
-        qa[k] = __builtin_bit_cast(bf16x8, w);
-      }
-    }
-    State st;
-    st.m = kNegInf;
-    st.l = 0.f;
-#pragma unroll
-    for (int d = 0; d < 8; ++d) st.acc[d] = f32x4{0.f, 0.f, 0.f, 0.f};
-    walk_tiles<G, FMT>(P, s, wave, lane, qa, stage, parts, st);
+    begin_group(s);
+    walk_tiles<G, FMT>(*fresh(args), s, lane, qa, stage, parts, st);
     leave_record<G>(st, rec, lane);
     __syncthreads();
 
     // the wavefronts' records joined: thread tid takes values tid, tid + 256 ..
+    Params& W = *fresh(args);
     const bool whole = s.n == tiles;
     // (of the line) a group that began in an earlier workgroup leaves its record in
     // this one's first place, one that began here and goes on in its second
-    float* const to = P.records + (cut.part ? me : 2 * me + (s.t0 == 0 ? 1 : 0)) * P.record_floats;
-    const int64_t row0 = (int64_t)s.b * P.num_q_heads + s.kvh * G;
+    float* const to = W.records + (in_parts ? me : 2 * me + (s.t0 == 0 ? 1 : 0)) * W.record_floats;
+    if (s.t0 == 0 && tid == 0) {
+      // who holds the group: the last w with w line / workers <= its last tile
+      const int64_t last = in_parts ? me + each - 1 : ((x + tiles) * workers - 1) / line;
+      W.flags[(int64_t)s.b * W.num_kv_heads + s.kvh] = split_word(me, last, in_parts);
+    }
+    const int64_t row0 = (int64_t)s.b * W.num_q_heads + s.kvh * G;
 #pragma unroll 1
     for (int i = tid; i < G * kD; i += kThreads) {
       const int h2 = i / kD;
@@ -580,8 +650,8 @@ __global__ void __launch_bounds__(kThreads, 2) full_kernel(const KernelParams P,
         L += r[G * kD + G + h2] * f;
       }
       if (whole) {
-        write_out(P, row0 * kD + i, o / L);
-        if (i % kD == 0) P.lse[row0 + h2] = ln_of(top, L);
+        write_out(W, row0 * kD + i, o / L);
+        if (i % kD == 0) W.lse[row0 + h2] = ln_of(top, L);
       } else {
         to[i] = o;
         if (i % kD == 0) {
@@ -590,101 +660,62 @@ __global__ void __launch_bounds__(kThreads, 2) full_kernel(const KernelParams P,
         }
       }
     }
-    if (cut.part) return;
+    if (in_parts) return;
     __syncthreads();   // the records are read before the next segment's tiles
     x += s.n;
   }
 }
 
-// The second launch: one workgroup for every query head.  Groups in several
+// The second launch: `each` query heads to a workgroup.  Groups in several
 // workgroups are joined from their records, in the order of the line; empty
 // ones are written; every group's stop_block is its number of blocks.
 template <int G>
-__global__ void __launch_bounds__(kThreads) join_kernel(const KernelParams P, const int most) {
-  __shared__ int64_t s_sum[2][kWaves];
+__global__ void __launch_bounds__(kThreads) join_kernel(const KernelParams, const int each) {
+  Params& P = *(Params*)__builtin_amdgcn_kernarg_segment_ptr();
   __shared__ float s_o[kThreads], s_l[kThreads];
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  const int gidx = blockIdx.x / G, hq = blockIdx.x % G;
-  const int b = gidx / P.num_kv_heads, kvh = gidx % P.num_kv_heads;
-  const int units = unit_count(P), heads = unit_heads(P);
-  const int unit = per_group_units(P) ? gidx : b;
-  int64_t before = 0, total = 0;
-  for (int u = tid; u < units; u += kThreads) {
-    const int n = unit_tiles(P, u);
-    total += n;
-    before += u < unit ? n : 0;
-  }
-  before = wave_sum(before);
-  total = wave_sum(total);
-  if (lane == 0) {
-    s_sum[0][wave] = before;
-    s_sum[1][wave] = total;
-  }
-  __syncthreads();
-  before = total = 0;
+  const int tid = threadIdx.x, lane = tid & 63, d = tid & (kD - 1);
+  const int64_t items = (int64_t)P.batch * P.num_kv_heads * G;
+  for (int64_t it = (int64_t)blockIdx.x * each; it < min(items, ((int64_t)blockIdx.x + 1) * each); ++it) {
+    const int gidx = (int)(it / G), hq = (int)(it - (int64_t)gidx * G);
+    const int b = gidx / P.num_kv_heads, kvh = gidx - b * P.num_kv_heads;
+    const int unit = per_group_units(P) ? gidx : b;
+    const uint64_t split = P.flags[gidx];
+    const int64_t row = (int64_t)b * P.num_q_heads + kvh * G + hq;
+    const int blocks = unit_blocks(P, unit, seq_len(P, b));
+    if (hq == 0 && tid == 0) P.stop_block[gidx] = blocks;
+    if (blocks == 0) {
+      if (tid < kD) write_out(P, row * kD + tid, 0.f);
+      if (tid == 0) P.lse[row] = kNegInf;
+      continue;
+    }
+    const int first = (int)(split & 0x7fffffu), last = (int)(split >> 24), n = last - first + 1;
+    const bool in_parts = (split >> 23) & 1u;
+    if (n == 1) continue;   // written by its workgroup
+    // (of a line, the group's first record is in its workgroup's second place)
+    auto record = [&](int i) {
+      return P.records + (int64_t)(in_parts ? first + i : 2 * (first + i) + (i == 0 ? 1 : 0)) * P.record_floats;
+    };
+    float top = kNegInf;
+    for (int i = lane; i < n; i += 64) top = fmaxf(top, record(i)[G * kD + hq]);
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    before += s_sum[0][w];
-    total += s_sum[1][w];
-  }
-  total *= heads;
-  const Cut cut = cut_of(P, total, most);
-  const int64_t row = (int64_t)b * P.num_q_heads + kvh * G + hq;
-  const int L = seq_len(P, b), tiles = unit_tiles(P, unit);
-  if (hq == 0 && tid == 0) P.stop_block[gidx] = unit_blocks(P, unit, L);
-  if (tiles == 0) {
-    if (tid < kD) write_out(P, row * kD + tid, 0.f);
-    if (tid == 0) P.lse[row] = kNegInf;
-    return;
-  }
-  const int in_unit = per_group_units(P) ? 0 : kvh;
-  int64_t first, last;
-  if (cut.part) {
-    const int each = parts_of(tiles, cut.part);
-    if (each == 1) return;   // written by its workgroup
-    // the parts before this unit's
-    int64_t parts = 0;
-    for (int u = tid; u < unit; u += kThreads) parts += parts_of(unit_tiles(P, u), cut.part);
-    parts = wave_sum(parts);
-    __syncthreads();
-    if (lane == 0) s_sum[0][wave] = parts;
-    __syncthreads();
-    parts = 0;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) parts += s_sum[0][w];
-    first = parts * heads + (int64_t)in_unit * each;
-    last = first + each - 1;
-  } else {
-    // the workgroup that holds tile x of the line: the last w with w total / workers <= x
-    const int64_t start = before * heads + (int64_t)in_unit * tiles;
-    first = ((start + 1) * cut.workers - 1) / total;
-    last = ((start + tiles) * cut.workers - 1) / total;
-    if (first == last) return;   // written by that workgroup
-  }
-  const int n = (int)(last - first + 1);
-  auto record = [&](int i) {
-    return P.records + (cut.part ? first + i : 2 * (first + i) + (i == 0 ? 1 : 0)) * P.record_floats;
-  };
-  float top = kNegInf;
-  for (int i = lane; i < n; i += 64) top = fmaxf(top, record(i)[G * kD + hq]);
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-  float o = 0.f, l = 0.f;
-  const int d = tid & (kD - 1);
+    for (int o = 32; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+    float o = 0.f, l = 0.f;
 #pragma unroll 4
-  for (int i = tid / kD; i < n; i += kThreads / kD) {
-    const float* r = record(i);
-    const float f = factor(r[G * kD + hq], top);
-    o += r[hq * kD + d] * f;
-    l += r[G * kD + G + hq] * f;
-  }
-  s_o[tid] = o;
-  s_l[tid] = l;
-  __syncthreads();
-  if (tid < kD) {
-    const float os = s_o[tid] + s_o[tid + kD], ls = s_l[tid] + s_l[tid + kD];
-    write_out(P, row * kD + tid, os / ls);
-    if (tid == 0) P.lse[row] = ln_of(top, ls);
+    for (int i = tid / kD; i < n; i += kThreads / kD) {
+      const float* r = record(i);
+      const float f = factor(r[G * kD + hq], top);
+      o += r[hq * kD + d] * f;
+      l += r[G * kD + G + hq] * f;
+    }
+    s_o[tid] = o;
+    s_l[tid] = l;
+    __syncthreads();
+    if (tid < kD) {
+      const float os = s_o[tid] + s_o[tid + kD], ls = s_l[tid] + s_l[tid + kD];
+      write_out(P, row * kD + tid, os / ls);
+      if (tid == 0) P.lse[row] = ln_of(top, ls);
+    }
+    __syncthreads();   // read before the next one's
   }
 }
 
@@ -723,7 +754,11 @@ int launch(const Plan& plan, const KernelParams& params, hipStream_t stream) {
   hipLaunchKernelGGL((full_kernel<G, FMT>), dim3((unsigned)most), dim3(kThreads), bytes, stream, params, (int)most);
   e = hipGetLastError();
   if (e != hipSuccess) return (int)e;
-  hipLaunchKernelGGL(join_kernel<G>, dim3((unsigned)(plan.n_groups * G)), dim3(kThreads), 0, stream, params, (int)most);
+  // one head to a workgroup, and of many, most of them written already, up to 16
+  // (a launch has less than 2^32 threads)
+  const int64_t items = (int64_t)plan.n_groups * G;
+  const int each = (int)max(min(max(items >> 12, (int64_t)1), (int64_t)16), items >> 22);
+  hipLaunchKernelGGL(join_kernel<G>, dim3((unsigned)((items + each - 1) / each)), dim3(kThreads), 0, stream, params, each);
   return (int)hipGetLastError();
 }
 

@@ -5,7 +5,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
-#include "art.h"
+#include "art_internal.h"
 
 namespace art {
 namespace {
@@ -17,6 +17,19 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef int v2i32 __attribute__((ext_vector_type(2)));
 
 constexpr float kNegInf = -__builtin_inff();
+
+// The kernel's parameters, read where they are used from the kernel argument
+// segment through the scalar cache.  fresh() hides the pointer's origin from
+// the compiler: it then loads a phase's fields in that phase, instead of
+// holding all of them (about 60 registers' worth, with what it derives from
+// them) in scalar registers across the whole kernel.  Held so, 140 of them
+// were spilled to lanes of vector registers, and 1170 of the kernel's 3600
+// instructions (g = 4) were v_readlane to fetch them back.
+typedef const __attribute__((address_space(4))) KernelParams Params;
+__device__ __forceinline__ Params* fresh(Params* p) {
+  __asm__ __volatile__("" : "+s"(p));
+  return p;
+}
 
 __device__ __forceinline__ float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }

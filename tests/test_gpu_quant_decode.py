@@ -121,6 +121,8 @@ def test_full_attention_random_shape(i):
     (4, [1 + 37 * (i % 9) for i in range(700)]),        # more sequences than threads
     (8, [0, 0, 5, 0, 40000, 0, 1, 0, 0, 64, 129, 0]),   # empty ones between, one in many parts
     (1, [90000]), (16, [30000, 17]), (2, [0] * 300 + [4000] + [0] * 300),
+    (4, [(7 * i) % 130 for i in range(3000)]),          # a wavefront to every group
+    (1, [i % 3 for i in range(5000)]),
 ])
 def test_full_attention_ragged(g, lens):
     rng = np.random.default_rng(len(lens))
@@ -365,3 +367,45 @@ def test_same_bits_again_and_on_another_stream():
     for got in again:
         for a, b in zip(want, got):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("per_head", [True, False])
+def test_full_attention_lists_of_many_groups(per_head):
+    """Lists (one per KV head or shared) over many sequences: a wavefront to
+    every group, empty lists among them."""
+    rng = np.random.default_rng(31)
+    B, H, g, Ps, bk = 1500, 2, 4, 64, 64
+    lens = rng.integers(0, 400, B).tolist()
+    width = 7
+    cache = _random_cache(rng, "int8", 512, H, Ps, 64, spread=2.0)
+    table = rng.integers(0, 512, (B, width)).astype(np.int32)
+    rows = (B, H) if per_head else (B,)
+    lists = np.full((*rows, width), -1, dtype=np.int32)
+    counts = np.zeros(rows, dtype=np.int32)
+    for i in np.ndindex(*rows):
+        n = -(-lens[i[0]] // bk)
+        counts[i] = rng.integers(0, n + 1)
+        lists[i][: counts[i]] = rng.permutation(n)[: counts[i]]
+    q = torch.from_numpy(rng.standard_normal((B, H * g, 128)).astype(np.float32)).to(DEV).bfloat16()
+    out, lse, stop = api.decode_attention_quant(
+        q, cache, torch.from_numpy(table).to(DEV), torch.tensor(lens, dtype=torch.int32, device=DEV),
+        block_size=bk, tau=0.0, phi=0.0, patience=1, softmax_scale=0.1, no_detector=True,
+        block_list=torch.from_numpy(lists).to(DEV), block_list_len=torch.from_numpy(counts).to(DEV),
+        list_per_head=per_head)
+    out, lse, stop = (x.double().cpu().numpy() for x in (out, lse, stop))
+    qd, host = q.double().cpu().numpy(), _host(cache)
+    for b in range(0, B, 7):
+        for h in range(H):
+            i = (b, h) if per_head else (b,)
+            n = int(counts[i])
+            assert stop[b, h] == n
+            at = np.concatenate([np.arange(j * bk, min((j + 1) * bk, lens[b])) for j in lists[i][:n]]) if n else []
+            qs = slice(h * g, (h + 1) * g)
+            if n == 0:
+                assert not out[b, qs].any() and np.all(np.isneginf(lse[b, qs]))
+                continue
+            k, v = _dequantised(cache, table[b], lens[b], h, host)
+            o, l, ds = R.full_attention(qd[b, qs], k[at], v[at], float(np.float32(0.1)))
+            tol = (2 * ds + 64 * 2.0 ** -24) * np.abs(v[at]).max()
+            assert np.all(np.abs(out[b, qs] - o) <= tol[:, None]), (b, h)
+            assert np.all(np.abs(lse[b, qs] - l) <= ds + 64 * 2.0 ** -24 * np.maximum(1, np.abs(l)))
