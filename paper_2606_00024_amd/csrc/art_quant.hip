@@ -85,9 +85,16 @@ __device__ __forceinline__ Span span_of(const QuantParams& P, const SpanTable& t
     s.first = s.b * P.per_seq;
     s.end = s.first + P.per_seq;
   } else {
+    // 64 places a step: each narrows the range to one 64th
+    int n = P.batch;
     s.b = 0;
-    for (int i = 0; i < P.batch; i += 64)
-      s.b += __popcll(__ballot(i + lane < P.batch && P.offsets[i + lane + 1] <= row));
+    while (n > 64) {
+      const int each = (n + 63) / 64, at = (lane + 1) * each;   // sequences s.b + at - each .. s.b + at - 1
+      const int c = __popcll(__ballot(at <= n && P.offsets[s.b + at] <= row)) * each;
+      s.b += c;
+      n = min(each, n - c);
+    }
+    s.b += __popcll(__ballot(lane < n && P.offsets[s.b + lane + 1] <= row));
     s.first = s.end = row;
     if (s.b < P.batch) {
       s.first = P.offsets[s.b];
@@ -399,34 +406,43 @@ __global__ void __launch_bounds__(kThreads) read_kernel(const QuantParams P) {
   const Side& S = P.side[u >= P.heads ? 1 : 0];
   const int head = u >= P.heads ? u - P.heads : u, c = lane % C::LANES;
   const int row0 = part * (C::ROWS * STEPS), in_step = lane / C::LANES;
-  const Span s0 = span_of(P, span_table(P, lane), row0, lane);
+  const SpanTable table = span_table(P, lane);
+  Span s = span_of(P, table, row0, lane);
+  int b[STEPS];
+  int64_t t[STEPS];
+  const int stop = min(row0 + C::ROWS * STEPS, P.rows);
+  if (s.first <= row0 && stop <= s.end && s.pos >= 0) {   // all rows are one sequence's
+#pragma unroll
+    for (int k = 0; k < STEPS; ++k) {
+      const int row = row0 + C::ROWS * k + in_step;
+      b[k] = s.b;
+      t[k] = row < stop ? s.pos + ((int64_t)row - s.first) : -1;
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < STEPS; ++k) {
+      // the spans that the step's rows belong to, one after the other
+      const int first = row0 + C::ROWS * k, last = min(first + C::ROWS, P.rows), row = first + in_step;
+      b[k] = 0;
+      t[k] = -1;
+      for (int r = first; r < last;) {
+        if (r >= s.end) s = span_of(P, table, r, lane);
+        if (s.b >= P.batch) break;                                             // rows behind the last sequence
+        if (s.first > r || s.end <= r) { r = max(r + 1, s.first); continue; }  // before the first one (or no offsets)
+        if (row >= r && row < s.end && s.pos >= 0) {
+          b[k] = s.b;
+          t[k] = s.pos + ((int64_t)row - s.first);
+        }
+        r = s.end;
+      }
+      if (row >= last) t[k] = -1;
+    }
+  }
   int pg[STEPS], slot[STEPS];
 #pragma unroll
   for (int k = 0; k < STEPS; ++k) {
-    const int row = row0 + C::ROWS * k + in_step;
-    Span s = s0;
-    if (P.offsets) {
-      // lanes whose row lies behind the span go on to their own
-      while (s.b < P.batch && row >= s.end) {
-        ++s.b;
-        if (s.b < P.batch) {
-          s.first = P.offsets[s.b];
-          s.end = max(s.end, min(P.offsets[s.b + 1], P.rows));
-          s.pos = P.positions ? P.positions[s.b] : 0;
-        }
-      }
-    } else if (row >= s.end) {
-      s.b = row / P.per_seq;
-      s.first = s.b * P.per_seq;
-      s.pos = s.b < P.batch && P.positions ? P.positions[s.b] : 0;
-    }
-    pg[k] = -1;
-    slot[k] = 0;
-    if (row < P.rows && s.b < P.batch && s.pos >= 0 && s.first >= 0 && row >= s.first) {
-      const int64_t t = s.pos + ((int64_t)row - s.first);
-      pg[k] = page_of(P, s.b, t);
-      slot[k] = (int)(t & ((1 << P.page_shift) - 1));
-    }
+    pg[k] = page_of(P, b[k], t[k]);
+    slot[k] = (int)(t[k] & ((1 << P.page_shift) - 1));
   }
   float scale[STEPS];
   uint32_t w[STEPS][C::CODES / 4];

@@ -299,12 +299,13 @@ def test_strides(form):
     assert not out[:, :512].any()
 
 
-def test_many_sequences():
+@pytest.mark.parametrize("B", [64, 65, 300, 5000])
+def test_many_sequences(B):
     """More sequences than a wavefront has lanes, most of them empty."""
     rng = np.random.default_rng(27)
-    B, H = 300, 1
+    H = 1
     counts = rng.integers(0, 3, B).tolist()
-    counts[100:200] = [0] * 100
+    counts[B // 3: 2 * B // 3] = [0] * (2 * B // 3 - B // 3)
     cache, host = _filled(rng, "e4m3", B + 1, H, 16, 16)
     pages = _pages(rng, B, 1)
     offsets = np.concatenate([[0], np.cumsum(counts)]).tolist()
