@@ -246,15 +246,22 @@ __device__ __forceinline__ uint32_t needed_scale(uint32_t a) {
 
 // Append.  One wavefront quantises one run of slots of one head's K or V: 16
 // bytes of a row to a lane, four rows a step (two of 32-bit values), and up to
-// 64 rows (32) stay in registers between the pass that takes their largest
+// 64 rows stay in registers between the pass that takes their largest
 // magnitude and the one that rounds them (of longer runs the second pass reads
-// them again, from the L2).  They are read past the caches (88 us with plain
-// loads and 65 without, for 54K rows of 8 heads: 5.1 TB/s).  A run that a sequence has begun before keeps its
-// scale unless it has to grow; only then are its old codes read and rounded
-// anew.
-constexpr int kSlab = 16;   // steps in registers
+// them again).  A run that a sequence has begun before keeps its scale unless
+// it has to grow; only then are its old codes read and rounded anew.
+//
+// The bound is HBM: rows read once and codes written once.  54K rows of 8
+// heads, K and V: 65 us in bf16 (5.1 TB/s; 88 with loads that go through the
+// caches), and 48K rows of fp32 91 us (5.4 TB/s; 186 with 32 rows in
+// registers).  Appends of a few rows a sequence are bound by the chain of
+// lookups (offsets, position, page, rows) and want many wavefronts: with 4
+// steps in registers instead of 16, 4096 sequences of one token take 49 us
+// instead of 80, and 8 of one 3.0 instead of 3.9.
 template <int DT>
 struct Step {
+  static constexpr int SLAB = DT == ART_ROWS_F32 ? 32 : 16;   // steps in registers, of long spans
+  static constexpr int SHORT = 4;                             // ... of short ones
   static constexpr int LANES = kHeadDim / kValues<DT>;   // lanes of a row
   static constexpr int ROWS = 64 / LANES;                // rows of a step
 };
@@ -270,7 +277,7 @@ __device__ __forceinline__ void store_codes(uint8_t* p, const u32x4& r, float in
     *reinterpret_cast<uint32_t*>(p) = encode4<FMT, WILD>(x);
 }
 
-template <int FMT, int DT>
+template <int FMT, int DT, int kSlab>
 __device__ void append_run(const QuantParams& P, const Side& S, int head, int b, int64_t t, int row, int n, int old,
                            int lane) {
   constexpr int ROWS = Step<DT>::ROWS, LANES = Step<DT>::LANES;
@@ -351,8 +358,8 @@ __device__ void append_run(const QuantParams& P, const Side& S, int head, int b,
 }
 
 // A wavefront takes the runs whose first new row lies in its window of rows.
-template <int FMT, int DT>
-__global__ void __launch_bounds__(kThreads, 3) append_kernel(const QuantParams P) {
+template <int FMT, int DT, int SLAB>
+__global__ void __launch_bounds__(kThreads, SLAB == Step<DT>::SHORT ? 6 : 3) append_kernel(const QuantParams P) {
   const int lane = threadIdx.x & 63;
   const uint32_t slices = (uint32_t)(2 * P.heads + kWaves - 1) / kWaves, part = blockIdx.x / slices;
   const int u = (blockIdx.x - part * slices) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -373,7 +380,7 @@ __global__ void __launch_bounds__(kThreads, 3) append_kernel(const QuantParams P
     if (s.pos < 0 || t >= cap) { row = s.end; continue; }
     const int in = (int)(t & (run - 1));
     const int left = min(run - in, s.end - row);                   // rows to the run's or the span's end
-    if (row == s.first || in == 0) append_run<FMT, DT>(P, S, head, s.b, t, row, left, row == s.first ? in : 0, lane);
+    if (row == s.first || in == 0) append_run<FMT, DT, SLAB>(P, S, head, s.b, t, row, left, row == s.first ? in : 0, lane);
     row += left;
   }
 }
@@ -546,12 +553,18 @@ art_status check_rows(const art_decode_shape* s, const art_quant_cache* c, const
   return ART_OK;
 }
 
+template <int FMT, int DT>
+void launch_append(const QuantParams& p, dim3 grid, hipStream_t stream) {
+  // few rows a sequence: few of them in registers, which leaves room for twice
+  // the wavefronts
+  auto k = p.window <= 4 ? append_kernel<FMT, DT, Step<DT>::SHORT> : append_kernel<FMT, DT, Step<DT>::SLAB>;
+  hipLaunchKernelGGL(k, grid, dim3(kThreads), 0, stream, p);
+}
 template <int FMT>
 void launch_append(const QuantParams& p, int dtype, dim3 grid, hipStream_t stream) {
-  auto k = dtype == ART_ROWS_BF16  ? append_kernel<FMT, ART_ROWS_BF16>
-           : dtype == ART_ROWS_F16 ? append_kernel<FMT, ART_ROWS_F16>
-                                   : append_kernel<FMT, ART_ROWS_F32>;
-  hipLaunchKernelGGL(k, grid, dim3(kThreads), 0, stream, p);
+  if (dtype == ART_ROWS_BF16) launch_append<FMT, ART_ROWS_BF16>(p, grid, stream);
+  else if (dtype == ART_ROWS_F16) launch_append<FMT, ART_ROWS_F16>(p, grid, stream);
+  else launch_append<FMT, ART_ROWS_F32>(p, grid, stream);
 }
 template <int FMT, int DT>
 void launch_read(const QuantParams& p, hipStream_t stream) {

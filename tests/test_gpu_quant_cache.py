@@ -121,6 +121,24 @@ def test_append(form, dtype, i):
 
 
 @pytest.mark.parametrize("form", R.FORMATS)
+@pytest.mark.parametrize("dtype", list(ROWS))
+def test_append_a_prompt_among_decode_steps(form, dtype):
+    """Few rows a sequence on average, hundreds of one, some of them not finite."""
+    rng = np.random.default_rng(29)
+    counts = [1] * 100 + [130] + [2] * 30
+    B, H, Ps, run = len(counts), 2, 64, 64
+    positions = rng.integers(0, 100, B).tolist()
+    cache, host = _filled(rng, form, B * 4 + 1, H, Ps, run)
+    pages = _pages(rng, B, 4)
+    offsets = np.concatenate([[0], np.cumsum(counts)]).tolist()
+    rows = [_rows(rng, offsets[-1], H, ROWS[dtype]) for _ in range(2)]
+    for r, (at, bad) in zip(rows, ((3, float("inf")), (150, float("nan")))):
+        r[at, 1, 77] = bad
+    _append(cache, host, rows, pages, positions, offsets, form)
+    _same(cache, host)
+
+
+@pytest.mark.parametrize("form", R.FORMATS)
 @pytest.mark.parametrize("H", [1, 8])
 def test_append_uniform_counts(form, H):
     """No offsets: every sequence has as many rows; no positions: from 0."""
