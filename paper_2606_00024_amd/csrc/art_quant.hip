@@ -245,19 +245,21 @@ __device__ __forceinline__ uint32_t needed_scale(uint32_t a) {
 }
 
 // Append.  One wavefront quantises one run of slots of one head's K or V: 16
-// bytes of a row to a lane, four rows a step (two of 32-bit values), and up to
-// 64 rows stay in registers between the pass that takes their largest
-// magnitude and the one that rounds them (of longer runs the second pass reads
-// them again).  A run that a sequence has begun before keeps its scale unless
-// it has to grow; only then are its old codes read and rounded anew.
+// bytes of a row to a lane, four rows a step (two of 32-bit values), and 64
+// rows stay in registers between the pass that takes their largest magnitude
+// and the one that rounds them.  Longer runs have a workgroup each, whose
+// wavefronts take the steps in turn and join their maxima in LDS.  A run that a
+// sequence has begun before keeps its scale unless it has to grow; only then
+// are its old codes read and rounded anew.
 //
 // The bound is HBM: rows read once and codes written once.  54K rows of 8
 // heads, K and V: 65 us in bf16 (5.1 TB/s; 88 with loads that go through the
-// caches), and 48K rows of fp32 91 us (5.4 TB/s; 186 with 32 rows in
-// registers).  Appends of a few rows a sequence are bound by the chain of
-// lookups (offsets, position, page, rows) and want many wavefronts: with 4
-// steps in registers instead of 16, 4096 sequences of one token take 49 us
-// instead of 80, and 8 of one 3.0 instead of 3.9.
+// caches), and 48K rows of fp32 88 us (5.6 TB/s; 184 with 32 rows in
+// registers).  48K bf16 rows in runs of 256: 52 us (one wavefront a run: 137).
+// Appends of a few rows a sequence are bound by the chain of lookups (offsets,
+// position, page, rows) and want many wavefronts: with 4 steps in registers
+// instead of 16, 4096 sequences of one token take 49 us instead of 80, and 8 of
+// one 3.0 instead of 3.9; a long run among them has its rows read twice.
 template <int DT>
 struct Step {
   static constexpr int SLAB = DT == ART_ROWS_F32 ? 32 : 16;   // steps in registers, of long spans
@@ -277,24 +279,36 @@ __device__ __forceinline__ void store_codes(uint8_t* p, const u32x4& r, float in
     *reinterpret_cast<uint32_t*>(p) = encode4<FMT, WILD>(x);
 }
 
-template <int FMT, int DT, int kSlab>
+// What a team's wavefronts (4 of a run longer than one holds, or 1) tell each
+// other of a run: their largest magnitudes, and the run's scale so far.
+struct Team {
+  uint32_t top[2][kWaves];
+  float scale[2];
+};
+
+// The run's new rows are n from token t on, row `row` the first of them;
+// `old` slots of the run were written before.  Uniform over a team, which takes
+// the steps in turn; `turn` counts the team's exchanges (two buffers, as the
+// next one may begin while a wavefront still reads the last).
+template <int FMT, int DT, int kSlab, int TEAM>
 __device__ void append_run(const QuantParams& P, const Side& S, int head, int b, int64_t t, int row, int n, int old,
-                           int lane) {
-  constexpr int ROWS = Step<DT>::ROWS, LANES = Step<DT>::LANES;
+                           int lane, int wave, Team* team, int& turn) {
+  constexpr int ROWS = Step<DT>::ROWS, LANES = Step<DT>::LANES, EACH = ROWS * TEAM;
   // uniform bases and 32-bit lane offsets; the rows are on their way before
   // the page is known (they need none)
-  const int r0 = lane / LANES, c = lane % LANES;
-  const char* src = S.rows + (int64_t)row * S.row + head * S.head;
+  const int r0 = lane / LANES, c = lane % LANES, mine = wave * ROWS;
+  const char* src = S.rows + ((int64_t)row + mine) * S.row + head * S.head;
   const uint32_t from = (uint32_t)(r0 * (int)S.row) + c * 16, to = (uint32_t)(r0 * (int)S.st) + c * kValues<DT>;
+  n -= mine;   // rows from this wavefront's first one on
   auto load = [&](int i) { return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src + (int64_t)i * S.row + from)); };  // row i + r0
   const int page = page_of(P, b, t);
   u32x4 raw[kSlab];
-  const bool held = n <= kSlab * ROWS;
+  const bool held = n + mine <= kSlab * EACH;
   if (held) {
 #pragma unroll
     for (int k = 0; k < kSlab; ++k) {
       raw[k] = u32x4{0u, 0u, 0u, 0u};
-      if (ROWS * k + r0 < n) raw[k] = load(ROWS * k);
+      if (EACH * k + r0 < n) raw[k] = load(EACH * k);
     }
   }
   const int pg = __builtin_amdgcn_readfirstlane(page);
@@ -302,8 +316,25 @@ __device__ void append_run(const QuantParams& P, const Side& S, int head, int b,
   const int slot = (int)(t & ((1 << P.page_shift) - 1));
   float* sp = S.scale + pg * S.scp + head * S.sch + (slot >> P.run_shift);
   uint8_t* pool = S.codes + pg * S.sp + head * S.sh + slot * S.st;
-  auto at = [&](int i) { return pool + (int64_t)i * S.st + to; };
-  const float old_scale = old > 0 ? *sp : 0.f;
+  auto at = [&](int i) { return pool + ((int64_t)i + mine) * S.st + to; };
+  // one wavefront of a team reads the scale, and writes it only after all know it
+  float old_scale = old > 0 && wave == 0 ? *sp : 0.f;
+  auto joined = [&](uint32_t a) {
+    a = wave_max(a);
+    if constexpr (TEAM > 1) {
+      const int e = turn++ & 1;
+      if (lane == 0) {
+        team->top[e][wave] = a;
+        if (wave == 0) team->scale[e] = old_scale;
+      }
+      __syncthreads();
+      old_scale = team->scale[e];
+#pragma unroll
+      for (int i = 0; i < TEAM; ++i) a = max(a, team->top[e][i]);
+      a = __builtin_amdgcn_readfirstlane(a);
+    }
+    return a;
+  };
 
   // the run's scale from its new rows' largest finite magnitude (fp32 bits);
   // old codes follow it where it grows.  Returns 1 / scale.
@@ -313,7 +344,7 @@ __device__ void append_run(const QuantParams& P, const Side& S, int head, int b,
     const float inv = 1.0f / scale;
     if (old > 0 && scale != old_scale) {
       const float ratio = old_scale * inv;
-      for (int i = lane >> 3; i < old; i += 8) {
+      for (int i = wave * 8 + (lane >> 3); i < old; i += 8 * TEAM) {
         u32x4* p = reinterpret_cast<u32x4*>(pool + (int64_t)(i - old) * S.st + (lane & 7) * 16);
         u32x4 w = *p;
 #pragma unroll
@@ -327,7 +358,7 @@ __device__ void append_run(const QuantParams& P, const Side& S, int head, int b,
         *p = w;
       }
     }
-    if (lane == 0 && (old == 0 || scale != old_scale)) *sp = scale;
+    if (wave == 0 && lane == 0 && (old == 0 || scale != old_scale)) *sp = scale;
     return inv;
   };
   if (held) {
@@ -335,12 +366,12 @@ __device__ void append_run(const QuantParams& P, const Side& S, int head, int b,
 #pragma unroll
     for (int k = 0; k < kSlab; ++k) a = max_bits<DT>(a, raw[k]);
     if constexpr (DT != ART_ROWS_F32) a = max(a & 0xffffu, a >> 16);
-    a = wave_max(a);
+    a = joined(a);
     if (a < kNotFinite<DT>) {
       const float inv = settle(as_f32_bits<DT>(a));
 #pragma unroll
       for (int k = 0; k < kSlab; ++k) {
-        if (ROWS * k + r0 < n) store_codes<FMT, DT, false>(at(ROWS * k), raw[k], inv);
+        if (EACH * k + r0 < n) store_codes<FMT, DT, false>(at(EACH * k), raw[k], inv);
       }
       return;
     }
@@ -349,26 +380,30 @@ __device__ void append_run(const QuantParams& P, const Side& S, int head, int b,
   // largest finite magnitude, then codes with clamps, from the rows once more
   uint32_t a = 0;
 #pragma unroll 4
-  for (int i = 0; i < n; i += ROWS)
+  for (int i = 0; i < n; i += EACH)
     if (i + r0 < n) a = max_finite_bits<DT>(a, load(i));
-  const float inv = settle(wave_max(a));
+  const float inv = settle(joined(a));
 #pragma unroll 4
-  for (int i = 0; i < n; i += ROWS)
+  for (int i = 0; i < n; i += EACH)
     if (i + r0 < n) store_codes<FMT, DT, true>(at(i), load(i), inv);
 }
 
-// A wavefront takes the runs whose first new row lies in its window of rows.
-template <int FMT, int DT, int SLAB>
+// A wavefront, or a team, takes the runs whose first new row lies in its window
+// of rows.
+template <int FMT, int DT, int SLAB, int TEAM>
 __global__ void __launch_bounds__(kThreads, SLAB == Step<DT>::SHORT ? 6 : 3) append_kernel(const QuantParams P) {
-  const int lane = threadIdx.x & 63;
-  const uint32_t slices = (uint32_t)(2 * P.heads + kWaves - 1) / kWaves, part = blockIdx.x / slices;
-  const int u = (blockIdx.x - part * slices) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  static_assert(TEAM == 1 || (TEAM == kWaves && SLAB * Step<DT>::ROWS * TEAM >= kMaxRun));
+  __shared__ Team team;
+  constexpr int kSlices = kWaves / TEAM;   // heads of K or V in a workgroup
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t slices = (uint32_t)(2 * P.heads + kSlices - 1) / kSlices, part = blockIdx.x / slices;
+  const int u = (blockIdx.x - part * slices) * kSlices + (TEAM > 1 ? 0 : wave);
   if (u >= 2 * P.heads) return;
   const Side& S = P.side[u >= P.heads ? 1 : 0];
   const int head = u >= P.heads ? u - P.heads : u;
   const int run = 1 << P.run_shift;
   const int64_t cap = (int64_t)P.max_pages << P.page_shift;
-  int row = part * P.window;
+  int row = part * P.window, turn = 0;
   const int stop = min(row + P.window, P.rows);
   const SpanTable table = span_table(P, lane);
   Span s{0, 0, 0, 0};
@@ -380,7 +415,9 @@ __global__ void __launch_bounds__(kThreads, SLAB == Step<DT>::SHORT ? 6 : 3) app
     if (s.pos < 0 || t >= cap) { row = s.end; continue; }
     const int in = (int)(t & (run - 1));
     const int left = min(run - in, s.end - row);                   // rows to the run's or the span's end
-    if (row == s.first || in == 0) append_run<FMT, DT, SLAB>(P, S, head, s.b, t, row, left, row == s.first ? in : 0, lane);
+    if (row == s.first || in == 0)
+      append_run<FMT, DT, SLAB, TEAM>(P, S, head, s.b, t, row, left, row == s.first ? in : 0, lane, TEAM > 1 ? wave : 0,
+                                      &team, turn);
     row += left;
   }
 }
@@ -554,17 +591,23 @@ art_status check_rows(const art_decode_shape* s, const art_quant_cache* c, const
 }
 
 template <int FMT, int DT>
-void launch_append(const QuantParams& p, dim3 grid, hipStream_t stream) {
+void launch_append(const QuantParams& p, hipStream_t stream) {
+  constexpr int kShort = Step<DT>::SHORT, kSlab = Step<DT>::SLAB;
   // few rows a sequence: few of them in registers, which leaves room for twice
-  // the wavefronts
-  auto k = p.window <= 4 ? append_kernel<FMT, DT, Step<DT>::SHORT> : append_kernel<FMT, DT, Step<DT>::SLAB>;
+  // the wavefronts; runs longer than a wavefront holds: a workgroup for each
+  const bool brief = p.window <= 4, team = !brief && (1 << p.run_shift) > kSlab * Step<DT>::ROWS;
+  auto k = brief  ? append_kernel<FMT, DT, kShort, 1>
+           : team ? append_kernel<FMT, DT, kSlab, kWaves>
+                  : append_kernel<FMT, DT, kSlab, 1>;
+  const int64_t slices = team ? 2 * (int64_t)p.heads : (2 * (int64_t)p.heads + kWaves - 1) / kWaves;
+  const dim3 grid((unsigned)(((int64_t)p.rows + p.window - 1) / p.window * slices));
   hipLaunchKernelGGL(k, grid, dim3(kThreads), 0, stream, p);
 }
 template <int FMT>
-void launch_append(const QuantParams& p, int dtype, dim3 grid, hipStream_t stream) {
-  if (dtype == ART_ROWS_BF16) launch_append<FMT, ART_ROWS_BF16>(p, grid, stream);
-  else if (dtype == ART_ROWS_F16) launch_append<FMT, ART_ROWS_F16>(p, grid, stream);
-  else launch_append<FMT, ART_ROWS_F32>(p, grid, stream);
+void launch_append(const QuantParams& p, int dtype, hipStream_t stream) {
+  if (dtype == ART_ROWS_BF16) launch_append<FMT, ART_ROWS_BF16>(p, stream);
+  else if (dtype == ART_ROWS_F16) launch_append<FMT, ART_ROWS_F16>(p, stream);
+  else launch_append<FMT, ART_ROWS_F32>(p, stream);
 }
 template <int FMT, int DT>
 void launch_read(const QuantParams& p, hipStream_t stream) {
@@ -604,11 +647,10 @@ art_status art_quant_append(const art_decode_shape* shape, const art_quant_cache
   int window = 1;
   while (window < cache->scale_tokens && window * 2 <= p.per_seq) window *= 2;
   p.window = window;
-  const dim3 grid((unsigned)((p.rows + window - 1) / window * ((2 * p.heads + kWaves - 1) / kWaves)));
   if (cache->format == ART_QUANT_E4M3)
-    launch_append<ART_QUANT_E4M3>(p, rows->rows_dtype, grid, stream);
+    launch_append<ART_QUANT_E4M3>(p, rows->rows_dtype, stream);
   else
-    launch_append<ART_QUANT_INT8>(p, rows->rows_dtype, grid, stream);
+    launch_append<ART_QUANT_INT8>(p, rows->rows_dtype, stream);
   return hipGetLastError() == hipSuccess ? ART_OK : ART_ERR_HIP;
 }
 

@@ -139,6 +139,29 @@ def test_append_a_prompt_among_decode_steps(form, dtype):
 
 
 @pytest.mark.parametrize("form", R.FORMATS)
+@pytest.mark.parametrize("dtype", list(ROWS))
+@pytest.mark.parametrize("run", [128, 256])
+def test_append_in_parts_to_long_runs(form, dtype, run):
+    """Runs of many rows that come in parts, each larger than the one before,
+    some with infinities and NaN; the last row of a run is its largest."""
+    rng = np.random.default_rng(run)
+    B, H, Ps = 5, 3, 256
+    cache, host = _filled(rng, form, B * 6 + 1, H, Ps, run)
+    pages = _pages(rng, B, 6)
+    positions = [0, 1, 127, 130, 300]
+    for step, counts in enumerate([[600, 7, 1, 126, 250], [3, 120, 129, 0, 33], [200, 5, 128, 257, 6]]):
+        offsets = np.concatenate([[0], np.cumsum(counts)]).tolist()
+        rows = [_rows(rng, offsets[-1], H, ROWS[dtype], 3.0 * 4 ** step) for _ in range(2)]
+        rows[0][offsets[1] - 1] *= 16.0
+        if step == 1:
+            rows[1][offsets[2], 1, 5] = float("-inf")
+            rows[1][offsets[3] - 1, 2, 127] = float("nan")
+        _append(cache, host, rows, pages, positions, offsets, form)
+        _same(cache, host)
+        positions = [p + n for p, n in zip(positions, counts)]
+
+
+@pytest.mark.parametrize("form", R.FORMATS)
 @pytest.mark.parametrize("H", [1, 8])
 def test_append_uniform_counts(form, H):
     """No offsets: every sequence has as many rows; no positions: from 0."""
