@@ -4,14 +4,12 @@
 // cut for the memory system alone.  The 64-token tiles of all (sequence, KV
 // head) groups form one line, and every workgroup takes an equal, contiguous
 // part of it, however ragged the batch is; the part of a group in a
-// workgroup's range is a segment.  (Where that leaves a workgroup few tiles, a
-// second segment costs more than an uneven share: groups are then cut into
-// equal parts, a workgroup to each, or, where there are many, each is one
-// wavefront's.)  The four wavefronts of a workgroup take a
-// segment's tiles in turn, each with its own running maximum, mass and output
-// sums in registers, and join at its end through LDS.  A group that lies in
-// one workgroup is written out there; of the others each segment leaves a
-// record (m, L, o) in the workspace and a second, small launch joins them.
+// workgroup's range is a segment.  (Short batches are cut by groups instead,
+// see cut_of.)  The four wavefronts of a workgroup take a segment's tiles in
+// turn, each with its own running maximum, mass and output sums in registers,
+// and join at its end through LDS.  A group that lies in one workgroup is
+// written out there; of the others each segment leaves a record (m, L, o) in
+// the workspace and a second, small launch joins them.
 //
 //   s_j = scale * (ks_j (q . ck_j)),  p_j = 2^(s_j log2 e - m),
 //   out = sum_j p_j vs_j cv_j / sum_j p_j
@@ -69,22 +67,27 @@ __device__ __forceinline__ int unit_tiles(Params& P, int u) {
 __device__ __forceinline__ int unit_heads(Params& P) { return per_group_units(P) ? 1 : P.num_kv_heads; }
 
 // How the tiles are cut for `most` workgroups.
-//   kLine   the line in `workers` equal ranges (every wavefront gets a tile)
+//   kLine   the line in `workers` equal ranges.  A segment's set-up and end take
+//           a workgroup about as long as 8 tiles, so every group has 8 more
+//           places on the line, before its tiles: a range of many short groups
+//           is then no longer than others (60 sequences of 100 to 3000 tokens, 8
+//           heads: 78 us without them and 53 with).
 //   kParts  every group in parts of `part` tiles, of which there are no more
-//           than `most`: where a range would hold 16 tiles or fewer (16 ragged
-//           sequences of up to 2K tokens 26.5 -> 19.3 us)
-//   kWaves1 every group to one wavefront
-// A segment's set-up and end take about as long as three tiles of a wavefront;
-// with that the last takes the rounds of groups times the longest one, and the
-// line a wavefront's share of the tiles and the segments of its workgroup.
-// (4096 sequences of 100 tokens, 8 heads: 783 us by the line.)
+//           than `most`: for few groups, where a range would hold 16 tiles or
+//           fewer (16 ragged sequences of up to 2K tokens 26.5 -> 19.3 us), and
+//           whole groups where the longest is not much longer than a range (45
+//           sequences of 376 to 1056 tokens, 8 heads: 36 -> 32.5 us)
+//   kWaves1 every group to one wavefront: where the rounds of groups, each as
+//           long as the longest one, end before the line's ranges with their
+//           segments (4096 sequences of 100 tokens, 8 heads: 783 -> 275 us)
+constexpr int kSegment = 8;
 enum CutKind { kLine, kParts, kWaves1 };
 struct Cut {
   CutKind kind;
   int64_t workers;
   int part;
 };
-__device__ __forceinline__ Cut cut_of(Params& P, int64_t total, int64_t longest, int64_t most) {
+__device__ __forceinline__ Cut cut_of(Params& P, int64_t total, int longest, int64_t most) {
   const int64_t groups = (int64_t)P.batch * P.num_kv_heads, waves = most * kWaves;
   const Cut line{kLine, max((int64_t)1, min(most, (total + kWaves - 1) / kWaves)), 0};
   if (2 * groups <= most) {
@@ -92,6 +95,7 @@ __device__ __forceinline__ Cut cut_of(Params& P, int64_t total, int64_t longest,
     const int64_t room = most - groups;
     return Cut{kParts, most, max((int)((total + room - 1) / room), kWaves)};
   }
+  if (groups <= most && longest <= (total + kSegment * groups) / most + 6) return Cut{kParts, most, max(longest, 1)};
   if ((groups + waves - 1) / waves * (2 + longest) <= total / waves + 3 * (groups / most + 1))
     return Cut{kWaves1, most, 0};
   return line;
@@ -235,163 +239,163 @@ __device__ __forceinline__ void walk_tiles(Params& P, const Segment& s, int lane
 
 #pragma unroll 1
   for (int first = 0; first < n_mine; first += 16) {
-  const int n_set = min(16, n_mine - first);
-  const TileAt over = tile_at(nxt, 0);
-  ahead_scales(P, s, lane, nxt);
-  ahead_pages(P, s, first + 32, n_mine, lane, far);
+    const int n_set = min(16, n_mine - first);
+    const TileAt over = tile_at(nxt, 0);
+    ahead_scales(P, s, lane, nxt);
+    ahead_pages(P, s, first + 32, n_mine, lane, far);
 #pragma unroll 1
-  for (int m = 0; m < n_set; ++m) {
-    const int tok0 = at.tok0;
-    // (behind the last tile, that tile once more)
-    if (m + 1 < n_set) at = tile_at(cur, m + 1);
-    else if (first + 16 < n_mine) at = over;
-    float ks[4], vs[4];
+    for (int m = 0; m < n_set; ++m) {
+      const int tok0 = at.tok0;
+      // (behind the last tile, that tile once more)
+      if (m + 1 < n_set) at = tile_at(cur, m + 1);
+      else if (first + 16 < n_mine) at = over;
+      float ks[4], vs[4];
 #pragma unroll
-    for (int n = 0; n < 4; ++n) {
-      ks[n] = read_lane(cur.ks, 4 * m + n);
-      vs[n] = read_lane(cur.vs, 4 * m + n);
-    }
-
-    // scores, transposed: St[n][r] is token 16n + 4g + r, head lo mod COLS
-    f32x4 St[4];
-#pragma unroll
-    for (int n = 0; n < 4; ++n) {
-      St[n] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-        St[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-            __builtin_bit_cast(bf16x8, codes_bf16<FMT>(t.k[n][k >> 1], k & 1)), qa[k], St[n], 0, 0, 0);
-    }
-    // K's registers are free: the next tile's K is on its way while this one
-    // goes through the softmax and P.V (at the end the last tile once more)
-    load_k(P, s.kvh, s.L, at, lane, t);
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      *reinterpret_cast<u32x4*>(stage + code_stage_off(8 * j + (lane >> 3), lane & 7)) = t.v[j];
-    load_v(P, s.kvh, s.L, at, lane, t);
-    __builtin_amdgcn_sched_barrier(0);
-
-    float sc[NS][4];
-    float top = kNegInf;
-#pragma unroll
-    for (int j = 0; j < NS; ++j) {
-      const float c = own_scale<REP>(ks[0], ks[1], ks[2], ks[3], j, u) * P.scale_log2;
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        float x = St[REP * j][r];
-        if constexpr (REP == 2) {
-          x = u ? St[2 * j + 1][r] : x;
-        } else if constexpr (REP == 4) {
-          const float y = (u & 1) ? St[1][r] : x, z = (u & 1) ? St[3][r] : St[2][r];
-          x = (u & 2) ? z : y;
-        }
-        sc[j][r] = x * c;
+      for (int n = 0; n < 4; ++n) {
+        ks[n] = read_lane(cur.ks, 4 * m + n);
+        vs[n] = read_lane(cur.vs, 4 * m + n);
       }
-    }
-    if (tok0 + kTile > s.L) {
+
+      // scores, transposed: St[n][r] is token 16n + 4g + r, head lo mod COLS
+      f32x4 St[4];
+#pragma unroll
+      for (int n = 0; n < 4; ++n) {
+        St[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          St[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+              __builtin_bit_cast(bf16x8, codes_bf16<FMT>(t.k[n][k >> 1], k & 1)), qa[k], St[n], 0, 0, 0);
+      }
+      // K's registers are free: the next tile's K is on its way while this one
+      // goes through the softmax and P.V (at the end the last tile once more)
+      load_k(P, s.kvh, s.L, at, lane, t);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        *reinterpret_cast<u32x4*>(stage + code_stage_off(8 * j + (lane >> 3), lane & 7)) = t.v[j];
+      load_v(P, s.kvh, s.L, at, lane, t);
+      __builtin_amdgcn_sched_barrier(0);
+
+      float sc[NS][4];
+      float top = kNegInf;
+#pragma unroll
+      for (int j = 0; j < NS; ++j) {
+        const float c = own_scale<REP>(ks[0], ks[1], ks[2], ks[3], j, u) * P.scale_log2;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          float x = St[REP * j][r];
+          if constexpr (REP == 2) {
+            x = u ? St[2 * j + 1][r] : x;
+          } else if constexpr (REP == 4) {
+            const float y = (u & 1) ? St[1][r] : x, z = (u & 1) ? St[3][r] : St[2][r];
+            x = (u & 2) ? z : y;
+          }
+          sc[j][r] = x * c;
+        }
+      }
+      if (tok0 + kTile > s.L) {
+#pragma unroll
+        for (int j = 0; j < NS; ++j)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (tok0 + 16 * (REP * j + u) + 4 * g + r >= s.L) sc[j][r] = kNegInf;
+      }
 #pragma unroll
       for (int j = 0; j < NS; ++j)
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-          if (tok0 + 16 * (REP * j + u) + 4 * g + r >= s.L) sc[j][r] = kNegInf;
-    }
+        for (int r = 0; r < 4; ++r) top = fmaxf(top, sc[j][r]);
+      if (__any(top > st.m + 8.0f)) {
+        if constexpr (REP >= 2) top = fmaxf(top, dpp_f<kRowRor8>(top));
+        if constexpr (REP == 4) top = fmaxf(top, dpp_f<kRowRor4>(top));
+        const float mn = fmaxf(st.m, rows_max(top));
+        const float a = st.m == kNegInf ? 0.f : fast_exp2(st.m - mn);
+        st.m = mn;
+        st.l *= a;
 #pragma unroll
-    for (int j = 0; j < NS; ++j)
+        for (int r = 0; r < 4; ++r) {
+          // the factor of row 4g + r's head
+          float f = read_lane(a, r);
+          if constexpr (COLS >= 8) f = (g & 1) ? read_lane(a, 4 + r) : f;
+          if constexpr (COLS == 16) f = g == 2 ? read_lane(a, 8 + r) : g == 3 ? read_lane(a, 12 + r) : f;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) top = fmaxf(top, sc[j][r]);
-    if (__any(top > st.m + 8.0f)) {
-      if constexpr (REP >= 2) top = fmaxf(top, dpp_f<kRowRor8>(top));
-      if constexpr (REP == 4) top = fmaxf(top, dpp_f<kRowRor4>(top));
-      const float mn = fmaxf(st.m, rows_max(top));
-      const float a = st.m == kNegInf ? 0.f : fast_exp2(st.m - mn);
-      st.m = mn;
-      st.l *= a;
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        // the factor of row 4g + r's head
-        float f = read_lane(a, r);
-        if constexpr (COLS >= 8) f = (g & 1) ? read_lane(a, 4 + r) : f;
-        if constexpr (COLS == 16) f = g == 2 ? read_lane(a, 8 + r) : g == 3 ? read_lane(a, 12 + r) : f;
-#pragma unroll
-        for (int d = 0; d < 8; ++d) st.acc[d][r] *= f;
+          for (int d = 0; d < 8; ++d) st.acc[d][r] *= f;
+        }
       }
-    }
-    const float ref = st.m == kNegInf ? 0.f : st.m;
+      const float ref = st.m == kNegInf ? 0.f : st.m;
 #pragma unroll
-    for (int j = 0; j < NS; ++j)
+      for (int j = 0; j < NS; ++j)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        sc[j][r] = fast_exp2(sc[j][r] - ref);
-        st.l += sc[j][r];
-      }
+        for (int r = 0; r < 4; ++r) {
+          sc[j][r] = fast_exp2(sc[j][r] - ref);
+          st.l += sc[j][r];
+        }
 
-    // P times V's scales, in three bf16 parts (24 significant bits); the
-    // parts' rows of A are laid out as in the decode kernel: up to four heads
-    // have all of them in one operand, eight in two
-    uint32_t own[NS][3][2];
+      // P times V's scales, in three bf16 parts (24 significant bits); the
+      // parts' rows of A are laid out as in the decode kernel: up to four heads
+      // have all of them in one operand, eight in two
+      uint32_t own[NS][3][2];
 #pragma unroll
-    for (int j = 0; j < NS; ++j) {
-      const float c = own_scale<REP>(vs[0], vs[1], vs[2], vs[3], j, u);
+      for (int j = 0; j < NS; ++j) {
+        const float c = own_scale<REP>(vs[0], vs[1], vs[2], vs[3], j, u);
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        float a0 = sc[j][2 * e] * c, a1 = sc[j][2 * e + 1] * c;
+        for (int e = 0; e < 2; ++e) {
+          float a0 = sc[j][2 * e] * c, a1 = sc[j][2 * e + 1] * c;
 #pragma unroll
-        for (int k = 0; k < 3; ++k) {
-          const uint32_t w = pack_bf16(a0, a1);
-          own[j][k][e] = w;
-          a0 = a0 - bf_lo(w);
-          a1 = a1 - bf_hi(w);
-          if (G <= 8 && k == 1) {
-            a0 = 0.5f * a0;
-            a1 = 0.5f * a1;
+          for (int k = 0; k < 3; ++k) {
+            const uint32_t w = pack_bf16(a0, a1);
+            own[j][k][e] = w;
+            a0 = a0 - bf_lo(w);
+            a1 = a1 - bf_hi(w);
+            if (G <= 8 && k == 1) {
+              a0 = 0.5f * a0;
+              a1 = 0.5f * a1;
+            }
           }
         }
       }
-    }
-    bf16x8 a[2][NP];
-    if constexpr (G > 8) {
+      bf16x8 a[2][NP];
+      if constexpr (G > 8) {
 #pragma unroll
-      for (int k = 0; k < 3; ++k)
+        for (int k = 0; k < 3; ++k)
 #pragma unroll
-        for (int c = 0; c < 2; ++c)
-          a[c][k] = __builtin_bit_cast(
-              bf16x8, u32x4{own[2 * c][k][0], own[2 * c][k][1], own[2 * c + 1][k][0], own[2 * c + 1][k][1]});
-    } else {
-      const int h = lo & (COLS - 1);
+          for (int c = 0; c < 2; ++c)
+            a[c][k] = __builtin_bit_cast(
+                bf16x8, u32x4{own[2 * c][k][0], own[2 * c][k][1], own[2 * c + 1][k][0], own[2 * c + 1][k][1]});
+      } else {
+        const int h = lo & (COLS - 1);
 #pragma unroll
-      for (int k = 0; k < (G > 4 ? 3 : 4); ++k)
+        for (int k = 0; k < (G > 4 ? 3 : 4); ++k)
 #pragma unroll
-        for (int j = 0; j < NS; ++j)
-          *reinterpret_cast<u32x2*>(parts + (COLS * k + h) * 64 + g * 16 + 4 * (REP * j + u)) =
-              u32x2{own[j][k < 3 ? k : 2][0], own[j][k < 3 ? k : 2][1]};
+          for (int j = 0; j < NS; ++j)
+            *reinterpret_cast<u32x2*>(parts + (COLS * k + h) * 64 + g * 16 + 4 * (REP * j + u)) =
+                u32x2{own[j][k < 3 ? k : 2][0], own[j][k < 3 ? k : 2][1]};
+        wave_lds_order();
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          a[c][0] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(parts + lo * 64 + g * 16 + 8 * c));
+          if constexpr (NP == 2)
+            a[c][1] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(parts + (16 + h) * 64 + g * 16 + 8 * c));
+        }
+      }
       wave_lds_order();
+
+      // P.V: element e of lane (lo, g) of K-step c is token 16(2c + e/4) + 4g +
+      // e%4, dim 16d + lo
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
-        a[c][0] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(parts + lo * 64 + g * 16 + 8 * c));
-        if constexpr (NP == 2)
-          a[c][1] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(parts + (16 + h) * 64 + g * 16 + 8 * c));
+        const int k = lo >> 1, row = 16 * (2 * c + (k >> 2)) + 4 * g + (k & 3);
+#pragma unroll
+        for (int d = 0; d < 8; ++d) {
+          const bf16x8 b = codes_tr<FMT>(stage, row, d, lo);
+#pragma unroll
+          for (int j = 0; j < NP; ++j)
+            st.acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[c][j], b, st.acc[d], 0, 0, 0);
+        }
       }
+      wave_lds_order();   // these reads come before the next tile's writes
     }
-    wave_lds_order();
-
-    // P.V: element e of lane (lo, g) of K-step c is token 16(2c + e/4) + 4g +
-    // e%4, dim 16d + lo
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      const int k = lo >> 1, row = 16 * (2 * c + (k >> 2)) + 4 * g + (k & 3);
-#pragma unroll
-      for (int d = 0; d < 8; ++d) {
-        const bf16x8 b = codes_tr<FMT>(stage, row, d, lo);
-#pragma unroll
-        for (int j = 0; j < NP; ++j)
-          st.acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[c][j], b, st.acc[d], 0, 0, 0);
-      }
-    }
-    wave_lds_order();   // these reads come before the next tile's writes
-  }
-  cur = nxt;
-  nxt = far;
+    cur = nxt;
+    nxt = far;
   }
 }
 
@@ -555,7 +559,7 @@ __global__ void __launch_bounds__(kThreads, 2) full_kernel(const KernelParams, c
   const bool in_parts = cut.kind == kParts;
   auto weight = [&](int u) {
     const int n = unit_tiles(P, u);
-    return (int64_t)heads * (in_parts ? parts_of(n, cut.part) : n);
+    return (int64_t)heads * (n == 0 ? 0 : in_parts ? parts_of(n, cut.part) : n + kSegment);
   };
   const int per = (units + kThreads - 1) / kThreads;
   const int u0 = tid * per, u1 = min(units, u0 + per);
@@ -576,7 +580,7 @@ __global__ void __launch_bounds__(kThreads, 2) full_kernel(const KernelParams, c
     line += s_wave[1][w];
   }
   before -= own;
-  line = uniform(line);   // tiles of the line, or parts
+  line = uniform(line);   // places on the line, or parts
   const int64_t workers = in_parts ? line : cut.workers, me = blockIdx.x;
   if (me >= workers) return;
   const int64_t begin = in_parts ? me : uniform(me * line / workers);
@@ -597,20 +601,25 @@ __global__ void __launch_bounds__(kThreads, 2) full_kernel(const KernelParams, c
   for (int64_t x = begin; x < end;) {
     Params& P = *fresh(args);
     int tiles = __builtin_amdgcn_readfirstlane(unit_tiles(P, u));
-    while (!in_parts && x >= base + (int64_t)tiles * heads) {
-      base += (int64_t)tiles * heads;
+    while (!in_parts && (tiles == 0 || x >= base + (int64_t)(tiles + kSegment) * heads)) {
+      base += tiles == 0 ? 0 : (int64_t)(tiles + kSegment) * heads;
       tiles = __builtin_amdgcn_readfirstlane(unit_tiles(P, ++u));
     }
-    // in parts: part x - base - h * parts of head h
-    const int each = in_parts ? parts_of(tiles, cut.part) : tiles;
+    // a group's places on the line (or its parts), from `start` on
+    const int each = in_parts ? parts_of(tiles, cut.part) : tiles + kSegment;
     const int h = __builtin_amdgcn_readfirstlane((int)((x - base) / each));
-    const int64_t start = base + (int64_t)h * each;   // of the group
+    const int64_t start = base + (int64_t)h * each;
+    const int64_t next = min(end, start + each);
+    const int t0 = in_parts ? (int)(x - start) * cut.part : max((int)(x - start) - kSegment, 0);
+    const int n = in_parts ? min(cut.part, tiles - t0) : (int)(next - start) - kSegment - t0;
+    x = next;
+    if (n <= 0) continue;   // only the places before its tiles
     Segment s;
     s.b = per_group_units(P) ? u / P.num_kv_heads : u;
     s.kvh = per_group_units(P) ? u % P.num_kv_heads : h;
     s.L = __builtin_amdgcn_readfirstlane(seq_len(P, s.b));
-    s.t0 = (int)(x - start) * (in_parts ? cut.part : 1);
-    s.n = in_parts ? min(cut.part, tiles - s.t0) : (int)(min(end, start + tiles) - x);
+    s.t0 = t0;
+    s.n = n;
     s.off = wave;
     s.step = kWaves;
     s.list = P.block_list ? P.block_list + (int64_t)u * P.max_list : nullptr;
@@ -627,8 +636,8 @@ __global__ void __launch_bounds__(kThreads, 2) full_kernel(const KernelParams, c
     // this one's first place, one that began here and goes on in its second
     float* const to = W.records + (in_parts ? me : 2 * me + (s.t0 == 0 ? 1 : 0)) * W.record_floats;
     if (s.t0 == 0 && tid == 0) {
-      // who holds the group: the last w with w line / workers <= its last tile
-      const int64_t last = in_parts ? me + each - 1 : ((x + tiles) * workers - 1) / line;
+      // who holds the group: the last w with w line / workers <= its last place
+      const int64_t last = in_parts ? me + each - 1 : ((start + each) * workers - 1) / line;
       W.flags[(int64_t)s.b * W.num_kv_heads + s.kvh] = split_word(me, last, in_parts);
     }
     const int64_t row0 = (int64_t)s.b * W.num_q_heads + s.kvh * G;
@@ -662,7 +671,6 @@ __global__ void __launch_bounds__(kThreads, 2) full_kernel(const KernelParams, c
     }
     if (in_parts) return;
     __syncthreads();   // the records are read before the next segment's tiles
-    x += s.n;
   }
 }
 
