@@ -391,7 +391,8 @@ typedef struct {
 /*
  * art_decode_attention over a cache held in 8 bits: the definition at the top
  * of this header with k = code * k_scale and v = code * v_scale.  Scales are
- * any finite fp32 values (art_quant_append writes powers of two).  All
+ * any finite fp32 values (art_quant_append writes powers of two; V's below
+ * 2^-100 lose low bits, as probabilities are multiplied by them).  All
  * options, the workspace (art_decode_workspace_bytes of the same shape and
  * options), lists, outputs and restrictions are those of
  * art_decode_attention.  k_cache and v_cache are the code pools.  Codes and
@@ -452,9 +453,9 @@ typedef struct {
  *           rounded the same way
  * A scale that is a power of two costs e4m3 codes nothing but their smallest
  * values and int8 codes less than one bit, and when a run's scale grows its
- * old codes lose nothing (e4m3) or half a step of the new scale (int8).  Results depend on no
- * order of execution.  Slots that no row or old token of a touched run occupies
- * keep their bytes.  Tokens that two sequences share must not lie in a run
+ * old codes lose nothing but what falls below the smallest (e4m3) or half a
+ * step of the new scale (int8).  Results depend on no order of execution.
+ * Slots that no row or old token of a touched run occupies keep their bytes.  Tokens that two sequences share must not lie in a run
  * that either of them appends to, and no run may get rows twice in a call
  * (positions that overlap): the result for such input is unspecified.
  */

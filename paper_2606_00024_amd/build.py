@@ -8,6 +8,9 @@ floating-point contraction (fused multiply-adds are written explicitly where
 they are wanted), so that every code path that merges softmax states
 produces the same bits.
 
+The decode kernels (art_kernels.hip) compile three times into it: for bf16
+pools and for each format of 8-bit pools (ART_KV_FORMAT).
+
 Besides the product library, the build links three test and measurement
 builds of the same sources:
   libart_bench.so   read-only streaming kernels (the benchmark's measured

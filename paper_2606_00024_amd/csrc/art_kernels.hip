@@ -59,7 +59,9 @@
 
 // This source builds once for each kind of cache (ART_KV_FORMAT): 0, bf16
 // pools; 1 and 2, pools of 8-bit codes (e4m3, int8) with a scale for every run
-// of slots, whose kernels differ in how a tile is loaded (load_tile below).
+// of slots, whose kernels differ in how a tile is loaded and fed to the matrix
+// instructions (load_codes and compute_tile below) and in how many workgroups
+// share a CU.
 #ifndef ART_KV_FORMAT
 #define ART_KV_FORMAT 0
 #endif
