@@ -409,3 +409,63 @@ def test_full_attention_lists_of_many_groups(per_head):
             tol = (2 * ds + 64 * 2.0 ** -24) * np.abs(v[at]).max()
             assert np.all(np.abs(out[b, qs] - o) <= tol[:, None]), (b, h)
             assert np.all(np.abs(lse[b, qs] - l) <= ds + 64 * 2.0 ** -24 * np.maximum(1, np.abs(l)))
+
+
+@pytest.mark.parametrize("B,H,g,lo,hi", [
+    (60, 8, 4, 100, 3000),      # equal ranges of the line, some of many short groups
+    (45, 8, 8, 376, 1056),      # a workgroup to every group
+    (64, 8, 16, 1, 200),
+    (40, 8, 1, 0, 5000),        # ranges again, sequences of no token among them
+    (24, 8, 2, 2000, 6000),     # groups in parts
+    (300, 4, 4, 1, 1500),
+    (9, 8, 8, 1000, 1000),
+])
+def test_full_attention_cuts(B, H, g, lo, hi):
+    rng = np.random.default_rng(B)
+    Ps, pages = 64, 700
+    lens = rng.integers(lo, hi + 1, B).tolist()
+    lens[B // 2] = lo
+    width = -(-hi // Ps)
+    cache = _random_cache(rng, R.FORMATS[B % 2], pages, H, Ps, 16, spread=2.0)
+    table = rng.integers(0, pages, (B, width)).astype(np.int32)
+    q = torch.from_numpy(rng.standard_normal((B, H * g, 128)).astype(np.float32)).to(DEV).bfloat16()
+    out, lse, stop = (x.double().cpu().numpy() for x in api.decode_attention_quant(
+        q, cache, torch.from_numpy(table).to(DEV), torch.tensor(lens, dtype=torch.int32, device=DEV),
+        block_size=64, tau=0.0, phi=0.0, patience=1, softmax_scale=0.1, no_detector=True))
+    assert np.array_equal(stop, np.repeat([[-(-n // 64)] for n in lens], H, axis=1))
+    assert np.isfinite(out).all()
+    qd, host = q.double().cpu().numpy(), _host(cache)
+    for b, h in [divmod(i, H) for i in range(0, B * H, 7)]:
+        qs = slice(h * g, (h + 1) * g)
+        if lens[b] == 0:
+            assert not out[b, qs].any() and np.all(np.isneginf(lse[b, qs]))
+            continue
+        k, v = _dequantised(cache, table[b], lens[b], h, host)
+        o, l, ds = R.full_attention(qd[b, qs], k, v, float(np.float32(0.1)))
+        tol = (2 * ds + 64 * 2.0 ** -24) * np.abs(v).max()
+        assert np.all(np.abs(out[b, qs] - o) <= tol[:, None]), (b, h)
+        assert np.all(np.abs(lse[b, qs] - l) <= ds + 64 * 2.0 ** -24 * np.maximum(1, np.abs(l)))
+
+
+def test_calls_of_every_kind_share_a_workspace():
+    """Full attention, the stability test and the bf16 call in turn over one
+    workspace, each with the bits that it has over one of its own."""
+    wl = small_workload(78, batch=5, kv_heads=2, group=4, seq_len=(9000, 1, 64, 5000, 333), needles=2)
+    cache, plain = R.quantised(wl, "int8", 64)
+    _on_gpu(plain)
+    cache = R.to_device(cache, DEV)
+    kw = dict(block_size=plain.spec.block_size, tau=1e-2, phi=1e-2, patience=2)
+    rest = (plain.page_table, plain.seq_lens)
+    kinds = {
+        "full": lambda **w: api.decode_attention_quant(plain.q, cache, *rest, no_detector=True, **kw, **w),
+        "test": lambda **w: api.decode_attention_quant(plain.q, cache, *rest, **kw, **w),
+        "bf16": lambda **w: api.decode_attention(plain.q, plain.k_cache, plain.v_cache, *rest, **kw, **w),
+        "bf16 full": lambda **w: api.decode_attention(plain.q, plain.k_cache, plain.v_cache, *rest,
+                                                      no_detector=True, **kw, **w),
+    }
+    size = 1 << 24
+    want = {n: call(workspace=api.new_workspace(size, DEV)) for n, call in kinds.items()}
+    shared = api.new_workspace(size, DEV)
+    for n in ["full", "test", "full", "bf16", "full", "full", "bf16 full", "test", "test", "full"]:
+        for a, b in zip(want[n], kinds[n](workspace=shared)):
+            assert torch.equal(a, b), n
