@@ -456,12 +456,12 @@ def test_calls_of_every_kind_share_a_workspace():
     cache = R.to_device(cache, DEV)
     kw = dict(block_size=plain.spec.block_size, tau=1e-2, phi=1e-2, patience=2)
     rest = (plain.page_table, plain.seq_lens)
+    pools = [t.to(DEV) for t in (plain.k_cache, plain.v_cache)]
     kinds = {
         "full": lambda **w: api.decode_attention_quant(plain.q, cache, *rest, no_detector=True, **kw, **w),
         "test": lambda **w: api.decode_attention_quant(plain.q, cache, *rest, **kw, **w),
-        "bf16": lambda **w: api.decode_attention(plain.q, plain.k_cache, plain.v_cache, *rest, **kw, **w),
-        "bf16 full": lambda **w: api.decode_attention(plain.q, plain.k_cache, plain.v_cache, *rest,
-                                                      no_detector=True, **kw, **w),
+        "bf16": lambda **w: api.decode_attention(plain.q, *pools, *rest, **kw, **w),
+        "bf16 full": lambda **w: api.decode_attention(plain.q, *pools, *rest, no_detector=True, **kw, **w),
     }
     size = 1 << 24
     want = {n: call(workspace=api.new_workspace(size, DEV)) for n, call in kinds.items()}
