@@ -95,6 +95,7 @@ art_status check_shape(const art_decode_shape* s, const art_decode_opts* o) {
 struct Walk {
     bool detector;  // the stability test runs
     bool early;     // and tends to stop the walk soon (see walk_of)
+    bool codes;     // over an 8-bit cache, with the test
 };
 
 // Walks that tend to stop early: of groups of few heads, those over lists
@@ -103,9 +104,9 @@ struct Walk {
 // lose as much as they gain: at g = 8 and thresholds of 1e-2, 25 % lists of 4 x 128K tokens
 // take 99 us with 16 leading chunks and 96 with 4, of 8 x 32K 70 and 74,
 // oldest-first 4 x 16K 70 and 67.
-Walk walk_of(const art_decode_shape* s, const art_decode_opts* o, bool listed) {
+Walk walk_of(const art_decode_shape* s, const art_decode_opts* o, bool listed, bool codes) {
     const bool early = s->num_q_heads / s->num_kv_heads <= 4 && (listed || o->dense_order == ART_ORDER_FORWARD);
-    return Walk{!o->no_detector, !o->no_detector && early};
+    return Walk{!o->no_detector, !o->no_detector && early, !o->no_detector && codes};
 }
 
 // Everything about the launch is decided here, never from the data.  What
@@ -131,10 +132,23 @@ art_status plan_chunks(const art_decode_shape* s, const art_decode_opts* o, Walk
     // the loaders stage V in the record the tile is about to write, and the
     // staging buffers go.
     // Kept within 78 KiB, so that two workgroups share a CU's 160 KiB.
+    // Over codes the staging buffers are 4 KiB each.  There the chain of a
+    // group's chunks, 0.3 to 0.8 us each, is soon the longest part of a call,
+    // and longer chunks shorten it.  Two kinds of walk may have a CU's LDS for
+    // one workgroup's: `heavy`, 16 heads, whose 3 blocks are the most that two
+    // workgroups leave room for, from 128 blocks on, and `few`, up to 8 groups
+    // from 768 blocks on.  In us, chunks of 9 in place of 3 at 16 heads: 4
+    // groups of 55K tokens 228 and 100, 1 of 16K 79 and 49, 28 of up to 17K 109
+    // and 63, 128 of 4K to 16K 201 and 162 (256 of up to 2K 53 and 62, which
+    // keep 3); chunks of 15 in place of 9: g = 8, 8 groups of 128K 141 and 122,
+    // g = 4 of 512K 398 and 285, of 50K 51 and 44 (of 30K, g = 2, 31 and 33; 32
+    // groups of 32K 63 and 70).
     const size_t rec_bytes = (size_t)(g * art::kHeadDim + 2 * g) * 4;
     const bool v_in_record = g >= 8 && tpb == 1;
-    const size_t pbuf_bytes = v_in_record ? 0 : (g >= 8 ? (size_t)3 * 4096 : (size_t)3 * 32 * 288) + 16;
-    const size_t lds_cap = 78 * 1024;
+    const size_t pbuf_bytes = v_in_record ? 0 : (g >= 8 || walk.codes ? (size_t)3 * 4096 : (size_t)3 * 32 * 288) + 16;
+    const bool few = walk.codes && n_groups <= 8 && t_cap >= 768;
+    const bool heavy = walk.codes && g == 16 && t_cap >= 128;
+    const size_t lds_cap = few || heavy ? 156 * 1024 : 78 * 1024;
     auto lds_for = [&](int blocks) { return art::kChunkSlots * (size_t)blocks * rec_bytes + pbuf_bytes; };
     int c_max = art::kMaxChunkBlocks;
     while (c_max > 0 && lds_for(c_max) > lds_cap) --c_max;
@@ -149,7 +163,7 @@ art_status plan_chunks(const art_decode_shape* s, const art_decode_opts* o, Walk
         // up to 9 blocks per chunk (12 without the test, which has nothing
         // to decide sooner), a multiple of the three loaders when the
         // budget allows; less when the whole problem has fewer than 64
-        // chunks, or when five chunks would cover the longest traversal that
+        // chunks (unless `heavy`), or when five chunks would cover the longest traversal that
         // the shape allows (cache or list, whichever is longer).  The
         // last rule serves short contexts, which are all latency: 16 ragged
         // sequences of up to 2048 tokens, g = 4, 34.6 us with chunks of 9 and
@@ -163,10 +177,10 @@ art_status plan_chunks(const art_decode_shape* s, const art_decode_opts* o, Walk
         // there were fewer chunks than 1024 cost 17-210 % on problems of 2 to
         // 16 groups; the per-chunk work of the resolver outweighs the wider
         // spread.)
-        const int most = walk.detector ? 9 : 12;
+        const int most = !walk.detector ? 12 : few ? 15 : 9;
         C = c_max < most ? c_max : most;
         if (C >= 3) C -= C % 3;
-        while (C > 3 && (n_groups * ((t_cap + C - 1) / C) < 64 || (!compact && 5 * C > t_cap))) C -= 3;
+        while (C > 3 && ((!heavy && n_groups * ((t_cap + C - 1) / C) < 64) || (!compact && 5 * C > t_cap))) C -= 3;
         // the work list must fit a queue word
         while (C < c_max && n_groups * ((t_cap + C - 1) / C) + art::kQueueSlack >= (1 << art::kQueueBits)) C *= 2;
     }
@@ -246,16 +260,16 @@ art_status choose_plan(const art_decode_shape* s, const art_decode_opts* o, Walk
 
 // Workspace bytes of a shape: the most that the plan of any kind of walk
 // takes, so that one workspace serves every order, lists or none, with and
-// without the test.  (A kind that no plan holds has no say, save the call's
-// own.)
+// without the test, over bf16 and over codes (whose chunks are as long or
+// longer).  (A kind that no plan holds has no say, save the call's own.)
 art_status workspace_of(const art_decode_shape* s, const art_decode_opts* o, size_t* need) {
     art_status st = check_shape(s, o);
     if (st != ART_OK) return st;
     Plan p;
-    st = choose_plan(s, o, walk_of(s, o, false), &p);
+    st = choose_plan(s, o, walk_of(s, o, false, false), &p);
     if (st != ART_OK) return st;
     *need = p.ws.total;
-    for (const Walk walk : {Walk{true, false}, Walk{true, true}, Walk{false, false}})
+    for (const Walk walk : {Walk{true, false, false}, Walk{true, true, false}, Walk{false, false, false}})
         if (choose_plan(s, o, walk, &p) == ART_OK && p.ws.total > *need) *need = p.ws.total;
     return ART_OK;
 }
@@ -264,9 +278,9 @@ art_status workspace_of(const art_decode_shape* s, const art_decode_opts* o, siz
 // of a walk with the test, which serves every kind.  (A program may size its
 // workspace for its longest sequences, and the plan of shorter ones can take
 // more: 44 blocks in chunks of 6, 48 in chunks of 9.)
-art_status fit_plan(const art_decode_shape* s, const art_decode_opts* o, size_t bytes, Plan* p) {
+art_status fit_plan(const art_decode_shape* s, const art_decode_opts* o, bool codes, size_t bytes, Plan* p) {
     if (p->ws.total <= bytes) return ART_OK;
-    const art_status st = plan_chunks(s, o, Walk{true, false}, true, p);
+    const art_status st = plan_chunks(s, o, Walk{true, false, codes && !o->no_detector}, true, p);
     return st == ART_OK && p->ws.total <= bytes ? ART_OK : ART_ERR_WORKSPACE_TOO_SMALL;
 }
 
@@ -276,9 +290,9 @@ art_status check_decode_call(const art_decode_shape* shape, const art_decode_opt
                              const int32_t* page_table, const int32_t* seq_lens,
                              const int32_t* block_list, const int32_t* block_list_len,
                              const void* out, const float* lse, const int32_t* stop_block,
-                             size_t bytes, Plan* plan) {
+                             size_t bytes, Plan* plan, bool codes = false) {
     art_status st = check_shape(shape, opts);
-    if (st == ART_OK) st = choose_plan(shape, opts, walk_of(shape, opts, block_list != nullptr), plan);
+    if (st == ART_OK) st = choose_plan(shape, opts, walk_of(shape, opts, block_list != nullptr, codes), plan);
     if (st != ART_OK) return st;
     if (shape->batch == 0) return ART_OK;
     if (!q || !k_cache || !v_cache || !page_table || !seq_lens || !out || !lse || !stop_block)
@@ -287,7 +301,7 @@ art_status check_decode_call(const art_decode_shape* shape, const art_decode_opt
     if (block_list && shape->max_blocks_per_list <= 0) return ART_ERR_INVALID_ARG;
     if (((uintptr_t)q | (uintptr_t)k_cache | (uintptr_t)v_cache | (uintptr_t)out) % 16)
         return ART_ERR_UNSUPPORTED;
-    return fit_plan(shape, opts, bytes, plan);
+    return fit_plan(shape, opts, codes, bytes, plan);
 }
 
 // What a call over an 8-bit cache adds (nullptr for bf16 pools).
@@ -448,7 +462,7 @@ art_status art_decode_attention_quant(const art_decode_shape* shape, const art_d
     if (st != ART_OK) return st;
     Plan plan;
     st = check_decode_call(shape, opts, q, k_cache, v_cache, page_table, seq_lens, block_list,
-                           block_list_len, out, lse, stop_block, workspace ? workspace_bytes : 0, &plan);
+                           block_list_len, out, lse, stop_block, workspace ? workspace_bytes : 0, &plan, true);
     if (st != ART_OK || shape->batch == 0) return st;
     if (!k_scale || !v_scale || (uintptr_t)workspace % 8 || ((uintptr_t)k_scale | (uintptr_t)v_scale) % 4)
         return ART_ERR_INVALID_ARG;
