@@ -141,8 +141,8 @@ art_status plan_chunks(const art_decode_shape* s, const art_decode_opts* o, Walk
     // groups of 55K tokens 228 and 100, 1 of 16K 79 and 49, 28 of up to 17K 109
     // and 63, 128 of 4K to 16K 201 and 162 (256 of up to 2K 53 and 62, which
     // keep 3); chunks of 15 in place of 9: g = 8, 8 groups of 128K 141 and 122,
-    // g = 4 of 512K 398 and 285, of 50K 51 and 44 (of 30K, g = 2, 31 and 33; 32
-    // groups of 32K 63 and 70).
+    // g = 4 of 512K 398 and 285, of 50K 51 and 44 (of 30K, g = 2, 31 and 33; 16
+    // groups of 100K, g = 4, 120 and 111, but 54 and 64 where they stop early).
     const size_t rec_bytes = (size_t)(g * art::kHeadDim + 2 * g) * 4;
     const bool v_in_record = g >= 8 && tpb == 1;
     const size_t pbuf_bytes = v_in_record ? 0 : (g >= 8 || walk.codes ? (size_t)3 * 4096 : (size_t)3 * 32 * 288) + 16;
