@@ -171,6 +171,11 @@ struct Segment {
   const int32_t* list;
 };
 
+// tiles of this wavefront
+__device__ __forceinline__ int mine_of(const Segment& s) {
+  return s.n > s.off ? (s.n - s.off + s.step - 1) / s.step : 0;
+}
+
 __device__ __forceinline__ void ahead_pages(Params& P, const Segment& s, int first, int n_mine,
                                             int lane, Ahead& a) {
   const int m = first + (lane >> 2);
@@ -219,18 +224,17 @@ struct State {
 
 template <int G, int FMT>
 __device__ __forceinline__ void walk_tiles(Params& P, const Segment& s, int lane,
-                                           const bf16x8 (&qa)[4], uint8_t* stage, uint16_t* parts, State& st) {
+                                           const bf16x8 (&qa)[4], const Ahead (&first_sets)[2], uint8_t* stage,
+                                           uint16_t* parts, State& st) {
   using C = Full<G>;
   constexpr int REP = C::REP, COLS = C::COLS, NS = C::NS, NP = C::NP;
   const int lo = lane & 15, g = lane >> 4, u = lo / COLS;
-  const int n_mine = s.n > s.off ? (s.n - s.off + s.step - 1) / s.step : 0;
+  const int n_mine = mine_of(s);
   if (n_mine == 0) return;
   // Pages are fetched two sets of 16 tiles ahead and scales one, before the
   // loads of a set's first tile: no wait for them then holds up for the tiles
   // in flight behind them.
-  Ahead cur, nxt, far;
-  ahead_pages(P, s, 0, n_mine, lane, cur);
-  ahead_pages(P, s, 16, n_mine, lane, nxt);
+  Ahead cur = first_sets[0], nxt = first_sets[1], far;
   ahead_scales(P, s, lane, cur);
   TileAt at = tile_at(cur, 0);
   Tile t;
@@ -509,11 +513,14 @@ __global__ void __launch_bounds__(kThreads, 2) full_kernel(const KernelParams, c
   float* const rec = reinterpret_cast<float*>(lds + wave * C::WAVE_BYTES);
   uint8_t* const stage = lds + wave * C::WAVE_BYTES;
   uint16_t* const parts = reinterpret_cast<uint16_t*>(stage + 8192);
-  // group (b, kvh)'s query and the state before its first tile
+  // what a segment begins with: its group's query and its first pages.  They
+  // are asked for while the segment before is joined and written.
   bf16x8 qa[4];
-  State st;
-  auto begin_group = [&](const Segment& s) {
+  Ahead sets[2];
+  auto ask = [&](const Segment& s) {
     Params& P = *fresh(args);
+    ahead_pages(P, s, 0, mine_of(s), lane, sets[0]);
+    ahead_pages(P, s, 16, mine_of(s), lane, sets[1]);
     const int head = (lane & 15) & (C::COLS - 1);
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
@@ -523,6 +530,9 @@ __global__ void __launch_bounds__(kThreads, 2) full_kernel(const KernelParams, c
                                             64 * (k >> 1) + 16 * (lane >> 4) + 8 * (k & 1));
       qa[k] = __builtin_bit_cast(bf16x8, w);
     }
+  };
+  State st;
+  auto clear = [&]() {
     st.m = kNegInf;
     st.l = 0.f;
 #pragma unroll
@@ -531,27 +541,40 @@ __global__ void __launch_bounds__(kThreads, 2) full_kernel(const KernelParams, c
 
   if (cut.kind == kWaves1) {
     const int groups = P.batch * P.num_kv_heads;
-    for (int g = blockIdx.x * kWaves + wave; g < groups; g += most * kWaves) {
-      Params& P = *fresh(args);
-      Segment s;
-      s.b = g / P.num_kv_heads;
-      s.kvh = g - s.b * P.num_kv_heads;
-      const int u = per_group_units(P) ? g : s.b;
-      s.L = __builtin_amdgcn_readfirstlane(seq_len(P, s.b));
-      s.n = __builtin_amdgcn_readfirstlane(unit_tiles(P, u));
-      s.t0 = s.off = 0;
-      s.step = 1;
-      s.list = P.block_list ? P.block_list + (int64_t)u * P.max_list : nullptr;
-      if (s.n == 0) continue;   // (the second launch writes empty groups)
-      begin_group(s);
-      walk_tiles<G, FMT>(*fresh(args), s, lane, qa, stage, parts, st);
+    int g = blockIdx.x * kWaves + wave;
+    // the next group that holds tiles (the second launch writes empty ones)
+    auto next_group = [&](Segment& s) {
+      for (; g < groups; g += most * kWaves) {
+        Params& P = *fresh(args);
+        s.b = g / P.num_kv_heads;
+        s.kvh = g - s.b * P.num_kv_heads;
+        const int u = per_group_units(P) ? g : s.b;
+        s.L = __builtin_amdgcn_readfirstlane(seq_len(P, s.b));
+        s.n = __builtin_amdgcn_readfirstlane(unit_tiles(P, u));
+        s.t0 = s.off = 0;
+        s.step = 1;
+        s.list = P.block_list ? P.block_list + (int64_t)u * P.max_list : nullptr;
+        if (s.n > 0) return true;
+      }
+      return false;
+    };
+    Segment s;
+    bool more = next_group(s);
+    if (more) ask(s);
+    while (more) {
+      clear();
+      walk_tiles<G, FMT>(*fresh(args), s, lane, qa, sets, stage, parts, st);
+      const int b = s.b, kvh = s.kvh, done = g;
+      g += most * kWaves;
+      more = next_group(s);
+      if (more) ask(s);
       leave_record<G>(st, rec, lane);
       wave_lds_sync();
       Params& W = *fresh(args);
-      const int64_t row0 = (int64_t)s.b * W.num_q_heads + s.kvh * G;
+      const int64_t row0 = (int64_t)b * W.num_q_heads + kvh * G;
       for (int i = lane; i < G * kD; i += 64) write_out(W, row0 * kD + i, rec[i] / rec[G * kD + G + i / kD]);
       if (lane < G) W.lse[row0 + lane] = ln_of(rec[G * kD + lane], rec[G * kD + G + lane]);
-      if (lane == 0) W.flags[g] = split_word(0, 0, false);
+      if (lane == 0) W.flags[done] = split_word(0, 0, false);
       wave_lds_sync();   // the record is read before the next group's tiles
     }
     return;
@@ -601,49 +624,58 @@ __global__ void __launch_bounds__(kThreads, 2) full_kernel(const KernelParams, c
   int u = __builtin_amdgcn_readfirstlane(s_unit);
   int64_t base = uniform(s_base);
 
-  for (int64_t x = begin; x < end;) {
-    Params& P = *fresh(args);
-    int tiles = __builtin_amdgcn_readfirstlane(unit_tiles(P, u));
-    while (!in_parts && (tiles == 0 || x >= base + (int64_t)(tiles + kSegment) * heads)) {
-      base += tiles == 0 ? 0 : (int64_t)(tiles + kSegment) * heads;
-      tiles = __builtin_amdgcn_readfirstlane(unit_tiles(P, ++u));
+  // A segment and where it lies: its group's places on the line (or its parts)
+  // begin at `start` and are `each` of them.
+  int64_t x = begin, start = 0;
+  int tiles = 0, each = 0;
+  auto next_segment = [&](Segment& s) {
+    while (x < end) {
+      Params& P = *fresh(args);
+      tiles = __builtin_amdgcn_readfirstlane(unit_tiles(P, u));
+      while (!in_parts && (tiles == 0 || x >= base + (int64_t)(tiles + kSegment) * heads)) {
+        base += tiles == 0 ? 0 : (int64_t)(tiles + kSegment) * heads;
+        tiles = __builtin_amdgcn_readfirstlane(unit_tiles(P, ++u));
+      }
+      each = in_parts ? parts_of(tiles, cut.part) : tiles + kSegment;
+      const int h = __builtin_amdgcn_readfirstlane((int)((x - base) / each));
+      start = base + (int64_t)h * each;
+      const int64_t next = min(end, start + each);
+      s.t0 = in_parts ? (int)(x - start) * cut.part : max((int)(x - start) - kSegment, 0);
+      s.n = in_parts ? min(cut.part, tiles - s.t0) : (int)(next - start) - kSegment - s.t0;
+      x = next;
+      if (s.n <= 0) continue;   // only the places before its tiles
+      s.b = per_group_units(P) ? u / P.num_kv_heads : u;
+      s.kvh = per_group_units(P) ? u % P.num_kv_heads : h;
+      s.L = __builtin_amdgcn_readfirstlane(seq_len(P, s.b));
+      s.off = wave;
+      s.step = kWaves;
+      s.list = P.block_list ? P.block_list + (int64_t)u * P.max_list : nullptr;
+      return true;
     }
-    // a group's places on the line (or its parts), from `start` on
-    const int each = in_parts ? parts_of(tiles, cut.part) : tiles + kSegment;
-    const int h = __builtin_amdgcn_readfirstlane((int)((x - base) / each));
-    const int64_t start = base + (int64_t)h * each;
-    const int64_t next = min(end, start + each);
-    const int t0 = in_parts ? (int)(x - start) * cut.part : max((int)(x - start) - kSegment, 0);
-    const int n = in_parts ? min(cut.part, tiles - t0) : (int)(next - start) - kSegment - t0;
-    x = next;
-    if (n <= 0) continue;   // only the places before its tiles
-    Segment s;
-    s.b = per_group_units(P) ? u / P.num_kv_heads : u;
-    s.kvh = per_group_units(P) ? u % P.num_kv_heads : h;
-    s.L = __builtin_amdgcn_readfirstlane(seq_len(P, s.b));
-    s.t0 = t0;
-    s.n = n;
-    s.off = wave;
-    s.step = kWaves;
-    s.list = P.block_list ? P.block_list + (int64_t)u * P.max_list : nullptr;
-
-    begin_group(s);
-    walk_tiles<G, FMT>(*fresh(args), s, lane, qa, stage, parts, st);
+    return false;
+  };
+  Segment s;
+  bool more = next_segment(s);
+  if (more) ask(s);
+  while (more) {
+    clear();
+    walk_tiles<G, FMT>(*fresh(args), s, lane, qa, sets, stage, parts, st);
+    const int b = s.b, kvh = s.kvh;
+    const bool whole = s.n == tiles, begins = s.t0 == 0;
+    // who holds the group: the last w with w line / workers <= its last place
+    const int64_t last = in_parts ? me + each - 1 : ((start + each) * workers - 1) / line;
+    more = !in_parts && next_segment(s);
+    if (more) ask(s);
     leave_record<G>(st, rec, lane);
     __syncthreads();
 
     // the wavefronts' records joined: thread tid takes values tid, tid + 256 ..
     Params& W = *fresh(args);
-    const bool whole = s.n == tiles;
     // (of the line) a group that began in an earlier workgroup leaves its record in
     // this one's first place, one that began here and goes on in its second
-    float* const to = W.records + (in_parts ? me : 2 * me + (s.t0 == 0 ? 1 : 0)) * W.record_floats;
-    if (s.t0 == 0 && tid == 0) {
-      // who holds the group: the last w with w line / workers <= its last place
-      const int64_t last = in_parts ? me + each - 1 : ((start + each) * workers - 1) / line;
-      W.flags[(int64_t)s.b * W.num_kv_heads + s.kvh] = split_word(me, last, in_parts);
-    }
-    const int64_t row0 = (int64_t)s.b * W.num_q_heads + s.kvh * G;
+    float* const to = W.records + (in_parts ? me : 2 * me + (begins ? 1 : 0)) * W.record_floats;
+    if (begins && tid == 0) W.flags[(int64_t)b * W.num_kv_heads + kvh] = split_word(me, last, in_parts);
+    const int64_t row0 = (int64_t)b * W.num_q_heads + kvh * G;
 #pragma unroll 1
     for (int i = tid; i < G * kD; i += kThreads) {
       const int h2 = i / kD;
@@ -672,8 +704,7 @@ __global__ void __launch_bounds__(kThreads, 2) full_kernel(const KernelParams, c
         }
       }
     }
-    if (in_parts) return;
-    __syncthreads();   // the records are read before the next segment's tiles
+    if (more) __syncthreads();   // the records are read before the next segment's tiles
   }
 }
 
