@@ -4,8 +4,8 @@
 // cut for the memory system alone.  The 64-token tiles of all (sequence, KV
 // head) groups form one line, and every workgroup takes an equal, contiguous
 // part of it, however ragged the batch is; the part of a group in a
-// workgroup's range is a segment.  (Short batches are cut by groups instead,
-// see cut_of.)  The four wavefronts of a workgroup take a segment's tiles in
+// workgroup's range is a segment.  (Short batches are cut by groups, many groups
+// by wavefronts instead, see cut_of.)  The four wavefronts of a workgroup take a segment's tiles in
 // turn, each with its own running maximum, mass and output sums in registers,
 // and join at its end through LDS.  A group that lies in one workgroup is
 // written out there; of the others each segment leaves a record (m, L, o) in
@@ -66,38 +66,50 @@ __device__ __forceinline__ int unit_tiles(Params& P, int u) {
 }
 __device__ __forceinline__ int unit_heads(Params& P) { return per_group_units(P) ? 1 : P.num_kv_heads; }
 
-// How the tiles are cut for `most` workgroups.
-//   kLine   the line in `workers` equal ranges.  A segment's set-up and end take
-//           a workgroup about as long as 8 tiles, so every group has 8 more
-//           places on the line, before its tiles: a range of many short groups
-//           is then no longer than others (60 sequences of 100 to 3000 tokens, 8
-//           heads: 78 us without them and 53 with).
+// How the tiles are cut for `most` workgroups.  Up to as many groups:
+//   kLine   the line in equal ranges, one to a workgroup
 //   kParts  every group in parts of `part` tiles, of which there are no more
 //           than `most`: for few groups, where a range would hold 16 tiles or
 //           fewer (16 ragged sequences of up to 2K tokens 26.5 -> 19.3 us), and
 //           whole groups where the longest is not much longer than a range (45
 //           sequences of 376 to 1056 tokens, 8 heads: 36 -> 32.5 us)
-//   kWaves1 every group to one wavefront: where the rounds of groups, each as
-//           long as the longest one, end before the line's ranges with their
-//           segments (4096 sequences of 100 tokens, 8 heads: 783 -> 275 us)
-constexpr int kSegment = 8;
-enum CutKind { kLine, kParts, kWaves1 };
+// More groups (MANY): a workgroup would join its wavefronts at the end of every
+// few tiles, so each wavefront works for itself.
+//   kWaveLine  the line in equal ranges, one to a wavefront (256 sequences of
+//              200 to 2000 tokens, 8 heads: 137 us by kLine, 123 so; of one
+//              query head a group 131, 109)
+//   kEach      every group to one wavefront: where the rounds of groups, each as
+//              long as the longest one, end before the line's ranges with their
+//              segments (4096 sequences of 100 tokens, 8 heads: 783 us by kLine,
+//              310 by kWaveLine, 288 so)
+// A segment's set-up and end take a wavefront about as long as 3 tiles (a
+// workgroup, 8), so every group has kLead places for that on the line, before
+// its tiles: a range of many short groups is then no longer than others (60
+// sequences of 100 to 3000 tokens, 8 heads: 78 us without them and 53 with).
+enum CutKind { kLine, kParts, kWaveLine, kEach };
 struct Cut {
   CutKind kind;
-  int64_t workers;
+  int64_t workers;   // ranges of the line
   int part;
 };
+template <bool MANY>
+constexpr int kLead = MANY ? 3 : 8;
+template <bool MANY>
 __device__ __forceinline__ Cut cut_of(Params& P, int64_t total, int longest, int64_t most) {
-  const int64_t groups = (int64_t)P.batch * P.num_kv_heads, waves = most * kWaves;
+  const int64_t groups = (int64_t)P.batch * P.num_kv_heads;
+  if constexpr (MANY) {
+    const int64_t waves = most * kWaves;
+    if ((groups + waves - 1) / waves * (2 + longest) <= (total + 3 * groups) / waves + 3) return Cut{kEach, waves, 0};
+    // (two records for each of its ranges, in the area of two for every chunk)
+    return Cut{kWaveLine, max((int64_t)1, min(min(waves, groups * P.max_chunks), total)), 0};
+  }
   const Cut line{kLine, max((int64_t)1, min(most, (total + kWaves - 1) / kWaves)), 0};
   if (2 * groups <= most) {
     if (total > 16 * most) return line;
     const int64_t room = most - groups;
     return Cut{kParts, most, max((int)((total + room - 1) / room), kWaves)};
   }
-  if (groups <= most && longest <= (total + kSegment * groups) / most + 6) return Cut{kParts, most, max(longest, 1)};
-  if ((groups + waves - 1) / waves * (2 + longest) <= total / waves + 3 * (groups / most + 1))
-    return Cut{kWaves1, most, 0};
+  if (longest <= (total + 8 * groups) / most + 6) return Cut{kParts, most, max(longest, 1)};
   return line;
 }
 __device__ __forceinline__ int parts_of(int tiles, int part) { return (tiles + part - 1) / part; }
@@ -472,15 +484,15 @@ __device__ __forceinline__ uint64_t split_word(int64_t first, int64_t last, bool
   return (uint64_t)last << 24 | (in_parts ? 1ull << 23 : 0ull) | (uint64_t)first;
 }
 
-template <int G, int FMT>
+template <int G, int FMT, bool MANY>
 __global__ void __launch_bounds__(kThreads, 2) full_kernel(const KernelParams, const int most) {
   Params* const args = (Params*)__builtin_amdgcn_kernarg_segment_ptr();
   Params& P = *args;
   using C = Full<G>;
   extern __shared__ __align__(16) uint8_t lds[];
   __shared__ int64_t s_wave[2][kWaves];
-  __shared__ int64_t s_base;
-  __shared__ int s_unit, s_longest[kWaves];
+  __shared__ int64_t s_base[kWaves];
+  __shared__ int s_unit[kWaves], s_longest[kWaves];
   // (the wavefront's number in a scalar register: everything that follows from
   // it, page addresses above all, then stays there too)
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
@@ -508,7 +520,7 @@ __global__ void __launch_bounds__(kThreads, 2) full_kernel(const KernelParams, c
     total += s_wave[0][w];
     longest = max(longest, s_longest[w]);
   }
-  const Cut cut = cut_of(P, uniform(total * heads), __builtin_amdgcn_readfirstlane(longest), most);
+  const Cut cut = cut_of<MANY>(P, uniform(total * heads), __builtin_amdgcn_readfirstlane(longest), most);
 
   float* const rec = reinterpret_cast<float*>(lds + wave * C::WAVE_BYTES);
   uint8_t* const stage = lds + wave * C::WAVE_BYTES;
@@ -539,90 +551,154 @@ __global__ void __launch_bounds__(kThreads, 2) full_kernel(const KernelParams, c
     for (int d = 0; d < 8; ++d) st.acc[d] = f32x4{0.f, 0.f, 0.f, 0.f};
   };
 
-  if (cut.kind == kWaves1) {
+  // A scan of the units' weights (places on the line, or parts): thread tid has
+  // units u0 .. u1 - 1, `own` places behind the first `before`; returns the line.
+  const int per = (units + kThreads - 1) / kThreads;
+  const int u0 = tid * per, u1 = min(units, u0 + per);
+  auto scan = [&](auto weight, int64_t& own, int64_t& before) {
+    own = 0;
+    for (int u = u0; u < u1; ++u) own += weight(u);
+    before = own;   // inclusive scan over the wavefront, then the workgroup
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int64_t x = __shfl_up((long long)before, o);
+      if (lane >= o) before += x;
+    }
+    if (lane == 63) s_wave[1][wave] = before;
+    __syncthreads();
+    int64_t line = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      if (w < wave) before += s_wave[1][w];
+      line += s_wave[1][w];
+    }
+    before -= own;
+    return uniform(line);
+  };
+  // (one thread) the unit that holds place `at`
+  auto find = [&](auto weight, int64_t at, int64_t own, int64_t before, int i) {
+    if (before <= at && at < before + own) {
+      int u = u0;
+      int64_t base = before;
+      for (int64_t n; base + (n = weight(u)) <= at; ++u) base += n;
+      s_unit[i] = u;
+      s_base[i] = base;
+    }
+  };
+
+  if constexpr (MANY) {
+    const int64_t me = (int64_t)blockIdx.x * kWaves + wave, workers = cut.workers;
+    const bool each_one = cut.kind == kEach;
+    int64_t line = 0, x = 0, end = 0, base = 0;
+    int u = 0;
+    auto places = [&](int tiles) { return tiles == 0 ? 0 : kLead<true> + tiles; };
+    if (!each_one) {
+      auto weight = [&](int u) { return (int64_t)heads * places(unit_tiles(P, u)); };
+      int64_t own, before;
+      line = scan(weight, own, before);
+#pragma unroll 1
+      for (int i = 0; i < kWaves; ++i) {
+        const int64_t w = (int64_t)blockIdx.x * kWaves + i;
+        if (w < workers) find(weight, uniform(w * line / workers), own, before, i);
+      }
+      __syncthreads();
+      if (me >= workers) return;
+      x = uniform(me * line / workers);
+      end = uniform((me + 1) * line / workers);
+      if (x >= end) return;
+      u = __builtin_amdgcn_readfirstlane(s_unit[wave]);
+      base = uniform(s_base[wave]);
+    }
+    // A segment: of the line, its group's places begin at `start`; of kEach, a
+    // group that holds tiles (the second launch writes empty ones).
     const int groups = P.batch * P.num_kv_heads;
-    int g = blockIdx.x * kWaves + wave;
-    // the next group that holds tiles (the second launch writes empty ones)
-    auto next_group = [&](Segment& s) {
-      for (; g < groups; g += most * kWaves) {
+    int64_t start = 0;
+    int tiles = 0, group = (int)me;
+    auto next_segment = [&](Segment& s) {
+      s.off = 0;
+      s.step = 1;
+      while (each_one ? group < groups : x < end) {
         Params& P = *fresh(args);
-        s.b = g / P.num_kv_heads;
-        s.kvh = g - s.b * P.num_kv_heads;
-        const int u = per_group_units(P) ? g : s.b;
+        int v = u;   // its unit
+        if (each_one) {
+          s.b = group / P.num_kv_heads;
+          s.kvh = group - s.b * P.num_kv_heads;
+          v = per_group_units(P) ? group : s.b;
+          s.n = tiles = __builtin_amdgcn_readfirstlane(unit_tiles(P, v));
+          s.t0 = 0;
+          group += most * kWaves;
+        } else {
+          tiles = __builtin_amdgcn_readfirstlane(unit_tiles(P, u));
+          while (x >= base + (int64_t)places(tiles) * heads) {
+            base += (int64_t)places(tiles) * heads;
+            tiles = __builtin_amdgcn_readfirstlane(unit_tiles(P, ++u));
+          }
+          const int h = __builtin_amdgcn_readfirstlane((int)((x - base) / places(tiles)));
+          start = base + (int64_t)h * places(tiles);
+          const int64_t next = min(end, start + places(tiles));
+          s.t0 = max((int)(x - start) - kLead<true>, 0);
+          s.n = (int)(next - start) - kLead<true> - s.t0;
+          x = next;
+          v = u;
+          s.b = per_group_units(P) ? u / P.num_kv_heads : u;
+          s.kvh = per_group_units(P) ? u % P.num_kv_heads : h;
+        }
+        if (s.n <= 0) continue;
         s.L = __builtin_amdgcn_readfirstlane(seq_len(P, s.b));
-        s.n = __builtin_amdgcn_readfirstlane(unit_tiles(P, u));
-        s.t0 = s.off = 0;
-        s.step = 1;
-        s.list = P.block_list ? P.block_list + (int64_t)u * P.max_list : nullptr;
-        if (s.n > 0) return true;
+        s.list = P.block_list ? P.block_list + (int64_t)v * P.max_list : nullptr;
+        return true;
       }
       return false;
     };
     Segment s;
-    bool more = next_group(s);
+    bool more = next_segment(s);
     if (more) ask(s);
     while (more) {
       clear();
       walk_tiles<G, FMT>(*fresh(args), s, lane, qa, sets, stage, parts, st);
-      const int b = s.b, kvh = s.kvh, done = g;
-      g += most * kWaves;
-      more = next_group(s);
+      const int b = s.b, kvh = s.kvh;
+      const bool whole = s.n == tiles, begins = s.t0 == 0;
+      const int64_t behind = start + kLead<true> + tiles;   // the place behind its last tile's
+      more = next_segment(s);
       if (more) ask(s);
       leave_record<G>(st, rec, lane);
       wave_lds_sync();
       Params& W = *fresh(args);
-      const int64_t row0 = (int64_t)b * W.num_q_heads + kvh * G;
-      for (int i = lane; i < G * kD; i += 64) write_out(W, row0 * kD + i, rec[i] / rec[G * kD + G + i / kD]);
-      if (lane < G) W.lse[row0 + lane] = ln_of(rec[G * kD + lane], rec[G * kD + G + lane]);
-      if (lane == 0) W.flags[done] = split_word(0, 0, false);
-      wave_lds_sync();   // the record is read before the next group's tiles
+      if (whole) {
+        const int64_t row0 = (int64_t)b * W.num_q_heads + kvh * G;
+        for (int i = lane; i < G * kD; i += 64) write_out(W, row0 * kD + i, rec[i] / rec[G * kD + G + i / kD]);
+        if (lane < G) W.lse[row0 + lane] = ln_of(rec[G * kD + lane], rec[G * kD + G + lane]);
+      } else {
+        // (a group that began in an earlier range: this one's first place, one
+        // that began here and goes on: its second)
+        float* const to = W.records + (2 * me + (begins ? 1 : 0)) * W.record_floats;
+        for (int i = lane; i < C::REC; i += 64) to[i] = rec[i];
+      }
+      // who holds it: up to the last w with w line / workers <= its last tile's place
+      if (begins && lane == 0)
+        W.flags[(int64_t)b * W.num_kv_heads + kvh] = split_word(me, whole ? me : (behind * workers - 1) / line, false);
+      wave_lds_sync();   // the record is read before the next segment's tiles
     }
     return;
   }
 
-  // this workgroup's part of the line: a scan of the units' tiles (or parts)
-  // that finds the unit where it begins
+  // this workgroup's part of the line, and the unit where it begins
   const bool in_parts = cut.kind == kParts;
   auto weight = [&](int u) {
     const int n = unit_tiles(P, u);
-    return (int64_t)heads * (n == 0 ? 0 : in_parts ? parts_of(n, cut.part) : n + kSegment);
+    return (int64_t)heads * (n == 0 ? 0 : in_parts ? parts_of(n, cut.part) : n + kLead<false>);
   };
-  const int per = (units + kThreads - 1) / kThreads;
-  const int u0 = tid * per, u1 = min(units, u0 + per);
-  int64_t own = 0;
-  for (int u = u0; u < u1; ++u) own += weight(u);
-  int64_t before = own;   // inclusive scan over the wavefront, then the workgroup
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int64_t x = __shfl_up((long long)before, o);
-    if (lane >= o) before += x;
-  }
-  if (lane == 63) s_wave[1][wave] = before;
-  __syncthreads();
-  int64_t line = 0;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    if (w < wave) before += s_wave[1][w];
-    line += s_wave[1][w];
-  }
-  before -= own;
-  line = uniform(line);   // places on the line, or parts
+  int64_t own, before;
+  const int64_t line = scan(weight, own, before);   // places on the line, or parts
   const int64_t workers = in_parts ? line : cut.workers, me = blockIdx.x;
   if (me >= workers) return;
   const int64_t begin = in_parts ? me : uniform(me * line / workers);
   const int64_t end = in_parts ? me + 1 : uniform((me + 1) * line / workers);
   if (begin >= end) return;
-  if (before <= begin && begin < before + own) {
-    // (one thread) the unit that holds the first tile
-    int u = u0;
-    int64_t base = before;
-    for (int64_t n; base + (n = weight(u)) <= begin; ++u) base += n;
-    s_unit = u;
-    s_base = base;
-  }
+  find(weight, begin, own, before, 0);
   __syncthreads();
-  int u = __builtin_amdgcn_readfirstlane(s_unit);
-  int64_t base = uniform(s_base);
+  int u = __builtin_amdgcn_readfirstlane(s_unit[0]);
+  int64_t base = uniform(s_base[0]);
 
   // A segment and where it lies: its group's places on the line (or its parts)
   // begin at `start` and are `each` of them.
@@ -632,16 +708,16 @@ __global__ void __launch_bounds__(kThreads, 2) full_kernel(const KernelParams, c
     while (x < end) {
       Params& P = *fresh(args);
       tiles = __builtin_amdgcn_readfirstlane(unit_tiles(P, u));
-      while (!in_parts && (tiles == 0 || x >= base + (int64_t)(tiles + kSegment) * heads)) {
-        base += tiles == 0 ? 0 : (int64_t)(tiles + kSegment) * heads;
+      while (!in_parts && (tiles == 0 || x >= base + (int64_t)(tiles + kLead<false>) * heads)) {
+        base += tiles == 0 ? 0 : (int64_t)(tiles + kLead<false>) * heads;
         tiles = __builtin_amdgcn_readfirstlane(unit_tiles(P, ++u));
       }
-      each = in_parts ? parts_of(tiles, cut.part) : tiles + kSegment;
+      each = in_parts ? parts_of(tiles, cut.part) : tiles + kLead<false>;
       const int h = __builtin_amdgcn_readfirstlane((int)((x - base) / each));
       start = base + (int64_t)h * each;
       const int64_t next = min(end, start + each);
-      s.t0 = in_parts ? (int)(x - start) * cut.part : max((int)(x - start) - kSegment, 0);
-      s.n = in_parts ? min(cut.part, tiles - s.t0) : (int)(next - start) - kSegment - s.t0;
+      s.t0 = in_parts ? (int)(x - start) * cut.part : max((int)(x - start) - kLead<false>, 0);
+      s.n = in_parts ? min(cut.part, tiles - s.t0) : (int)(next - start) - kLead<false> - s.t0;
       x = next;
       if (s.n <= 0) continue;   // only the places before its tiles
       s.b = per_group_units(P) ? u / P.num_kv_heads : u;
@@ -774,7 +850,7 @@ hipError_t resident(int* n) {
   if (*n > 0) return hipSuccess;
   e = hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev);
   if (e == hipSuccess)
-    e = hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, full_kernel<G, FMT>, kThreads,
+    e = hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, full_kernel<G, FMT, false>, kThreads,
                                                      (size_t)kWaves * Full<G>::WAVE_BYTES);
   *n = cus * max(per_cu, 1);
   if (e == hipSuccess && dev < kDevices) known[dev].store(*n, std::memory_order_relaxed);
@@ -793,7 +869,9 @@ int launch(const Plan& plan, const KernelParams& params, hipStream_t stream) {
   const int64_t tiles = (int64_t)plan.n_groups * max((cap + kTile - 1) / kTile, (int64_t)params.max_list * params.tiles_per_block);
   const int64_t most = min(min((int64_t)held, (int64_t)plan.n_groups * plan.max_chunks),
                            (tiles + kWaves - 1) / kWaves + plan.n_groups);
-  hipLaunchKernelGGL((full_kernel<G, FMT>), dim3((unsigned)most), dim3(kThreads), bytes, stream, params, (int)most);
+  const dim3 grid((unsigned)most), block(kThreads);
+  if (plan.n_groups > most) hipLaunchKernelGGL((full_kernel<G, FMT, true>), grid, block, bytes, stream, params, (int)most);
+  else hipLaunchKernelGGL((full_kernel<G, FMT, false>), grid, block, bytes, stream, params, (int)most);
   e = hipGetLastError();
   if (e != hipSuccess) return (int)e;
   // one head to a workgroup, and of many, most of them written already, up to 16
