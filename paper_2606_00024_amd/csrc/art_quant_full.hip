@@ -1,15 +1,15 @@
 // Full attention (no stability test) over a cache held in 8 bits.
 //
-// Without the test nothing has to be decided block by block, so the work is
-// cut for the memory system alone.  The 64-token tiles of all (sequence, KV
-// head) groups form one line, and every workgroup takes an equal, contiguous
-// part of it, however ragged the batch is; the part of a group in a
-// workgroup's range is a segment.  (Short batches are cut by groups, many groups
-// by wavefronts instead, see cut_of.)  The four wavefronts of a workgroup take a segment's tiles in
-// turn, each with its own running maximum, mass and output sums in registers,
-// and join at its end through LDS.  A group that lies in one workgroup is
-// written out there; of the others each segment leaves a record (m, L, o) in
-// the workspace and a second, small launch joins them.
+// Without the test nothing has to be decided block by block, so the work is cut
+// for the memory system alone.  The 64-token tiles of all (sequence, KV head)
+// groups form one line, and every workgroup takes an equal, contiguous part of
+// it, however ragged the batch is; the part of a group in a workgroup's range
+// is a segment.  (Short batches are cut by groups, many groups by wavefronts
+// instead, see cut_of.)  The four wavefronts of a workgroup take a segment's
+// tiles in turn, each with its own running maximum, mass and output sums in
+// registers, and join at its end through LDS.  A group that lies in one
+// workgroup is written out there; of the others each segment leaves a record
+// (m, L, o) in the workspace and a second, small launch joins them.
 //
 //   s_j = scale * (ks_j (q . ck_j)),  p_j = 2^(s_j log2 e - m),
 //   out = sum_j p_j vs_j cv_j / sum_j p_j
