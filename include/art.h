@@ -391,8 +391,12 @@ typedef struct {
 /*
  * art_decode_attention over a cache held in 8 bits: the definition at the top
  * of this header with k = code * k_scale and v = code * v_scale.  Scales are
- * any finite fp32 values (art_quant_append writes powers of two; V's below
- * 2^-100 lose low bits, as probabilities are multiplied by them).  All
+ * any fp32 values of magnitude up to 2^127 whose products with the codes are
+ * finite (art_quant_append writes powers of two; V's below 2^-100 lose low
+ * bits, as probabilities of at most 1 are multiplied by them).  Sums of p v
+ * are held in fp32 over the tokens of a block, and without the stability test
+ * over all of them: values of V within 2^127 over that number of tokens cannot
+ * overflow.  All
  * options, the workspace (art_decode_workspace_bytes of the same shape and
  * options), lists, outputs and restrictions are those of
  * art_decode_attention.  k_cache and v_cache are the code pools.  Codes and

@@ -228,7 +228,8 @@ __device__ __forceinline__ TileAt tile_at(const Ahead& a, int m) {
 // head (base 2) and the lane's share of its mass.  The maximum is a reference
 // that is moved only where a score passes it by more than 2^8 (and by the
 // first score): the sums keep their relative precision either way, and a tile
-// needs no reduction over the lanes, only a vote.
+// needs no reduction over the lanes, only a vote.  (Large values of V: by any
+// score, see walk_tiles.)
 struct State {
   f32x4 acc[8];
   float m, l;
@@ -259,6 +260,11 @@ __device__ __forceinline__ void walk_tiles(Params& P, const Segment& s, int lane
     const TileAt over = tile_at(nxt, 0);
     ahead_scales(P, s, lane, nxt);
     ahead_pages(P, s, first + 32, n_mine, lane, far);
+    // Where V is so large that 2^8 times a value of it, over 2^20 tokens, could
+    // leave fp32's range (448 * 2^90 < 2^99), the reference follows the maximum:
+    // no probability passes 1 and the sums have the room of plain ones.
+    const bool large = first + (lane >> 2) < n_mine && fabsf(cur.vs) >= 0x1p90f;
+    const float slack = __any(large) ? 0.f : 8.f;
 #pragma unroll 1
     for (int m = 0; m < n_set; ++m) {
       const int tok0 = at.tok0;
@@ -323,7 +329,7 @@ __device__ __forceinline__ void walk_tiles(Params& P, const Segment& s, int lane
       for (int j = 0; j < NS; ++j)
 #pragma unroll
         for (int r = 0; r < 4; ++r) top = fmaxf(top, sc[j][r]);
-      if (__any(top > st.m + 8.0f)) {
+      if (__any(top > st.m + slack)) {
         if constexpr (REP >= 2) top = fmaxf(top, dpp_f<kRowRor8>(top));
         if constexpr (REP == 4) top = fmaxf(top, dpp_f<kRowRor4>(top));
         const float mn = fmaxf(st.m, rows_max(top));
