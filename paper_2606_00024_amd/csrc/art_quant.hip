@@ -244,6 +244,27 @@ __device__ __forceinline__ uint32_t needed_scale(uint32_t a) {
   return (uint32_t)(e + 127) << 23;
 }
 
+// Runs whose scale is no power of two (a cache that another writer began): the
+// quotients and products are not exact in fp32, and rounding them there first
+// could turn a value next to the midpoint of two codes into the midpoint.
+// 64 bits hold them well enough (the quotient of two fp32 values that is not a
+// midpoint lies 2^-29 of itself away from it, or more), and fp32 values rounded
+// to odd (the neighbour with a set last bit, where the value is inexact) still
+// tell which side of a midpoint they lie on.
+__device__ __forceinline__ float odd_f32(double x) {
+  const float f = (float)x;
+  if ((double)f == x || x != x) return f;
+  uint32_t u = __float_as_uint(f);
+  if (fabs((double)f) > fabs(x)) --u;   // towards zero
+  return __uint_as_float(u | 1u);
+}
+// x / s, inv = 1 / s rounded: one Newton step makes exact quotients exact.
+__device__ __forceinline__ float quotient(float x, double s, double inv) {
+  const double q = (double)x * inv, r = __builtin_fma(-q, s, (double)x);
+  return odd_f32(fabs(r) > 0.0 ? __builtin_fma(r, inv, q) : q);   // (infinite x, or -0: q)
+}
+__device__ __forceinline__ bool power_of_two(float s) { return (__float_as_uint(s) & 0x7fffffu) == 0; }
+
 // Append.  One wavefront quantises one run of slots of one head's K or V: 16
 // bytes of a row to a lane, four rows a step (two of 32-bit values), and 64
 // rows stay in registers between the pass that takes their largest magnitude
@@ -277,6 +298,14 @@ __device__ __forceinline__ void store_codes(uint8_t* p, const u32x4& r, float in
     *reinterpret_cast<u32x2*>(p) = u32x2{encode4<FMT, WILD>(x), encode4<FMT, WILD>(x + 4)};
   else
     *reinterpret_cast<uint32_t*>(p) = encode4<FMT, WILD>(x);
+}
+template <int FMT, int DT>
+__device__ __forceinline__ void store_quotients(uint8_t* p, const u32x4& r, double scale, double inv) {
+  float x[kValues<DT>];
+#pragma unroll
+  for (int i = 0; i < kValues<DT>; ++i) x[i] = quotient(value<DT>(r, i), scale, inv);
+#pragma unroll
+  for (int q = 0; q < kValues<DT> / 4; ++q) reinterpret_cast<uint32_t*>(p)[q] = encode4<FMT, true>(x + 4 * q);
 }
 
 // What a team's wavefronts (4 of a run longer than one holds, or 1) tell each
@@ -337,13 +366,12 @@ __device__ void append_run(const QuantParams& P, const Side& S, int head, int b,
   };
 
   // the run's scale from its new rows' largest finite magnitude (fp32 bits);
-  // old codes follow it where it grows.  Returns 1 / scale.
+  // old codes follow it where it grows (to a power of two)
   auto settle = [&](uint32_t top) {
     const float need = __uint_as_float(needed_scale<FMT>(top));
     const float scale = old > 0 ? fmaxf(need, old_scale) : need;
-    const float inv = 1.0f / scale;
     if (old > 0 && scale != old_scale) {
-      const float ratio = old_scale * inv;
+      const double ratio = (double)old_scale / (double)scale;
       for (int i = wave * 8 + (lane >> 3); i < old; i += 8 * TEAM) {
         u32x4* p = reinterpret_cast<u32x4*>(pool + (int64_t)(i - old) * S.st + (lane & 7) * 16);
         u32x4 w = *p;
@@ -352,15 +380,16 @@ __device__ void append_run(const QuantParams& P, const Side& S, int head, int b,
           float x[4];
           decode4<FMT>(w[q], x);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) x[j] *= ratio;
+          for (int j = 0; j < 4; ++j) x[j] = odd_f32((double)x[j] * ratio);
           w[q] = encode4<FMT, true>(x);
         }
         *p = w;
       }
     }
     if (wave == 0 && lane == 0 && (old == 0 || scale != old_scale)) *sp = scale;
-    return inv;
+    return scale;
   };
+  float scale = 0.f;
   if (held) {
     uint32_t a = 0;
 #pragma unroll
@@ -368,24 +397,38 @@ __device__ void append_run(const QuantParams& P, const Side& S, int head, int b,
     if constexpr (DT != ART_ROWS_F32) a = max(a & 0xffffu, a >> 16);
     a = joined(a);
     if (a < kNotFinite<DT>) {
-      const float inv = settle(as_f32_bits<DT>(a));
+      scale = settle(as_f32_bits<DT>(a));
+      if (power_of_two(scale)) {
+        const float inv = 1.0f / scale;
 #pragma unroll
-      for (int k = 0; k < kSlab; ++k) {
-        if (EACH * k + r0 < n) store_codes<FMT, DT, false>(at(EACH * k), raw[k], inv);
+        for (int k = 0; k < kSlab; ++k) {
+          if (EACH * k + r0 < n) store_codes<FMT, DT, false>(at(EACH * k), raw[k], inv);
+        }
+        return;
       }
-      return;
     }
   }
-  // more rows than the registers hold, or infinities or NaN among them: the
-  // largest finite magnitude, then codes with clamps, from the rows once more
-  uint32_t a = 0;
+  // more rows than the registers hold, infinities or NaN among them, or a kept
+  // scale that is no power of two: the largest finite magnitude, then codes with
+  // clamps, from the rows once more
+  if (scale == 0.f) {
+    uint32_t a = 0;
 #pragma unroll 4
-  for (int i = 0; i < n; i += EACH)
-    if (i + r0 < n) a = max_finite_bits<DT>(a, load(i));
-  const float inv = settle(joined(a));
+    for (int i = 0; i < n; i += EACH)
+      if (i + r0 < n) a = max_finite_bits<DT>(a, load(i));
+    scale = settle(joined(a));
+  }
+  if (power_of_two(scale)) {
+    const float inv = 1.0f / scale;
 #pragma unroll 4
-  for (int i = 0; i < n; i += EACH)
-    if (i + r0 < n) store_codes<FMT, DT, true>(at(i), load(i), inv);
+    for (int i = 0; i < n; i += EACH)
+      if (i + r0 < n) store_codes<FMT, DT, true>(at(i), load(i), inv);
+  } else {
+    const double inv = 1.0 / (double)scale;
+#pragma unroll 1
+    for (int i = 0; i < n; i += EACH)
+      if (i + r0 < n) store_quotients<FMT, DT>(at(i), load(i), (double)scale, inv);
+  }
 }
 
 // A wavefront, or a team, takes the runs whose first new row lies in its window
