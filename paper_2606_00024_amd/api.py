@@ -368,7 +368,10 @@ def decode_attention_quant(q: torch.Tensor, cache: QuantCache, page_table: torch
         raise ValueError("block_list and block_list_len go together")
     max_list = 0
     if block_list is not None:
+        # [B][Hkv][n], or one list a sequence as [B][1][n] or [B][n]
         rows, max_list = ((B, Hkv) if list_per_head else (B,)), block_list.shape[-1]
+        if not list_per_head and block_list.dim() == 3:
+            rows = (B, 1)
         _check(block_list, "block_list", torch.int32, dev, (*rows, max_list))
         if block_list_len.numel() != math.prod(rows):
             raise ValueError(f"block_list_len must hold {math.prod(rows)} lengths")
