@@ -469,8 +469,10 @@ art_status art_quant_append(const art_decode_shape* shape, const art_quant_cache
                             const int32_t* page_table, void* k_cache, void* v_cache,
                             float* k_scale, float* v_scale, hipStream_t stream);
 
-/* The rows' values, code * scale rounded once to rows_dtype, ties to even.
- * Rows that are passed over keep their bytes. */
+/* The rows' values: the fp32 product code * scale, rounded to rows_dtype, both
+ * to nearest, ties to even (under scales of up to 16 significant bits, powers
+ * of two among them, the product is exact and the one rounding is to
+ * rows_dtype).  Rows that are passed over keep their bytes. */
 art_status art_quant_read(const art_decode_shape* shape, const art_quant_cache* cache,
                           const art_quant_rows* rows, const void* k_cache, const void* v_cache,
                           const float* k_scale, const float* v_scale,

@@ -477,8 +477,8 @@ def quant_read(cache: QuantCache, page_table: torch.Tensor, positions: Optional[
 
     Rows token_offsets[b] .. token_offsets[b + 1] - 1 receive sequence b's
     tokens positions[b], positions[b] + 1, ... (as in ``quant_append``).
-    Returns (k, v) [rows][Hkv][D] in ``dtype`` (bf16, fp16 or fp32; code * scale
-    rounded once); ``rows`` sizes them where they are not given.  Rows of no
+    Returns (k, v) [rows][Hkv][D] in ``dtype`` (bf16, fp16 or fp32; the fp32
+    product code * scale rounded to it); ``rows`` sizes them where they are not given.  Rows of no
     token are left as they were (not initialised, where they are not given).
     """
     if k is None or v is None:
