@@ -71,6 +71,10 @@ namespace {
 
 constexpr int kFormat = ART_KV_FORMAT;
 
+// Full attention (no stability test): over codes it has a kernel of its own
+// (art_quant_full.hip).
+__device__ __forceinline__ bool no_test(Params& P) { return kFormat == 0 && P.no_detector; }
+
 constexpr int kD = kHeadDim;
 
 // ---- workspace: cross-workgroup data ---------------------------------------
@@ -1333,7 +1337,7 @@ __device__ __forceinline__ int live_chunks(Params& P, const int* s_len, int x, i
   int live = 0;
   if (lane < nx) {
     const int g = queue_group(x, lane, n_groups), b = g / P.num_kv_heads;
-    const uint64_t sw = P.no_detector ? 0ull : ld_relaxed(P.stop_word + g);
+    const uint64_t sw = no_test(P) ? 0ull : ld_relaxed(P.stop_word + g);
     live = max(group_info_raw(P, g, b < kLenCache ? s_len[b] : P.seq_lens[b], raw_list_len(P, g)).n_chunks, 1);
     if ((sw >> kQueueBits) == P.epoch) live = min(live, (int)(sw & ((1ull << kQueueBits) - 1ull)) + 1);
   }
@@ -1625,7 +1629,7 @@ __device__ void resolve_chunk(Params& P, int gidx, int k, const GroupInfo& gi,
   // this chunk's inclusive state, published before the replay: the next
   // chunks wait for it (measured: raising its flag only after the replay's
   // first blocks, to overlap the stores' completion, was 0.5 % slower)
-  if (!last || P.no_detector) {
+  if (!last || no_test(P)) {
     State<G> inc = pre;
     merge<G>(inc, agg);
     if (!last) {
@@ -1636,7 +1640,7 @@ __device__ void resolve_chunk(Params& P, int gidx, int k, const GroupInfo& gi,
       // holds the output
       write_outputs<G>(P, b, kvh, inc, T, lane);
     }
-    if (P.no_detector) return;
+    if (no_test(P)) return;
   }
 
   // Replay the chunk's blocks from the prefix with the stability test.  The
@@ -1952,7 +1956,7 @@ __global__ void __launch_bounds__(kThreads, kWorkgroupsPerCu<G>) art_decode_kern
         const GroupInfo gi = group_info_raw(P, g, L_raw, T_raw);
         if (gi.n_chunks == 0 && kh == 0) write_empty_wave<G>(P, gi.b, gi.kvh, lane);
         if (kh >= gi.n_chunks || (P.block_list && stop_word_before(ld_relaxed(P.stop_word + g), P.epoch, kh))) {
-          stale = P.block_list || P.no_detector;  // (elsewhere the lengths, in LDS, tell it as fast)
+          stale = P.block_list || no_test(P);  // (elsewhere the lengths, in LDS, tell it as fast)
           continue;
         }
         gsel = g;
@@ -2010,7 +2014,7 @@ __global__ void __launch_bounds__(kThreads, kWorkgroupsPerCu<G>) art_decode_kern
       // it makes progress without this one.
       if (P.max_ahead > 0 && k >= P.max_ahead) {
         const uint64_t* fw = P.flags + (int64_t)gidx * P.max_chunks + (k - P.max_ahead);
-        const uint32_t need = P.no_detector ? kInclusive : kStabSummary;
+        const uint32_t need = no_test(P) ? kInclusive : kStabSummary;
         for (uint32_t spin = 0;; ++spin) {
           if (flag_state(ld_relaxed(fw), P.epoch) >= need) break;
           if (stop_announced_before(P, gidx, k) || wait_expired(P, spin)) {
