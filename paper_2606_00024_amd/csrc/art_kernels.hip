@@ -2102,15 +2102,10 @@ int launch_w(const Plan& plan, const KernelParams& params, hipStream_t stream) {
   const int64_t work = (int64_t)plan.n_groups * plan.max_chunks;
   if (work <= 0) return (int)hipSuccess;
   int dev = 0, cus = 0, per_cu = 0;
-  // (the plan counts the staging buffers of bf16 tiles)
-  size_t lds = plan.lds_bytes;
-  if (kFormat != 0)
-    lds = (size_t)kChunkSlots * plan.chunk_blocks * Cfg<G>::REC * 4 +
-          (plan.v_in_record ? 0 : (size_t)kLoaders * kCodeStage + 16);
   hipError_t e = hipGetDevice(&dev);
   if (e == hipSuccess) e = hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev);
   if (e == hipSuccess)
-    e = hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, art_decode_kernel<G, PH, WIDE>, kThreads, lds);
+    e = hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, art_decode_kernel<G, PH, WIDE>, kThreads, plan.lds_bytes);
   if (e != hipSuccess) return (int)e;
   if (per_cu < 1) per_cu = 1;
   // As many workgroups as the chip holds, but no more than the plan allows
@@ -2130,7 +2125,7 @@ int launch_w(const Plan& plan, const KernelParams& params, hipStream_t stream) {
   p.look_first = grid * kChunkSlots <= (int64_t)8 * plan.n_groups ? 1 : 0;
   auto kernel = art_decode_kernel<G, PH, WIDE>;
   hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(kThreads),
-                     lds, stream, p);
+                     plan.lds_bytes, stream, p);
   return (int)hipGetLastError();
 }
 
