@@ -16,7 +16,8 @@ builds of the same sources:
   libart_bench.so   read-only streaming kernels (the benchmark's measured
                     read ceiling; not part of the decode path)
   libart_stress.so  the library with ART_RACE_STRESS: seeded delays at every
-                    hand-over between workgroups (the race-stress test)
+                    hand-over between workgroups, over every kind of pool
+                    (the race-stress tests)
   libart_asan.so    the library with its host code (art_api.cpp) compiled by
                     g++ with AddressSanitizer; the device code is the same
                     (the host-ASan test runs the CPU suite against it)
@@ -111,17 +112,21 @@ def build(verbose: bool = False, extra=()) -> str:
     for name, define in KV_FORMATS.items():
         jobs.append((f"art_kernels.hip ({name})", [cc, *flags(extra), define, "-c", "-o", _obj(name),
                                                    src("art_kernels.hip")]))
-    jobs.append(("art_kernels.hip (stress)", [cc, *flags(extra), "-DART_RACE_STRESS", "-c",
-                                              "-o", _obj("art_kernels_stress"), src("art_kernels.hip")]))
+    # the decode kernels of every kind of cache again, with race stress
+    for name, define in {"art_kernels": "-DART_KV_FORMAT=0", **KV_FORMATS}.items():
+        jobs.append((f"{name} (stress)", [cc, *flags(extra), define, "-DART_RACE_STRESS", "-c",
+                                          "-o", _obj(name + "_stress"), src("art_kernels.hip")]))
     jobs.append(("art_read_peak.hip", [cc, *flags(extra), "-c", "-o", _obj("art_read_peak.hip"),
                                        src("art_read_peak.hip")]))
     jobs.append(("art_api.cpp (asan)", [*_asan_host_flags(), "-c", "-o", _obj("art_api_asan"),
                                         src(HOST_SOURCE)]))
     _run_all(jobs, verbose)
     dev = [_obj(s) for s in DEVICE_SOURCES] + [_obj(name) for name in KV_FORMATS]
+    stress = [_obj(name + "_stress") for name in ("art_kernels", *KV_FORMATS)]
+    stress += [_obj(s) for s in DEVICE_SOURCES if s != "art_kernels.hip"]
     links = {
         LIB: dev + [_obj(HOST_SOURCE)],
-        STRESS_LIB: [_obj("art_kernels_stress")] + dev[1:] + [_obj(HOST_SOURCE)],
+        STRESS_LIB: stress + [_obj(HOST_SOURCE)],
         BENCH_LIB: [_obj("art_read_peak.hip")],
         # the AddressSanitizer runtime is not linked in: the process that
         # loads this library preloads gcc's libasan (tests/test_host_asan.py)
