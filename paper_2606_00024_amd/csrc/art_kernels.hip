@@ -1218,8 +1218,9 @@ constexpr int kLoaders = kWaves - 1;   // wavefronts 1..3 stream tiles
 // Workgroups that share a CU (a wavefront of each on every SIMD).  A tile of
 // codes is half the bytes of a bf16 tile and waits as long for them, so groups
 // of up to 4 heads, whose chunk buffers leave the LDS for it, have three where
-// the registers allow (168): 8 x 32K tokens, int8, the test never passing, 143
-// us with two and 135 with three, thresholds of 1e-2 77 and 69.
+// the registers allow (168; at g = 2, and g = 4 with a stop per head, 2 to 8 of
+// them go to scratch): 8 x 32K tokens, int8, the test never passing, 143 us with
+// two and 135 with three, thresholds of 1e-2 77 and 69.
 template <int G>
 constexpr int kWorkgroupsPerCu = kFormat != 0 && G <= 4 ? 3 : 2;
 constexpr int kSlots = kChunkSlots;    // chunk buffers in LDS
