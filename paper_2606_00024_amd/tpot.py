@@ -19,8 +19,10 @@ One step, per layer (batch B, one new token per sequence):
 then rms_norm and the LM head.  The attention consumes the cache's own
 query (the workload's q: the synthetic caches are built around it, which is
 what makes their early stops representative) and the projected q is left
-unused; appending the new token's K and V to the cache is not modelled
-(B Hkv 512 bytes per layer).  The step runs eagerly on one stream.
+unused.  Over 8-bit caches (--kv) the step first appends the projected K and V
+as every sequence's last token (art_quant_append); over bf16 caches, which have
+no such call, appending is not modelled (B Hkv 512 bytes per layer).  The step
+runs eagerly on one stream.
 
 Modes: NODET (full attention, no stability test: the baseline), OFF (test on,
 never stops) and ON (the workload thresholds).  Reported per mode: TPOT, the
@@ -59,9 +61,12 @@ class ModelShape:
                      + self.hidden * 2 * self.ffn + self.ffn * self.hidden)
         return 2 * (self.layers * per_layer + self.hidden * self.vocab)
 
-    def kv_bytes(self, batch: int, seq_len: int) -> int:
-        """bf16 K and V bytes of the whole cache (all layers)."""
-        return self.layers * batch * seq_len * self.kv_heads * 128 * 2 * 2
+    def kv_bytes(self, batch: int, seq_len: int, kv: str = "bf16") -> int:
+        """K and V bytes of the whole cache (all layers); of an 8-bit one, its
+        codes and a fp32 scale for every 64 tokens."""
+        token_bytes = 128 * 2 if kv == "bf16" else 128
+        scales = 0 if kv == "bf16" else 4 * -(-seq_len // 64)
+        return self.layers * batch * self.kv_heads * 2 * (seq_len * token_bytes + scales)
 
 
 MODELS = {
@@ -233,9 +238,8 @@ class Step:
 def measure(model: ModelShape, batch: int, seq_len: int, steps: int = 10, warmup: int = 3,
             kv: str = "bf16") -> dict:
     step = Step(model, batch, seq_len, kv=kv)
-    kv_bytes = model.kv_bytes(batch, seq_len) / (1 if kv == "bf16" else 2)
     res = {"model": model.name, "batch": batch, "seq_len": seq_len, "layers": model.layers, "kv": kv,
-           "weight_gb": model.weight_bytes() / 1e9, "kv_gb": kv_bytes / 1e9,
+           "weight_gb": model.weight_bytes() / 1e9, "kv_gb": model.kv_bytes(batch, seq_len, kv) / 1e9,
            "dense_only_ms": float(np.median(step.time_ms("nodet", steps, warmup, attention=False))),
            "modes": {}}
     for mode in ("nodet", "off", "on"):
