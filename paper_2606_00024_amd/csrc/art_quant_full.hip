@@ -260,10 +260,11 @@ __device__ __forceinline__ void walk_tiles(Params& P, const Segment& s, int lane
     const TileAt over = tile_at(nxt, 0);
     ahead_scales(P, s, lane, nxt);
     ahead_pages(P, s, first + 32, n_mine, lane, far);
-    // Where V is so large that 2^8 times a value of it, over 2^20 tokens, could
-    // leave fp32's range (448 * 2^90 < 2^99), the reference follows the maximum:
-    // no probability passes 1 and the sums have the room of plain ones.
-    const bool large = first + (lane >> 2) < n_mine && fabsf(cur.vs) >= 0x1p90f;
+    // Where V is so large that 2^8 times a value of it, over the 2^29 tokens that
+    // a traversal can have, could leave fp32's range (448 * 2^80 < 2^89), the
+    // reference follows the maximum: no probability passes 1 and the sums have
+    // the room of plain ones.
+    const bool large = first + (lane >> 2) < n_mine && fabsf(cur.vs) >= 0x1p80f;
     const float slack = __any(large) ? 0.f : 8.f;
 #pragma unroll 1
     for (int m = 0; m < n_set; ++m) {
@@ -479,8 +480,7 @@ __device__ __forceinline__ void write_out(Params& P, int64_t i, float x) {
 }
 __device__ __forceinline__ float ln_of(float m, float L) { return (m + __log2f(L)) * 0.69314718055994531f; }
 
-// Joins `n` records (base 2 maxima): `rec(i)` points at the i-th one's floats.
-// Called by all threads for value (h, d).
+// What a record of maximum m (base 2) counts for beside the largest one, `top`.
 __device__ __forceinline__ float factor(float m, float top) { return m == kNegInf ? 0.f : fast_exp2(m - top); }
 
 // What the first launch tells the second of a group that holds tiles: the

@@ -46,7 +46,7 @@ def _two_tokens(form, v_low, v_high):
 
 @pytest.mark.parametrize("form", R.FORMATS)
 @pytest.mark.parametrize("g", [1, 2, 4, 8, 16])
-@pytest.mark.parametrize("exponents", [(124, 123), (-3, 124), (126, -20), (0, 1), (-100, -101)])
+@pytest.mark.parametrize("exponents", [(124, 123), (-3, 124), (126, -20), (80, 79), (79, 85), (0, 1), (-100, -101)])
 def test_large_and_small_values(form, g, exponents):
     """600 sequences of two tiles, both of which one wavefront takes without the
     test, so that the first tile's maximum meets the second one's larger score."""
