@@ -99,9 +99,11 @@ typedef struct {
  * patience = 1 is "no patience"; INT32_MAX runs the detector without ever
  * stopping.  chunk_blocks = 0 lets the library pick the split of each
  * traversal into chunks from the shape, the kind of walk (order, list or
- * none, no_detector) and whether the workspace holds art_decode_workspace_bytes()
- * alone (never from the data or the thresholds: with the test, short leading
- * chunks of 3 blocks, then chunks of up to 9; without it, chunks of up to 12);
+ * none, no_detector), the kind of cache and whether the workspace holds
+ * art_decode_workspace_bytes() alone (never from the data or the thresholds:
+ * with the test, short leading chunks of 3 blocks, then chunks of up to 9, over
+ * an 8-bit cache of up to 15; without it, chunks of up to 12, which over an
+ * 8-bit cache only bound the number of workgroups);
  * 1..16 asks for that many blocks in every chunk (capped at what the
  * shared-memory budget holds for the shape).  The chunking changes
  * rounding only.
@@ -396,11 +398,13 @@ typedef struct {
  * bits, as probabilities of at most 1 are multiplied by them).  Sums of p v
  * are held in fp32 over the tokens of a block, and without the stability test
  * over all of them: values of V within 2^127 over that number of tokens cannot
- * overflow.  All
- * options, the workspace (art_decode_workspace_bytes of the same shape and
- * options), lists, outputs and restrictions are those of
+ * overflow.  All options, the workspace (art_decode_workspace_bytes of the same
+ * shape and options), lists, outputs and restrictions are those of
  * art_decode_attention.  k_cache and v_cache are the code pools.  Codes and
- * scales of slots past a sequence's length are never used.
+ * scales of slots past a sequence's length are never used.  There is no form
+ * over the library's own scratch (art_decode_attention_static), and
+ * art_build_block_list reads bf16 keys: over an 8-bit cache importance lists
+ * come from the caller, streaming lists from that call (it needs no keys).
  */
 art_status art_decode_attention_quant(const art_decode_shape* shape, const art_decode_opts* opts,
                                       const art_quant_cache* cache,

@@ -267,19 +267,19 @@ __device__ __forceinline__ bool power_of_two(float s) { return (__float_as_uint(
 
 // Append.  One wavefront quantises one run of slots of one head's K or V: 16
 // bytes of a row to a lane, four rows a step (two of 32-bit values), and 64
-// rows stay in registers between the pass that takes their largest magnitude
-// and the one that rounds them.  Longer runs have a workgroup each, whose
+// rows stay in registers (of fp32 rows, 128 registers, 4 to 6 in scratch) between
+// the pass that takes their largest magnitude and the one that rounds them.  Longer runs have a workgroup each, whose
 // wavefronts take the steps in turn and join their maxima in LDS.  A run that a
 // sequence has begun before keeps its scale unless it has to grow; only then
 // are its old codes read and rounded anew.
 //
 // The bound is HBM: rows read once and codes written once.  54K rows of 8
-// heads, K and V: 65 us in bf16 (5.1 TB/s; 88 with loads that go through the
-// caches), and 48K rows of fp32 88 us (5.6 TB/s; 184 with 32 rows in
-// registers).  48K bf16 rows in runs of 256: 52 us (one wavefront a run: 137).
+// heads, K and V: 68 us in bf16 (4.9 TB/s; 88 with loads that go through the
+// caches), and 48K rows of fp32 93 us (5.3 TB/s; 184 with 32 rows in
+// registers).  48K bf16 rows in runs of 256: 55 us (one wavefront a run: 137).
 // Appends of a few rows a sequence are bound by the chain of lookups (offsets,
 // position, page, rows) and want many wavefronts: with 4 steps in registers
-// instead of 16, 4096 sequences of one token take 49 us instead of 80, and 8 of
+// instead of 16, 4096 sequences of one token take 51 us instead of 80, and 8 of
 // one 3.0 instead of 3.9; a long run among them has its rows read twice.
 template <int DT>
 struct Step {
@@ -468,13 +468,13 @@ __global__ void __launch_bounds__(kThreads, SLAB == Step<DT>::SHORT ? 6 : 3) app
 // Read.  A wavefront brings back 8 steps of 4 rows (of 2 rows of 32-bit values)
 // of one head's K or V: the page lookups of all of them, then their scales and
 // codes, are in flight together.  A lane takes the codes that one 16-byte
-// store holds the values of, so that a store instruction writes whole rows
-// (with 16 codes a lane, 54K rows of 8 heads to fp32 took 182 us, not 106, and
-// 103K rows to bf16 132, not 126).  The wavefronts of a workgroup take
+// store holds the values of, so that a store instruction writes whole rows: 54K
+// rows of 8 heads to fp32 take 101 us and 103K rows to bf16 121 (with 16 codes a
+// lane 182 and 132, when this form took 106 and 126).  The wavefronts of a workgroup take
 // neighbouring heads, whose parts of a row lie side by side, and neighbouring
 // workgroups the rest of the row: all of a row moves at about the same time
 // and meets every memory channel (with the heads far apart in the launch, fp32
-// 121 us and the append 110, not 88).
+// 121 us where this form took 107, and the append 110 where it took 88).
 template <int DT>
 struct ReadCfg {
   static constexpr int CODES = kValues<DT>;        // codes of a lane
