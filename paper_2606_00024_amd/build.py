@@ -142,10 +142,13 @@ def build(verbose: bool = False, extra=()) -> str:
 def resource_usage() -> str:
     """Per-kernel register/LDS/scratch report of the device code."""
     cc = hipcc()
-    cmd = [cc, *flags(), "--cuda-device-only", "-c", "-o", os.devnull,
-           "-Rpass-analysis=kernel-resource-usage", os.path.join(CSRC, "art_kernels.hip")]
-    res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
-    return res.stdout
+    parts = []
+    for name, extra in [(s, ()) for s in DEVICE_SOURCES] + [("art_kernels.hip", (d,)) for d in KV_FORMATS.values()]:
+        cmd = [cc, *flags(extra), "--cuda-device-only", "-c", "-o", os.devnull,
+               "-Rpass-analysis=kernel-resource-usage", os.path.join(CSRC, name)]
+        res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+        parts += [" ".join((f"== {name}", *extra)), res.stdout]
+    return "\n".join(parts)
 
 
 if __name__ == "__main__":
