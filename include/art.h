@@ -484,6 +484,202 @@ art_status art_quant_read(const art_decode_shape* shape, const art_quant_cache* 
                           const int32_t* page_table, void* k_rows, void* v_rows,
                           hipStream_t stream);
 
+/*
+ * Drafted tokens.  A decode step that verifies drafts gives every sequence a
+ * few new tokens at once, its nodes.  A call takes the nodes of all sequences
+ * as packed rows, in the manner of art_quant_append: rows row_offsets[b] ..
+ * row_offsets[b+1]-1 are sequence b's nodes 0, 1, ... (row_offsets int32
+ * [batch + 1], non-decreasing, in 0 .. rows; NULL when every sequence has
+ * rows / batch of them).  context_lens int32 [batch] holds the tokens that each
+ * sequence has already; node i lies in slot context_lens[b] + i of the cache.
+ *
+ * Node 0 is the sequence's newest token.  The others are drafts, each the
+ * child of an earlier node of its sequence, parents[row] (the parent's number
+ * within the sequence; -1 for node 0).  Drafts may form a chain or a tree.
+ *
+ * Rows of no sequence, of a sequence with a negative context (an unused row of
+ * a padded batch) and of one whose nodes do not all fit its table (context +
+ * nodes > max_pages_per_seq * page_size) are passed over: what the call would
+ * write for them is left as it was, unless a call says otherwise.  Arrays are
+ * device memory; index arrays are checked on the device, and no malformed index
+ * makes a call read or write outside the arrays.  The calls are asynchronous on
+ * `stream`, keep nothing, and may be captured in a HIP graph and replayed.
+ * A workspace of these calls needs no initialisation, holds nothing between
+ * calls, and serves one call at a time.
+ */
+
+/* Packed rows [rows][heads][128] of a type: strides in elements of it, multiples
+ * of 16 bytes (>= 0), row strides less than 256 MiB, arrays 16-byte aligned;
+ * head_dim is contiguous. */
+typedef struct {
+    int32_t dtype;                 /* art_rows_dtype */
+    int32_t heads;
+    int64_t stride_row, stride_head;
+} art_rows;
+
+/*
+ * Rotary positions.  Pair i of a head's first rot_dim dims turns by the angle
+ * a = position * freqs[i]:
+ *   (x, y) -> scale * (x cos a - y sin a, y cos a + x sin a)
+ * Pair i is dims (i, i + rot_dim / 2) (ART_ROPE_HALF) or (2i, 2i + 1)
+ * (ART_ROPE_INTERLEAVED).  freqs holds rot_dim / 2 doubles, radians per
+ * position (device memory): the angle is reduced in 64 bits, so that any int32
+ * position keeps 2^-22 of a turn (|freqs| <= 1); cosine, sine and products are in
+ * fp32, with one rounding to the output's type.  Scaled variants for
+ * long contexts differ in freqs and scale only.  Negated freqs (and 1 / scale)
+ * turn rows back; the gradient of a rotation is that with scale itself.
+ * Dims from rot_dim on are copied.  rot_dim is even, 0 .. 128.
+ */
+typedef enum { ART_ROPE_HALF = 0, ART_ROPE_INTERLEAVED = 1 } art_rope_layout;
+typedef struct {
+    int32_t layout;                /* art_rope_layout */
+    int32_t rot_dim;
+    float scale;                   /* finite; usually 1 */
+} art_rope;
+
+/* Rotate rows to positions[row] (int32 [rows]).  `out` may be `x` itself with
+ * the same description, and must not overlap it otherwise. */
+art_status art_rope_rows(const art_rope* rope, int32_t rows, const art_rows* x_rows, const void* x,
+                         const art_rows* out_rows, void* out, const int32_t* positions,
+                         const double* freqs, hipStream_t stream);
+
+/*
+ * Append to the bf16 cache: the nodes' keys, rotated, and values are rounded to
+ * bf16 and written to their slots (no two rows may have the same slot).  With
+ * q, the queries are rotated too, into q_out (bf16; q may be q_out itself, as in
+ * art_rope_rows).  q, k and v have one type.  A row's position is
+ * row_positions[row], or its slot where row_positions is NULL.  rope NULL: no
+ * rotation (freqs is then NULL).  q NULL: no queries.
+ * Shape fields used: batch, num_q_heads (with q), num_kv_heads, head_dim (128),
+ * page_size (a power of two >= 16), num_pages, max_pages_per_seq and the K and V
+ * strides (multiples of 8).  q rows that are passed over keep what q_out held.
+ * A page id outside 0 .. num_pages-1 passes over the row's key and value.
+ */
+art_status art_rope_append(const art_decode_shape* shape, const art_rope* rope, int32_t rows,
+                           const art_rows* q_rows, const void* q,
+                           const art_rows* q_out_rows, void* q_out,
+                           const art_rows* k_rows, const void* k,
+                           const art_rows* v_rows, const void* v,
+                           const int32_t* row_offsets, const int32_t* context_lens,
+                           const int32_t* row_positions, const double* freqs,
+                           const int32_t* page_table, void* k_cache, void* v_cache,
+                           hipStream_t stream);
+
+/*
+ * A tree's masks and positions from its parents.
+ *   mask       uint64 [rows][mask_words], out: bit j of a row (bit j % 64 of word
+ *              j / 64) is 1 for the node itself and its ancestors j.  Bits that
+ *              mask_words has no room for are dropped.
+ *   positions  int32 [rows], out, or NULL: context_lens[b] plus the node's depth
+ *              (node 0 has depth 0).
+ * A parent that is not an earlier node (-1 among them) ends the walk.  1 <=
+ * mask_words <= 16; sequences of more than ART_MAX_NODES nodes are passed over.
+ */
+#define ART_MAX_NODES 1024
+art_status art_tree_layout(int32_t batch, int32_t rows, const int32_t* parents,
+                           const int32_t* row_offsets, const int32_t* context_lens,
+                           int32_t mask_words, uint64_t* mask, int32_t* positions,
+                           hipStream_t stream);
+
+/*
+ * Attention of the nodes over the bf16 cache, which holds their keys and values
+ * already.  A node sees the whole context and, of its sequence's nodes, those
+ * that its mask row has a bit for; without a mask, node i sees nodes 0 .. i (a
+ * chain of drafts, or a chunk of a prompt).  Bits of nodes that do not exist,
+ * and keys and values that a node does not see, have no influence, whatever they
+ * hold.
+ *   q      bf16 [rows][num_q_heads][128] with the strides below
+ *   mask   uint64 [rows][mask_words], NULL iff mask_words is 0 (masks of any
+ *          number of nodes: those past 64 * mask_words are not seen)
+ *   out    [rows][num_q_heads][128] of out_dtype, contiguous:
+ *          sum_j p_j v_j / sum_j p_j, p_j = exp(softmax_scale q.k_j)
+ *   lse    fp32 [rows][num_q_heads]: ln of sum_j p_j
+ * A row that sees nothing gets zeros and -inf (scores of -inf count as unseen).
+ * Values of V within 2^118 over the number of tokens cannot overflow the sums,
+ * which are held in fp32.  With an fp32 output probabilities carry 24 bits, with
+ * a bf16 output 8 (as the output itself).
+ * Shape fields used: those of art_decode_attention but block_size and the list's;
+ * num_q_heads / num_kv_heads is any whole number up to 128.
+ */
+typedef struct {
+    float softmax_scale;
+    int32_t out_dtype;             /* art_out_dtype */
+    int32_t rows;
+    int32_t mask_words;            /* 0: no mask */
+    int64_t q_stride_row, q_stride_head;  /* elements, multiples of 8 */
+} art_tree_opts;
+
+/* Workspace bytes of such a call (0 and *status on invalid input): a function of
+ * shape and opts alone, never of the data. */
+size_t art_tree_workspace_bytes(const art_decode_shape* shape, const art_tree_opts* opts,
+                                int32_t* status);
+
+art_status art_tree_attention(const art_decode_shape* shape, const art_tree_opts* opts,
+                              const void* q, const void* k_cache, const void* v_cache,
+                              const int32_t* page_table, const int32_t* context_lens,
+                              const int32_t* row_offsets, const uint64_t* mask,
+                              void* out, float* lse, void* workspace, size_t workspace_bytes,
+                              hipStream_t stream);
+
+/*
+ * Verification of drafts against the target's probabilities, with random
+ * numbers that the caller gives.  target row r holds the probabilities p of the
+ * token that follows node r.  From node 0 (accepted) on, the children of the
+ * current node are tried in order, child c with token x = tokens[c] and u =
+ * uniforms[c]:
+ *   with `draft` (row r holds the probabilities q from which the children of
+ *   node r were drawn, independently): accepted if
+ *       u q(x) F < max(p(x) - a q(x), 0),        a = 0, F = 1 at first;
+ *     on rejection a += F, then F = sum_v max(p(v) - a q(v), 0)
+ *   without it (the drafts are given): accepted if
+ *       u R < p(x),        R = 1 at first;
+ *     on rejection R -= p(x), not below 0, and p(x) counts as 0 from then on
+ * The first accepted child becomes the current node.  Where no child is accepted
+ * (or max_path nodes are), the next token is drawn from w = max(p - a q, 0), or
+ * from p without the rejected tokens (w = p where w has no mass): the first v
+ * with w(0) + .. + w(v) > last_uniforms[b] * (w(0) + .. + w(V-1)), or the last
+ * of positive weight.  Accepted tokens and next token are then distributed as
+ * tokens drawn from p one after the other.  Sums and comparisons are in fp64.
+ * A chain without drafts' probabilities and with one-hot rows of p is greedy
+ * verification.  p and q need not sum to 1; where they hold NaN the result is
+ * some token.  Tokens outside 0 .. vocab-1 are passed over as children.
+ *   accepted     int32 [batch][max_path], out: the accepted nodes in order, node
+ *                0 first, then -1
+ *   counts       int32 [batch], out: their number
+ *   next_tokens  int32 [batch], out
+ * A sequence of no nodes, or of more than ART_MAX_NODES, gets 0, -1 and a row of
+ * -1.  target and draft have the same type; row strides in elements, any that are
+ * >= vocab, and any alignment to the type.  vocab < 2^24.
+ */
+typedef struct {
+    int32_t batch, rows, vocab, max_path;
+    int32_t dtype;                 /* art_rows_dtype of target and draft */
+    int64_t target_stride, draft_stride;
+} art_verify_opts;
+
+size_t art_verify_workspace_bytes(const art_verify_opts* opts, int32_t* status);
+
+art_status art_verify_drafts(const art_verify_opts* opts, const void* target, const void* draft,
+                             const int32_t* tokens, const int32_t* parents,
+                             const int32_t* row_offsets, const float* uniforms,
+                             const float* last_uniforms, int32_t* accepted, int32_t* counts,
+                             int32_t* next_tokens, void* workspace, size_t workspace_bytes,
+                             hipStream_t stream);
+
+/*
+ * Keep the accepted nodes: the keys and values of node accepted[b][j] move to
+ * slot context_lens[b] + j, j = 0 .. counts[b]-1 (the bf16 cache; accepted as
+ * art_verify_drafts writes it: nodes in increasing order).  Other slots keep
+ * their bytes.  A sequence whose list is not increasing from 0 or more, is longer
+ * than max_path or reaches past its table is passed over, and so is a node whose
+ * page id, or whose slot's, is out of range.  Nodes' slots must belong to their
+ * sequence alone.
+ */
+art_status art_keep_accepted(const art_decode_shape* shape, int32_t max_path,
+                             const int32_t* accepted, const int32_t* counts,
+                             const int32_t* context_lens, const int32_t* page_table,
+                             void* k_cache, void* v_cache, hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -27,7 +27,10 @@ EXPORTS = ("art_abi_version", "art_status_str", "art_decode_workspace_bytes",
            "art_workspace_init", "art_decode_attention", "art_validate_inputs",
            "art_workspace_status", "art_block_list_workspace_bytes", "art_build_block_list",
            "art_decode_attention_static", "art_build_block_list_padded",
-           "art_decode_attention_quant", "art_quant_append", "art_quant_read")
+           "art_decode_attention_quant", "art_quant_append", "art_quant_read",
+           "art_rope_rows", "art_rope_append", "art_tree_layout", "art_tree_workspace_bytes",
+           "art_tree_attention", "art_verify_workspace_bytes", "art_verify_drafts",
+           "art_keep_accepted")
 STATIC_SCRATCH_BYTES = 64 << 20   # ART_STATIC_SCRATCH_BYTES
 
 LIST_IMPORTANCE = 0
@@ -40,6 +43,10 @@ QUANT_INT8 = 1
 ROWS_BF16 = 0
 ROWS_F16 = 1
 ROWS_F32 = 2
+
+ROPE_HALF = 0
+ROPE_INTERLEAVED = 1
+MAX_NODES = 1024                  # ART_MAX_NODES
 
 
 class DecodeShape(ctypes.Structure):
@@ -82,6 +89,30 @@ class QuantRows(ctypes.Structure):
     _fields_ = [("rows_dtype", ctypes.c_int32), ("rows", ctypes.c_int32)] + [
         (n, ctypes.c_int64) for n in ("k_stride_row", "k_stride_head", "v_stride_row",
                                       "v_stride_head")]
+
+
+class Rows(ctypes.Structure):
+    """art_rows"""
+    _fields_ = [("dtype", ctypes.c_int32), ("heads", ctypes.c_int32),
+                ("stride_row", ctypes.c_int64), ("stride_head", ctypes.c_int64)]
+
+
+class RopeSpec(ctypes.Structure):
+    """art_rope"""
+    _fields_ = [("layout", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+class TreeOpts(ctypes.Structure):
+    """art_tree_opts"""
+    _fields_ = [("softmax_scale", ctypes.c_float), ("out_dtype", ctypes.c_int32),
+                ("rows", ctypes.c_int32), ("mask_words", ctypes.c_int32),
+                ("q_stride_row", ctypes.c_int64), ("q_stride_head", ctypes.c_int64)]
+
+
+class VerifyOpts(ctypes.Structure):
+    """art_verify_opts"""
+    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "rows", "vocab", "max_path", "dtype")] + [
+        (n, ctypes.c_int64) for n in ("target_stride", "draft_stride")]
 
 
 class ArtError(RuntimeError):
@@ -155,6 +186,25 @@ def load_variant(path: str) -> ctypes.CDLL:
             call.restype = ctypes.c_int
             call.argtypes = [ctypes.POINTER(DecodeShape), spec, ctypes.POINTER(QuantRows),
                              vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+    if hasattr(lib, "art_tree_attention"):   # (and those for drafted tokens)
+        shape, rows, i32 = ctypes.POINTER(DecodeShape), ctypes.POINTER(Rows), ctypes.c_int32
+        rope, tree, verify = (ctypes.POINTER(t) for t in (RopeSpec, TreeOpts, VerifyOpts))
+        for name, args in (
+                ("art_rope_rows", [rope, i32, rows, vp, rows, vp, vp, vp, vp]),
+                ("art_rope_append", [shape, rope, i32, rows, vp, rows, vp, rows, vp, rows, vp, vp, vp, vp,
+                                     vp, vp, vp, vp, vp]),
+                ("art_tree_layout", [i32, i32, vp, vp, vp, i32, vp, vp, vp]),
+                ("art_tree_attention", [shape, tree, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp,
+                                        ctypes.c_size_t, vp]),
+                ("art_verify_drafts", [verify, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp,
+                                       ctypes.c_size_t, vp]),
+                ("art_keep_accepted", [shape, i32, vp, vp, vp, vp, vp, vp, vp])):
+            getattr(lib, name).restype = ctypes.c_int
+            getattr(lib, name).argtypes = args
+        for name, args in (("art_tree_workspace_bytes", [shape, tree, i32p]),
+                           ("art_verify_workspace_bytes", [verify, i32p])):
+            getattr(lib, name).restype = ctypes.c_size_t
+            getattr(lib, name).argtypes = args
     got = int(lib.art_abi_version())
     if got != ABI_VERSION:
         raise RuntimeError(f"{path} has ABI version {got}, this binding needs "
@@ -247,6 +297,75 @@ def quant_read(shape, cache, rows, k, v, k_scale, v_scale, row_offsets, position
     return int(load().art_quant_read(
         ctypes.byref(shape), ctypes.byref(cache), ctypes.byref(rows), k, v, k_scale, v_scale,
         row_offsets or None, positions or None, page_table, k_rows, v_rows, stream or None))
+
+
+def rope_rows(rope, rows, x_rows, x, out_rows, out, positions, freqs, stream) -> int:
+    """Raw call; pointers are ints (0 for NULL).  Returns the status."""
+    return int(load().art_rope_rows(
+        ctypes.byref(rope), rows, ctypes.byref(x_rows), x or None, ctypes.byref(out_rows), out or None,
+        positions or None, freqs or None, stream or None))
+
+
+def rope_append(shape, rope, rows, q_rows, q, q_out_rows, q_out, k_rows, k, v_rows, v, row_offsets,
+                context_lens, row_positions, freqs, page_table, k_cache, v_cache, stream) -> int:
+    """Raw call; pointers are ints (0 for NULL), rope, q_rows and q_out_rows may
+    be None.  Returns the status."""
+    ref = lambda s: None if s is None else ctypes.byref(s)  # noqa: E731
+    return int(load().art_rope_append(
+        ctypes.byref(shape), ref(rope), rows, ref(q_rows), q or None, ref(q_out_rows), q_out or None,
+        ctypes.byref(k_rows), k or None, ctypes.byref(v_rows), v or None, row_offsets or None,
+        context_lens or None, row_positions or None, freqs or None, page_table or None,
+        k_cache or None, v_cache or None, stream or None))
+
+
+def tree_layout(batch, rows, parents, row_offsets, context_lens, mask_words, mask, positions,
+                stream) -> int:
+    """Raw call; pointers are ints (0 for NULL).  Returns the status."""
+    return int(load().art_tree_layout(batch, rows, parents or None, row_offsets or None,
+                                      context_lens or None, mask_words, mask or None,
+                                      positions or None, stream or None))
+
+
+def tree_workspace_bytes(shape: DecodeShape, opts: TreeOpts) -> int:
+    st = ctypes.c_int32(0)
+    n = load().art_tree_workspace_bytes(ctypes.byref(shape), ctypes.byref(opts), ctypes.byref(st))
+    if st.value != OK:
+        raise ArtError(st.value, "art_tree_workspace_bytes")
+    return int(n)
+
+
+def tree_attention(shape, opts, q, k, v, page_table, context_lens, row_offsets, mask, out, lse,
+                   workspace, workspace_bytes, stream) -> int:
+    """Raw call; pointers are ints (0 for NULL).  Returns the status."""
+    return int(load().art_tree_attention(
+        ctypes.byref(shape), ctypes.byref(opts), q or None, k or None, v or None, page_table or None,
+        context_lens or None, row_offsets or None, mask or None, out or None, lse or None,
+        workspace or None, workspace_bytes, stream or None))
+
+
+def verify_workspace_bytes(opts: VerifyOpts) -> int:
+    st = ctypes.c_int32(0)
+    n = load().art_verify_workspace_bytes(ctypes.byref(opts), ctypes.byref(st))
+    if st.value != OK:
+        raise ArtError(st.value, "art_verify_workspace_bytes")
+    return int(n)
+
+
+def verify_drafts(opts, target, draft, tokens, parents, row_offsets, uniforms, last_uniforms,
+                  accepted, counts, next_tokens, workspace, workspace_bytes, stream) -> int:
+    """Raw call; pointers are ints (0 for NULL).  Returns the status."""
+    return int(load().art_verify_drafts(
+        ctypes.byref(opts), target or None, draft or None, tokens or None, parents or None,
+        row_offsets or None, uniforms or None, last_uniforms or None, accepted or None, counts or None,
+        next_tokens or None, workspace or None, workspace_bytes, stream or None))
+
+
+def keep_accepted(shape, max_path, accepted, counts, context_lens, page_table, k_cache, v_cache,
+                  stream) -> int:
+    """Raw call; pointers are ints (0 for NULL).  Returns the status."""
+    return int(load().art_keep_accepted(
+        ctypes.byref(shape), max_path, accepted or None, counts or None, context_lens or None,
+        page_table or None, k_cache or None, v_cache or None, stream or None))
 
 
 def validate_inputs(shape, opts, page_table, seq_lens, block_list, block_list_len, stream):

@@ -495,3 +495,339 @@ def quant_read(cache: QuantCache, page_table: torch.Tensor, positions: Optional[
     if st != _lib.OK:
         raise ArtError(st, "art_quant_read")
     return k, v
+
+
+# ---- drafted tokens over the bf16 cache -------------------------------------------
+#
+# The nodes of all sequences are packed rows: rows token_offsets[b] ..
+# token_offsets[b + 1] - 1 are sequence b's nodes 0, 1, ... (int32 [B + 1]; without
+# it every sequence has rows / B of them), node i in slot context_lens[b] + i of the
+# cache.  A sequence with a negative context is an unused one of a padded batch.
+
+_ROPE_LAYOUTS = {"half": _lib.ROPE_HALF, "interleaved": _lib.ROPE_INTERLEAVED}
+
+
+class Rope(NamedTuple):
+    """Rotary positions: pair i of a head's first 2 len(freqs) dims turns by
+    position * freqs[i] radians and is multiplied by ``scale``.  ``freqs`` fp64 on
+    the GPU; ``layout`` "half" (dims i and i + len(freqs)) or "interleaved"
+    (dims 2i and 2i + 1)."""
+    freqs: torch.Tensor
+    layout: str = "half"
+    scale: float = 1.0
+
+
+def rope_frequencies(rot_dim: int = 128, *, base: float = 10000.0, layout: str = "half",
+                     factor: float = 1.0, original_len: Optional[int] = None,
+                     beta_fast: float = 32.0, beta_slow: float = 1.0, device="cuda") -> Rope:
+    """The usual frequencies, base ** (-2i / rot_dim), as a ``Rope``.
+
+    ``factor`` > 1 scales them for contexts that many times as long: all alike
+    (positions divided by it), or with ``original_len`` the way of YaRN
+    (arXiv 2309.00071): pairs that turn more than ``beta_fast`` times over the
+    original length keep their frequency, those of fewer than ``beta_slow`` turns
+    have it divided, with a linear ramp over the pairs between them, and rotated
+    values are multiplied by 0.1 ln(factor) + 1.
+    """
+    if rot_dim < 2 or rot_dim % 2 or rot_dim > 128 or factor < 1.0:
+        raise ValueError("rot_dim must be even, 2 .. 128, and factor at least 1")
+    half = rot_dim // 2
+    i = torch.arange(half, dtype=torch.float64)
+    freqs, scale = base ** (-i / half), 1.0
+    if original_len is None:
+        freqs = freqs / factor
+    else:
+        # the pair that turns n times over the original length
+        pair = lambda n: half * math.log(original_len / (2 * math.pi * n)) / math.log(base)  # noqa: E731
+        low, high = max(math.floor(pair(beta_fast)), 0), min(math.ceil(pair(beta_slow)), rot_dim - 1)
+        ramp = ((i - low) / max(high - low, 1e-3)).clamp(0, 1)
+        freqs, scale = freqs * (1 - ramp) + freqs / factor * ramp, 0.1 * math.log(factor) + 1.0
+    return Rope(freqs.to(device), layout, scale)
+
+
+def _rope_spec(rope: Rope, dev: int) -> _lib.RopeSpec:
+    freqs, layout, scale = rope
+    if layout not in _ROPE_LAYOUTS:
+        raise ValueError('layout must be "half" or "interleaved"')
+    _check(freqs, "freqs", torch.float64, dev, (freqs.numel(),))
+    return _lib.RopeSpec(_ROPE_LAYOUTS[layout], 2 * freqs.numel(), float(scale))
+
+
+def _packed_rows(t: torch.Tensor, name: str, dev: int) -> _lib.Rows:
+    """ABI description of rows [rows][heads][head_dim] on GPU ``dev``."""
+    kind = _ROWS_TYPES.get(t.dtype)
+    if kind is None:
+        raise ValueError(f"{name} must be bfloat16, float16 or float32")
+    if t.get_device() != dev or dev < 0:
+        _require_cuda(t, name)
+        raise ValueError(f"{name} must be on cuda:{dev}, got {t.device}")
+    if t.dim() != 3 or t.shape[2] != 128 or t.stride(2) != 1:
+        raise ValueError(f"{name} must be [rows][heads][128] with a unit head-dim stride")
+    return _lib.Rows(kind, t.shape[1], t.stride(0), t.stride(1))
+
+
+def _bf16_pools(k_cache, v_cache, page_table):
+    """(device index, heads, batch, shape fields from page_size on) of a bf16
+    cache and its table, checked."""
+    dev = k_cache.get_device()
+    for t, name in ((k_cache, "k_cache"), (v_cache, "v_cache")):
+        if t.dtype is not torch.bfloat16 or t.get_device() != dev or dev < 0:
+            _require_cuda(t, name, torch.bfloat16)
+            raise ValueError("the cache's tensors must be on one device")
+    if k_cache.dim() != 4 or v_cache.shape != k_cache.shape:
+        raise ValueError("k_cache/v_cache must both be [pages][kv_heads][page_size][head_dim]")
+    a, b = k_cache.stride(), v_cache.stride()
+    if a[3] != 1 or b[3] != 1:
+        raise ValueError("head_dim must be the innermost (unit-stride) dimension")
+    if page_table.dim() != 2:
+        raise ValueError("page_table must be [batch][max_pages]")
+    B, width = page_table.shape
+    _check(page_table, "page_table", torch.int32, dev, (B, width))
+    P, H, Ps, _ = k_cache.shape
+    return dev, H, B, (Ps, P, width, 0, 1, a[0], a[1], a[2], b[0], b[1], b[2])
+
+
+def rope_rows(x: torch.Tensor, positions: torch.Tensor, rope: Rope, *,
+              out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Rotate rows ``x`` [rows][heads][128] (bf16, fp16 or fp32) to ``positions``
+    (int32 [rows]), on the current stream.  ``out`` (default: like ``x``) may be
+    ``x`` itself, or of another of the three types.  Keys of an 8-bit cache are
+    rotated so before ``quant_append``.  ``Rope(-freqs, layout, scale)`` gives the
+    gradient of a rotation, which is the way back where scale is 1."""
+    dev = x.get_device()
+    x_rows = _packed_rows(x, "x", dev)
+    _check(positions, "positions", torch.int32, dev, (x.shape[0],))
+    spec = _rope_spec(rope, dev)
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    elif out.shape != x.shape:
+        raise ValueError("out must have the shape of x")
+    st = _on_device(dev, _lib.rope_rows, spec, x.shape[0], x_rows, x.data_ptr(),
+                    _packed_rows(out, "out", dev), out.data_ptr(), positions.data_ptr(),
+                    rope.freqs.data_ptr())
+    if st != _lib.OK:
+        raise ArtError(st, "art_rope_rows")
+    return out
+
+
+def rope_append(k_cache: torch.Tensor, v_cache: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                page_table: torch.Tensor, context_lens: torch.Tensor, *, rope: Optional[Rope] = None,
+                q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+                token_offsets: Optional[torch.Tensor] = None,
+                row_positions: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+    """Append new tokens to the bf16 cache, on the current stream: keys rotated
+    on the way, values as they are, both rounded to bf16.
+
+    ``k`` and ``v`` [rows][Hkv][128] (bf16, fp16 or fp32) are the packed nodes (or
+    prompts) of all sequences, ``context_lens`` int32 [B] the tokens that each holds
+    already.  A row's position is its slot, or row_positions[row] (int32, e.g. from
+    ``tree_layout``).  With ``q`` [rows][Hq][128], of the type of ``k``, the queries are
+    rotated too; returns them in bf16 (``q_out``, or new), else None.  ``rope`` None:
+    no rotation.  ``context_lens`` stays the caller's to advance.
+    """
+    dev, H, B, fields = _bf16_pools(k_cache, v_cache, page_table)
+    k_rows, v_rows = _packed_rows(k, "k", dev), _packed_rows(v, "v", dev)
+    if k.shape[1] != H or v.shape != k.shape or v.dtype is not k.dtype:
+        raise ValueError(f"k and v must both be [rows][{H}][128] of one type")
+    rows = k.shape[0]
+    _check(context_lens, "context_lens", torch.int32, dev, (B,))
+    if token_offsets is not None:
+        _check(token_offsets, "token_offsets", torch.int32, dev, (B + 1,))
+    if row_positions is not None:
+        _check(row_positions, "row_positions", torch.int32, dev, (rows,))
+    q_rows = out_rows = None
+    heads = H
+    if q is not None:
+        q_rows, heads = _packed_rows(q, "q", dev), q.shape[1]
+        if q.shape[0] != rows or q.dtype is not k.dtype:
+            raise ValueError("q must have the rows and the type of k")
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
+        elif q_out.shape != q.shape or q_out.dtype is not torch.bfloat16:
+            raise ValueError("q_out must be bfloat16 of the shape of q")
+        out_rows = _packed_rows(q_out, "q_out", dev)
+    elif q_out is not None:
+        raise ValueError("q_out goes with q")
+    spec = None if rope is None else _rope_spec(rope, dev)
+    shape = DecodeShape(B, heads, H, k_cache.shape[3], 64, *fields)
+    st = _on_device(dev, _lib.rope_append, shape, spec, rows, q_rows, _ptr(q), out_rows, _ptr(q_out),
+                    k_rows, k.data_ptr(), v_rows, v.data_ptr(), _ptr(token_offsets),
+                    context_lens.data_ptr(), _ptr(row_positions),
+                    0 if rope is None else rope.freqs.data_ptr(), page_table.data_ptr(),
+                    k_cache.data_ptr(), v_cache.data_ptr())
+    if st != _lib.OK:
+        raise ArtError(st, "art_rope_append")
+    return q_out
+
+
+def tree_layout(parents: torch.Tensor, context_lens: torch.Tensor, *, mask_words: int = 1,
+                token_offsets: Optional[torch.Tensor] = None):
+    """Masks and positions of trees of nodes, on the current stream.
+
+    ``parents`` int32 [rows]: the parent's number within the sequence, -1 for node
+    0.  Returns (mask int64 [rows][mask_words], positions int32 [rows]): bit j % 64
+    of word j / 64 is set for the node and its ancestors j; a node's position is
+    its sequence's context plus its depth.  Rows of no sequence are not written.
+    """
+    dev, B = parents.get_device(), context_lens.shape[0]
+    rows = parents.shape[0]
+    _check(parents, "parents", torch.int32, dev, (rows,))
+    _check(context_lens, "context_lens", torch.int32, dev, (B,))
+    if dev < 0:
+        _require_cuda(parents, "parents")
+    if token_offsets is not None:
+        _check(token_offsets, "token_offsets", torch.int32, dev, (B + 1,))
+    mask = torch.empty((rows, int(mask_words)), dtype=torch.int64, device=parents.device)
+    positions = torch.empty(rows, dtype=torch.int32, device=parents.device)
+    st = _on_device(dev, _lib.tree_layout, B, rows, parents.data_ptr(), _ptr(token_offsets),
+                    context_lens.data_ptr(), int(mask_words), mask.data_ptr(), positions.data_ptr())
+    if st != _lib.OK:
+        raise ArtError(st, "art_tree_layout")
+    return mask, positions
+
+
+def _call_workspace(workspace, need: int, dev: int, device) -> torch.Tensor:
+    """The caller's workspace, or one of this call's own: the allocator orders its
+    reuse on the stream, and under capture it belongs to the graph."""
+    if workspace is None:
+        return torch.empty(need, dtype=torch.uint8, device=device)
+    if workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be contiguous and on cuda:{dev}")
+    return workspace
+
+
+def tree_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
+                   page_table: torch.Tensor, context_lens: torch.Tensor, *,
+                   mask: Optional[torch.Tensor] = None,
+                   token_offsets: Optional[torch.Tensor] = None,
+                   softmax_scale: Optional[float] = None, out_dtype=torch.float32,
+                   workspace: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                   lse: Optional[torch.Tensor] = None):
+    """Full attention of several new tokens a sequence over the bf16 cache, which
+    holds their keys and values already, on the current stream.
+
+    ``q`` bf16 [rows][Hq][128] are the packed nodes' queries.  A node sees its
+    sequence's context and the nodes that its row of ``mask`` (int64
+    [rows][words], as from ``tree_layout``) has a bit for; without a mask node i sees
+    nodes 0 .. i (a chain of drafts, a chunk of a prompt).  Returns (out
+    [rows][Hq][128] out_dtype, lse [rows][Hq] fp32); a row that sees nothing gets 0
+    and -inf, and rows of no sequence are not written.  ``workspace`` (uint8 of
+    ``tree_workspace_bytes``, needs no initialisation) defaults to one of the call's
+    own.
+    """
+    dev, H, B, fields = _bf16_pools(k_cache, v_cache, page_table)
+    if q.dim() != 3 or q.dtype is not torch.bfloat16 or q.get_device() != dev:
+        _require_cuda(q, "q", torch.bfloat16)
+        raise ValueError(f"q must be [rows][q_heads][head_dim] on cuda:{dev}")
+    rows, Hq, D = q.shape
+    if D != k_cache.shape[3] or q.stride(2) != 1:
+        raise ValueError("head_dim must be that of the cache, and innermost (unit stride)")
+    _check(context_lens, "context_lens", torch.int32, dev, (B,))
+    if token_offsets is not None:
+        _check(token_offsets, "token_offsets", torch.int32, dev, (B + 1,))
+    words = 0
+    if mask is not None:
+        words = mask.shape[-1]
+        _check(mask, "mask", torch.int64, dev, (rows, words))
+    if out_dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("out_dtype must be float32 or bfloat16")
+    if out is None:
+        out = torch.empty((rows, Hq, D), dtype=out_dtype, device=q.device)
+    else:
+        _check(out, "out", out_dtype, dev, (rows, Hq, D))
+    if lse is None:
+        lse = torch.empty((rows, Hq), dtype=torch.float32, device=q.device)
+    else:
+        _check(lse, "lse", torch.float32, dev, (rows, Hq))
+    shape = DecodeShape(B, Hq, H, D, 64, *fields)
+    opts = _lib.TreeOpts(1.0 / math.sqrt(D) if softmax_scale is None else float(softmax_scale),
+                         _lib.OUT_BF16 if out_dtype is torch.bfloat16 else _lib.OUT_F32, rows, words,
+                         q.stride(0), q.stride(1))
+    ws = _call_workspace(workspace, _lib.tree_workspace_bytes(shape, opts), dev, q.device)
+    st = _on_device(dev, _lib.tree_attention, shape, opts, q.data_ptr(), k_cache.data_ptr(),
+                    v_cache.data_ptr(), page_table.data_ptr(), context_lens.data_ptr(),
+                    _ptr(token_offsets), _ptr(mask), out.data_ptr(), lse.data_ptr(), ws.data_ptr(),
+                    ws.numel() * ws.element_size())
+    if st != _lib.OK:
+        raise ArtError(st, "art_tree_attention")
+    return out, lse
+
+
+def verify_drafts(target: torch.Tensor, tokens: torch.Tensor, parents: torch.Tensor,
+                  uniforms: torch.Tensor, last_uniforms: torch.Tensor, *,
+                  draft: Optional[torch.Tensor] = None,
+                  token_offsets: Optional[torch.Tensor] = None, max_path: Optional[int] = None,
+                  workspace: Optional[torch.Tensor] = None):
+    """Verify drafted tokens against the target's probabilities, on the current
+    stream, so that the accepted tokens and the one that follows are distributed as
+    tokens drawn from the target.
+
+    ``target`` [rows][V] (fp32, bf16 or fp16): row r holds the probabilities of the
+    token that follows node r.  ``draft``, likewise and of the same type: those from
+    which node r's children were drawn (independently); without it the drafts are
+    taken as given.  ``tokens`` and ``parents`` int32 [rows] (node 0, parent -1, is
+    the sequence's newest token), ``uniforms`` fp32 [rows] and ``last_uniforms`` fp32
+    [B] random numbers in [0, 1).  One-hot rows verify greedily.  Returns (accepted
+    int32 [B][max_path], the accepted nodes in order and -1 behind them; counts int32
+    [B]; next_tokens int32 [B]).  ``max_path`` defaults to rows / B (needed with
+    ``token_offsets``).
+    """
+    dev, kind = target.get_device(), _ROWS_TYPES.get(target.dtype)
+    if kind is None or dev < 0:
+        _require_cuda(target, "target")
+        raise ValueError("target must be bfloat16, float16 or float32")
+    if target.dim() != 2 or target.stride(1) != 1:
+        raise ValueError("target must be [rows][vocab] with a unit vocab stride")
+    rows, vocab = target.shape
+    B = last_uniforms.shape[0]
+    if draft is not None:
+        if draft.get_device() != dev or draft.dtype is not target.dtype:
+            _require_cuda(draft, "draft", target.dtype)
+            raise ValueError("draft must be on the target's device")
+        if draft.shape != target.shape or draft.stride(1) != 1:
+            raise ValueError("draft must have the shape of target, with a unit vocab stride")
+    _check(tokens, "tokens", torch.int32, dev, (rows,))
+    _check(parents, "parents", torch.int32, dev, (rows,))
+    _check(uniforms, "uniforms", torch.float32, dev, (rows,))
+    _check(last_uniforms, "last_uniforms", torch.float32, dev, (B,))
+    if token_offsets is not None:
+        _check(token_offsets, "token_offsets", torch.int32, dev, (B + 1,))
+    if max_path is None:
+        if token_offsets is not None:
+            raise ValueError("max_path is needed with token_offsets")
+        max_path = max(1, rows // max(1, B))
+    # (the stride of a single row says nothing)
+    strides = [max(t.stride(0), vocab) if rows < 2 else t.stride(0)
+               for t in (target, target if draft is None else draft)]
+    opts = _lib.VerifyOpts(B, rows, vocab, int(max_path), kind, *strides)
+    ws = _call_workspace(workspace, _lib.verify_workspace_bytes(opts), dev, target.device)
+    accepted = torch.empty((B, int(max_path)), dtype=torch.int32, device=target.device)
+    counts, following = (torch.empty(B, dtype=torch.int32, device=target.device) for _ in range(2))
+    st = _on_device(dev, _lib.verify_drafts, opts, target.data_ptr(), _ptr(draft), tokens.data_ptr(),
+                    parents.data_ptr(), _ptr(token_offsets), uniforms.data_ptr(),
+                    last_uniforms.data_ptr(), accepted.data_ptr(), counts.data_ptr(),
+                    following.data_ptr(), ws.data_ptr(), ws.numel() * ws.element_size())
+    if st != _lib.OK:
+        raise ArtError(st, "art_verify_drafts")
+    return accepted, counts, following
+
+
+def keep_accepted(k_cache: torch.Tensor, v_cache: torch.Tensor, page_table: torch.Tensor,
+                  context_lens: torch.Tensor, accepted: torch.Tensor, counts: torch.Tensor) -> None:
+    """Move the accepted nodes' keys and values up to the context's end, on the
+    current stream: node accepted[b][j] to slot context_lens[b] + j for j <
+    counts[b] (as ``verify_drafts`` returns them).  The sequence then holds
+    context_lens[b] + counts[b] tokens; ``context_lens`` stays the caller's to
+    advance."""
+    dev, H, B, fields = _bf16_pools(k_cache, v_cache, page_table)
+    _check(context_lens, "context_lens", torch.int32, dev, (B,))
+    if accepted.dim() != 2:
+        raise ValueError("accepted must be [batch][max_path]")
+    _check(accepted, "accepted", torch.int32, dev, (B, accepted.shape[1]))
+    _check(counts, "counts", torch.int32, dev, (B,))
+    shape = DecodeShape(B, H, H, k_cache.shape[3], 64, *fields)
+    st = _on_device(dev, _lib.keep_accepted, shape, accepted.shape[1], accepted.data_ptr(),
+                    counts.data_ptr(), context_lens.data_ptr(), page_table.data_ptr(),
+                    k_cache.data_ptr(), v_cache.data_ptr())
+    if st != _lib.OK:
+        raise ArtError(st, "art_keep_accepted")

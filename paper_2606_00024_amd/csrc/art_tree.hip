@@ -1,0 +1,690 @@
+// Attention of drafted tokens over a paged bf16 cache (art_tree_attention).
+//
+//   out = sum_j p_j v_j / sum_j p_j,  p_j = 2^(c q.k_j - m),  c = scale log2 e
+//
+// over the tokens j that a row sees: the context, and of its sequence's nodes
+// those in its mask (or the earlier ones and itself).
+//
+// The rows of a sequence's nodes that share a KV head lie together: a row tile is
+// as many whole nodes as fit kRows rows.  Row tiles of all sequences and heads are
+// the units of work; a unit has a tile of 64 or 128 tokens after the other to go
+// through.  The tiles of all units, kLead places for each unit's set-up in front
+// of them, form one line, and every workgroup takes an equal, contiguous part of
+// it, however ragged the batch is.  A unit that lies in one workgroup is written
+// there; of the others each workgroup leaves a record (o, m, l) in the workspace
+// and a second, small launch joins them in the order of the line.
+//
+// Scores are computed transposed, S^T = K Q^T, by 32x32x16 matrix instructions: a
+// lane then holds 16 tokens' scores of one row, so that maximum and sum need no
+// other lane but its partner 32 further, and the probabilities are, as they lie,
+// the B operand of O^T = V^T P^T.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+#include <string.h>
+
+#include "art.h"
+#include "art_internal.h"
+#include "art_rows.h"
+#include "art_wave.h"
+
+namespace art {
+namespace {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short v4i16 __attribute__((ext_vector_type(4)));
+
+constexpr int kD = kHeadDim;
+constexpr int kMaxWorkers = 512;   // two workgroups for each of 256 CUs
+constexpr int kLead = 4;           // places of a unit's set-up and end
+
+// RB: blocks of 32 rows of a row tile, one or more wavefronts to each
+template <int RB>
+struct Tree {
+  static constexpr int kRows = 32 * RB;
+  static constexpr int TS = kWaves / RB;            // wavefronts that share a block's tokens
+  static constexpr int TK = RB == 1 ? 128 : 64;     // tokens of a tile
+  static constexpr int SUB = TK / 32 / TS;          // 32-token pieces of a wavefront
+  static constexpr int LOADS = TK / 16;             // 16-byte pieces of K (and V) a thread loads
+  static constexpr int PITCH = kD + 4;              // floats of a row of a wavefront's record
+  static constexpr int TILE_BYTES = 2 * TK * kD * 2;
+  static constexpr int REC_BYTES = kWaves * 32 * PITCH * 4;
+  static constexpr int LDS = TILE_BYTES > REC_BYTES ? TILE_BYTES : REC_BYTES;
+};
+
+struct TreeParams {
+  int32_t batch, rows, per_seq;
+  int32_t q_heads, kv_heads, group;
+  int32_t nodes;               // of a row tile
+  int32_t words;               // of a mask row; 0: chains
+  int32_t page_shift, num_pages, max_pages;
+  int32_t slots;               // entries of `units`
+  int32_t by_unit;             // entries are units (else workgroups)
+  int32_t out_bf16, negate;    // negate: a negative scale
+  float scale_log2;            // its magnitude
+  int64_t qs_row, qs_head;
+  int64_t ks_page, ks_head, ks_tok, vs_page, vs_head, vs_tok;
+  const int32_t* offsets;
+  const int32_t* context;
+  const int32_t* table;
+  const uint16_t* q;
+  const uint16_t* k;
+  const uint16_t* v;
+  const uint64_t* mask;
+  void* out;
+  float* lse;
+  int4* units;                 // what the second launch has to join
+  float* records;              // two for every workgroup
+};
+
+// A sequence: its first row, nodes, context and row tiles.
+struct Seq {
+  int first, n, context, tiles;
+};
+__device__ __forceinline__ Seq seq_of(const TreeParams& P, int b) {
+  int first = P.offsets ? P.offsets[b] : b * P.per_seq, end = P.offsets ? P.offsets[b + 1] : first + P.per_seq;
+  first = min(max(first, 0), P.rows);
+  end = min(max(end, first), P.rows);
+  Seq s{first, end - first, P.context[b], 0};
+  if (s.context < 0 || (int64_t)s.context + s.n > (int64_t)P.max_pages << P.page_shift) s.n = 0;
+  s.tiles = (s.n + P.nodes - 1) / P.nodes;
+  return s;
+}
+
+// Tokens that row tile i goes through.
+__device__ __forceinline__ int tokens_of(const TreeParams& P, const Seq& s, int i) {
+  return s.context + (P.words ? s.n : (int)min((int64_t)s.n, (int64_t)(i + 1) * P.nodes));
+}
+// sum of floor((a i + b) / m) over i = 0 .. n - 1, by the steps of Euclid's
+// algorithm (a, m <= 128, n < 2^24)
+__device__ __forceinline__ int64_t floor_sum(uint32_t n, uint32_t m, uint32_t a, uint32_t b) {
+  int64_t sum = 0;
+  while (n > 0) {
+    sum += (int64_t)n * (n - 1) / 2 * (a / m) + (int64_t)n * (b / m);
+    a %= m;
+    b %= m;
+    const uint32_t y = a * n + b;
+    if (y < m) break;
+    n = y / m;
+    b = y % m;
+    const uint32_t t = m;
+    m = a;
+    a = t;
+  }
+  return sum;
+}
+// Places of a head's first `k` row tiles on the line.
+template <int RB>
+__device__ __forceinline__ int64_t places(const TreeParams& P, const Seq& s, int k) {
+  constexpr int TK = Tree<RB>::TK;
+  if (k == 0) return 0;                            // (a sequence of no nodes has no tiles)
+  const int64_t all = (s.context + s.n + TK - 1) / TK;
+  if (P.words || s.tiles == 1) return k * (kLead + all);
+  // all but the last row tile end a whole number of nodes further each
+  const int64_t sum = floor_sum(min(k, s.tiles - 1), TK, P.nodes, s.context + P.nodes + TK - 1);
+  return (int64_t)k * kLead + sum + (k == s.tiles ? all : 0);
+}
+
+__device__ __forceinline__ int64_t uniform(int64_t x) {
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((int)x), hi = __builtin_amdgcn_readfirstlane((int)(x >> 32));
+  return (int64_t)((uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// Offsets (in elements) of a token's 16-byte piece in LDS.  K: the eight rows that
+// are read together lie on distinct banks; V: the four rows that a transposing
+// read takes do.
+__device__ __forceinline__ int k_off(int r, int piece) { return r * kD + ((piece ^ (r & 7)) << 3); }
+__device__ __forceinline__ int v_off(int r, int piece) { return r * kD + ((piece ^ (2 * (r & 3))) << 3); }
+
+__device__ __forceinline__ bool not_finite(uint32_t w) {
+  return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
+}
+
+// Which of nodes j0 .. j0 + 31 row node i sees (bit k: node j0 + k; nodes below 0
+// are context).
+__device__ __forceinline__ uint32_t sees(const TreeParams& P, const uint64_t* mask, int i, int n, int j0) {
+  if (j0 <= -32) return 0xffffffffu;
+  uint64_t v;
+  int count;                     // of the 32 that may be seen
+  if (!P.words) {
+    v = ~0ull;
+    count = i + 1 - j0;
+  } else {
+    count = n - j0;
+    if (j0 < 0) {
+      v = mask[0] << -j0 | ((1ull << -j0) - 1);
+    } else {
+      const int w = j0 >> 6, sh = j0 & 63;
+      v = w < P.words ? mask[w] >> sh : 0;
+      if (sh > 32 && w + 1 < P.words) v |= mask[w + 1] << (64 - sh);
+    }
+  }
+  if (count <= 0) return 0;
+  return (uint32_t)v & (count >= 32 ? 0xffffffffu : (1u << count) - 1);
+}
+
+__device__ __forceinline__ float ln_of(float m, float l) { return (m + __log2f(l)) * 0.69314718055994531f; }
+__device__ __forceinline__ float factor(float m, float top) {
+  return m == kNegInf ? 0.f : fast_exp2(fmaxf(m - top, -126.f));
+}
+
+__device__ __forceinline__ void write4(const TreeParams& P, int64_t row, int d, const f32x4& x) {
+  if (P.out_bf16) {
+    *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(P.out) + row * kD + d) =
+        u32x2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+  } else {
+    *reinterpret_cast<f32x4*>(static_cast<float*>(P.out) + row * kD + d) = x;
+  }
+}
+__device__ __forceinline__ f32x4 over(const f32x4& o, float l) {
+  const float inv = l == 0.f ? 0.f : 1.f / l;     // (l is 0 where nothing is seen)
+  return f32x4{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+}
+
+// PARTS: bf16 parts that a probability is multiplied in: one (8 bits) for bf16
+// outputs, three (24) for fp32.
+template <int RB, int PARTS>
+__global__ void __launch_bounds__(kThreads, 2) tree_kernel(const TreeParams P) {
+  using C = Tree<RB>;
+  __shared__ __align__(16) uint8_t lds[C::LDS];
+  __shared__ float s_m[kWaves][32], s_l[kWaves][32];
+  __shared__ int64_t s_scan[2][kWaves], s_base;
+  __shared__ int s_seq, s_units;
+  const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63, lo = lane & 31, half = lane >> 5;
+
+  // ---- this workgroup's part of the line ----
+  // thread tid has sequences b0 .. b1 - 1: `own` places and `mine` units, behind
+  // `before` and `earlier`
+  const int per = (P.batch + kThreads - 1) / kThreads;
+  const int b0 = min(tid * per, P.batch), b1 = min(b0 + per, P.batch);
+  int64_t own = 0, mine = 0;
+  for (int b = b0; b < b1; ++b) {
+    const Seq s = seq_of(P, b);
+    own += P.kv_heads * places<RB>(P, s, s.tiles);
+    mine += (int64_t)P.kv_heads * s.tiles;
+  }
+  int64_t before = own, earlier = mine;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int64_t x = __shfl_up((long long)before, o), y = __shfl_up((long long)earlier, o);
+    if (lane >= o) {
+      before += x;
+      earlier += y;
+    }
+  }
+  if (lane == 63) {
+    s_scan[0][wave] = before;
+    s_scan[1][wave] = earlier;
+  }
+  __syncthreads();
+  int64_t line = 0, n_units = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    if (w < wave) {
+      before += s_scan[0][w];
+      earlier += s_scan[1][w];
+    }
+    line += s_scan[0][w];
+    n_units += s_scan[1][w];
+  }
+  before -= own;
+  earlier -= mine;
+  line = uniform(line);
+  const int64_t workers = min((int64_t)gridDim.x, max(line / (2 * kLead), (int64_t)1)), me = blockIdx.x;
+  // entries that no unit (or working workgroup) fills
+  if (tid == 0) {
+    if (!P.by_unit) {
+      P.units[me] = int4{0, 0, 0, 0};
+    } else {
+      for (int64_t i = n_units + me; i < P.slots; i += gridDim.x) P.units[i] = int4{0, 0, 0, 0};
+    }
+  }
+  if (me >= workers) return;
+  const int64_t begin = uniform(me * line / workers), end = uniform((me + 1) * line / workers);
+  if (begin >= end) return;
+  if (before <= begin && begin < before + own) {
+    int b = b0;
+    for (;; ++b) {
+      const Seq s = seq_of(P, b);
+      const int64_t n = P.kv_heads * places<RB>(P, s, s.tiles);
+      if (begin < before + n) break;
+      before += n;
+      earlier += (int64_t)P.kv_heads * s.tiles;
+    }
+    s_seq = b;
+    s_base = before;
+    s_units = (int)earlier;
+  }
+  __syncthreads();
+  int b = uniform(s_seq);
+  int64_t base = uniform(s_base), unit0 = uniform(s_units);
+
+  uint16_t* const s_k = reinterpret_cast<uint16_t*>(lds);
+  uint16_t* const s_v = s_k + C::TK * kD;
+  float* const s_rec = reinterpret_cast<float*>(lds);
+  const int rb = wave / C::TS, ts = wave % C::TS;
+
+  int64_t x = begin;
+  while (x < end) {
+    // ---- the segment at x: sequence, head, row tile, tiles ----
+    Seq s = seq_of(P, b);
+    int64_t each = places<RB>(P, s, s.tiles);          // of a head
+    while (x >= base + each * P.kv_heads) {
+      base += each * P.kv_heads;
+      unit0 += (int64_t)P.kv_heads * s.tiles;
+      s = seq_of(P, ++b);
+      each = places<RB>(P, s, s.tiles);
+    }
+    s.first = uniform(s.first);
+    s.n = uniform(s.n);
+    s.context = uniform(s.context);
+    s.tiles = uniform(s.tiles);
+    const int kvh = uniform((int)((x - base) / each));
+    const int64_t at = x - base - kvh * each;
+    int rt = 0, rt_end = s.tiles;                      // the last row tile whose places begin at or before
+    while (rt_end - rt > 1) {
+      const int mid = (rt + rt_end) / 2;
+      if (places<RB>(P, s, mid) <= at) rt = mid;
+      else rt_end = mid;
+    }
+    rt = uniform(rt);
+    const int64_t start = base + kvh * each + uniform(places<RB>(P, s, rt));
+    const int seen = tokens_of(P, s, rt), all = (seen + C::TK - 1) / C::TK;
+    const int64_t next = min(end, start + kLead + all);
+    const int t0 = max((int)(x - start) - kLead, 0), t1 = (int)(next - start) - kLead;
+    x = next;
+    if (t1 <= t0) continue;                            // only places before its tiles
+    const bool begins = t0 == 0, whole = begins && t1 == all;
+    const int64_t last = ((start + kLead + all) * workers - 1) / line;   // who holds its last place
+
+    const int node0 = rt * P.nodes, M = min(P.nodes, s.n - node0) * P.group;
+    const int row = 32 * rb + lo, node = node0 + row / P.group, head = kvh * P.group + row % P.group;
+    bf16x8 qf[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      u32x4 w{0u, 0u, 0u, 0u};
+      if (row < M) {
+        w = *reinterpret_cast<const u32x4*>(P.q + (int64_t)(s.first + node) * P.qs_row + (int64_t)head * P.qs_head + 16 * i + 8 * half);
+        if (P.negate) w = w ^ 0x80008000u;
+      }
+      qf[i] = __builtin_bit_cast(bf16x8, w);
+    }
+    const uint64_t* const mask = P.words && row < M ? P.mask + (int64_t)(s.first + node) * P.words : P.mask;
+    f32x16 acc[4];
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[d][r] = 0.f;
+    float m = kNegInf, l = 0.f;
+
+#pragma unroll 1
+    for (int t = t0; t < t1; ++t) {
+      const int tok0 = t * C::TK;
+      const bool tail = tok0 + C::TK > s.context;
+      // rows tid / 16, + 16, ..: 16 of them share a page.  Tokens past the end are
+      // redirected to the last one.
+      u32x4 kr[C::LOADS], vr[C::LOADS];
+      bool bad = false;
+#pragma unroll
+      for (int i = 0; i < C::LOADS; ++i) {
+        const int tok = min(tok0 + 16 * i + (tid >> 4), seen - 1);
+        const int first = min(tok0 + 16 * i, seen - 1);
+        int page = P.table[(int64_t)b * P.max_pages + (first >> P.page_shift)];
+        page = min(max(page, 0), P.num_pages - 1);
+        const int slot = tok & ((1 << P.page_shift) - 1);
+        kr[i] = *reinterpret_cast<const u32x4*>(P.k + page * P.ks_page + kvh * P.ks_head + slot * P.ks_tok + 8 * (tid & 15));
+        vr[i] = *reinterpret_cast<const u32x4*>(P.v + page * P.vs_page + kvh * P.vs_head + slot * P.vs_tok + 8 * (tid & 15));
+      }
+      if (tail) {
+#pragma unroll
+        for (int i = 0; i < C::LOADS; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) bad |= not_finite(vr[i][j]);
+      }
+      __syncthreads();     // the tile before (or the record) has been read
+#pragma unroll
+      for (int i = 0; i < C::LOADS; ++i) {
+        *reinterpret_cast<u32x4*>(s_k + k_off(16 * i + (tid >> 4), tid & 15)) = kr[i];
+        *reinterpret_cast<u32x4*>(s_v + v_off(16 * i + (tid >> 4), tid & 15)) = vr[i];
+      }
+      if (__syncthreads_or(bad)) {
+        // Infinities and NaN among the nodes' values: 0 times them is no 0, and a
+        // row that does not see them must not get them.  Rows that do get them
+        // added, then they leave the tile.
+#pragma unroll 1
+        for (int k = 0; k < 32 * C::SUB; ++k) {
+          const int r = ts * 32 * C::SUB + k;
+          if (!(sees(P, mask, node, s.n, tok0 + r - s.context) & 1u) || tok0 + r >= seen) continue;
+#pragma unroll
+          for (int d = 0; d < 4; ++d)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const int dim = 32 * d + 8 * (e >> 2) + 4 * half + (e & 3);
+              const uint32_t w = s_v[v_off(r, dim >> 3) + (dim & 7)];
+              if ((w & 0x7f80u) == 0x7f80u) acc[d][e] += __uint_as_float(w << 16);
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < C::LOADS; ++i) {
+          u32x4 w = vr[i];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            if ((w[j] & 0x7f80u) == 0x7f80u) w[j] &= 0xffff0000u;
+            if ((w[j] & 0x7f800000u) == 0x7f800000u) w[j] &= 0xffffu;
+          }
+          *reinterpret_cast<u32x4*>(s_v + v_off(16 * i + (tid >> 4), tid & 15)) = w;
+        }
+        __syncthreads();
+      }
+
+#pragma unroll
+      for (int sub = 0; sub < C::SUB; ++sub) {
+        const int o = 32 * (ts * C::SUB + sub);
+        f32x16 st;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) st[r] = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const bf16x8 a = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(s_k + k_off(o + lo, 2 * i + half)));
+          st = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[i], st, 0, 0, 0);
+        }
+        // st[r]: token o + 8 (r / 4) + 4 half + r % 4
+        if (tail) {
+          const uint32_t bits = sees(P, mask, node, s.n, tok0 + o - s.context) >> (4 * half);
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if (!(bits >> (8 * (r >> 2) + (r & 3)) & 1u)) st[r] = kNegInf;
+        }
+        float top = st[0];
+#pragma unroll
+        for (int r = 1; r < 16; ++r) top = fmaxf(top, st[r]);
+        top *= P.scale_log2;
+        // The reference m moves only where a score passes it by more than 2^8 (and
+        // at the first score): sums keep their relative precision either way.
+        if (__any(top > m + 8.f)) {
+          float a, c;
+          swap_rows32(top, a, c);
+          const float mn = fmaxf(m, fmaxf(a, c));
+          // (never 0: infinite sums stay so; the first reference finds no others)
+          const float f = m == kNegInf ? 1.f : fast_exp2(fmaxf(m - mn, -126.f));
+          m = mn;
+          l *= f;
+#pragma unroll
+          for (int d = 0; d < 4; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[d][r] *= f;
+        }
+        const float ref = m == kNegInf ? 0.f : m;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          st[r] = fast_exp2(fmaf(st[r], P.scale_log2, -ref));
+          l += st[r];
+        }
+        bf16x8 p[PARTS][2];
+#pragma unroll
+        for (int k = 0; k < PARTS; ++k) {
+          uint32_t w[8];
+#pragma unroll
+          for (int r = 0; r < 8; ++r) {
+            w[r] = pack_bf16(st[2 * r], st[2 * r + 1]);
+            if (k + 1 < PARTS) {
+              st[2 * r] -= bf_lo(w[r]);
+              st[2 * r + 1] -= bf_hi(w[r]);
+            }
+          }
+          p[k][0] = __builtin_bit_cast(bf16x8, u32x4{w[0], w[1], w[2], w[3]});
+          p[k][1] = __builtin_bit_cast(bf16x8, u32x4{w[4], w[5], w[6], w[7]});
+        }
+        // V^T, dims 32 d + lane % 32: element e of K-step i is token o + 16 i + 8 (e / 4)
+        // + 4 half + e % 4.  Of the 16 lanes of a group lane 4 k + h points at
+        // elements 4 h .. 4 h + 3 of the group's 16 dims in row k, and lane j receives
+        // dim j of the four rows.
+        const int k = (lane & 15) >> 2, h = lane & 3, dims = (lane >> 4) & 1;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int d = 0; d < 4; ++d) {
+            v4i16 w[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const int r = o + 16 * i + 8 * e + 4 * half + k;
+              w[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                  (__attribute__((address_space(3))) v4i16*)(s_v + v_off(r, 4 * d + 2 * dims + (h >> 1)) + 4 * (h & 1)));
+            }
+            const bf16x8 a = __builtin_bit_cast(bf16x8, __builtin_shufflevector(w[0], w[1], 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+            for (int j = 0; j < PARTS; ++j) acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, p[j][i], acc[d], 0, 0, 0);
+          }
+      }
+    }
+
+    // ---- the wavefronts' records, joined ----
+    {
+      float a, c;
+      swap_rows32(l, a, c);
+      l = a + c;
+    }
+    __syncthreads();
+    float* const rec = s_rec + wave * 32 * C::PITCH;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        *reinterpret_cast<f32x4*>(rec + lo * C::PITCH + 32 * d + 8 * e + 4 * half) =
+            f32x4{acc[d][4 * e], acc[d][4 * e + 1], acc[d][4 * e + 2], acc[d][4 * e + 3]};
+    if (half == 0) {
+      s_m[wave][lo] = m;
+      s_l[wave][lo] = l;
+    }
+    __syncthreads();
+    float* const to = P.records + (2 * me + (begins ? 1 : 0)) * (C::kRows * (kD + 2));
+    const int64_t row0 = (int64_t)(s.first + node0) * P.q_heads + kvh * P.group;
+    for (int i = tid; i < M * (kD / 4); i += kThreads) {
+      const int r = i / (kD / 4), d = i % (kD / 4) * 4, w0 = r / 32 * C::TS, rr = r % 32;
+      float top = kNegInf;
+#pragma unroll
+      for (int w = 0; w < C::TS; ++w) top = fmaxf(top, s_m[w0 + w][rr]);
+      f32x4 sum{0.f, 0.f, 0.f, 0.f};
+      float mass = 0.f;
+#pragma unroll
+      for (int w = 0; w < C::TS; ++w) {
+        const float f = factor(s_m[w0 + w][rr], top);
+        const f32x4 y = *reinterpret_cast<const f32x4*>(s_rec + (w0 + w) * 32 * C::PITCH + rr * C::PITCH + d);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sum[j] = fmaf(y[j], f, sum[j]);
+        mass = fmaf(s_l[w0 + w][rr], f, mass);
+      }
+      if (whole) {
+        const int64_t at_row = row0 + (int64_t)(r / P.group) * P.q_heads + r % P.group;
+        write4(P, at_row, d, over(sum, mass));
+        if (d == 0) P.lse[at_row] = mass == 0.f ? kNegInf : ln_of(top, mass);
+      } else {
+        *reinterpret_cast<f32x4*>(to + r * kD + d) = sum;
+        if (d == 0) {
+          to[C::kRows * kD + r] = top;
+          to[C::kRows * kD + C::kRows + r] = mass;
+        }
+      }
+    }
+    // what the second launch joins
+    if (begins && tid == 0 && (P.by_unit || !whole))
+      P.units[P.by_unit ? unit0 + (int64_t)kvh * s.tiles + rt : me] =
+          whole ? int4{0, 0, 0, 0} : int4{s.first + node0, kvh << 8 | M, (int)me, (int)last};
+  }
+}
+
+// The second launch: rows of units that lie in several workgroups.  ROWS rows to a
+// workgroup, 32 lanes to a record of one.
+template <int RB, int ROWS>
+__global__ void __launch_bounds__(kThreads) tree_join_kernel(const TreeParams P) {
+  using C = Tree<RB>;
+  constexpr int kGroups = kThreads / 32;
+  __shared__ f32x4 s_o[kGroups][32];
+  __shared__ float s_l[kGroups];
+  const int per = C::kRows / ROWS;
+  const int entry = blockIdx.x / per, r0 = (blockIdx.x - entry * per) * ROWS;
+  const int4 u = P.units[entry];
+  const int M = u.y & 255, kvh = u.y >> 8, first = u.z, n = u.w - u.z + 1;
+  if (r0 >= M) return;
+  const int group = threadIdx.x / 32, lane = threadIdx.x & 31;
+  auto record = [&](int i) {
+    return P.records + (2 * (int64_t)(first + i) + (i == 0 ? 1 : 0)) * (C::kRows * (kD + 2));
+  };
+  const int r = ROWS == 1 ? r0 : r0 + group;
+  const bool live = r < M;
+  float top = kNegInf;
+  for (int i = lane; live && i < n; i += 32) top = fmaxf(top, record(i)[C::kRows * kD + r]);
+#pragma unroll
+  for (int o = 16; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+  f32x4 sum{0.f, 0.f, 0.f, 0.f};
+  float mass = 0.f;
+#pragma unroll 4
+  for (int i = ROWS == 1 ? group : 0; live && i < n; i += ROWS == 1 ? kGroups : 1) {
+    const float* p = record(i);
+    const float f = factor(p[C::kRows * kD + r], top);
+    const f32x4 y = *reinterpret_cast<const f32x4*>(p + r * kD + 4 * lane);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sum[j] = fmaf(y[j], f, sum[j]);
+    mass = fmaf(p[C::kRows * kD + C::kRows + r], f, mass);
+  }
+  if constexpr (ROWS == 1) {
+    s_o[group][lane] = sum;
+    if (lane == 0) s_l[group] = mass;
+    __syncthreads();
+    if (group > 0) return;
+#pragma unroll
+    for (int g = 1; g < kGroups; ++g) {
+      sum = sum + s_o[g][lane];
+      mass += s_l[g];
+    }
+  }
+  if (!live) return;
+  const int64_t row = (int64_t)(u.x + r / P.group) * P.q_heads + kvh * P.group + r % P.group;
+  write4(P, row, 4 * lane, over(sum, mass));
+  if (lane == 0) P.lse[row] = mass == 0.f ? kNegInf : ln_of(top, mass);
+}
+
+// ---- the host side ---------------------------------------------------------------
+
+struct TreePlan {
+  int rb, nodes, workers, slots;
+  size_t records_off, total;
+};
+
+int rows_of(int rb) { return 32 * rb; }
+
+art_status plan_tree(const art_decode_shape* s, const art_tree_opts* o, TreePlan* p) {
+  const art_status st = check_cache(s);
+  if (st != ART_OK) return st;
+  if (!o || o->rows < 0 || o->mask_words < 0 || !isfinite(o->softmax_scale) ||
+      (o->out_dtype != ART_OUT_F32 && o->out_dtype != ART_OUT_BF16) || o->q_stride_row < 0 || o->q_stride_head < 0 ||
+      s->num_q_heads <= 0 || s->num_q_heads % s->num_kv_heads)
+    return ART_ERR_INVALID_ARG;
+  const int g = s->num_q_heads / s->num_kv_heads;
+  const int64_t cap = (int64_t)s->max_pages_per_seq * s->page_size;
+  if (g > 128 || s->num_kv_heads >= (1 << 20) || o->rows >= (1 << 24) || s->batch >= (1 << 20) || cap >= (1ll << 31) - 256 ||
+      (o->q_stride_row | o->q_stride_head) % 8)
+    return ART_ERR_UNSUPPORTED;
+  // a row tile that holds a sequence's rows, on average
+  const int64_t rows = s->batch > 0 ? ((int64_t)o->rows + s->batch - 1) / s->batch * g : 0;
+  p->rb = rows <= 32 && g <= 32 ? 1 : rows <= 64 && g <= 64 ? 2 : 4;
+  p->nodes = rows_of(p->rb) / g;
+  const int tk = p->rb == 1 ? 128 : 64;
+  const int64_t units = (int64_t)s->num_kv_heads * (o->rows / p->nodes + s->batch);   // at most
+  const int64_t tiles = units < kMaxWorkers ? units * ((cap + tk - 1) / tk) : units;
+  p->workers = (int)(tiles < kMaxWorkers ? (tiles < 1 ? 1 : tiles) : kMaxWorkers);
+  p->slots = (int)(units < p->workers ? units : p->workers);
+  if (p->slots < 1) p->slots = 1;
+  p->records_off = ((size_t)p->slots * sizeof(int4) + 255) / 256 * 256;
+  p->total = p->records_off + (size_t)2 * p->workers * rows_of(p->rb) * (kD + 2) * 4;
+  return ART_OK;
+}
+
+template <int RB, int PARTS>
+void launch(const TreePlan& plan, const TreeParams& p, hipStream_t stream) {
+  constexpr int kJoinRows = RB == 4 ? 8 : 1;
+  hipLaunchKernelGGL((tree_kernel<RB, PARTS>), dim3((unsigned)plan.workers), dim3(kThreads), 0, stream, p);
+  hipLaunchKernelGGL((tree_join_kernel<RB, kJoinRows>), dim3((unsigned)(plan.slots * (rows_of(RB) / kJoinRows))),
+                     dim3(kThreads), 0, stream, p);
+}
+template <int RB>
+void launch(const TreePlan& plan, const TreeParams& p, hipStream_t stream) {
+  if (p.out_bf16) launch<RB, 1>(plan, p, stream);
+  else launch<RB, 3>(plan, p, stream);
+}
+
+}  // namespace
+}  // namespace art
+
+extern "C" {
+
+size_t art_tree_workspace_bytes(const art_decode_shape* shape, const art_tree_opts* opts, int32_t* status) {
+  art::TreePlan plan;
+  const art_status st = art::plan_tree(shape, opts, &plan);
+  if (status) *status = st;
+  return st == ART_OK ? plan.total : 0;
+}
+
+art_status art_tree_attention(const art_decode_shape* shape, const art_tree_opts* opts, const void* q,
+                              const void* k_cache, const void* v_cache, const int32_t* page_table,
+                              const int32_t* context_lens, const int32_t* row_offsets, const uint64_t* mask, void* out,
+                              float* lse, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  using namespace art;
+  TreePlan plan;
+  const art_status st = plan_tree(shape, opts, &plan);
+  if (st != ART_OK) return st;
+  if (!row_offsets && shape->batch > 0 && opts->rows % shape->batch) return ART_ERR_INVALID_ARG;
+  if (shape->batch == 0 || opts->rows == 0) return ART_OK;
+  if (!q || !k_cache || !v_cache || !page_table || !context_lens || !out || !lse || (opts->mask_words > 0) != (mask != nullptr) ||
+      (uintptr_t)mask % 8 || (uintptr_t)workspace % 16)
+    return ART_ERR_INVALID_ARG;
+  if (((uintptr_t)q | (uintptr_t)k_cache | (uintptr_t)v_cache | (uintptr_t)out) % 16) return ART_ERR_UNSUPPORTED;
+  if (!workspace || workspace_bytes < plan.total) return ART_ERR_WORKSPACE_TOO_SMALL;
+  TreeParams p;
+  memset(&p, 0, sizeof p);
+  p.batch = shape->batch;
+  p.rows = opts->rows;
+  p.per_seq = opts->rows / shape->batch;
+  p.q_heads = shape->num_q_heads;
+  p.kv_heads = shape->num_kv_heads;
+  p.group = shape->num_q_heads / shape->num_kv_heads;
+  p.nodes = plan.nodes;
+  p.words = opts->mask_words;
+  while ((1 << p.page_shift) < shape->page_size) ++p.page_shift;
+  p.num_pages = shape->num_pages;
+  p.max_pages = shape->max_pages_per_seq;
+  p.slots = plan.slots;
+  p.by_unit = plan.slots < plan.workers;
+  p.out_bf16 = opts->out_dtype == ART_OUT_BF16;
+  p.negate = opts->softmax_scale < 0.f;
+  // (a scale of 0 weighs all tokens alike; hidden scores of -inf times 0 would not be -inf)
+  p.scale_log2 = (float)(fabs((double)opts->softmax_scale) * 1.4426950408889634);
+  if (p.scale_log2 < 1e-37f) p.scale_log2 = 1e-37f;
+  p.qs_row = opts->q_stride_row;
+  p.qs_head = opts->q_stride_head;
+  p.ks_page = shape->k_stride_page;
+  p.ks_head = shape->k_stride_head;
+  p.ks_tok = shape->k_stride_token;
+  p.vs_page = shape->v_stride_page;
+  p.vs_head = shape->v_stride_head;
+  p.vs_tok = shape->v_stride_token;
+  p.offsets = row_offsets;
+  p.context = context_lens;
+  p.table = page_table;
+  p.q = static_cast<const uint16_t*>(q);
+  p.k = static_cast<const uint16_t*>(k_cache);
+  p.v = static_cast<const uint16_t*>(v_cache);
+  p.mask = mask;
+  p.out = out;
+  p.lse = lse;
+  p.units = static_cast<int4*>(workspace);
+  p.records = reinterpret_cast<float*>(static_cast<char*>(workspace) + plan.records_off);
+  if (plan.rb == 1) launch<1>(plan, p, stream);
+  else if (plan.rb == 2) launch<2>(plan, p, stream);
+  else launch<4>(plan, p, stream);
+  return hipGetLastError() == hipSuccess ? ART_OK : ART_ERR_HIP;
+}
+
+}  // extern "C"
