@@ -599,7 +599,8 @@ art_status art_tree_layout(int32_t batch, int32_t rows, const int32_t* parents,
  * which are held in fp32.  With an fp32 output probabilities carry 24 bits, with
  * a bf16 output 8 (as the output itself).
  * Shape fields used: those of art_decode_attention but block_size and the list's;
- * num_q_heads / num_kv_heads is any whole number up to 128.
+ * num_q_heads / num_kv_heads is any whole number up to 128, and token strides are
+ * less than 2^27 elements.
  */
 typedef struct {
     float softmax_scale;

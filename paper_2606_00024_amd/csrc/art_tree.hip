@@ -45,11 +45,13 @@ struct Tree {
   static constexpr int TS = kWaves / RB;            // wavefronts that share a block's tokens
   static constexpr int TK = RB == 1 ? 128 : 64;     // tokens of a tile
   static constexpr int SUB = TK / 32 / TS;          // 32-token pieces of a wavefront
-  static constexpr int LOADS = TK / 16;             // 16-byte pieces of K (and V) a thread loads
+  static constexpr int OWN = TK / kWaves;           // tokens of a tile that a wavefront loads
+  static constexpr int LOADS = OWN / 4;             // its load instructions for K (and for V)
+  static constexpr int BUFS = 2;                    // tiles in LDS
   static constexpr int PITCH = kD + 4;              // floats of a row of a wavefront's record
   static constexpr int TILE_BYTES = 2 * TK * kD * 2;
   static constexpr int REC_BYTES = kWaves * 32 * PITCH * 4;
-  static constexpr int LDS = TILE_BYTES > REC_BYTES ? TILE_BYTES : REC_BYTES;
+  static constexpr int LDS = BUFS * TILE_BYTES > REC_BYTES ? BUFS * TILE_BYTES : REC_BYTES;
 };
 
 struct TreeParams {
@@ -131,11 +133,35 @@ __device__ __forceinline__ int64_t uniform(int64_t x) {
 }
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
-// Offsets (in elements) of a token's 16-byte piece in LDS.  K: the eight rows that
-// are read together lie on distinct banks; V: the four rows that a transposing
-// read takes do.
+// A token's 16-byte piece in LDS: piece j of K lies at place j ^ (r & 7) of row r,
+// so that the eight rows that are read together fall on distinct banks, and of V at
+// j ^ 2 (r & 3), as a transposing read takes four rows.
 __device__ __forceinline__ int k_off(int r, int piece) { return r * kD + ((piece ^ (r & 7)) << 3); }
 __device__ __forceinline__ int v_off(int r, int piece) { return r * kD + ((piece ^ (2 * (r & 3))) << 3); }
+
+// Waits until at most N of the wavefront's loads are on their way.
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  __asm__ __volatile__("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4) << 14 | 7 << 4 | 15 << 8);
+  __asm__ __volatile__("" ::: "memory");
+}
+// (the wavefront's own reads of LDS have then ended: what they read may be overwritten)
+__device__ __forceinline__ void end_reads() {
+  __asm__ __volatile__("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0)
+  __asm__ __volatile__("" ::: "memory");
+}
+__device__ __forceinline__ void barrier() {
+  end_reads();
+  __builtin_amdgcn_s_barrier();
+  __asm__ __volatile__("" ::: "memory");
+}
+// 16 bytes for every lane straight into LDS, lane after lane from `to` on.
+__device__ __forceinline__ void load_lds(const uint8_t* from, uint8_t* to) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
+                                   (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+}
 
 __device__ __forceinline__ bool not_finite(uint32_t w) {
   return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
@@ -260,10 +286,18 @@ __global__ void __launch_bounds__(kThreads, 2) tree_kernel(const TreeParams P) {
   int b = uniform(s_seq);
   int64_t base = uniform(s_base), unit0 = uniform(s_units);
 
-  uint16_t* const s_k = reinterpret_cast<uint16_t*>(lds);
-  uint16_t* const s_v = s_k + C::TK * kD;
   float* const s_rec = reinterpret_cast<float*>(lds);
   const int rb = wave / C::TS, ts = wave % C::TS;
+
+  // Loading.  A wavefront loads tokens OWN wave .. of a tile, four rows an
+  // instruction; lane l fetches the piece of row l / 16 that belongs at place l % 16.
+  // (Its offset within the four rows: K's places depend on whether the instruction's
+  // number is even.)
+  uint32_t k_lane[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    k_lane[i] = (uint32_t)(lane >> 4) * (uint32_t)P.ks_tok * 2 + 16 * ((lane & 15) ^ ((lane >> 4) + 4 * i));
+  const uint32_t v_lane = (uint32_t)(lane >> 4) * (uint32_t)P.vs_tok * 2 + 16 * ((lane & 15) ^ (2 * (lane >> 4)));
 
   int64_t x = begin;
   while (x < end) {
@@ -318,65 +352,108 @@ __global__ void __launch_bounds__(kThreads, 2) tree_kernel(const TreeParams P) {
       for (int r = 0; r < 16; ++r) acc[d][r] = 0.f;
     float m = kNegInf, l = 0.f;
 
+    // Pages: lane i has that of the wavefront's 16-token group i from tile `paged` on,
+    // and of 64 more, asked for that much ahead.
+    constexpr int kGroups = C::OWN / 16, kAhead = 64 / kGroups;   // tiles that 64 lanes serve
+    auto pages_from = [&](int t) {
+      const int tok = min((t + lane / kGroups) * C::TK + wave * C::OWN + 16 * (lane % kGroups), seen - 1);
+      const int page = P.table[(int64_t)b * P.max_pages + (tok >> P.page_shift)];
+      return min(max(page, 0), P.num_pages - 1);
+    };
+    int paged = t0, pages = pages_from(t0), more_pages = t0 + kAhead < t1 ? pages_from(t0 + kAhead) : 0;
+    auto load_tile = [&](int t, int buf) {
+      uint8_t* const to = lds + buf * C::TILE_BYTES + wave * C::OWN * kD * 2;
+      if (t >= paged + kAhead) {
+        paged += kAhead;
+        pages = more_pages;
+        more_pages = paged + kAhead < t1 ? pages_from(paged + kAhead) : 0;
+      }
+      const int tok0 = t * C::TK + wave * C::OWN;
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g) {
+        const int first = tok0 + 16 * g;
+        const int page = __builtin_amdgcn_readlane(pages, (t - paged) * kGroups + g);
+        const uint8_t* const k = reinterpret_cast<const uint8_t*>(P.k + page * P.ks_page + kvh * P.ks_head);
+        const uint8_t* const v = reinterpret_cast<const uint8_t*>(P.v + page * P.vs_page + kvh * P.vs_head);
+        const int slots = (1 << P.page_shift) - 1;
+        if (first + 16 <= seen) {
+          const int slot = first & slots;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            load_lds(k + (slot + 4 * i) * P.ks_tok * 2 + k_lane[i & 1], to + (16 * g + 4 * i) * kD * 2);
+            load_lds(v + (slot + 4 * i) * P.vs_tok * 2 + v_lane, to + C::TK * kD * 2 + (16 * g + 4 * i) * kD * 2);
+          }
+        } else {
+          // tokens past the end are redirected to the last one
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int slot = min(first + 4 * i + (lane >> 4), seen - 1) & slots;
+            load_lds(k + slot * P.ks_tok * 2 + 16 * ((lane & 15) ^ ((lane >> 4) + 4 * (i & 1))), to + (16 * g + 4 * i) * kD * 2);
+            load_lds(v + slot * P.vs_tok * 2 + 16 * ((lane & 15) ^ (2 * (lane >> 4))),
+                     to + C::TK * kD * 2 + (16 * g + 4 * i) * kD * 2);
+          }
+        }
+      }
+    };
+
+    __syncthreads();       // the segment before has left LDS
+    load_tile(t0, t0 & 1);
 #pragma unroll 1
     for (int t = t0; t < t1; ++t) {
       const int tok0 = t * C::TK;
       const bool tail = tok0 + C::TK > s.context;
-      // rows tid / 16, + 16, ..: 16 of them share a page.  Tokens past the end are
-      // redirected to the last one.
-      u32x4 kr[C::LOADS], vr[C::LOADS];
-      bool bad = false;
-#pragma unroll
-      for (int i = 0; i < C::LOADS; ++i) {
-        const int tok = min(tok0 + 16 * i + (tid >> 4), seen - 1);
-        const int first = min(tok0 + 16 * i, seen - 1);
-        int page = P.table[(int64_t)b * P.max_pages + (first >> P.page_shift)];
-        page = min(max(page, 0), P.num_pages - 1);
-        const int slot = tok & ((1 << P.page_shift) - 1);
-        kr[i] = *reinterpret_cast<const u32x4*>(P.k + page * P.ks_page + kvh * P.ks_head + slot * P.ks_tok + 8 * (tid & 15));
-        vr[i] = *reinterpret_cast<const u32x4*>(P.v + page * P.vs_page + kvh * P.vs_head + slot * P.vs_tok + 8 * (tid & 15));
+      uint16_t* const s_k = reinterpret_cast<uint16_t*>(lds + (t & 1) * C::TILE_BYTES);
+      uint16_t* const s_v = s_k + C::TK * kD;
+      if constexpr (C::TS == kWaves) {
+        // a wavefront works on the tokens that it loads itself: no other's are waited for
+        end_reads();
+        if (t + 1 < t1) {
+          load_tile(t + 1, (t + 1) & 1);
+          wait_loads<2 * C::LOADS>();
+        } else {
+          wait_loads<0>();
+        }
+      } else {
+        wait_loads<0>();
+        barrier();         // the tile is there, and the one before it has been read
+        if (t + 1 < t1) load_tile(t + 1, (t + 1) & 1);
       }
       if (tail) {
-#pragma unroll
-        for (int i = 0; i < C::LOADS; ++i)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) bad |= not_finite(vr[i][j]);
-      }
-      __syncthreads();     // the tile before (or the record) has been read
-#pragma unroll
-      for (int i = 0; i < C::LOADS; ++i) {
-        *reinterpret_cast<u32x4*>(s_k + k_off(16 * i + (tid >> 4), tid & 15)) = kr[i];
-        *reinterpret_cast<u32x4*>(s_v + v_off(16 * i + (tid >> 4), tid & 15)) = vr[i];
-      }
-      if (__syncthreads_or(bad)) {
         // Infinities and NaN among the nodes' values: 0 times them is no 0, and a
         // row that does not see them must not get them.  Rows that do get them
         // added, then they leave the tile.
+        bool bad = false;
+        for (int i = tid; i < C::TK * kD / 8; i += kThreads) {
+          const u32x4 w = *reinterpret_cast<const u32x4*>(s_v + 8 * i);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) bad |= not_finite(w[j]);
+        }
+        if (__syncthreads_or(bad)) {
 #pragma unroll 1
-        for (int k = 0; k < 32 * C::SUB; ++k) {
-          const int r = ts * 32 * C::SUB + k;
-          if (!(sees(P, mask, node, s.n, tok0 + r - s.context) & 1u) || tok0 + r >= seen) continue;
+          for (int k = 0; k < 32 * C::SUB; ++k) {
+            const int r = ts * 32 * C::SUB + k;
+            if (!(sees(P, mask, node, s.n, tok0 + r - s.context) & 1u) || tok0 + r >= seen) continue;
 #pragma unroll
-          for (int d = 0; d < 4; ++d)
+            for (int d = 0; d < 4; ++d)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const int dim = 32 * d + 8 * (e >> 2) + 4 * half + (e & 3);
-              const uint32_t w = s_v[v_off(r, dim >> 3) + (dim & 7)];
-              if ((w & 0x7f80u) == 0x7f80u) acc[d][e] += __uint_as_float(w << 16);
-            }
-        }
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < C::LOADS; ++i) {
-          u32x4 w = vr[i];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            if ((w[j] & 0x7f80u) == 0x7f80u) w[j] &= 0xffff0000u;
-            if ((w[j] & 0x7f800000u) == 0x7f800000u) w[j] &= 0xffffu;
+              for (int e = 0; e < 16; ++e) {
+                const int dim = 32 * d + 8 * (e >> 2) + 4 * half + (e & 3);
+                const uint32_t w = s_v[v_off(r, dim >> 3) + (dim & 7)];
+                if ((w & 0x7f80u) == 0x7f80u) acc[d][e] += __uint_as_float(w << 16);
+              }
           }
-          *reinterpret_cast<u32x4*>(s_v + v_off(16 * i + (tid >> 4), tid & 15)) = w;
+          __syncthreads();
+          for (int i = tid; i < C::TK * kD / 8; i += kThreads) {
+            u32x4 w = *reinterpret_cast<const u32x4*>(s_v + 8 * i);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              if ((w[j] & 0x7f80u) == 0x7f80u) w[j] &= 0xffff0000u;
+              if ((w[j] & 0x7f800000u) == 0x7f800000u) w[j] &= 0xffffu;
+            }
+            *reinterpret_cast<u32x4*>(s_v + 8 * i) = w;
+          }
+          __syncthreads();
         }
-        __syncthreads();
       }
 
 #pragma unroll
@@ -585,7 +662,7 @@ art_status plan_tree(const art_decode_shape* s, const art_tree_opts* o, TreePlan
   const int g = s->num_q_heads / s->num_kv_heads;
   const int64_t cap = (int64_t)s->max_pages_per_seq * s->page_size;
   if (g > 128 || s->num_kv_heads >= (1 << 20) || o->rows >= (1 << 24) || s->batch >= (1 << 20) || cap >= (1ll << 31) - 256 ||
-      (o->q_stride_row | o->q_stride_head) % 8)
+      (o->q_stride_row | o->q_stride_head) % 8 || s->k_stride_token >= (1 << 27) || s->v_stride_token >= (1 << 27))
     return ART_ERR_UNSUPPORTED;
   // a row tile that holds a sequence's rows, on average
   const int64_t rows = s->batch > 0 ? ((int64_t)o->rows + s->batch - 1) / s->batch * g : 0;
