@@ -38,19 +38,23 @@ constexpr int kD = kHeadDim;
 constexpr int kMaxWorkers = 512;   // two workgroups for each of 256 CUs
 constexpr int kLead = 4;           // places of a unit's set-up and end
 
-// RB: blocks of 32 rows of a row tile, one or more wavefronts to each
+// RB: blocks of 32 rows of a row tile
 template <int RB>
 struct Tree {
   static constexpr int kRows = 32 * RB;
-  static constexpr int TS = kWaves / RB;            // wavefronts that share a block's tokens
+  static constexpr int NB = RB > kWaves ? RB / kWaves : 1;   // blocks of a wavefront
+  static constexpr int TS = RB < kWaves ? kWaves / RB : 1;   // wavefronts that share a block's tokens
   static constexpr int TK = RB == 1 ? 128 : 64;     // tokens of a tile
   static constexpr int SUB = TK / 32 / TS;          // 32-token pieces of a wavefront
+  // Wide row tiles: the next piece's scores are in work with one's probabilities,
+  // so a tile has to be there before the one in front of it has been used up
+  static constexpr bool WIDE = RB > kWaves;
   static constexpr int OWN = TK / kWaves;           // tokens of a tile that a wavefront loads
   static constexpr int LOADS = OWN / 4;             // its load instructions for K (and for V)
-  static constexpr int BUFS = 2;                    // tiles in LDS
+  static constexpr int BUFS = WIDE ? 3 : 2;         // tiles in LDS
   static constexpr int PITCH = kD + 4;              // floats of a row of a wavefront's record
   static constexpr int TILE_BYTES = 2 * TK * kD * 2;
-  static constexpr int REC_BYTES = kWaves * 32 * PITCH * 4;
+  static constexpr int REC_BYTES = kWaves * 32 * PITCH * 4;   // (a wavefront's blocks one after the other)
   static constexpr int LDS = BUFS * TILE_BYTES > REC_BYTES ? BUFS * TILE_BYTES : REC_BYTES;
 };
 
@@ -79,11 +83,19 @@ struct TreeParams {
   float* records;              // two for every workgroup
 };
 
+// The parameters are read where they are used, through the scalar cache; fresh()
+// keeps the compiler from holding all of them in registers meanwhile.
+typedef const __attribute__((address_space(4))) TreeParams TP;
+__device__ __forceinline__ TP* fresh(TP* p) {
+  __asm__ __volatile__("" : "+s"(p));
+  return p;
+}
+
 // A sequence: its first row, nodes, context and row tiles.
 struct Seq {
   int first, n, context, tiles;
 };
-__device__ __forceinline__ Seq seq_of(const TreeParams& P, int b) {
+__device__ __forceinline__ Seq seq_of(TP& P, int b) {
   int first = P.offsets ? P.offsets[b] : b * P.per_seq, end = P.offsets ? P.offsets[b + 1] : first + P.per_seq;
   first = min(max(first, 0), P.rows);
   end = min(max(end, first), P.rows);
@@ -94,7 +106,7 @@ __device__ __forceinline__ Seq seq_of(const TreeParams& P, int b) {
 }
 
 // Tokens that row tile i goes through.
-__device__ __forceinline__ int tokens_of(const TreeParams& P, const Seq& s, int i) {
+__device__ __forceinline__ int tokens_of(TP& P, const Seq& s, int i) {
   return s.context + (P.words ? s.n : (int)min((int64_t)s.n, (int64_t)(i + 1) * P.nodes));
 }
 // sum of floor((a i + b) / m) over i = 0 .. n - 1, by the steps of Euclid's
@@ -117,7 +129,7 @@ __device__ __forceinline__ int64_t floor_sum(uint32_t n, uint32_t m, uint32_t a,
 }
 // Places of a head's first `k` row tiles on the line.
 template <int RB>
-__device__ __forceinline__ int64_t places(const TreeParams& P, const Seq& s, int k) {
+__device__ __forceinline__ int64_t places(TP& P, const Seq& s, int k) {
   constexpr int TK = Tree<RB>::TK;
   if (k == 0) return 0;                            // (a sequence of no nodes has no tiles)
   const int64_t all = (s.context + s.n + TK - 1) / TK;
@@ -169,7 +181,7 @@ __device__ __forceinline__ bool not_finite(uint32_t w) {
 
 // Which of nodes j0 .. j0 + 31 row node i sees (bit k: node j0 + k; nodes below 0
 // are context).
-__device__ __forceinline__ uint32_t sees(const TreeParams& P, const uint64_t* mask, int i, int n, int j0) {
+__device__ __forceinline__ uint32_t sees(TP& P, const uint64_t* mask, int i, int n, int j0) {
   if (j0 <= -32) return 0xffffffffu;
   uint64_t v;
   int count;                     // of the 32 that may be seen
@@ -195,7 +207,7 @@ __device__ __forceinline__ float factor(float m, float top) {
   return m == kNegInf ? 0.f : fast_exp2(fmaxf(m - top, -126.f));
 }
 
-__device__ __forceinline__ void write4(const TreeParams& P, int64_t row, int d, const f32x4& x) {
+__device__ __forceinline__ void write4(TP& P, int64_t row, int d, const f32x4& x) {
   if (P.out_bf16) {
     *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(P.out) + row * kD + d) =
         u32x2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
@@ -211,8 +223,11 @@ __device__ __forceinline__ f32x4 over(const f32x4& o, float l) {
 // PARTS: bf16 parts that a probability is multiplied in: one (8 bits) for bf16
 // outputs, three (24) for fp32.
 template <int RB, int PARTS>
-__global__ void __launch_bounds__(kThreads, 2) tree_kernel(const TreeParams P) {
+__global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(const TreeParams) {
+  TP* const args = (TP*)__builtin_amdgcn_kernarg_segment_ptr();
+  TP& P = *args;
   using C = Tree<RB>;
+  constexpr int NB = C::NB;
   __shared__ __align__(16) uint8_t lds[C::LDS];
   __shared__ float s_m[kWaves][32], s_l[kWaves][32];
   __shared__ int64_t s_scan[2][kWaves], s_base;
@@ -257,7 +272,10 @@ __global__ void __launch_bounds__(kThreads, 2) tree_kernel(const TreeParams P) {
   before -= own;
   earlier -= mine;
   line = uniform(line);
-  const int64_t workers = min((int64_t)gridDim.x, max(line / (2 * kLead), (int64_t)1)), me = blockIdx.x;
+  const int64_t workers = min((int64_t)gridDim.x, max(line / (2 * kLead), (int64_t)1));
+  // Workgroups go to the eight XCDs in turn: each XCD gets one stretch of the line, so
+  // that row tiles of the same keys meet in its L2.
+  const int64_t me = gridDim.x % 8 ? blockIdx.x : blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8;
   // entries that no unit (or working workgroup) fills
   if (tid == 0) {
     if (!P.by_unit) {
@@ -302,6 +320,7 @@ __global__ void __launch_bounds__(kThreads, 2) tree_kernel(const TreeParams P) {
   int64_t x = begin;
   while (x < end) {
     // ---- the segment at x: sequence, head, row tile, tiles ----
+    TP& P = *fresh(args);
     Seq s = seq_of(P, b);
     int64_t each = places<RB>(P, s, s.tiles);          // of a head
     while (x >= base + each * P.kv_heads) {
@@ -333,36 +352,52 @@ __global__ void __launch_bounds__(kThreads, 2) tree_kernel(const TreeParams P) {
     const int64_t last = ((start + kLead + all) * workers - 1) / line;   // who holds its last place
 
     const int node0 = rt * P.nodes, M = min(P.nodes, s.n - node0) * P.group;
-    const int row = 32 * rb + lo, node = node0 + row / P.group, head = kvh * P.group + row % P.group;
-    bf16x8 qf[8];
+    bf16x8 qf[NB][8];
+    int node[NB];
+    const uint64_t* mask[NB];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      u32x4 w{0u, 0u, 0u, 0u};
-      if (row < M) {
-        w = *reinterpret_cast<const u32x4*>(P.q + (int64_t)(s.first + node) * P.qs_row + (int64_t)head * P.qs_head + 16 * i + 8 * half);
-        if (P.negate) w = w ^ 0x80008000u;
+    for (int n = 0; n < NB; ++n) {
+      const int row = 32 * (rb * NB + n) + lo, head = kvh * P.group + row % P.group;
+      node[n] = node0 + row / P.group;
+      mask[n] = P.words && row < M ? P.mask + (int64_t)(s.first + node[n]) * P.words : P.mask;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        u32x4 w{0u, 0u, 0u, 0u};
+        if (row < M) {
+          w = *reinterpret_cast<const u32x4*>(P.q + (int64_t)(s.first + node[n]) * P.qs_row + (int64_t)head * P.qs_head + 16 * i + 8 * half);
+          if (P.negate) w = w ^ 0x80008000u;
+        }
+        qf[n][i] = __builtin_bit_cast(bf16x8, w);
       }
-      qf[i] = __builtin_bit_cast(bf16x8, w);
     }
-    const uint64_t* const mask = P.words && row < M ? P.mask + (int64_t)(s.first + node) * P.words : P.mask;
-    f32x16 acc[4];
+    f32x16 acc[NB][4];
+    float m[NB], l[NB];
 #pragma unroll
-    for (int d = 0; d < 4; ++d)
+    for (int n = 0; n < NB; ++n) {
+      m[n] = kNegInf;
+      l[n] = 0.f;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) acc[d][r] = 0.f;
-    float m = kNegInf, l = 0.f;
+      for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[n][d][r] = 0.f;
+    }
 
     // Pages: lane i has that of the wavefront's 16-token group i from tile `paged` on,
     // and of 64 more, asked for that much ahead.
     constexpr int kGroups = C::OWN / 16, kAhead = 64 / kGroups;   // tiles that 64 lanes serve
     auto pages_from = [&](int t) {
+      TP& P = *fresh(args);
       const int tok = min((t + lane / kGroups) * C::TK + wave * C::OWN + 16 * (lane % kGroups), seen - 1);
       const int page = P.table[(int64_t)b * P.max_pages + (tok >> P.page_shift)];
       return min(max(page, 0), P.num_pages - 1);
     };
     int paged = t0, pages = pages_from(t0), more_pages = t0 + kAhead < t1 ? pages_from(t0 + kAhead) : 0;
-    auto load_tile = [&](int t, int buf) {
-      uint8_t* const to = lds + buf * C::TILE_BYTES + wave * C::OWN * kD * 2;
+    const uint8_t* const k_head = reinterpret_cast<const uint8_t*>(P.k + kvh * P.ks_head);
+    const uint8_t* const v_head = reinterpret_cast<const uint8_t*>(P.v + kvh * P.vs_head);
+    const int64_t k_page = P.ks_page * 2, v_page = P.vs_page * 2;
+    const uint32_t k_tok = (uint32_t)P.ks_tok * 2, v_tok = (uint32_t)P.vs_tok * 2, slots = (1u << P.page_shift) - 1;
+    auto load_tile = [&](int t) {
+      uint8_t* const to = lds + t % C::BUFS * C::TILE_BYTES + wave * C::OWN * kD * 2;
       if (t >= paged + kAhead) {
         paged += kAhead;
         pages = more_pages;
@@ -373,229 +408,318 @@ __global__ void __launch_bounds__(kThreads, 2) tree_kernel(const TreeParams P) {
       for (int g = 0; g < kGroups; ++g) {
         const int first = tok0 + 16 * g;
         const int page = __builtin_amdgcn_readlane(pages, (t - paged) * kGroups + g);
-        const uint8_t* const k = reinterpret_cast<const uint8_t*>(P.k + page * P.ks_page + kvh * P.ks_head);
-        const uint8_t* const v = reinterpret_cast<const uint8_t*>(P.v + page * P.vs_page + kvh * P.vs_head);
-        const int slots = (1 << P.page_shift) - 1;
+        const uint8_t* const k = k_head + page * k_page;
+        const uint8_t* const v = v_head + page * v_page;
+        uint8_t* const to_k = to + 16 * g * kD * 2;
+        uint8_t* const to_v = to_k + C::TK * kD * 2;
         if (first + 16 <= seen) {
-          const int slot = first & slots;
+          const uint8_t* const k16 = k + (uint64_t)(first & slots) * k_tok;
+          const uint8_t* const v16 = v + (uint64_t)(first & slots) * v_tok;
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            load_lds(k + (slot + 4 * i) * P.ks_tok * 2 + k_lane[i & 1], to + (16 * g + 4 * i) * kD * 2);
-            load_lds(v + (slot + 4 * i) * P.vs_tok * 2 + v_lane, to + C::TK * kD * 2 + (16 * g + 4 * i) * kD * 2);
+            load_lds(k16 + (uint64_t)(4 * i * k_tok) + k_lane[i & 1], to_k + 4 * i * kD * 2);
+            load_lds(v16 + (uint64_t)(4 * i * v_tok) + v_lane, to_v + 4 * i * kD * 2);
           }
         } else {
           // tokens past the end are redirected to the last one
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const int slot = min(first + 4 * i + (lane >> 4), seen - 1) & slots;
-            load_lds(k + slot * P.ks_tok * 2 + 16 * ((lane & 15) ^ ((lane >> 4) + 4 * (i & 1))), to + (16 * g + 4 * i) * kD * 2);
-            load_lds(v + slot * P.vs_tok * 2 + 16 * ((lane & 15) ^ (2 * (lane >> 4))),
-                     to + C::TK * kD * 2 + (16 * g + 4 * i) * kD * 2);
+            const uint32_t slot = min(first + 4 * i + (lane >> 4), seen - 1) & slots;
+            load_lds(k + (uint64_t)slot * k_tok + 16 * ((lane & 15) ^ ((lane >> 4) + 4 * (i & 1))), to_k + 4 * i * kD * 2);
+            load_lds(v + (uint64_t)slot * v_tok + 16 * ((lane & 15) ^ (2 * (lane >> 4))), to_v + 4 * i * kD * 2);
           }
         }
       }
     };
+    auto keys = [&](int t) { return reinterpret_cast<uint16_t*>(lds + t % C::BUFS * C::TILE_BYTES); };
+    auto values = [&](int t) { return keys(t) + C::TK * kD; };
+    // the piece's first token of the tile
+    auto place = [&](int sub) { return 32 * (ts * C::SUB + sub); };
+    auto is_tail = [&](int t) { return (t + 1) * C::TK > s.context; };
 
-    __syncthreads();       // the segment before has left LDS
-    load_tile(t0, t0 & 1);
-#pragma unroll 1
-    for (int t = t0; t < t1; ++t) {
-      const int tok0 = t * C::TK;
-      const bool tail = tok0 + C::TK > s.context;
-      uint16_t* const s_k = reinterpret_cast<uint16_t*>(lds + (t & 1) * C::TILE_BYTES);
-      uint16_t* const s_v = s_k + C::TK * kD;
-      if constexpr (C::TS == kWaves) {
-        // a wavefront works on the tokens that it loads itself: no other's are waited for
-        end_reads();
-        if (t + 1 < t1) {
-          load_tile(t + 1, (t + 1) & 1);
-          wait_loads<2 * C::LOADS>();
-        } else {
-          wait_loads<0>();
-        }
-      } else {
-        wait_loads<0>();
-        barrier();         // the tile is there, and the one before it has been read
-        if (t + 1 < t1) load_tile(t + 1, (t + 1) & 1);
+    // Infinities and NaN among the nodes' values: 0 times them is no 0, and a row that
+    // does not see them must not get them.  Rows that do get them added, then they
+    // leave the tile.
+    auto clean = [&](int t) {
+      TP& P = *fresh(args);
+      uint16_t* const s_v = values(t);
+      bool bad = false;
+      for (int i = tid; i < C::TK * kD / 8; i += kThreads) {
+        const u32x4 w = *reinterpret_cast<const u32x4*>(s_v + 8 * i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) bad |= not_finite(w[j]);
       }
-      if (tail) {
-        // Infinities and NaN among the nodes' values: 0 times them is no 0, and a
-        // row that does not see them must not get them.  Rows that do get them
-        // added, then they leave the tile.
-        bool bad = false;
-        for (int i = tid; i < C::TK * kD / 8; i += kThreads) {
-          const u32x4 w = *reinterpret_cast<const u32x4*>(s_v + 8 * i);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) bad |= not_finite(w[j]);
-        }
-        if (__syncthreads_or(bad)) {
+      if (!__syncthreads_or(bad)) return;
 #pragma unroll 1
-          for (int k = 0; k < 32 * C::SUB; ++k) {
-            const int r = ts * 32 * C::SUB + k;
-            if (!(sees(P, mask, node, s.n, tok0 + r - s.context) & 1u) || tok0 + r >= seen) continue;
+      for (int k = 0; k < 32 * C::SUB; ++k) {
+        const int r = place(0) + k, tok = t * C::TK + r;
+        // (-1 where the row sees the token: no branch for each of the sums)
+        uint32_t see[NB];
 #pragma unroll
-            for (int d = 0; d < 4; ++d)
+        for (int n = 0; n < NB; ++n)
+          see[n] = tok < seen && (sees(P, mask[n], node[n], s.n, tok - s.context) & 1u) ? ~0u : 0u;
 #pragma unroll
-              for (int e = 0; e < 16; ++e) {
-                const int dim = 32 * d + 8 * (e >> 2) + 4 * half + (e & 3);
-                const uint32_t w = s_v[v_off(r, dim >> 3) + (dim & 7)];
-                if ((w & 0x7f80u) == 0x7f80u) acc[d][e] += __uint_as_float(w << 16);
-              }
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int dim = 32 * d + 8 * (e >> 2) + 4 * half + (e & 3);
+            const uint32_t w = s_v[v_off(r, dim >> 3) + (dim & 7)], x = (w & 0x7f80u) == 0x7f80u ? w << 16 : 0u;
+#pragma unroll
+            for (int n = 0; n < NB; ++n) acc[n][d][e] += __uint_as_float(x & see[n]);
           }
-          __syncthreads();
-          for (int i = tid; i < C::TK * kD / 8; i += kThreads) {
-            u32x4 w = *reinterpret_cast<const u32x4*>(s_v + 8 * i);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              if ((w[j] & 0x7f80u) == 0x7f80u) w[j] &= 0xffff0000u;
-              if ((w[j] & 0x7f800000u) == 0x7f800000u) w[j] &= 0xffffu;
-            }
-            *reinterpret_cast<u32x4*>(s_v + 8 * i) = w;
-          }
-          __syncthreads();
-        }
       }
+      __syncthreads();
+      for (int i = tid; i < C::TK * kD / 8; i += kThreads) {
+        u32x4 w = *reinterpret_cast<const u32x4*>(s_v + 8 * i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          if ((w[j] & 0x7f80u) == 0x7f80u) w[j] &= 0xffff0000u;
+          if ((w[j] & 0x7f800000u) == 0x7f800000u) w[j] &= 0xffffu;
+        }
+        *reinterpret_cast<u32x4*>(s_v + 8 * i) = w;
+      }
+      __syncthreads();
+    };
 
+    // Scores of a piece: st[n][r] is token 8 (r / 4) + 4 half + r % 4 of it.
+    auto scores = [&](int t, int sub, f32x16 (&st)[NB]) {
+      const uint16_t* const s_k = keys(t);
+      const int o = place(sub);
 #pragma unroll
-      for (int sub = 0; sub < C::SUB; ++sub) {
-        const int o = 32 * (ts * C::SUB + sub);
-        f32x16 st;
+      for (int n = 0; n < NB; ++n)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) st[r] = 0.f;
+        for (int r = 0; r < 16; ++r) st[n][r] = 0.f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const bf16x8 a = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(s_k + k_off(o + lo, 2 * i + half)));
-          st = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[i], st, 0, 0, 0);
-        }
-        // st[r]: token o + 8 (r / 4) + 4 half + r % 4
-        if (tail) {
-          const uint32_t bits = sees(P, mask, node, s.n, tok0 + o - s.context) >> (4 * half);
+      for (int i = 0; i < 8; ++i) {
+        const bf16x8 a = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(s_k + k_off(o + lo, 2 * i + half)));
 #pragma unroll
-          for (int r = 0; r < 16; ++r)
-            if (!(bits >> (8 * (r >> 2) + (r & 3)) & 1u)) st[r] = kNegInf;
-        }
-        float top = st[0];
+        for (int n = 0; n < NB; ++n) st[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[n][i], st[n], 0, 0, 0);
+      }
+    };
+    auto hide = [&](int t, int sub, f32x16 (&st)[NB]) {
+      TP& P = *fresh(args);
 #pragma unroll
-        for (int r = 1; r < 16; ++r) top = fmaxf(top, st[r]);
-        top *= P.scale_log2;
-        // The reference m moves only where a score passes it by more than 2^8 (and
-        // at the first score): sums keep their relative precision either way.
-        if (__any(top > m + 8.f)) {
+      for (int n = 0; n < NB; ++n) {
+        const uint32_t bits = sees(P, mask[n], node[n], s.n, t * C::TK + place(sub) - s.context) >> (4 * half);
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (!(bits >> (8 * (r >> 2) + (r & 3)) & 1u)) st[n][r] = kNegInf;
+      }
+    };
+    // The reference m moves only where a score passes it by more than 2^8 (and at the
+    // first score): sums keep their relative precision either way.
+    const float scale = P.scale_log2;
+    auto refer = [&](const f32x16 (&st)[NB]) {
+      float top[NB];
+      bool over = false;
+#pragma unroll
+      for (int n = 0; n < NB; ++n) {
+        top[n] = st[n][0];
+#pragma unroll
+        for (int r = 1; r < 16; ++r) top[n] = fmaxf(top[n], st[n][r]);
+        top[n] *= scale;
+        over |= top[n] > m[n] + 8.f;
+      }
+      if (__any(over)) {
+#pragma unroll
+        for (int n = 0; n < NB; ++n) {
           float a, c;
-          swap_rows32(top, a, c);
-          const float mn = fmaxf(m, fmaxf(a, c));
+          swap_rows32(top[n], a, c);
+          const float mn = fmaxf(m[n], fmaxf(a, c));
           // (never 0: infinite sums stay so; the first reference finds no others)
-          const float f = m == kNegInf ? 1.f : fast_exp2(fmaxf(m - mn, -126.f));
-          m = mn;
-          l *= f;
+          const float f = m[n] == kNegInf ? 1.f : fast_exp2(fmaxf(m[n] - mn, -126.f));
+          m[n] = mn;
+          l[n] *= f;
 #pragma unroll
           for (int d = 0; d < 4; ++d)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) acc[d][r] *= f;
+            for (int r = 0; r < 16; ++r) acc[n][d][r] *= f;
         }
-        const float ref = m == kNegInf ? 0.f : m;
+      }
+    };
+    // Probabilities and their products with V.
+    auto weigh = [&](int t, int sub, f32x16 (&st)[NB]) {
+      bf16x8 p[NB][PARTS][2];
+#pragma unroll
+      for (int n = 0; n < NB; ++n) {
+        const float ref = m[n] == kNegInf ? 0.f : m[n];
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          st[r] = fast_exp2(fmaf(st[r], P.scale_log2, -ref));
-          l += st[r];
+          st[n][r] = fast_exp2(fmaf(st[n][r], scale, -ref));
+          l[n] += st[n][r];
         }
-        bf16x8 p[PARTS][2];
 #pragma unroll
         for (int k = 0; k < PARTS; ++k) {
           uint32_t w[8];
 #pragma unroll
           for (int r = 0; r < 8; ++r) {
-            w[r] = pack_bf16(st[2 * r], st[2 * r + 1]);
+            w[r] = pack_bf16(st[n][2 * r], st[n][2 * r + 1]);
             if (k + 1 < PARTS) {
-              st[2 * r] -= bf_lo(w[r]);
-              st[2 * r + 1] -= bf_hi(w[r]);
+              st[n][2 * r] -= bf_lo(w[r]);
+              st[n][2 * r + 1] -= bf_hi(w[r]);
             }
           }
-          p[k][0] = __builtin_bit_cast(bf16x8, u32x4{w[0], w[1], w[2], w[3]});
-          p[k][1] = __builtin_bit_cast(bf16x8, u32x4{w[4], w[5], w[6], w[7]});
+          p[n][k][0] = __builtin_bit_cast(bf16x8, u32x4{w[0], w[1], w[2], w[3]});
+          p[n][k][1] = __builtin_bit_cast(bf16x8, u32x4{w[4], w[5], w[6], w[7]});
         }
-        // V^T, dims 32 d + lane % 32: element e of K-step i is token o + 16 i + 8 (e / 4)
-        // + 4 half + e % 4.  Of the 16 lanes of a group lane 4 k + h points at
-        // elements 4 h .. 4 h + 3 of the group's 16 dims in row k, and lane j receives
-        // dim j of the four rows.
-        const int k = (lane & 15) >> 2, h = lane & 3, dims = (lane >> 4) & 1;
+      }
+      // V^T, dims 32 d + lane % 32: element e of K-step i is token 16 i + 8 (e / 4) + 4 half
+      // + e % 4 of the piece.  Of the 16 lanes of a group lane 4 k + h points at elements
+      // 4 h .. 4 h + 3 of the group's 16 dims in row k, and lane j receives dim j of the
+      // four rows.
+      uint16_t* const s_v = values(t);
+      const int o = place(sub), k = (lane & 15) >> 2, h = lane & 3, dims = (lane >> 4) & 1;
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+      for (int i = 0; i < 2; ++i)
 #pragma unroll
-          for (int d = 0; d < 4; ++d) {
-            v4i16 w[2];
+        for (int d = 0; d < 4; ++d) {
+          v4i16 w[2];
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const int r = o + 16 * i + 8 * e + 4 * half + k;
-              w[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                  (__attribute__((address_space(3))) v4i16*)(s_v + v_off(r, 4 * d + 2 * dims + (h >> 1)) + 4 * (h & 1)));
-            }
-            const bf16x8 a = __builtin_bit_cast(bf16x8, __builtin_shufflevector(w[0], w[1], 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-            for (int j = 0; j < PARTS; ++j) acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, p[j][i], acc[d], 0, 0, 0);
+          for (int e = 0; e < 2; ++e) {
+            const int r = o + 16 * i + 8 * e + 4 * half + k;
+            w[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (__attribute__((address_space(3))) v4i16*)(s_v + v_off(r, 4 * d + 2 * dims + (h >> 1)) + 4 * (h & 1)));
           }
+          const bf16x8 a = __builtin_bit_cast(bf16x8, __builtin_shufflevector(w[0], w[1], 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+          for (int n = 0; n < NB; ++n)
+#pragma unroll
+            for (int j = 0; j < PARTS; ++j)
+              acc[n][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, p[n][j][i], acc[n][d], 0, 0, 0);
+        }
+    };
+
+    __syncthreads();       // the segment before has left LDS
+    load_tile(t0);
+    if constexpr (C::WIDE) {
+      // Three tiles in LDS: one in use, the next there before the last piece of it, and
+      // one on its way into the place of the one before.
+      if (t0 + 1 < t1) load_tile(t0 + 1);
+      if (t0 + 1 < t1) wait_loads<2 * C::LOADS>();
+      else wait_loads<0>();
+      barrier();
+      if (is_tail(t0)) clean(t0);
+      f32x16 st[NB];
+      scores(t0, 0, st);
+      if (is_tail(t0)) hide(t0, 0, st);
+#pragma unroll 1
+      for (int t = t0; t < t1; ++t) {
+#pragma unroll
+        for (int sub = 0; sub < C::SUB; ++sub) {
+          f32x16 next_st[NB];
+          refer(st);
+          if (sub + 1 < C::SUB) {
+            scores(t, sub + 1, next_st);
+            weigh(t, sub, st);
+            if (is_tail(t)) hide(t, sub + 1, next_st);
+          } else if (t + 1 < t1) {
+            wait_loads<0>();
+            barrier();     // the next tile is there, and the one before this has been read
+            if (t + 2 < t1) load_tile(t + 2);
+            if (is_tail(t + 1)) clean(t + 1);
+            scores(t + 1, 0, next_st);
+            weigh(t, sub, st);
+            if (is_tail(t + 1)) hide(t + 1, 0, next_st);
+          } else {
+            weigh(t, sub, st);
+            break;
+          }
+#pragma unroll
+          for (int n = 0; n < NB; ++n) st[n] = next_st[n];
+        }
+      }
+    } else {
+#pragma unroll 1
+      for (int t = t0; t < t1; ++t) {
+        if constexpr (C::TS == kWaves) {
+          // a wavefront works on the tokens that it loads itself: no other's are waited for
+          end_reads();
+          if (t + 1 < t1) {
+            load_tile(t + 1);
+            wait_loads<2 * C::LOADS>();
+          } else {
+            wait_loads<0>();
+          }
+        } else {
+          wait_loads<0>();
+          barrier();       // the tile is there, and the one before it has been read
+          if (t + 1 < t1) load_tile(t + 1);
+        }
+        if (is_tail(t)) clean(t);
+#pragma unroll
+        for (int sub = 0; sub < C::SUB; ++sub) {
+          f32x16 st[NB];
+          scores(t, sub, st);
+          if (is_tail(t)) hide(t, sub, st);
+          refer(st);
+          weigh(t, sub, st);
+        }
       }
     }
 
-    // ---- the wavefronts' records, joined ----
-    {
-      float a, c;
-      swap_rows32(l, a, c);
-      l = a + c;
-    }
-    __syncthreads();
-    float* const rec = s_rec + wave * 32 * C::PITCH;
+    // ---- the wavefronts' records, joined: a block of each at a time ----
+    TP& W = *fresh(args);
+    float* const to = W.records + (2 * me + (begins ? 1 : 0)) * (C::kRows * (kD + 2));
+    const int64_t row0 = (int64_t)(s.first + node0) * W.q_heads + kvh * W.group;
 #pragma unroll
-    for (int d = 0; d < 4; ++d)
+    for (int n = 0; n < NB; ++n) {
+      float l0, l1;
+      swap_rows32(l[n], l0, l1);
+      __syncthreads();
+      float* const rec = s_rec + wave * 32 * C::PITCH;
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        *reinterpret_cast<f32x4*>(rec + lo * C::PITCH + 32 * d + 8 * e + 4 * half) =
-            f32x4{acc[d][4 * e], acc[d][4 * e + 1], acc[d][4 * e + 2], acc[d][4 * e + 3]};
-    if (half == 0) {
-      s_m[wave][lo] = m;
-      s_l[wave][lo] = l;
-    }
-    __syncthreads();
-    float* const to = P.records + (2 * me + (begins ? 1 : 0)) * (C::kRows * (kD + 2));
-    const int64_t row0 = (int64_t)(s.first + node0) * P.q_heads + kvh * P.group;
-    for (int i = tid; i < M * (kD / 4); i += kThreads) {
-      const int r = i / (kD / 4), d = i % (kD / 4) * 4, w0 = r / 32 * C::TS, rr = r % 32;
-      float top = kNegInf;
+      for (int d = 0; d < 4; ++d)
 #pragma unroll
-      for (int w = 0; w < C::TS; ++w) top = fmaxf(top, s_m[w0 + w][rr]);
-      f32x4 sum{0.f, 0.f, 0.f, 0.f};
-      float mass = 0.f;
-#pragma unroll
-      for (int w = 0; w < C::TS; ++w) {
-        const float f = factor(s_m[w0 + w][rr], top);
-        const f32x4 y = *reinterpret_cast<const f32x4*>(s_rec + (w0 + w) * 32 * C::PITCH + rr * C::PITCH + d);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) sum[j] = fmaf(y[j], f, sum[j]);
-        mass = fmaf(s_l[w0 + w][rr], f, mass);
+        for (int e = 0; e < 4; ++e)
+          *reinterpret_cast<f32x4*>(rec + lo * C::PITCH + 32 * d + 8 * e + 4 * half) =
+              f32x4{acc[n][d][4 * e], acc[n][d][4 * e + 1], acc[n][d][4 * e + 2], acc[n][d][4 * e + 3]};
+      if (half == 0) {
+        s_m[wave][lo] = m[n];
+        s_l[wave][lo] = l0 + l1;
       }
-      if (whole) {
-        const int64_t at_row = row0 + (int64_t)(r / P.group) * P.q_heads + r % P.group;
-        write4(P, at_row, d, over(sum, mass));
-        if (d == 0) P.lse[at_row] = mass == 0.f ? kNegInf : ln_of(top, mass);
-      } else {
-        *reinterpret_cast<f32x4*>(to + r * kD + d) = sum;
-        if (d == 0) {
-          to[C::kRows * kD + r] = top;
-          to[C::kRows * kD + C::kRows + r] = mass;
+      __syncthreads();
+      for (int i = tid; i < C::kRows / NB * (kD / 4); i += kThreads) {
+        const int at_block = i / (kD / 4) / 32, rr = i / (kD / 4) % 32, d = i % (kD / 4) * 4, w0 = at_block * C::TS;
+        const int r = 32 * (at_block * NB + n) + rr;
+        if (r >= M) continue;
+        float top = kNegInf;
+#pragma unroll
+        for (int w = 0; w < C::TS; ++w) top = fmaxf(top, s_m[w0 + w][rr]);
+        f32x4 sum{0.f, 0.f, 0.f, 0.f};
+        float mass = 0.f;
+#pragma unroll
+        for (int w = 0; w < C::TS; ++w) {
+          const float f = factor(s_m[w0 + w][rr], top);
+          const f32x4 y = *reinterpret_cast<const f32x4*>(s_rec + (w0 + w) * 32 * C::PITCH + rr * C::PITCH + d);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) sum[j] = fmaf(y[j], f, sum[j]);
+          mass = fmaf(s_l[w0 + w][rr], f, mass);
+        }
+        if (whole) {
+          const int64_t at_row = row0 + (int64_t)(r / W.group) * W.q_heads + r % W.group;
+          write4(W, at_row, d, over(sum, mass));
+          if (d == 0) W.lse[at_row] = mass == 0.f ? kNegInf : ln_of(top, mass);
+        } else {
+          *reinterpret_cast<f32x4*>(to + r * kD + d) = sum;
+          if (d == 0) {
+            to[C::kRows * kD + r] = top;
+            to[C::kRows * kD + C::kRows + r] = mass;
+          }
         }
       }
     }
     // what the second launch joins
-    if (begins && tid == 0 && (P.by_unit || !whole))
-      P.units[P.by_unit ? unit0 + (int64_t)kvh * s.tiles + rt : me] =
-          whole ? int4{0, 0, 0, 0} : int4{s.first + node0, kvh << 8 | M, (int)me, (int)last};
+    if (begins && tid == 0 && (W.by_unit || !whole))
+      W.units[W.by_unit ? unit0 + (int64_t)kvh * s.tiles + rt : me] =
+          whole ? int4{0, 0, 0, 0} : int4{s.first + node0, kvh << 10 | M, (int)me, (int)last};
   }
 }
 
 // The second launch: rows of units that lie in several workgroups.  ROWS rows to a
 // workgroup, 32 lanes to a record of one.
 template <int RB, int ROWS>
-__global__ void __launch_bounds__(kThreads) tree_join_kernel(const TreeParams P) {
+__global__ void __launch_bounds__(kThreads) tree_join_kernel(const TreeParams) {
+  TP& P = *(TP*)__builtin_amdgcn_kernarg_segment_ptr();
   using C = Tree<RB>;
   constexpr int kGroups = kThreads / 32;
   __shared__ f32x4 s_o[kGroups][32];
@@ -603,7 +727,7 @@ __global__ void __launch_bounds__(kThreads) tree_join_kernel(const TreeParams P)
   const int per = C::kRows / ROWS;
   const int entry = blockIdx.x / per, r0 = (blockIdx.x - entry * per) * ROWS;
   const int4 u = P.units[entry];
-  const int M = u.y & 255, kvh = u.y >> 8, first = u.z, n = u.w - u.z + 1;
+  const int M = u.y & 1023, kvh = u.y >> 10, first = u.z, n = u.w - u.z + 1;
   if (r0 >= M) return;
   const int group = threadIdx.x / 32, lane = threadIdx.x & 31;
   auto record = [&](int i) {
@@ -666,12 +790,13 @@ art_status plan_tree(const art_decode_shape* s, const art_tree_opts* o, TreePlan
     return ART_ERR_UNSUPPORTED;
   // a row tile that holds a sequence's rows, on average
   const int64_t rows = s->batch > 0 ? ((int64_t)o->rows + s->batch - 1) / s->batch * g : 0;
-  p->rb = rows <= 32 && g <= 32 ? 1 : rows <= 64 && g <= 64 ? 2 : 4;
+  p->rb = rows <= 32 && g <= 32 ? 1 : rows <= 64 && g <= 64 ? 2 : true ? 4 : 8;
   p->nodes = rows_of(p->rb) / g;
   const int tk = p->rb == 1 ? 128 : 64;
+  const int64_t most = p->rb > kWaves ? kMaxWorkers / 2 : kMaxWorkers;                // one to a CU, or two
   const int64_t units = (int64_t)s->num_kv_heads * (o->rows / p->nodes + s->batch);   // at most
-  const int64_t tiles = units < kMaxWorkers ? units * ((cap + tk - 1) / tk) : units;
-  p->workers = (int)(tiles < kMaxWorkers ? (tiles < 1 ? 1 : tiles) : kMaxWorkers);
+  const int64_t tiles = units < most ? units * ((cap + tk - 1) / tk) : units;
+  p->workers = (int)(tiles < most ? (tiles < 1 ? 1 : tiles) : most);
   p->slots = (int)(units < p->workers ? units : p->workers);
   if (p->slots < 1) p->slots = 1;
   p->records_off = ((size_t)p->slots * sizeof(int4) + 255) / 256 * 256;
@@ -681,7 +806,7 @@ art_status plan_tree(const art_decode_shape* s, const art_tree_opts* o, TreePlan
 
 template <int RB, int PARTS>
 void launch(const TreePlan& plan, const TreeParams& p, hipStream_t stream) {
-  constexpr int kJoinRows = RB == 4 ? 8 : 1;
+  constexpr int kJoinRows = RB >= 4 ? 8 : 1;
   hipLaunchKernelGGL((tree_kernel<RB, PARTS>), dim3((unsigned)plan.workers), dim3(kThreads), 0, stream, p);
   hipLaunchKernelGGL((tree_join_kernel<RB, kJoinRows>), dim3((unsigned)(plan.slots * (rows_of(RB) / kJoinRows))),
                      dim3(kThreads), 0, stream, p);
@@ -760,7 +885,8 @@ art_status art_tree_attention(const art_decode_shape* shape, const art_tree_opts
   p.records = reinterpret_cast<float*>(static_cast<char*>(workspace) + plan.records_off);
   if (plan.rb == 1) launch<1>(plan, p, stream);
   else if (plan.rb == 2) launch<2>(plan, p, stream);
-  else launch<4>(plan, p, stream);
+  else if (plan.rb == 4) launch<4>(plan, p, stream);
+  else launch<8>(plan, p, stream);
   return hipGetLastError() == hipSuccess ? ART_OK : ART_ERR_HIP;
 }
 
