@@ -68,13 +68,21 @@ __global__ void __launch_bounds__(kThreads) layout_kernel(const LayoutParams P) 
 // other, and a chain needs one: at its end.  The first launch walks to the first
 // sum that it needs, in every workgroup of a sequence alike (nothing but gathered
 // probabilities), and each of them adds up one slice of the vocabulary.  The
-// second walks again with that sum in hand, in one workgroup to a sequence, and
-// draws the token; the rare further sums (siblings rejected one after another) are
-// its own.  No workgroup ever waits for another.
+// second, one workgroup to a sequence, goes on with that sum in hand and draws the
+// token; the rare further sums (siblings rejected one after another) are its own.
+// No workgroup ever waits for another.
 
 constexpr int kMaxSlices = 64;
 constexpr int kSumThreads = 256;
 constexpr int kDrawThreads = 1024;
+
+// Where a walk stands.  It is the same in every lane of the wavefront.
+struct Walk {
+  double a, f;                 // with q: a and F; without: f is what is left of 1
+  int now, count, next;        // the current node, nodes accepted, the first one not tried
+  int done;                    // the next token is drawn from the current weights
+  int tried;                   // (without q) the current node's children have been rejected
+};
 
 struct VerifyParams {
   int32_t batch, rows, per_seq, vocab, max_path, slices;
@@ -90,6 +98,7 @@ struct VerifyParams {
   int32_t* counts;
   int32_t* next;
   double* sums;                // [batch][slices]
+  Walk* walks;                 // [batch]: after the first launch
 };
 
 template <int DT>
@@ -107,14 +116,21 @@ struct Nodes {
   int token[ART_MAX_NODES];
 };
 
-template <int DT, int THREADS>
-__device__ __forceinline__ void load_nodes(const VerifyParams& P, int first, int n, Nodes& s) {
+template <int THREADS>
+__device__ __forceinline__ void load_tree(const VerifyParams& P, int first, int n, int* parents, int* tokens) {
   for (int i = threadIdx.x; i < n; i += THREADS) {
     int parent = P.parents[first + i];
     const int x = P.tokens[first + i];
     if (i == 0 || parent < 0 || parent >= i || x < 0 || x >= P.vocab) parent = -1;
-    s.parent[i] = parent;
-    s.token[i] = x;
+    parents[i] = parent;
+    tokens[i] = x;
+  }
+}
+template <int DT, int THREADS>
+__device__ __forceinline__ void load_nodes(const VerifyParams& P, int first, int n, Nodes& s) {
+  load_tree<THREADS>(P, first, n, s.parent, s.token);
+  for (int i = threadIdx.x; i < n; i += THREADS) {   // (each thread those that it has just loaded)
+    const int parent = s.parent[i], x = s.token[i];
     s.u[i] = P.uniforms[first + i];
     s.p[i] = s.q[i] = 0.0;
     if (parent >= 0) {
@@ -123,64 +139,66 @@ __device__ __forceinline__ void load_nodes(const VerifyParams& P, int first, int
     }
   }
   __syncthreads();
-  if (P.draft) return;
-  // the token of an earlier sibling has been rejected when a node is tried
-  for (int i = threadIdx.x; i < n; i += THREADS) {
-    bool again = false;
-    for (int j = 1; j < i; ++j) again |= s.parent[j] == s.parent[i] && s.token[j] == s.token[i];
-    if (again) s.p[i] = 0.0;
-  }
-  __syncthreads();
 }
 
-// Where a walk stands.  It is the same in every lane of the wavefront.
-struct Walk {
-  int now, count, next;        // the current node, nodes accepted, the first one not tried
-  double a, f;                 // with q: a and F; without: f is what is left of 1
-  bool done;                   // the next token is drawn from the current weights
-  bool tried;                  // (without q) the current node's children have been rejected
-};
+// The first child of `now` from node `from` on, or -1.
+__device__ __forceinline__ int next_child(const Nodes& s, int n, int lane, int from, int now) {
+  for (int base = from & ~63; base < n; base += 64) {
+    const int i = base + lane;
+    const uint64_t m = __ballot(i >= from && i < n && s.parent[min(i, n - 1)] == now);
+    if (m) return base + __ffsll((unsigned long long)m) - 1;
+  }
+  return -1;
+}
+// Whether the token of child c is that of an earlier child of `now` (all of them
+// have been rejected).
+__device__ __forceinline__ bool again(const Nodes& s, int c, int lane, int now) {
+  const int x = s.token[c];
+  for (int base = 0; base < c; base += 64) {
+    const int i = min(base + lane, c);
+    if (__any(i < c && s.parent[i] == now && s.token[i] == x)) return true;
+  }
+  return false;
+}
 
-// Goes on until a sum is needed: of the weights with the new a, after a
-// rejection, or of those to draw from (done).
+// Goes on until a sum is needed: of the weights with the new a, after a rejection
+// that leaves other children, or of those to draw from (done).
 __device__ __forceinline__ void walk_on(const VerifyParams& P, const Nodes& s, int n, int lane, int32_t* path, Walk& w) {
   if (w.done) return;
   while (w.count < P.max_path) {
-    int c = -1;
-    for (int base = w.next & ~63; base < n && c < 0; base += 64) {
-      const int i = base + lane;
-      const uint64_t m = __ballot(i >= w.next && i < n && s.parent[min(i, n - 1)] == w.now);
-      if (m) c = base + __ffsll((unsigned long long)m) - 1;
-    }
+    const int c = next_child(s, n, lane, w.next, w.now);
     if (c < 0) {
-      w.tried = true;
+      w.tried = 1;
       break;
     }
     w.next = c + 1;
-    const double px = s.p[c], u = s.u[c];
+    const double u = s.u[c];
+    bool ok;
     if (P.draft) {
-      const double qx = s.q[c], left = px - w.a * qx;
-      if (u * qx * w.f < (left > 0.0 ? left : 0.0)) {
-        if (path && lane == 0) path[w.count] = c;
-        ++w.count;
-        w.now = c;
-        w.a = 0.0;
-        w.f = 1.0;
-      } else {
+      const double qx = s.q[c], left = s.p[c] - w.a * qx;
+      ok = u * qx * w.f < (left > 0.0 ? left : 0.0);
+      if (!ok) {
         w.a += w.f;
-        return;   // F is asked for
+        if (next_child(s, n, lane, w.next, w.now) >= 0) return;   // F is asked for
+        break;
       }
-    } else if (u * w.f < px) {
+    } else {
+      const double px = again(s, c, lane, w.now) ? 0.0 : s.p[c];
+      ok = u * w.f < px;
+      if (!ok) {
+        w.f -= px;
+        if (!(w.f > 0.0)) w.f = 0.0;
+      }
+    }
+    if (ok) {
       if (path && lane == 0) path[w.count] = c;
       ++w.count;
       w.now = c;
+      w.a = 0.0;
       w.f = 1.0;
-    } else {
-      w.f -= px;
-      if (!(w.f > 0.0)) w.f = 0.0;
     }
   }
-  w.done = true;
+  w.done = 1;
 }
 
 __device__ __forceinline__ double wave_sum(double x) {
@@ -189,41 +207,100 @@ __device__ __forceinline__ double wave_sum(double x) {
   return x;
 }
 
-// What a weight is made of: row `now`, a, and the tokens left out (the children
-// of `now`, where they were tried and rejected without q).
+// What a weight is made of: the current node's rows, a, and the tokens left out
+// (its children, where they were tried and rejected without q).
 struct Weights {
-  int64_t p, q;                // element indices of the rows
+  const void* p;
+  const void* q;
   double a;
-  int skip_parent;             // -1: no token is left out
-  int n;                       // nodes
+  const int* out;
+  int n_out;
 };
-
 template <int DT>
-__device__ __forceinline__ double weight(const VerifyParams& P, const Nodes& s, const Weights& w, int v) {
-  const double p = load<DT>(P.target, w.p + v);
-  if (w.a > 0.0) {
-    const double x = p - w.a * (double)load<DT>(P.draft, w.q + v);
-    return x > 0.0 ? x : 0.0;
+__device__ __forceinline__ Weights weights_of(const VerifyParams& P, const Walk& w, int first, const int* out, int n_out) {
+  constexpr int size = DT == ART_ROWS_F32 ? 4 : 2;
+  return Weights{static_cast<const char*>(P.target) + (first + w.now) * P.ts * size,
+                 static_cast<const char*>(P.draft) + (w.a > 0.0 ? (first + w.now) * P.ds * size : 0), w.a, out, w.tried ? n_out : 0};
+}
+// The children of `now` among the nodes: their tokens into `out` (one wavefront).
+__device__ __forceinline__ int left_out(const int* parent, const int* token, int n, int lane, int now, int* out) {
+  int count = 0;
+  for (int base = now + 1; base < n; base += 64) {
+    const int i = base + lane;
+    const bool mine = i < n && parent[min(i, n - 1)] == now;
+    const uint64_t m = __ballot(mine);
+    if (mine) out[count + __popcll(m & ((1ull << lane) - 1))] = token[i];
+    count += __popcll(m);
   }
-  if (w.skip_parent >= 0)
-    for (int i = w.skip_parent + 1; i < w.n; ++i)
-      if (s.parent[i] == w.skip_parent && s.token[i] == v) return 0.0;
-  return p;
+  return count;
 }
 
-__device__ __forceinline__ Weights weights_of(const VerifyParams& P, const Walk& w, int first, int n) {
-  return Weights{(first + w.now) * P.ts, (first + w.now) * P.ds, w.a, !P.draft && w.tried ? w.now : -1, n};
+// Sixteen bytes of a row (at any place that its type may lie at).
+template <int DT>
+constexpr int kSpan = DT == ART_ROWS_F32 ? 4 : 8;
+typedef u32x4 __attribute__((aligned(2))) u32x4_any;
+template <int DT>
+__device__ __forceinline__ u32x4 load16(const void* p, int v) {
+  return *reinterpret_cast<const u32x4_any*>(static_cast<const char*>(p) + (int64_t)v * (16 / kSpan<DT>));
+}
+// The weights of tokens v .. v + span - 1, those from `end` on 0.
+template <int DT>
+__device__ __forceinline__ void weigh(const Weights& w, int v, int end, double (&x)[kSpan<DT>]) {
+  constexpr int N = kSpan<DT>;
+  if (v + N <= end) {
+    const u32x4 p = load16<DT>(w.p, v);
+    u32x4 q{0u, 0u, 0u, 0u};
+    if (w.a > 0.0) q = load16<DT>(w.q, v);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const double y = (double)value<DT>(p, i) - w.a * (double)value<DT>(q, i);
+      x[i] = w.a > 0.0 && !(y > 0.0) ? 0.0 : y;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      x[i] = 0.0;
+      if (v + i < end) {
+        x[i] = load<DT>(w.p, v + i);
+        if (w.a > 0.0) {
+          const double y = x[i] - w.a * (double)load<DT>(w.q, v + i);
+          x[i] = y > 0.0 ? y : 0.0;
+        }
+      }
+    }
+  }
+  for (int j = 0; j < w.n_out; ++j) {
+    const int d = w.out[j] - v;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (d == i) x[i] = 0.0;
+  }
+}
+// A thread's share of the sum over a range: tokens range.x + span (thread + threads i).
+template <int DT>
+__device__ __forceinline__ double sum_of(const Weights& w, int2 range, int thread, int threads) {
+  constexpr int N = kSpan<DT>;
+  double sum = 0.0;
+#pragma unroll 4
+  for (int v = range.x + N * thread; v < range.y; v += N * threads) {
+    double x[N];
+    weigh<DT>(w, v, range.y, x);
+#pragma unroll
+    for (int i = 0; i < N; ++i) sum += x[i];
+  }
+  return sum;
 }
 
 // Slice i of the vocabulary.
 __device__ __forceinline__ int2 slice_of(const VerifyParams& P, int i) {
-  const int each = (P.vocab + P.slices - 1) / P.slices;
+  const int each = ((P.vocab + P.slices - 1) / P.slices + 7) & ~7;
   return make_int2(min(i * each, P.vocab), min((i + 1) * each, P.vocab));
 }
 
 template <int DT>
 __global__ void __launch_bounds__(kSumThreads) sum_kernel(const VerifyParams P) {
   __shared__ Nodes s;
+  __shared__ int s_out[ART_MAX_NODES], s_n_out;
   __shared__ double s_part[kSumThreads / 64];
   const int b = blockIdx.x / P.slices, slice = blockIdx.x - b * P.slices;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -231,13 +308,19 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(const VerifyParams P) 
   const int n = span.y - span.x;
   if (n == 0 || n > ART_MAX_NODES) return;
   load_nodes<DT, kSumThreads>(P, span.x, n, s);
-  Walk w{0, 1, 1, 0.0, 1.0, false, false};
-  walk_on(P, s, n, lane, nullptr, w);
-  const Weights at = weights_of(P, w, span.x, n);
-  const int2 range = slice_of(P, slice);
-  double sum = 0.0;
-  for (int v = range.x + threadIdx.x; v < range.y; v += kSumThreads) sum += weight<DT>(P, s, at, v);
-  sum = wave_sum(sum);
+  // (every wavefront walks; the first one of the first slice writes what is accepted)
+  int32_t* const path = slice == 0 && wave == 0 ? P.accepted + (int64_t)b * P.max_path : nullptr;
+  if (path && lane == 0) path[0] = 0;
+  Walk w{0.0, 1.0, 0, 1, 1, 0, 0};
+  walk_on(P, s, n, lane, path, w);
+  if (path && lane == 0) P.walks[b] = w;
+  if (wave == 0) {
+    const int count = !P.draft && w.tried ? left_out(s.parent, s.token, n, lane, w.now, s_out) : 0;
+    if (lane == 0) s_n_out = count;
+  }
+  __syncthreads();
+  const Weights at = weights_of<DT>(P, w, span.x, s_out, s_n_out);
+  const double sum = wave_sum(sum_of<DT>(at, slice_of(P, slice), threadIdx.x, kSumThreads));
   if (lane == 0) s_part[wave] = sum;
   __syncthreads();
   if (threadIdx.x == 0) {
@@ -247,33 +330,17 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(const VerifyParams P) 
   }
 }
 
-// Sums of the kDrawThreads / 64 equal parts of a range, one to a wavefront.
-template <int DT>
-__device__ __forceinline__ void part_sums(const VerifyParams& P, const Nodes& s, const Weights& at, int2 range, double* parts) {
-  constexpr int kParts = kDrawThreads / 64;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int each = (range.y - range.x + kParts - 1) / kParts;
-  const int end = min(range.x + (wave + 1) * each, range.y);
-  double sum = 0.0;
-  for (int v = range.x + wave * each + lane; v < end; v += 64) sum += weight<DT>(P, s, at, v);
-  sum = wave_sum(sum);
-  __syncthreads();
-  if (lane == 0) parts[wave] = sum;
-  __syncthreads();
-}
-
 template <int DT>
 __global__ void __launch_bounds__(kDrawThreads) draw_kernel(const VerifyParams P) {
-  constexpr int kParts = kDrawThreads / 64;
+  constexpr int kWavesHere = kDrawThreads / 64, N = kSpan<DT>;
   __shared__ Nodes s;
-  __shared__ double s_sums[kMaxSlices];
-  __shared__ double s_part[kParts];
-  const int b = blockIdx.x, lane = threadIdx.x & 63;
+  __shared__ int s_out[ART_MAX_NODES], s_n_out, s_found, s_positive;
+  __shared__ double s_sums[kMaxSlices], s_part[kWavesHere];
+  const int b = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int2 span = rows_of(P, b);
   const int n = span.y - span.x;
   int32_t* const path = P.accepted + (int64_t)b * P.max_path;
-  const bool none = n == 0 || n > ART_MAX_NODES;
-  if (none) {
+  if (n == 0 || n > ART_MAX_NODES) {
     for (int i = threadIdx.x; i < P.max_path; i += kDrawThreads) path[i] = -1;
     if (threadIdx.x == 0) {
       P.counts[b] = 0;
@@ -281,99 +348,109 @@ __global__ void __launch_bounds__(kDrawThreads) draw_kernel(const VerifyParams P
     }
     return;
   }
-  load_nodes<DT, kDrawThreads>(P, span.x, n, s);
-  // (every wavefront walks, the first one writes what is accepted)
-  if (threadIdx.x == 0) path[0] = 0;
-  int32_t* const mine = threadIdx.x < 64 ? path : nullptr;
-  Walk w{0, 1, 1, 0.0, 1.0, false, false};
+  Walk w = P.walks[b];
   const double u = P.last[b];
-  int2 range{0, 0};
+  if (threadIdx.x < P.slices) s_sums[threadIdx.x] = P.sums[(int64_t)b * P.slices + threadIdx.x];
+  if (!w.done) load_nodes<DT, kDrawThreads>(P, span.x, n, s);
+  else if (!P.draft && w.tried) load_tree<kDrawThreads>(P, span.x, n, s.parent, s.token);
   Weights at;
-  // the sums of the slices, from the first launch or, later ones, made here
-  for (int k = 0;; ++k) {
-    walk_on(P, s, n, lane, mine, w);
-    at = weights_of(P, w, span.x, n);
-    if (k == 0) {
-      if (threadIdx.x < P.slices) s_sums[threadIdx.x] = P.sums[(int64_t)b * P.slices + threadIdx.x];
-      __syncthreads();
-    } else {
-      for (int i = 0; i < P.slices; ++i) {
-        part_sums<DT>(P, s, at, slice_of(P, i), s_part);
-        if (threadIdx.x == 0) {
-          double total = 0.0;
-          for (int j = 0; j < kParts; ++j) total += s_part[j];
-          s_sums[i] = total;
-        }
+  double total;
+  for (bool first = true;; first = false) {
+    // (the tokens left out matter to the last weights only: nodes that are not done
+    // have q)
+    __syncthreads();
+    if (wave == 0) {
+      const int count = !P.draft && w.tried ? left_out(s.parent, s.token, n, lane, w.now, s_out) : 0;
+      if (lane == 0) s_n_out = count;
+    }
+    __syncthreads();
+    at = weights_of<DT>(P, w, span.x, s_out, s_n_out);
+    if (!first) {
+      // a sum of this workgroup's own: a slice to a wavefront
+      for (int i = wave; i < P.slices; i += kWavesHere) {
+        const double sum = wave_sum(sum_of<DT>(at, slice_of(P, i), lane, 64));
+        if (lane == 0) s_sums[i] = sum;
       }
       __syncthreads();
     }
-    double total = 0.0;
+    total = 0.0;
     for (int i = 0; i < P.slices; ++i) total += s_sums[i];
-    __syncthreads();
     if (!w.done) {
       w.f = total;
-      continue;
-    }
-    if (!(total > 0.0) && (w.a > 0.0 || at.skip_parent >= 0)) {
+      walk_on(P, s, n, lane, wave == 0 ? path : nullptr, w);
+    } else if (!(total > 0.0) && (w.a > 0.0 || at.n_out > 0)) {
       // nothing is left: from p itself (the walk is over: it changes nothing more)
       w.a = 0.0;
-      w.tried = false;
-      continue;
-    }
-    // the slice that the draw falls into, or the last of positive weight
-    const double want = u * total;
-    double before = 0.0, run = 0.0;
-    int chosen = -1;
-    for (int i = 0; i < P.slices; ++i) {
-      const double x = s_sums[i];
-      if (x > 0.0) {
-        before = run;
-        chosen = i;
-        if (run + x > want) break;
-      }
-      run += x;
-    }
-    if (chosen < 0) {
-      if (threadIdx.x == 0) P.next[b] = 0;
+      w.tried = 0;
+    } else {
       break;
     }
-    range = slice_of(P, chosen);
-    // narrowed to one part after the other, to 64 tokens at most
-    while (range.y - range.x > 64) {
-      part_sums<DT>(P, s, at, range, s_part);
-      const int each = (range.y - range.x + kParts - 1) / kParts;
-      run = before;
-      int part = -1;
-      for (int i = 0; i < kParts; ++i) {
-        const double x = s_part[i];
-        if (x > 0.0) {
-          before = run;
-          part = i;
-          if (run + x > want) break;
-        }
-        run += x;
-      }
-      part = max(part, 0);
-      range = make_int2(range.x + part * each, min(range.x + (part + 1) * each, range.y));
+  }
+  // the slice that the draw falls into, or the last of positive weight
+  const double want = u * total;
+  double before = 0.0, run = 0.0;
+  int chosen = -1;
+  for (int i = 0; i < P.slices; ++i) {
+    const double x = s_sums[i];
+    if (x > 0.0) {
+      before = run;
+      chosen = i;
+      if (run + x > want) break;
     }
-    if (threadIdx.x < 64) {
-      const int v = range.x + lane;
-      const double x = v < range.y ? weight<DT>(P, s, at, v) : 0.0;
-      double sum = x;
+    run += x;
+  }
+  int token = 0;
+  if (chosen >= 0) {
+    // a span to every thread, 1024 spans at a time: the first token whose running sum
+    // passes, or the last positive one
+    const int2 range = slice_of(P, chosen);
+    if (threadIdx.x == 0) {
+      s_found = P.vocab;
+      s_positive = -1;
+    }
+    for (int v0 = range.x; v0 < range.y; v0 += N * kDrawThreads) {
+      const int v = v0 + N * threadIdx.x;
+      double x[N], own = 0.0;
+#pragma unroll
+      for (int i = 0; i < N; ++i) x[i] = 0.0;
+      if (v < range.y) weigh<DT>(at, v, range.y, x);
+#pragma unroll
+      for (int i = 0; i < N; ++i) own += x[i];
+      double sum = own;
 #pragma unroll
       for (int o = 1; o < 64; o <<= 1) {
         const double y = __shfl_up(sum, o);
         if (lane >= o) sum += y;
       }
-      const uint64_t over = __ballot(x > 0.0 && before + sum > want), some = __ballot(x > 0.0);
-      int token = range.x;
-      if (over) token += __ffsll((unsigned long long)over) - 1;
-      else if (some) token += 63 - __clzll((long long)some);
-      if (lane == 0) P.next[b] = min(token, P.vocab - 1);
+      __syncthreads();     // (the parts of the spans before have been read)
+      if (lane == 63) s_part[wave] = sum;
+      __syncthreads();
+      double at_here = before + (sum - own);
+      for (int i = 0; i < kWavesHere; ++i) {
+        if (i < wave) at_here += s_part[i];
+        before += s_part[i];
+      }
+      int found = P.vocab, positive = -1;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        at_here += x[i];
+        if (x[i] > 0.0) {
+          positive = v + i;
+          if (at_here > want && found == P.vocab) found = v + i;
+        }
+      }
+      if (found < P.vocab) atomicMin(&s_found, found);
+      if (positive >= 0) atomicMax(&s_positive, positive);
+      __syncthreads();
+      if (s_found < P.vocab) break;
     }
-    break;
+    __syncthreads();
+    token = s_found < P.vocab ? s_found : max(s_positive, 0);
   }
-  if (threadIdx.x == 0) P.counts[b] = w.count;
+  if (threadIdx.x == 0) {
+    P.next[b] = token;
+    P.counts[b] = w.count;
+  }
   for (int i = w.count + threadIdx.x; i < P.max_path; i += kDrawThreads) path[i] = -1;
 }
 
@@ -495,7 +572,7 @@ size_t art_verify_workspace_bytes(const art_verify_opts* opts, int32_t* status) 
   const art_status st = art::check_verify(opts);
   if (status) *status = st;
   if (st != ART_OK) return 0;
-  const size_t bytes = sizeof(double) * opts->batch * art::slices_of(opts);
+  const size_t bytes = (sizeof(double) * art::slices_of(opts) + sizeof(art::Walk)) * opts->batch;
   return bytes < 256 ? 256 : bytes;
 }
 
@@ -537,6 +614,7 @@ art_status art_verify_drafts(const art_verify_opts* opts, const void* target, co
   p.counts = counts;
   p.next = next_tokens;
   p.sums = static_cast<double*>(workspace);
+  p.walks = reinterpret_cast<Walk*>(p.sums + (int64_t)p.batch * p.slices);
   if (opts->dtype == ART_ROWS_BF16) launch_verify<ART_ROWS_BF16>(p, stream);
   else if (opts->dtype == ART_ROWS_F16) launch_verify<ART_ROWS_F16>(p, stream);
   else launch_verify<ART_ROWS_F32>(p, stream);

@@ -37,6 +37,7 @@ typedef short v4i16 __attribute__((ext_vector_type(4)));
 constexpr int kD = kHeadDim;
 constexpr int kMaxWorkers = 512;   // two workgroups for each of 256 CUs
 constexpr int kLead = 4;           // places of a unit's set-up and end
+constexpr int kLeast = 3;          // places of a workgroup
 
 // RB: blocks of 32 rows of a row tile
 template <int RB>
@@ -103,6 +104,14 @@ __device__ __forceinline__ Seq seq_of(TP& P, int b) {
   if (s.context < 0 || (int64_t)s.context + s.n > (int64_t)P.max_pages << P.page_shift) s.n = 0;
   s.tiles = (s.n + P.nodes - 1) / P.nodes;
   return s;
+}
+
+// The first kSeqs sequences, kept in LDS by the workgroup that has looked them all up.
+constexpr int kSeqs = 256;
+__device__ __forceinline__ Seq seq_of(TP& P, const int4* known, int b) {
+  if (b >= kSeqs) return seq_of(P, b);
+  const int4 s = known[b];
+  return Seq{s.x, s.y, s.z, s.w};
 }
 
 // Tokens that row tile i goes through.
@@ -232,6 +241,7 @@ __global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(con
   __shared__ float s_m[kWaves][32], s_l[kWaves][32];
   __shared__ int64_t s_scan[2][kWaves], s_base;
   __shared__ int s_seq, s_units;
+  __shared__ int4 s_known[kSeqs];
   const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63, lo = lane & 31, half = lane >> 5;
 
   // ---- this workgroup's part of the line ----
@@ -242,6 +252,7 @@ __global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(con
   int64_t own = 0, mine = 0;
   for (int b = b0; b < b1; ++b) {
     const Seq s = seq_of(P, b);
+    if (b < kSeqs) s_known[b] = int4{s.first, s.n, s.context, s.tiles};
     own += P.kv_heads * places<RB>(P, s, s.tiles);
     mine += (int64_t)P.kv_heads * s.tiles;
   }
@@ -272,7 +283,7 @@ __global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(con
   before -= own;
   earlier -= mine;
   line = uniform(line);
-  const int64_t workers = min((int64_t)gridDim.x, max(line / (2 * kLead), (int64_t)1));
+  const int64_t workers = min((int64_t)gridDim.x, max(line / kLeast, (int64_t)1));
   // Workgroups go to the eight XCDs in turn: each XCD gets one stretch of the line, so
   // that row tiles of the same keys meet in its L2.
   const int64_t me = gridDim.x % 8 ? blockIdx.x : blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8;
@@ -290,7 +301,7 @@ __global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(con
   if (before <= begin && begin < before + own) {
     int b = b0;
     for (;; ++b) {
-      const Seq s = seq_of(P, b);
+      const Seq s = seq_of(P, s_known, b);
       const int64_t n = P.kv_heads * places<RB>(P, s, s.tiles);
       if (begin < before + n) break;
       before += n;
@@ -321,12 +332,12 @@ __global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(con
   while (x < end) {
     // ---- the segment at x: sequence, head, row tile, tiles ----
     TP& P = *fresh(args);
-    Seq s = seq_of(P, b);
+    Seq s = seq_of(P, s_known, b);
     int64_t each = places<RB>(P, s, s.tiles);          // of a head
     while (x >= base + each * P.kv_heads) {
       base += each * P.kv_heads;
       unit0 += (int64_t)P.kv_heads * s.tiles;
-      s = seq_of(P, ++b);
+      s = seq_of(P, s_known, ++b);
       each = places<RB>(P, s, s.tiles);
     }
     s.first = uniform(s.first);
@@ -806,10 +817,13 @@ art_status plan_tree(const art_decode_shape* s, const art_tree_opts* o, TreePlan
 
 template <int RB, int PARTS>
 void launch(const TreePlan& plan, const TreeParams& p, hipStream_t stream) {
-  constexpr int kJoinRows = RB >= 4 ? 8 : 1;
   hipLaunchKernelGGL((tree_kernel<RB, PARTS>), dim3((unsigned)plan.workers), dim3(kThreads), 0, stream, p);
-  hipLaunchKernelGGL((tree_join_kernel<RB, kJoinRows>), dim3((unsigned)(plan.slots * (rows_of(RB) / kJoinRows))),
-                     dim3(kThreads), 0, stream, p);
+  // a row to a workgroup where a unit may have a record in each of many workgroups,
+  // else eight
+  if (plan.workers > 32 * plan.slots)
+    hipLaunchKernelGGL((tree_join_kernel<RB, 1>), dim3((unsigned)(plan.slots * rows_of(RB))), dim3(kThreads), 0, stream, p);
+  else
+    hipLaunchKernelGGL((tree_join_kernel<RB, 8>), dim3((unsigned)(plan.slots * (rows_of(RB) / 8))), dim3(kThreads), 0, stream, p);
 }
 template <int RB>
 void launch(const TreePlan& plan, const TreeParams& p, hipStream_t stream) {
