@@ -302,28 +302,26 @@ def quant_read(shape, cache, rows, k, v, k_scale, v_scale, row_offsets, position
 def rope_rows(rope, rows, x_rows, x, out_rows, out, positions, freqs, stream) -> int:
     """Raw call; pointers are ints (0 for NULL).  Returns the status."""
     return int(load().art_rope_rows(
-        ctypes.byref(rope), rows, ctypes.byref(x_rows), x or None, ctypes.byref(out_rows), out or None,
-        positions or None, freqs or None, stream or None))
+        ctypes.byref(rope), rows, ctypes.byref(x_rows), x, ctypes.byref(out_rows), out,
+        positions, freqs, stream))
 
 
 def rope_append(shape, rope, rows, q_rows, q, q_out_rows, q_out, k_rows, k, v_rows, v, row_offsets,
                 context_lens, row_positions, freqs, page_table, k_cache, v_cache, stream) -> int:
     """Raw call; pointers are ints (0 for NULL), rope, q_rows and q_out_rows may
     be None.  Returns the status."""
-    ref = lambda s: None if s is None else ctypes.byref(s)  # noqa: E731
-    return int(load().art_rope_append(
-        ctypes.byref(shape), ref(rope), rows, ref(q_rows), q or None, ref(q_out_rows), q_out or None,
-        ctypes.byref(k_rows), k or None, ctypes.byref(v_rows), v or None, row_offsets or None,
-        context_lens or None, row_positions or None, freqs or None, page_table or None,
-        k_cache or None, v_cache or None, stream or None))
+    # (a structure is passed by reference where a pointer to its type is asked for)
+    return load().art_rope_append(shape, rope, rows, q_rows, q, q_out_rows, q_out, k_rows, k, v_rows, v,
+                                  row_offsets, context_lens, row_positions, freqs, page_table, k_cache,
+                                  v_cache, stream)
 
 
 def tree_layout(batch, rows, parents, row_offsets, context_lens, mask_words, mask, positions,
                 stream) -> int:
     """Raw call; pointers are ints (0 for NULL).  Returns the status."""
-    return int(load().art_tree_layout(batch, rows, parents or None, row_offsets or None,
-                                      context_lens or None, mask_words, mask or None,
-                                      positions or None, stream or None))
+    return int(load().art_tree_layout(batch, rows, parents, row_offsets,
+                                      context_lens, mask_words, mask,
+                                      positions, stream))
 
 
 def tree_workspace_bytes(shape: DecodeShape, opts: TreeOpts) -> int:
@@ -338,9 +336,9 @@ def tree_attention(shape, opts, q, k, v, page_table, context_lens, row_offsets, 
                    workspace, workspace_bytes, stream) -> int:
     """Raw call; pointers are ints (0 for NULL).  Returns the status."""
     return int(load().art_tree_attention(
-        ctypes.byref(shape), ctypes.byref(opts), q or None, k or None, v or None, page_table or None,
-        context_lens or None, row_offsets or None, mask or None, out or None, lse or None,
-        workspace or None, workspace_bytes, stream or None))
+        ctypes.byref(shape), ctypes.byref(opts), q, k, v, page_table,
+        context_lens, row_offsets, mask, out, lse,
+        workspace, workspace_bytes, stream))
 
 
 def verify_workspace_bytes(opts: VerifyOpts) -> int:
@@ -355,17 +353,17 @@ def verify_drafts(opts, target, draft, tokens, parents, row_offsets, uniforms, l
                   accepted, counts, next_tokens, workspace, workspace_bytes, stream) -> int:
     """Raw call; pointers are ints (0 for NULL).  Returns the status."""
     return int(load().art_verify_drafts(
-        ctypes.byref(opts), target or None, draft or None, tokens or None, parents or None,
-        row_offsets or None, uniforms or None, last_uniforms or None, accepted or None, counts or None,
-        next_tokens or None, workspace or None, workspace_bytes, stream or None))
+        ctypes.byref(opts), target, draft, tokens, parents,
+        row_offsets, uniforms, last_uniforms, accepted, counts,
+        next_tokens, workspace, workspace_bytes, stream))
 
 
 def keep_accepted(shape, max_path, accepted, counts, context_lens, page_table, k_cache, v_cache,
                   stream) -> int:
     """Raw call; pointers are ints (0 for NULL).  Returns the status."""
     return int(load().art_keep_accepted(
-        ctypes.byref(shape), max_path, accepted or None, counts or None, context_lens or None,
-        page_table or None, k_cache or None, v_cache or None, stream or None))
+        ctypes.byref(shape), max_path, accepted, counts, context_lens,
+        page_table, k_cache, v_cache, stream))
 
 
 def validate_inputs(shape, opts, page_table, seq_lens, block_list, block_list_len, stream):

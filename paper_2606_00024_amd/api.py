@@ -555,35 +555,37 @@ def _rope_spec(rope: Rope, dev: int) -> _lib.RopeSpec:
 
 def _packed_rows(t: torch.Tensor, name: str, dev: int) -> _lib.Rows:
     """ABI description of rows [rows][heads][head_dim] on GPU ``dev``."""
-    kind = _ROWS_TYPES.get(t.dtype)
-    if kind is None:
-        raise ValueError(f"{name} must be bfloat16, float16 or float32")
-    if t.get_device() != dev or dev < 0:
+    kind, size, stride = _ROWS_TYPES.get(t.dtype), t.shape, t.stride()
+    if kind is None or dev < 0 or t.get_device() != dev or len(size) != 3 or size[2] != 128 or stride[2] != 1:
+        if kind is None:
+            raise ValueError(f"{name} must be bfloat16, float16 or float32")
         _require_cuda(t, name)
-        raise ValueError(f"{name} must be on cuda:{dev}, got {t.device}")
-    if t.dim() != 3 or t.shape[2] != 128 or t.stride(2) != 1:
+        if t.get_device() != dev:
+            raise ValueError(f"{name} must be on cuda:{dev}, got {t.device}")
         raise ValueError(f"{name} must be [rows][heads][128] with a unit head-dim stride")
-    return _lib.Rows(kind, t.shape[1], t.stride(0), t.stride(1))
+    return _lib.Rows(kind, size[1], stride[0], stride[1])
 
 
 def _bf16_pools(k_cache, v_cache, page_table):
     """(device index, heads, batch, shape fields from page_size on) of a bf16
     cache and its table, checked."""
-    dev = k_cache.get_device()
-    for t, name in ((k_cache, "k_cache"), (v_cache, "v_cache")):
-        if t.dtype is not torch.bfloat16 or t.get_device() != dev or dev < 0:
+    dev, pool = k_cache.get_device(), k_cache.shape
+    if (dev < 0 or v_cache.get_device() != dev or k_cache.dtype is not torch.bfloat16
+            or v_cache.dtype is not torch.bfloat16):
+        for t, name in ((k_cache, "k_cache"), (v_cache, "v_cache")):
             _require_cuda(t, name, torch.bfloat16)
-            raise ValueError("the cache's tensors must be on one device")
-    if k_cache.dim() != 4 or v_cache.shape != k_cache.shape:
+        raise ValueError("the cache's tensors must be on one device")
+    if len(pool) != 4 or v_cache.shape != pool:
         raise ValueError("k_cache/v_cache must both be [pages][kv_heads][page_size][head_dim]")
     a, b = k_cache.stride(), v_cache.stride()
     if a[3] != 1 or b[3] != 1:
         raise ValueError("head_dim must be the innermost (unit-stride) dimension")
-    if page_table.dim() != 2:
+    table = page_table.shape
+    if len(table) != 2:
         raise ValueError("page_table must be [batch][max_pages]")
-    B, width = page_table.shape
-    _check(page_table, "page_table", torch.int32, dev, (B, width))
-    P, H, Ps, _ = k_cache.shape
+    B, width = table
+    _check(page_table, "page_table", torch.int32, dev, table)
+    P, H, Ps, _ = pool
     return dev, H, B, (Ps, P, width, 0, 1, a[0], a[1], a[2], b[0], b[1], b[2])
 
 
@@ -626,10 +628,10 @@ def rope_append(k_cache: torch.Tensor, v_cache: torch.Tensor, k: torch.Tensor, v
     no rotation.  ``context_lens`` stays the caller's to advance.
     """
     dev, H, B, fields = _bf16_pools(k_cache, v_cache, page_table)
-    k_rows, v_rows = _packed_rows(k, "k", dev), _packed_rows(v, "v", dev)
-    if k.shape[1] != H or v.shape != k.shape or v.dtype is not k.dtype:
+    k_rows, v_rows, size = _packed_rows(k, "k", dev), _packed_rows(v, "v", dev), k.shape
+    if size[1] != H or v.shape != size or v.dtype is not k.dtype:
         raise ValueError(f"k and v must both be [rows][{H}][128] of one type")
-    rows = k.shape[0]
+    rows = size[0]
     _check(context_lens, "context_lens", torch.int32, dev, (B,))
     if token_offsets is not None:
         _check(token_offsets, "token_offsets", torch.int32, dev, (B + 1,))
@@ -638,14 +640,17 @@ def rope_append(k_cache: torch.Tensor, v_cache: torch.Tensor, k: torch.Tensor, v
     q_rows = out_rows = None
     heads = H
     if q is not None:
-        q_rows, heads = _packed_rows(q, "q", dev), q.shape[1]
-        if q.shape[0] != rows or q.dtype is not k.dtype:
+        q_rows, size = _packed_rows(q, "q", dev), q.shape
+        heads = size[1]
+        if size[0] != rows or q.dtype is not k.dtype:
             raise ValueError("q must have the rows and the type of k")
         if q_out is None:
-            q_out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
-        elif q_out.shape != q.shape or q_out.dtype is not torch.bfloat16:
+            q_out = torch.empty(size, dtype=torch.bfloat16, device=q.device)
+            out_rows = _lib.Rows(_lib.ROWS_BF16, heads, 128 * heads, 128)
+        elif q_out.shape != size or q_out.dtype is not torch.bfloat16:
             raise ValueError("q_out must be bfloat16 of the shape of q")
-        out_rows = _packed_rows(q_out, "q_out", dev)
+        else:
+            out_rows = _packed_rows(q_out, "q_out", dev)
     elif q_out is not None:
         raise ValueError("q_out goes with q")
     spec = None if rope is None else _rope_spec(rope, dev)

@@ -207,6 +207,16 @@ __device__ __forceinline__ double wave_sum(double x) {
   return x;
 }
 
+// Sums of lanes 0 .. lane.
+__device__ __forceinline__ double scan(double x, int lane) {
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const double y = __shfl_up(x, o);
+    if (lane >= o) x += y;
+  }
+  return x;
+}
+
 // What a weight is made of: the current node's rows, a, and the tokens left out
 // (its children, where they were tried and rejected without q).
 struct Weights {
@@ -350,31 +360,35 @@ __global__ void __launch_bounds__(kDrawThreads) draw_kernel(const VerifyParams P
   }
   Walk w = P.walks[b];
   const double u = P.last[b];
-  if (threadIdx.x < P.slices) s_sums[threadIdx.x] = P.sums[(int64_t)b * P.slices + threadIdx.x];
+  // lane i has the sum of slice i
+  double mine = lane < P.slices ? P.sums[(int64_t)b * P.slices + lane] : 0.0;
   if (!w.done) load_nodes<DT, kDrawThreads>(P, span.x, n, s);
   else if (!P.draft && w.tried) load_tree<kDrawThreads>(P, span.x, n, s.parent, s.token);
   Weights at;
-  double total;
+  double upto, total;
   for (bool first = true;; first = false) {
-    // (the tokens left out matter to the last weights only: nodes that are not done
-    // have q)
-    __syncthreads();
-    if (wave == 0) {
-      const int count = !P.draft && w.tried ? left_out(s.parent, s.token, n, lane, w.now, s_out) : 0;
-      if (lane == 0) s_n_out = count;
+    at = weights_of<DT>(P, w, span.x, s_out, 0);
+    if (!P.draft && w.tried) {     // (the last weights only: nodes that are not done have q)
+      __syncthreads();
+      if (wave == 0) {
+        const int count = left_out(s.parent, s.token, n, lane, w.now, s_out);
+        if (lane == 0) s_n_out = count;
+      }
+      __syncthreads();
+      at.n_out = s_n_out;
     }
-    __syncthreads();
-    at = weights_of<DT>(P, w, span.x, s_out, s_n_out);
     if (!first) {
       // a sum of this workgroup's own: a slice to a wavefront
+      __syncthreads();
       for (int i = wave; i < P.slices; i += kWavesHere) {
         const double sum = wave_sum(sum_of<DT>(at, slice_of(P, i), lane, 64));
         if (lane == 0) s_sums[i] = sum;
       }
       __syncthreads();
+      mine = lane < P.slices ? s_sums[lane] : 0.0;
     }
-    total = 0.0;
-    for (int i = 0; i < P.slices; ++i) total += s_sums[i];
+    upto = scan(mine, lane);
+    total = __shfl(upto, 63);
     if (!w.done) {
       w.f = total;
       walk_on(P, s, n, lane, wave == 0 ? path : nullptr, w);
@@ -388,19 +402,11 @@ __global__ void __launch_bounds__(kDrawThreads) draw_kernel(const VerifyParams P
   }
   // the slice that the draw falls into, or the last of positive weight
   const double want = u * total;
-  double before = 0.0, run = 0.0;
-  int chosen = -1;
-  for (int i = 0; i < P.slices; ++i) {
-    const double x = s_sums[i];
-    if (x > 0.0) {
-      before = run;
-      chosen = i;
-      if (run + x > want) break;
-    }
-    run += x;
-  }
+  const uint64_t passed = __ballot(mine > 0.0 && upto > want), some = __ballot(mine > 0.0);
   int token = 0;
-  if (chosen >= 0) {
+  if (some) {
+    const int chosen = passed ? __ffsll((unsigned long long)passed) - 1 : 63 - __clzll((long long)some);
+    double before = __shfl(upto - mine, chosen);
     // a span to every thread, 1024 spans at a time: the first token whose running sum
     // passes, or the last positive one
     const int2 range = slice_of(P, chosen);
@@ -416,20 +422,13 @@ __global__ void __launch_bounds__(kDrawThreads) draw_kernel(const VerifyParams P
       if (v < range.y) weigh<DT>(at, v, range.y, x);
 #pragma unroll
       for (int i = 0; i < N; ++i) own += x[i];
-      double sum = own;
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const double y = __shfl_up(sum, o);
-        if (lane >= o) sum += y;
-      }
+      const double sum = scan(own, lane);
       __syncthreads();     // (the parts of the spans before have been read)
       if (lane == 63) s_part[wave] = sum;
       __syncthreads();
-      double at_here = before + (sum - own);
-      for (int i = 0; i < kWavesHere; ++i) {
-        if (i < wave) at_here += s_part[i];
-        before += s_part[i];
-      }
+      const double part = lane < kWavesHere ? s_part[lane] : 0.0, parts = scan(part, lane);
+      double at_here = before + __shfl(parts - part, wave) + (sum - own);
+      before += __shfl(parts, 63);
       int found = P.vocab, positive = -1;
 #pragma unroll
       for (int i = 0; i < N; ++i) {
@@ -439,8 +438,10 @@ __global__ void __launch_bounds__(kDrawThreads) draw_kernel(const VerifyParams P
           if (at_here > want && found == P.vocab) found = v + i;
         }
       }
-      if (found < P.vocab) atomicMin(&s_found, found);
-      if (positive >= 0) atomicMax(&s_positive, positive);
+      // (tokens grow with the lanes: one lane of each wavefront speaks)
+      const uint64_t f = __ballot(found < P.vocab), g = __ballot(positive >= 0);
+      if (f && lane == __ffsll((unsigned long long)f) - 1) atomicMin(&s_found, found);
+      if (g && lane == 63 - __clzll((long long)g)) atomicMax(&s_positive, positive);
       __syncthreads();
       if (s_found < P.vocab) break;
     }
@@ -525,9 +526,9 @@ art_status check_verify(const art_verify_opts* o) {
   return ART_OK;
 }
 
-// Slices of the vocabulary: about two workgroups a CU, of 2048 tokens at least.
+// Slices of the vocabulary: about four workgroups a CU, of 2048 tokens at least.
 int slices_of(const art_verify_opts* o) {
-  int n = o->batch > 0 ? 512 / o->batch : 1;
+  int n = o->batch > 0 ? 1024 / o->batch : 1;
   const int most = (o->vocab + 2047) / 2048;
   n = n < most ? n : most;
   return n < 1 ? 1 : n > kMaxSlices ? kMaxSlices : n;
