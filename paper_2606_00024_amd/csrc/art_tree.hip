@@ -154,11 +154,13 @@ __device__ __forceinline__ int64_t uniform(int64_t x) {
 }
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
-// A token's 16-byte piece in LDS: piece j of K lies at place j ^ (r & 7) of row r,
-// so that the eight rows that are read together fall on distinct banks, and of V at
-// j ^ 2 (r & 3), as a transposing read takes four rows.
-__device__ __forceinline__ int k_off(int r, int piece) { return r * kD + ((piece ^ (r & 7)) << 3); }
-__device__ __forceinline__ int v_off(int r, int piece) { return r * kD + ((piece ^ (2 * (r & 3))) << 3); }
+// A token's 16-byte piece in LDS: piece j of K lies at place j ^ (r & 15) of row r, so
+// that the sixteen rows whose pieces are read in one cycle fall on distinct banks, and
+// of V at j ^ 4 (r & 3), as the transposing reads of a cycle take four pieces of each
+// of four rows.  (Half of the swizzle, r & 7 and 2 (r & 3), had half of LDS's cycles
+// spent on conflicts.)
+__device__ __forceinline__ int k_off(int r, int piece) { return r * kD + ((piece ^ (r & 15)) << 3); }
+__device__ __forceinline__ int v_off(int r, int piece) { return r * kD + ((piece ^ (4 * (r & 3))) << 3); }
 
 // Waits until at most N of the wavefront's loads are on their way.
 template <int N>
@@ -320,13 +322,13 @@ __global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(con
 
   // Loading.  A wavefront loads tokens OWN wave .. of a tile, four rows an
   // instruction; lane l fetches the piece of row l / 16 that belongs at place l % 16.
-  // (Its offset within the four rows: K's places depend on whether the instruction's
-  // number is even.)
-  uint32_t k_lane[2];
+  // (Its offset within the four rows: K's places depend on which of four the
+  // instruction is.)
+  uint32_t k_lane[4];
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+  for (int i = 0; i < 4; ++i)
     k_lane[i] = (uint32_t)(lane >> 4) * (uint32_t)P.ks_tok * 2 + 16 * ((lane & 15) ^ ((lane >> 4) + 4 * i));
-  const uint32_t v_lane = (uint32_t)(lane >> 4) * (uint32_t)P.vs_tok * 2 + 16 * ((lane & 15) ^ (2 * (lane >> 4)));
+  const uint32_t v_lane = (uint32_t)(lane >> 4) * (uint32_t)P.vs_tok * 2 + 16 * ((lane & 15) ^ (4 * (lane >> 4)));
 
   int64_t x = begin;
   while (x < end) {
@@ -428,7 +430,7 @@ __global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(con
           const uint8_t* const v16 = v + (uint64_t)(first & slots) * v_tok;
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            load_lds(k16 + (uint64_t)(4 * i * k_tok) + k_lane[i & 1], to_k + 4 * i * kD * 2);
+            load_lds(k16 + (uint64_t)(4 * i * k_tok) + k_lane[i], to_k + 4 * i * kD * 2);
             load_lds(v16 + (uint64_t)(4 * i * v_tok) + v_lane, to_v + 4 * i * kD * 2);
           }
         } else {
@@ -436,8 +438,8 @@ __global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(con
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const uint32_t slot = min(first + 4 * i + (lane >> 4), seen - 1) & slots;
-            load_lds(k + (uint64_t)slot * k_tok + 16 * ((lane & 15) ^ ((lane >> 4) + 4 * (i & 1))), to_k + 4 * i * kD * 2);
-            load_lds(v + (uint64_t)slot * v_tok + 16 * ((lane & 15) ^ (2 * (lane >> 4))), to_v + 4 * i * kD * 2);
+            load_lds(k + (uint64_t)slot * k_tok + 16 * ((lane & 15) ^ ((lane >> 4) + 4 * i)), to_k + 4 * i * kD * 2);
+            load_lds(v + (uint64_t)slot * v_tok + 16 * ((lane & 15) ^ (4 * (lane >> 4))), to_v + 4 * i * kD * 2);
           }
         }
       }
