@@ -23,6 +23,8 @@
 #include <stdint.h>
 #include <string.h>
 
+#include <type_traits>
+
 #include "art.h"
 #include "art_internal.h"
 #include "art_rows.h"
@@ -45,14 +47,14 @@ struct Tree {
   static constexpr int kRows = 32 * RB;
   static constexpr int NB = RB > kWaves ? RB / kWaves : 1;   // blocks of a wavefront
   static constexpr int TS = RB < kWaves ? kWaves / RB : 1;   // wavefronts that share a block's tokens
-  static constexpr int TK = RB == 1 ? 128 : 64;     // tokens of a tile
+  // Wide row tiles, which the matrix cores bound: the next tile's scores are in work
+  // with one's probabilities, so it has to be there before that one has been used up
+  static constexpr bool WIDE = RB >= kWaves;
+  static constexpr int TK = RB == 1 ? 128 : WIDE ? 32 : 64;  // tokens of a tile
   static constexpr int SUB = TK / 32 / TS;          // 32-token pieces of a wavefront
-  // Wide row tiles: the next piece's scores are in work with one's probabilities,
-  // so a tile has to be there before the one in front of it has been used up
-  static constexpr bool WIDE = RB > kWaves;
   static constexpr int OWN = TK / kWaves;           // tokens of a tile that a wavefront loads
   static constexpr int LOADS = OWN / 4;             // its load instructions for K (and for V)
-  static constexpr int BUFS = WIDE ? 3 : 2;         // tiles in LDS
+  static constexpr int BUFS = WIDE ? 4 : 2;         // tiles in LDS
   static constexpr int PITCH = kD + 4;              // floats of a row of a wavefront's record
   static constexpr int TILE_BYTES = 2 * TK * kD * 2;
   static constexpr int REC_BYTES = kWaves * 32 * PITCH * 4;   // (a wavefront's blocks one after the other)
@@ -324,11 +326,23 @@ __global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(con
   // instruction; lane l fetches the piece of row l / 16 that belongs at place l % 16.
   // (Its offset within the four rows: K's places depend on which of four the
   // instruction is.)
+  const int k_row = wave * C::OWN % 16;
   uint32_t k_lane[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i)
-    k_lane[i] = (uint32_t)(lane >> 4) * (uint32_t)P.ks_tok * 2 + 16 * ((lane & 15) ^ ((lane >> 4) + 4 * i));
+    k_lane[i] = (uint32_t)(lane >> 4) * (uint32_t)P.ks_tok * 2 + 16 * ((lane & 15) ^ (k_row + (lane >> 4) + 4 * i));
   const uint32_t v_lane = (uint32_t)(lane >> 4) * (uint32_t)P.vs_tok * 2 + 16 * ((lane & 15) ^ (4 * (lane >> 4)));
+
+  // Reading.  K: lane l takes pieces 2 i + l / 32 of row l % 32 of a piece.  V^T, dims
+  // 32 d + lane % 32: element e of K-step i is token 16 i + 8 (e / 4) + 4 half + e % 4.
+  // Of the 16 lanes of a group lane 4 k + h points at elements 4 h .. 4 h + 3 of the
+  // group's 16 dims in row k, and lane j receives dim j of the four rows.
+  uint32_t k_read[8], v_read[4];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) k_read[i] = 2 * k_off(lo, 2 * i + half);
+#pragma unroll
+  for (int d = 0; d < 4; ++d)
+    v_read[d] = 2 * v_off(4 * half + ((lane & 15) >> 2), 4 * d + 2 * (lane >> 4 & 1) + ((lane & 3) >> 1)) + 8 * (lane & 1);
 
   int64_t x = begin;
   while (x < end) {
@@ -356,9 +370,9 @@ __global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(con
     }
     rt = uniform(rt);
     const int64_t start = base + kvh * each + uniform(places<RB>(P, s, rt));
-    const int seen = tokens_of(P, s, rt), all = (seen + C::TK - 1) / C::TK;
+    const int seen = uniform(tokens_of(P, s, rt)), all = (seen + C::TK - 1) / C::TK;
     const int64_t next = min(end, start + kLead + all);
-    const int t0 = max((int)(x - start) - kLead, 0), t1 = (int)(next - start) - kLead;
+    const int t0 = uniform(max((int)(x - start) - kLead, 0)), t1 = uniform((int)(next - start) - kLead);
     x = next;
     if (t1 <= t0) continue;                            // only places before its tiles
     const bool begins = t0 == 0, whole = begins && t1 == all;
@@ -397,10 +411,11 @@ __global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(con
 
     // Pages: lane i has that of the wavefront's 16-token group i from tile `paged` on,
     // and of 64 more, asked for that much ahead.
-    constexpr int kGroups = C::OWN / 16, kAhead = 64 / kGroups;   // tiles that 64 lanes serve
-    auto pages_from = [&](int t) {
+    constexpr int kRows = C::OWN < 16 ? C::OWN : 16;              // of one page
+    constexpr int kGroups = C::OWN / kRows, kAhead = 64 / kGroups;  // tiles that 64 lanes serve
+    auto pages_from = [&](int t) __attribute__((always_inline)) {
       TP& P = *fresh(args);
-      const int tok = min((t + lane / kGroups) * C::TK + wave * C::OWN + 16 * (lane % kGroups), seen - 1);
+      const int tok = min((t + lane / kGroups) * C::TK + wave * C::OWN + kRows * (lane % kGroups), seen - 1);
       const int page = P.table[(int64_t)b * P.max_pages + (tok >> P.page_shift)];
       return min(max(page, 0), P.num_pages - 1);
     };
@@ -409,8 +424,8 @@ __global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(con
     const uint8_t* const v_head = reinterpret_cast<const uint8_t*>(P.v + kvh * P.vs_head);
     const int64_t k_page = P.ks_page * 2, v_page = P.vs_page * 2;
     const uint32_t k_tok = (uint32_t)P.ks_tok * 2, v_tok = (uint32_t)P.vs_tok * 2, slots = (1u << P.page_shift) - 1;
-    auto load_tile = [&](int t) {
-      uint8_t* const to = lds + t % C::BUFS * C::TILE_BYTES + wave * C::OWN * kD * 2;
+    auto load_tile = [&](int t, int buf) __attribute__((always_inline)) {
+      uint8_t* const to = lds + buf * C::TILE_BYTES + wave * C::OWN * kD * 2;
       if (t >= paged + kAhead) {
         paged += kAhead;
         pages = more_pages;
@@ -419,43 +434,42 @@ __global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(con
       const int tok0 = t * C::TK + wave * C::OWN;
 #pragma unroll
       for (int g = 0; g < kGroups; ++g) {
-        const int first = tok0 + 16 * g;
+        const int first = tok0 + kRows * g;
         const int page = __builtin_amdgcn_readlane(pages, (t - paged) * kGroups + g);
         const uint8_t* const k = k_head + page * k_page;
         const uint8_t* const v = v_head + page * v_page;
-        uint8_t* const to_k = to + 16 * g * kD * 2;
+        uint8_t* const to_k = to + kRows * g * kD * 2;
         uint8_t* const to_v = to_k + C::TK * kD * 2;
-        if (first + 16 <= seen) {
+        if (first + kRows <= seen) {
           const uint8_t* const k16 = k + (uint64_t)(first & slots) * k_tok;
           const uint8_t* const v16 = v + (uint64_t)(first & slots) * v_tok;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
+          for (int i = 0; i < kRows / 4; ++i) {
             load_lds(k16 + (uint64_t)(4 * i * k_tok) + k_lane[i], to_k + 4 * i * kD * 2);
             load_lds(v16 + (uint64_t)(4 * i * v_tok) + v_lane, to_v + 4 * i * kD * 2);
           }
         } else {
           // tokens past the end are redirected to the last one
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
+          for (int i = 0; i < kRows / 4; ++i) {
             const uint32_t slot = min(first + 4 * i + (lane >> 4), seen - 1) & slots;
-            load_lds(k + (uint64_t)slot * k_tok + 16 * ((lane & 15) ^ ((lane >> 4) + 4 * i)), to_k + 4 * i * kD * 2);
+            load_lds(k + (uint64_t)slot * k_tok + 16 * ((lane & 15) ^ (k_row + (lane >> 4) + 4 * i)), to_k + 4 * i * kD * 2);
             load_lds(v + (uint64_t)slot * v_tok + 16 * ((lane & 15) ^ (4 * (lane >> 4))), to_v + 4 * i * kD * 2);
           }
         }
       }
     };
-    auto keys = [&](int t) { return reinterpret_cast<uint16_t*>(lds + t % C::BUFS * C::TILE_BYTES); };
-    auto values = [&](int t) { return keys(t) + C::TK * kD; };
     // the piece's first token of the tile
     auto place = [&](int sub) { return 32 * (ts * C::SUB + sub); };
-    auto is_tail = [&](int t) { return (t + 1) * C::TK > s.context; };
+    // Tokens that every row of the tile sees; only behind them are rows told apart.
+    const int open = P.words ? s.context : s.context + node0 + 1;
+    auto is_tail = [&](int t) { return (t + 1) * C::TK > open; };
 
     // Infinities and NaN among the nodes' values: 0 times them is no 0, and a row that
     // does not see them must not get them.  Rows that do get them added, then they
     // leave the tile.
-    auto clean = [&](int t) {
-      TP& P = *fresh(args);
-      uint16_t* const s_v = values(t);
+    auto clean = [&](int t, int buf) __attribute__((always_inline)) {
+      uint16_t* const s_v = reinterpret_cast<uint16_t*>(lds + buf * C::TILE_BYTES) + C::TK * kD;
       bool bad = false;
       for (int i = tid; i < C::TK * kD / 8; i += kThreads) {
         const u32x4 w = *reinterpret_cast<const u32x4*>(s_v + 8 * i);
@@ -494,22 +508,21 @@ __global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(con
       __syncthreads();
     };
 
-    // Scores of a piece: st[n][r] is token 8 (r / 4) + 4 half + r % 4 of it.
-    auto scores = [&](int t, int sub, f32x16 (&st)[NB]) {
-      const uint16_t* const s_k = keys(t);
-      const int o = place(sub);
+    // Scores of a piece: st[n][r] is token 8 (r / 4) + 4 half + r % 4 of it.  (`at`: its
+    // place in LDS, in bytes; where that is a constant, it goes into the reads.)
+    auto scores = [&](int at, f32x16 (&st)[NB]) __attribute__((always_inline)) {
 #pragma unroll
       for (int n = 0; n < NB; ++n)
 #pragma unroll
         for (int r = 0; r < 16; ++r) st[n][r] = 0.f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const bf16x8 a = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(s_k + k_off(o + lo, 2 * i + half)));
+        const bf16x8 a = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(lds + k_read[i] + at));
 #pragma unroll
         for (int n = 0; n < NB; ++n) st[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[n][i], st[n], 0, 0, 0);
       }
     };
-    auto hide = [&](int t, int sub, f32x16 (&st)[NB]) {
+    auto hide = [&](int t, int sub, f32x16 (&st)[NB]) __attribute__((always_inline)) {
       TP& P = *fresh(args);
 #pragma unroll
       for (int n = 0; n < NB; ++n) {
@@ -522,7 +535,7 @@ __global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(con
     // The reference m moves only where a score passes it by more than 2^8 (and at the
     // first score): sums keep their relative precision either way.
     const float scale = P.scale_log2;
-    auto refer = [&](const f32x16 (&st)[NB]) {
+    auto refer = [&](const f32x16 (&st)[NB]) __attribute__((always_inline)) {
       float top[NB];
       bool over = false;
 #pragma unroll
@@ -551,7 +564,7 @@ __global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(con
       }
     };
     // Probabilities and their products with V.
-    auto weigh = [&](int t, int sub, f32x16 (&st)[NB]) {
+    auto weigh = [&](int at, f32x16 (&st)[NB]) __attribute__((always_inline)) {
       bf16x8 p[NB][PARTS][2];
 #pragma unroll
       for (int n = 0; n < NB; ++n) {
@@ -576,12 +589,6 @@ __global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(con
           p[n][k][1] = __builtin_bit_cast(bf16x8, u32x4{w[4], w[5], w[6], w[7]});
         }
       }
-      // V^T, dims 32 d + lane % 32: element e of K-step i is token 16 i + 8 (e / 4) + 4 half
-      // + e % 4 of the piece.  Of the 16 lanes of a group lane 4 k + h points at elements
-      // 4 h .. 4 h + 3 of the group's 16 dims in row k, and lane j receives dim j of the
-      // four rows.
-      uint16_t* const s_v = values(t);
-      const int o = place(sub), k = (lane & 15) >> 2, h = lane & 3, dims = (lane >> 4) & 1;
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -589,9 +596,8 @@ __global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(con
           v4i16 w[2];
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const int r = o + 16 * i + 8 * e + 4 * half + k;
             w[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                (__attribute__((address_space(3))) v4i16*)(s_v + v_off(r, 4 * d + 2 * dims + (h >> 1)) + 4 * (h & 1)));
+                (__attribute__((address_space(3))) v4i16*)(lds + v_read[d] + at + C::TK * kD * 2 + (16 * i + 8 * e) * kD * 2));
           }
           const bf16x8 a = __builtin_bit_cast(bf16x8, __builtin_shufflevector(w[0], w[1], 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
@@ -603,52 +609,70 @@ __global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(con
     };
 
     __syncthreads();       // the segment before has left LDS
-    load_tile(t0);
     if constexpr (C::WIDE) {
-      // Three tiles in LDS: one in use, the next there before the last piece of it, and
-      // one on its way into the place of the one before.
-      if (t0 + 1 < t1) load_tile(t0 + 1);
-      if (t0 + 1 < t1) wait_loads<2 * C::LOADS>();
-      else wait_loads<0>();
-      barrier();
-      if (is_tail(t0)) clean(t0);
-      f32x16 st[NB];
-      scores(t0, 0, st);
-      if (is_tail(t0)) hide(t0, 0, st);
-#pragma unroll 1
-      for (int t = t0; t < t1; ++t) {
+      // Four tiles in LDS: one whose probabilities are in work, the next with its
+      // scores, and two on their way.
+      const int first_tail = max(min(open / C::TK, t1), t0);
 #pragma unroll
-        for (int sub = 0; sub < C::SUB; ++sub) {
+      for (int i = 0; i < 3; ++i)
+        if (t0 + i < t1) load_tile(t0 + i, i);
+      wait_loads<0>();
+      // the next tile is there, and the one before `t` has been used up
+      auto advance = [&](int t, int buf) __attribute__((always_inline)) {
+        if (t + 2 < t1) wait_loads<2 * C::LOADS>();
+        else wait_loads<0>();
+        barrier();
+        if (t + 3 < t1) load_tile(t + 3, buf);
+      };
+      barrier();
+      int t = t0;
+      if (t + 4 < first_tail) {
+        f32x16 st[NB];
+        scores(0, st);
+        // one tile, in buffer B, and the next one's scores
+        auto step = [&](auto B, int t) __attribute__((always_inline)) {
+          constexpr int kB = decltype(B)::value;
           f32x16 next_st[NB];
           refer(st);
-          if (sub + 1 < C::SUB) {
-            scores(t, sub + 1, next_st);
-            weigh(t, sub, st);
-            if (is_tail(t)) hide(t, sub + 1, next_st);
-          } else if (t + 1 < t1) {
-            wait_loads<0>();
-            barrier();     // the next tile is there, and the one before this has been read
-            if (t + 2 < t1) load_tile(t + 2);
-            if (is_tail(t + 1)) clean(t + 1);
-            scores(t + 1, 0, next_st);
-            weigh(t, sub, st);
-            if (is_tail(t + 1)) hide(t + 1, 0, next_st);
-          } else {
-            weigh(t, sub, st);
-            break;
-          }
+          advance(t, (kB + 3) % 4);
+          scores((kB + 1) % 4 * C::TILE_BYTES, next_st);
+          weigh(kB * C::TILE_BYTES, st);
 #pragma unroll
           for (int n = 0; n < NB; ++n) st[n] = next_st[n];
+        };
+#pragma unroll 1
+        for (; t + 4 < first_tail; t += 4) {
+          step(std::integral_constant<int, 0>{}, t);
+          step(std::integral_constant<int, 1>{}, t + 1);
+          step(std::integral_constant<int, 2>{}, t + 2);
+          step(std::integral_constant<int, 3>{}, t + 3);
         }
+        refer(st);
+        weigh(0, st);
+        advance(t, 3);
+        ++t;
+      }
+#pragma unroll 1
+      for (; t < t1; ++t) {
+        const int buf = (t - t0) & 3;
+        const bool tail = t >= first_tail;
+        if (tail) clean(t, buf);
+        f32x16 st[NB];
+        scores(buf * C::TILE_BYTES, st);
+        if (tail) hide(t, 0, st);
+        refer(st);
+        weigh(buf * C::TILE_BYTES, st);
+        if (t + 1 < t1) advance(t, (buf + 3) & 3);
       }
     } else {
+      load_tile(t0, t0 & 1);
 #pragma unroll 1
       for (int t = t0; t < t1; ++t) {
         if constexpr (C::TS == kWaves) {
           // a wavefront works on the tokens that it loads itself: no other's are waited for
           end_reads();
           if (t + 1 < t1) {
-            load_tile(t + 1);
+            load_tile(t + 1, (t + 1) & 1);
             wait_loads<2 * C::LOADS>();
           } else {
             wait_loads<0>();
@@ -656,16 +680,17 @@ __global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(con
         } else {
           wait_loads<0>();
           barrier();       // the tile is there, and the one before it has been read
-          if (t + 1 < t1) load_tile(t + 1);
+          if (t + 1 < t1) load_tile(t + 1, (t + 1) & 1);
         }
-        if (is_tail(t)) clean(t);
+        if (is_tail(t)) clean(t, t & 1);
 #pragma unroll
         for (int sub = 0; sub < C::SUB; ++sub) {
+          const int at = (t & 1) * C::TILE_BYTES + place(sub) * kD * 2;
           f32x16 st[NB];
-          scores(t, sub, st);
+          scores(at, st);
           if (is_tail(t)) hide(t, sub, st);
           refer(st);
-          weigh(t, sub, st);
+          weigh(at, st);
         }
       }
     }
@@ -805,7 +830,7 @@ art_status plan_tree(const art_decode_shape* s, const art_tree_opts* o, TreePlan
   const int64_t rows = s->batch > 0 ? ((int64_t)o->rows + s->batch - 1) / s->batch * g : 0;
   p->rb = rows <= 32 && g <= 32 ? 1 : rows <= 64 && g <= 64 ? 2 : true ? 4 : 8;
   p->nodes = rows_of(p->rb) / g;
-  const int tk = p->rb == 1 ? 128 : 64;
+  const int tk = p->rb == 1 ? 128 : p->rb == 2 ? 64 : 32;
   const int64_t most = p->rb > kWaves ? kMaxWorkers / 2 : kMaxWorkers;                // one to a CU, or two
   const int64_t units = (int64_t)s->num_kv_heads * (o->rows / p->nodes + s->batch);   // at most
   const int64_t tiles = units < most ? units * ((cap + tk - 1) / tk) : units;
