@@ -344,8 +344,22 @@ __global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(con
   for (int d = 0; d < 4; ++d)
     v_read[d] = 2 * v_off(4 * half + ((lane & 15) >> 2), 4 * d + 2 * (lane >> 4 & 1) + ((lane & 3) >> 1)) + 8 * (lane & 1);
 
+  // Where a part of the line begins inside a unit and goes on behind it, that rest of
+  // a unit comes last: workgroups of wide row tiles then begin whole units together,
+  // and go through the same keys at the same time, in the L2 of their XCD.
+  const int first_b = b;
+  const int64_t first_base = base, first_unit0 = unit0;
+  bool put_off = false, rest = false;
   int64_t x = begin;
-  while (x < end) {
+  while (x < end || put_off) {
+    if (x >= end) {
+      x = begin;
+      b = first_b;
+      base = first_base;
+      unit0 = first_unit0;
+      put_off = false;
+      rest = true;
+    }
     // ---- the segment at x: sequence, head, row tile, tiles ----
     TP& P = *fresh(args);
     Seq s = seq_of(P, s_known, b);
@@ -373,7 +387,12 @@ __global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(con
     const int seen = uniform(tokens_of(P, s, rt)), all = (seen + C::TK - 1) / C::TK;
     const int64_t next = min(end, start + kLead + all);
     const int t0 = uniform(max((int)(x - start) - kLead, 0)), t1 = uniform((int)(next - start) - kLead);
-    x = next;
+    if (C::WIDE && !rest && x == begin && start < begin && next < end) {
+      put_off = true;
+      x = next;
+      continue;
+    }
+    x = rest ? end : next;
     if (t1 <= t0) continue;                            // only places before its tiles
     const bool begins = t0 == 0, whole = begins && t1 == all;
     const int64_t last = ((start + kLead + all) * workers - 1) / line;   // who holds its last place
