@@ -443,32 +443,37 @@ __global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(con
     const uint8_t* const v_head = reinterpret_cast<const uint8_t*>(P.v + kvh * P.vs_head);
     const int64_t k_page = P.ks_page * 2, v_page = P.vs_page * 2;
     const uint32_t k_tok = (uint32_t)P.ks_tok * 2, v_tok = (uint32_t)P.vs_tok * 2, slots = (1u << P.page_shift) - 1;
+    // kRows rows, all of them before the end
+    auto load_rows = [&](int first, int page, uint8_t* to_k) __attribute__((always_inline)) {
+      const uint8_t* const k16 = k_head + page * k_page + (uint64_t)(first & slots) * k_tok;
+      const uint8_t* const v16 = v_head + page * v_page + (uint64_t)(first & slots) * v_tok;
+#pragma unroll
+      for (int i = 0; i < kRows / 4; ++i) {
+        load_lds(k16 + (uint64_t)(4 * i * k_tok) + k_lane[i], to_k + 4 * i * kD * 2);
+        load_lds(v16 + (uint64_t)(4 * i * v_tok) + v_lane, to_k + C::TK * kD * 2 + 4 * i * kD * 2);
+      }
+    };
+    auto next_pages = [&]() __attribute__((always_inline)) {
+      paged += kAhead;
+      pages = more_pages;
+      more_pages = paged + kAhead < t1 ? pages_from(paged + kAhead) : 0;
+    };
     auto load_tile = [&](int t, int buf) __attribute__((always_inline)) {
       uint8_t* const to = lds + buf * C::TILE_BYTES + wave * C::OWN * kD * 2;
-      if (t >= paged + kAhead) {
-        paged += kAhead;
-        pages = more_pages;
-        more_pages = paged + kAhead < t1 ? pages_from(paged + kAhead) : 0;
-      }
+      if (t >= paged + kAhead) next_pages();
       const int tok0 = t * C::TK + wave * C::OWN;
 #pragma unroll
       for (int g = 0; g < kGroups; ++g) {
         const int first = tok0 + kRows * g;
         const int page = __builtin_amdgcn_readlane(pages, (t - paged) * kGroups + g);
-        const uint8_t* const k = k_head + page * k_page;
-        const uint8_t* const v = v_head + page * v_page;
         uint8_t* const to_k = to + kRows * g * kD * 2;
         uint8_t* const to_v = to_k + C::TK * kD * 2;
         if (first + kRows <= seen) {
-          const uint8_t* const k16 = k + (uint64_t)(first & slots) * k_tok;
-          const uint8_t* const v16 = v + (uint64_t)(first & slots) * v_tok;
-#pragma unroll
-          for (int i = 0; i < kRows / 4; ++i) {
-            load_lds(k16 + (uint64_t)(4 * i * k_tok) + k_lane[i], to_k + 4 * i * kD * 2);
-            load_lds(v16 + (uint64_t)(4 * i * v_tok) + v_lane, to_v + 4 * i * kD * 2);
-          }
+          load_rows(first, page, to_k);
         } else {
           // tokens past the end are redirected to the last one
+          const uint8_t* const k = k_head + page * k_page;
+          const uint8_t* const v = v_head + page * v_page;
 #pragma unroll
           for (int i = 0; i < kRows / 4; ++i) {
             const uint32_t slot = min(first + 4 * i + (lane >> 4), seen - 1) & slots;
@@ -527,6 +532,18 @@ __global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(con
       __syncthreads();
     };
 
+    // The A operands: K-step i of a piece's keys; K-step i and dims 32 d .. of V^T.
+    auto key_part = [&](int at, int i) __attribute__((always_inline)) {
+      return __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(lds + k_read[i] + at));
+    };
+    auto value_part = [&](int at, int i, int d) __attribute__((always_inline)) {
+      v4i16 w[2];
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+        w[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (__attribute__((address_space(3))) v4i16*)(lds + v_read[d] + at + C::TK * kD * 2 + (16 * i + 8 * e) * kD * 2));
+      return __builtin_bit_cast(bf16x8, __builtin_shufflevector(w[0], w[1], 0, 1, 2, 3, 4, 5, 6, 7));
+    };
     // Scores of a piece: st[n][r] is token 8 (r / 4) + 4 half + r % 4 of it.  (`at`: its
     // place in LDS, in bytes; where that is a constant, it goes into the reads.)
     auto scores = [&](int at, f32x16 (&st)[NB]) __attribute__((always_inline)) {
@@ -536,7 +553,7 @@ __global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(con
         for (int r = 0; r < 16; ++r) st[n][r] = 0.f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const bf16x8 a = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(lds + k_read[i] + at));
+        const bf16x8 a = key_part(at, i);
 #pragma unroll
         for (int n = 0; n < NB; ++n) st[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[n][i], st[n], 0, 0, 0);
       }
@@ -554,17 +571,19 @@ __global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(con
     // The reference m moves only where a score passes it by more than 2^8 (and at the
     // first score): sums keep their relative precision either way.
     const float scale = P.scale_log2;
-    auto refer = [&](const f32x16 (&st)[NB]) __attribute__((always_inline)) {
-      float top[NB];
-      bool over = false;
+    auto tops = [&](const f32x16 (&st)[NB], float (&top)[NB]) __attribute__((always_inline)) {
 #pragma unroll
       for (int n = 0; n < NB; ++n) {
         top[n] = st[n][0];
 #pragma unroll
         for (int r = 1; r < 16; ++r) top[n] = fmaxf(top[n], st[n][r]);
         top[n] *= scale;
-        over |= top[n] > m[n] + 8.f;
       }
+    };
+    auto refer = [&](const float (&top)[NB]) __attribute__((always_inline)) {
+      bool over = false;
+#pragma unroll
+      for (int n = 0; n < NB; ++n) over |= top[n] > m[n] + 8.f;
       if (__any(over)) {
 #pragma unroll
         for (int n = 0; n < NB; ++n) {
@@ -582,9 +601,7 @@ __global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(con
         }
       }
     };
-    // Probabilities and their products with V.
-    auto weigh = [&](int at, f32x16 (&st)[NB]) __attribute__((always_inline)) {
-      bf16x8 p[NB][PARTS][2];
+    auto weights = [&](f32x16 (&st)[NB], bf16x8 (&p)[NB][PARTS][2]) __attribute__((always_inline)) {
 #pragma unroll
       for (int n = 0; n < NB; ++n) {
         const float ref = m[n] == kNegInf ? 0.f : m[n];
@@ -608,23 +625,25 @@ __global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(con
           p[n][k][1] = __builtin_bit_cast(bf16x8, u32x4{w[4], w[5], w[6], w[7]});
         }
       }
+    };
+    auto products = [&](int at, const bf16x8 (&p)[NB][PARTS][2]) __attribute__((always_inline)) {
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int d = 0; d < 4; ++d) {
-          v4i16 w[2];
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            w[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                (__attribute__((address_space(3))) v4i16*)(lds + v_read[d] + at + C::TK * kD * 2 + (16 * i + 8 * e) * kD * 2));
-          }
-          const bf16x8 a = __builtin_bit_cast(bf16x8, __builtin_shufflevector(w[0], w[1], 0, 1, 2, 3, 4, 5, 6, 7));
+          const bf16x8 a = value_part(at, i, d);
 #pragma unroll
           for (int n = 0; n < NB; ++n)
 #pragma unroll
             for (int j = 0; j < PARTS; ++j)
               acc[n][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, p[n][j][i], acc[n][d], 0, 0, 0);
         }
+    };
+
+    auto weigh = [&](int at, f32x16 (&st)[NB]) __attribute__((always_inline)) {
+      bf16x8 p[NB][PARTS][2];
+      weights(st, p);
+      products(at, p);
     };
 
     __syncthreads();       // the segment before has left LDS
@@ -645,28 +664,88 @@ __global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(con
       };
       barrier();
       int t = t0;
-      if (t + 4 < first_tail) {
+      if (t + 7 < first_tail) {
         f32x16 st[NB];
+        float top[NB];
         scores(0, st);
-        // one tile, in buffer B, and the next one's scores
+        tops(st, top);
+        // One tile, in buffer B, and the next one's scores; the loads of the one three
+        // further (before the tail: all rows are there).  No branch but the reference's.
         auto step = [&](auto B, int t) __attribute__((always_inline)) {
           constexpr int kB = decltype(B)::value;
           f32x16 next_st[NB];
-          refer(st);
-          advance(t, (kB + 3) % 4);
-          scores((kB + 1) % 4 * C::TILE_BYTES, next_st);
-          weigh(kB * C::TILE_BYTES, st);
+          bf16x8 p[NB][PARTS][2];
+          refer(top);
+          const int at = t + 3 - paged, here = __builtin_amdgcn_readlane(pages, at & 63);
+          const int ahead = __builtin_amdgcn_readlane(more_pages, at & 63), page = at < kAhead ? here : ahead;
+          wait_loads<2 * C::LOADS>();
+          barrier();
+          constexpr int kNext = (kB + 1) % 4 * C::TILE_BYTES, kHere = kB * C::TILE_BYTES;
+          uint8_t* const free_place = lds + (kB + 3) % 4 * C::TILE_BYTES + wave * C::OWN * kD * 2;
+          if constexpr (PARTS > 1) {
+            scores(kNext, next_st);
+            weights(st, p);
+            products(kHere, p);
+            tops(next_st, top);
+            load_rows((t + 3) * C::TK + wave * C::OWN, page, free_place);
+          } else {
+            // In this order: two probabilities and a piece of V behind every matrix
+            // instruction of the scores, maxima and loads behind those of the products.
+            bf16x8 k_part[8], v_part[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) k_part[i] = key_part(kNext, i);
+            float ref[NB];
+#pragma unroll
+            for (int n = 0; n < NB; ++n) {
+              ref[n] = m[n] == kNegInf ? 0.f : m[n];
+#pragma unroll
+              for (int r = 0; r < 16; ++r) next_st[n][r] = 0.f;
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            uint32_t w[NB][8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+#pragma unroll
+              for (int n = 0; n < NB; ++n)
+                next_st[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_part[i], qf[n][i], next_st[n], 0, 0, 0);
+              v_part[i] = value_part(kHere, i >> 2, i & 3);
+#pragma unroll
+              for (int n = 0; n < NB; ++n) {
+                const float x = fast_exp2(fmaf(st[n][2 * i], scale, -ref[n]));
+                const float y = fast_exp2(fmaf(st[n][2 * i + 1], scale, -ref[n]));
+                l[n] += x;
+                l[n] += y;
+                w[n][i] = pack_bf16(x, y);
+              }
+              __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+#pragma unroll
+              for (int n = 0; n < NB; ++n) {
+                const uint32_t* const u = w[n] + (i >> 2) * 4;
+                acc[n][i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                    v_part[i], __builtin_bit_cast(bf16x8, u32x4{u[0], u[1], u[2], u[3]}), acc[n][i & 3], 0, 0, 0);
+                if (i == 0) top[n] = next_st[n][0];
+                top[n] = fmaxf(fmaxf(top[n], next_st[n][2 * i]), next_st[n][2 * i + 1]);
+                if (i == 7) top[n] *= scale;
+              }
+              if (i == 3) load_rows((t + 3) * C::TK + wave * C::OWN, page, free_place);
+              __builtin_amdgcn_sched_barrier(0);
+            }
+          }
 #pragma unroll
           for (int n = 0; n < NB; ++n) st[n] = next_st[n];
         };
 #pragma unroll 1
-        for (; t + 4 < first_tail; t += 4) {
+        for (; t + 7 < first_tail; t += 4) {
+          if (t + 3 >= paged + kAhead) next_pages();
           step(std::integral_constant<int, 0>{}, t);
           step(std::integral_constant<int, 1>{}, t + 1);
           step(std::integral_constant<int, 2>{}, t + 2);
           step(std::integral_constant<int, 3>{}, t + 3);
         }
-        refer(st);
+        refer(top);
         weigh(0, st);
         advance(t, 3);
         ++t;
@@ -679,7 +758,9 @@ __global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(con
         f32x16 st[NB];
         scores(buf * C::TILE_BYTES, st);
         if (tail) hide(t, 0, st);
-        refer(st);
+        float top[NB];
+        tops(st, top);
+        refer(top);
         weigh(buf * C::TILE_BYTES, st);
         if (t + 1 < t1) advance(t, (buf + 3) & 3);
       }
@@ -708,7 +789,9 @@ __global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(con
           f32x16 st[NB];
           scores(at, st);
           if (is_tail(t)) hide(t, sub, st);
-          refer(st);
+          float top[NB];
+          tops(st, top);
+          refer(top);
           weigh(at, st);
         }
       }
