@@ -701,10 +701,17 @@ __global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(con
 #pragma unroll
               for (int r = 0; r < 16; ++r) next_st[n][r] = 0.f;
             }
+            __builtin_amdgcn_s_setprio(1);
             __builtin_amdgcn_sched_barrier(0);
             uint32_t w[NB][8];
+            const int first = (t + 3) * C::TK + wave * C::OWN;
+            const uint8_t *k16 = nullptr, *v16 = nullptr;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
+              if (i == 1) k16 = k_head + page * k_page;
+              if (i == 2) v16 = v_head + page * v_page;
+              if (i == 3) k16 += (uint64_t)(first & slots) * k_tok;
+              if (i == 4) v16 += (uint64_t)(first & slots) * v_tok;
 #pragma unroll
               for (int n = 0; n < NB; ++n)
                 next_st[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_part[i], qf[n][i], next_st[n], 0, 0, 0);
@@ -730,10 +737,14 @@ __global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(con
                 top[n] = fmaxf(fmaxf(top[n], next_st[n][2 * i]), next_st[n][2 * i + 1]);
                 if (i == 7) top[n] *= scale;
               }
-              if (i == 3) load_rows((t + 3) * C::TK + wave * C::OWN, page, free_place);
+              if (i < kRows / 4) {
+                load_lds(k16 + (uint64_t)(4 * i * k_tok) + k_lane[i], free_place + 4 * i * kD * 2);
+                load_lds(v16 + (uint64_t)(4 * i * v_tok) + v_lane, free_place + C::TK * kD * 2 + 4 * i * kD * 2);
+              }
               __builtin_amdgcn_sched_barrier(0);
             }
           }
+          __builtin_amdgcn_s_setprio(0);
 #pragma unroll
           for (int n = 0; n < NB; ++n) st[n] = next_st[n];
         };
