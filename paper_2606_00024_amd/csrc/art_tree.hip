@@ -182,10 +182,20 @@ __device__ __forceinline__ void barrier() {
   __builtin_amdgcn_s_barrier();
   __asm__ __volatile__("" ::: "memory");
 }
-// 16 bytes for every lane straight into LDS, lane after lane from `to` on.
+// 16 bytes for every lane straight into LDS, lane after lane from `to` on: `base`
+// uniform, `offset` the lane's.  In assembly, as the compiler would have every later
+// read of LDS wait for all loads on their way; wait_loads says when they are there.
+// (It has no output register, so nothing can be taken for loaded too early.)
+__device__ __forceinline__ void load_lds(const uint8_t* base, uint32_t offset, uint8_t* to) {
+  const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)to);
+  __asm__ __volatile__("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                       : : "s"(at), "v"(offset), "s"(base) : "memory");
+}
+// ... of a lane's own address
 __device__ __forceinline__ void load_lds(const uint8_t* from, uint8_t* to) {
-  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
-                                   (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+  const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)to);
+  __asm__ __volatile__("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+                       : : "s"(at), "v"(from) : "memory");
 }
 
 __device__ __forceinline__ bool not_finite(uint32_t w) {
@@ -449,8 +459,8 @@ __global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(con
       const uint8_t* const v16 = v_head + page * v_page + (uint64_t)(first & slots) * v_tok;
 #pragma unroll
       for (int i = 0; i < kRows / 4; ++i) {
-        load_lds(k16 + (uint64_t)(4 * i * k_tok) + k_lane[i], to_k + 4 * i * kD * 2);
-        load_lds(v16 + (uint64_t)(4 * i * v_tok) + v_lane, to_k + C::TK * kD * 2 + 4 * i * kD * 2);
+        load_lds(k16 + (uint64_t)(4 * i * k_tok), k_lane[i], to_k + 4 * i * kD * 2);
+        load_lds(v16 + (uint64_t)(4 * i * v_tok), v_lane, to_k + C::TK * kD * 2 + 4 * i * kD * 2);
       }
     };
     auto next_pages = [&]() __attribute__((always_inline)) {
@@ -652,49 +662,47 @@ __global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(con
       // scores, and two on their way.
       const int first_tail = max(min(open / C::TK, t1), t0);
 #pragma unroll
-      for (int i = 0; i < 3; ++i)
+      for (int i = 0; i < 4; ++i)
         if (t0 + i < t1) load_tile(t0 + i, i);
       wait_loads<0>();
-      // the next tile is there, and the one before `t` has been used up
-      auto advance = [&](int t, int buf) __attribute__((always_inline)) {
-        if (t + 2 < t1) wait_loads<2 * C::LOADS>();
-        else wait_loads<0>();
-        barrier();
-        if (t + 3 < t1) load_tile(t + 3, buf);
-      };
       barrier();
       int t = t0;
-      if (t + 7 < first_tail) {
+      if (t + 8 < first_tail) {
         f32x16 st[NB];
         float top[NB];
+        bf16x8 k_part[8];
         scores(0, st);
         tops(st, top);
-        // One tile, in buffer B, and the next one's scores; the loads of the one three
-        // further (before the tail: all rows are there).  No branch but the reference's.
+#pragma unroll
+        for (int i = 0; i < 8; ++i) k_part[i] = key_part(C::TILE_BYTES, i);
+        // One tile, in buffer B, and the next one's scores, whose keys are in registers;
+        // then that buffer is free for the tile four further, and the keys two further
+        // are there.  (All of it is before the tail: every row of a tile exists.)  No
+        // branch but the reference's.
         auto step = [&](auto B, int t) __attribute__((always_inline)) {
-          constexpr int kB = decltype(B)::value;
+          constexpr int kB = decltype(B)::value, kHere = kB * C::TILE_BYTES;
+          constexpr int kNext = (kB + 1) % 4 * C::TILE_BYTES, kAfter = (kB + 2) % 4 * C::TILE_BYTES;
+          uint8_t* const free_place = lds + kHere + wave * C::OWN * kD * 2;
           f32x16 next_st[NB];
-          bf16x8 p[NB][PARTS][2];
           refer(top);
-          const int at = t + 3 - paged, here = __builtin_amdgcn_readlane(pages, at & 63);
+          const int at = t + 4 - paged, here = __builtin_amdgcn_readlane(pages, at & 63);
           const int ahead = __builtin_amdgcn_readlane(more_pages, at & 63), page = at < kAhead ? here : ahead;
-          wait_loads<2 * C::LOADS>();
-          barrier();
-          constexpr int kNext = (kB + 1) % 4 * C::TILE_BYTES, kHere = kB * C::TILE_BYTES;
-          uint8_t* const free_place = lds + (kB + 3) % 4 * C::TILE_BYTES + wave * C::OWN * kD * 2;
+          const int first = (t + 4) * C::TK + wave * C::OWN;
           if constexpr (PARTS > 1) {
             scores(kNext, next_st);
-            weights(st, p);
-            products(kHere, p);
+            weigh(kHere, st);
+            wait_loads<2 * C::LOADS>();
+            barrier();
+            load_rows(first, page, free_place);
             tops(next_st, top);
-            load_rows((t + 3) * C::TK + wave * C::OWN, page, free_place);
           } else {
             // In this order: two probabilities and a piece of V behind every matrix
-            // instruction of the scores, maxima and loads behind those of the products.
-            bf16x8 k_part[8], v_part[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) k_part[i] = key_part(kNext, i);
+            // instruction of the scores, maxima, keys and loads behind those of the
+            // products.  V is in registers by then, so the barrier comes between.
+            bf16x8 v_part[8];
             float ref[NB];
+            uint32_t w[NB][8];
+            const uint8_t *k16 = nullptr, *v16 = nullptr;
 #pragma unroll
             for (int n = 0; n < NB; ++n) {
               ref[n] = m[n] == kNegInf ? 0.f : m[n];
@@ -703,9 +711,6 @@ __global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(con
             }
             __builtin_amdgcn_s_setprio(1);
             __builtin_amdgcn_sched_barrier(0);
-            uint32_t w[NB][8];
-            const int first = (t + 3) * C::TK + wave * C::OWN;
-            const uint8_t *k16 = nullptr, *v16 = nullptr;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
               if (i == 1) k16 = k_head + page * k_page;
@@ -726,6 +731,8 @@ __global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(con
               }
               __builtin_amdgcn_sched_barrier(0);
             }
+            wait_loads<2 * C::LOADS>();
+            barrier();
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
 #pragma unroll
@@ -737,30 +744,30 @@ __global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(con
                 top[n] = fmaxf(fmaxf(top[n], next_st[n][2 * i]), next_st[n][2 * i + 1]);
                 if (i == 7) top[n] *= scale;
               }
-              if (i < kRows / 4) {
-                load_lds(k16 + (uint64_t)(4 * i * k_tok) + k_lane[i], free_place + 4 * i * kD * 2);
-                load_lds(v16 + (uint64_t)(4 * i * v_tok) + v_lane, free_place + C::TK * kD * 2 + 4 * i * kD * 2);
+              if (i < 4) {
+                k_part[2 * i] = key_part(kAfter, 2 * i);
+                k_part[2 * i + 1] = key_part(kAfter, 2 * i + 1);
+              } else if (i - 4 < kRows / 4) {
+                load_lds(k16 + (uint64_t)(4 * (i - 4) * k_tok), k_lane[i - 4], free_place + 4 * (i - 4) * kD * 2);
+                load_lds(v16 + (uint64_t)(4 * (i - 4) * v_tok), v_lane, free_place + C::TK * kD * 2 + 4 * (i - 4) * kD * 2);
               }
               __builtin_amdgcn_sched_barrier(0);
             }
+            __builtin_amdgcn_s_setprio(0);
           }
-          __builtin_amdgcn_s_setprio(0);
 #pragma unroll
           for (int n = 0; n < NB; ++n) st[n] = next_st[n];
         };
 #pragma unroll 1
-        for (; t + 7 < first_tail; t += 4) {
-          if (t + 3 >= paged + kAhead) next_pages();
+        for (; t + 8 < first_tail; t += 4) {
+          if (t + 4 >= paged + kAhead) next_pages();
           step(std::integral_constant<int, 0>{}, t);
           step(std::integral_constant<int, 1>{}, t + 1);
           step(std::integral_constant<int, 2>{}, t + 2);
           step(std::integral_constant<int, 3>{}, t + 3);
         }
-        refer(top);
-        weigh(0, st);
-        advance(t, 3);
-        ++t;
       }
+      // (behind the steps: the tile of the pending scores again, from its keys)
 #pragma unroll 1
       for (; t < t1; ++t) {
         const int buf = (t - t0) & 3;
@@ -773,7 +780,13 @@ __global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(con
         tops(st, top);
         refer(top);
         weigh(buf * C::TILE_BYTES, st);
-        if (t + 1 < t1) advance(t, (buf + 3) & 3);
+        if (t + 1 < t1) {
+          // the next tile is there, and this one has been used up
+          if (t + 3 < t1) wait_loads<4 * C::LOADS>();
+          else wait_loads<0>();
+          barrier();
+          if (t + 4 < t1) load_tile(t + 4, buf);
+        }
       }
     } else {
       load_tile(t0, t0 & 1);
