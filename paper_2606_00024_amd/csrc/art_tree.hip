@@ -45,11 +45,10 @@ constexpr int kLeast = 3;          // places of a workgroup
 template <int RB>
 struct Tree {
   static constexpr int kRows = 32 * RB;
-  static constexpr int NB = RB > kWaves ? RB / kWaves : 1;   // blocks of a wavefront
-  static constexpr int TS = RB < kWaves ? kWaves / RB : 1;   // wavefronts that share a block's tokens
+  static constexpr int TS = kWaves / RB;            // wavefronts that share a block's tokens
   // Wide row tiles, which the matrix cores bound: the next tile's scores are in work
   // with one's probabilities, so it has to be there before that one has been used up
-  static constexpr bool WIDE = RB >= kWaves;
+  static constexpr bool WIDE = RB == kWaves;
   static constexpr int TK = RB == 1 ? 128 : WIDE ? 32 : 64;  // tokens of a tile
   static constexpr int SUB = TK / 32 / TS;          // 32-token pieces of a wavefront
   static constexpr int OWN = TK / kWaves;           // tokens of a tile that a wavefront loads
@@ -57,7 +56,7 @@ struct Tree {
   static constexpr int BUFS = WIDE ? 4 : 2;         // tiles in LDS
   static constexpr int PITCH = kD + 4;              // floats of a row of a wavefront's record
   static constexpr int TILE_BYTES = 2 * TK * kD * 2;
-  static constexpr int REC_BYTES = kWaves * 32 * PITCH * 4;   // (a wavefront's blocks one after the other)
+  static constexpr int REC_BYTES = kWaves * 32 * PITCH * 4;
   static constexpr int LDS = BUFS * TILE_BYTES > REC_BYTES ? BUFS * TILE_BYTES : REC_BYTES;
 };
 
@@ -246,11 +245,10 @@ __device__ __forceinline__ f32x4 over(const f32x4& o, float l) {
 // PARTS: bf16 parts that a probability is multiplied in: one (8 bits) for bf16
 // outputs, three (24) for fp32.
 template <int RB, int PARTS>
-__global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(const TreeParams) {
+__global__ void __launch_bounds__(kThreads, 2) tree_kernel(const TreeParams) {
   TP* const args = (TP*)__builtin_amdgcn_kernarg_segment_ptr();
   TP& P = *args;
   using C = Tree<RB>;
-  constexpr int NB = C::NB;
   __shared__ __align__(16) uint8_t lds[C::LDS];
   __shared__ float s_m[kWaves][32], s_l[kWaves][32];
   __shared__ int64_t s_scan[2][kWaves], s_base;
@@ -408,35 +406,25 @@ __global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(con
     const int64_t last = ((start + kLead + all) * workers - 1) / line;   // who holds its last place
 
     const int node0 = rt * P.nodes, M = min(P.nodes, s.n - node0) * P.group;
-    bf16x8 qf[NB][8];
-    int node[NB];
-    const uint64_t* mask[NB];
+    bf16x8 qf[8];
+    const int row = 32 * rb + lo, head = kvh * P.group + row % P.group;
+    const int node = node0 + row / P.group;
+    const uint64_t* const mask = P.words && row < M ? P.mask + (int64_t)(s.first + node) * P.words : P.mask;
 #pragma unroll
-    for (int n = 0; n < NB; ++n) {
-      const int row = 32 * (rb * NB + n) + lo, head = kvh * P.group + row % P.group;
-      node[n] = node0 + row / P.group;
-      mask[n] = P.words && row < M ? P.mask + (int64_t)(s.first + node[n]) * P.words : P.mask;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        u32x4 w{0u, 0u, 0u, 0u};
-        if (row < M) {
-          w = *reinterpret_cast<const u32x4*>(P.q + (int64_t)(s.first + node[n]) * P.qs_row + (int64_t)head * P.qs_head + 16 * i + 8 * half);
-          if (P.negate) w = w ^ 0x80008000u;
-        }
-        qf[n][i] = __builtin_bit_cast(bf16x8, w);
+    for (int i = 0; i < 8; ++i) {
+      u32x4 w{0u, 0u, 0u, 0u};
+      if (row < M) {
+        w = *reinterpret_cast<const u32x4*>(P.q + (s.first + node) * P.qs_row + head * P.qs_head + 16 * i + 8 * half);
+        if (P.negate) w = w ^ 0x80008000u;
       }
+      qf[i] = __builtin_bit_cast(bf16x8, w);
     }
-    f32x16 acc[NB][4];
-    float m[NB], l[NB];
+    f32x16 acc[4];
+    float m = kNegInf, l = 0.f;
 #pragma unroll
-    for (int n = 0; n < NB; ++n) {
-      m[n] = kNegInf;
-      l[n] = 0.f;
+    for (int d = 0; d < 4; ++d)
 #pragma unroll
-      for (int d = 0; d < 4; ++d)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) acc[n][d][r] = 0.f;
-    }
+      for (int r = 0; r < 16; ++r) acc[d][r] = 0.f;
 
     // Pages: lane i has that of the wavefront's 16-token group i from tile `paged` on,
     // and of 64 more, asked for that much ahead.
@@ -503,6 +491,7 @@ __global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(con
     // does not see them must not get them.  Rows that do get them added, then they
     // leave the tile.
     auto clean = [&](int t, int buf) __attribute__((always_inline)) {
+      __syncthreads();     // (a wavefront may have waited for its own tokens only)
       uint16_t* const s_v = reinterpret_cast<uint16_t*>(lds + buf * C::TILE_BYTES) + C::TK * kD;
       bool bad = false;
       for (int i = tid; i < C::TK * kD / 8; i += kThreads) {
@@ -515,19 +504,16 @@ __global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(con
       for (int k = 0; k < 32 * C::SUB; ++k) {
         const int r = place(0) + k, tok = t * C::TK + r;
         // (-1 where the row sees the token: no branch for each of the sums)
-        uint32_t see[NB];
-#pragma unroll
-        for (int n = 0; n < NB; ++n)
-          see[n] = tok < seen && (sees(P, mask[n], node[n], s.n, tok - s.context) & 1u) ? ~0u : 0u;
+        uint32_t see;
+        see = tok < seen && (sees(P, mask, node, s.n, tok - s.context) & 1u) ? ~0u : 0u;
 #pragma unroll
         for (int d = 0; d < 4; ++d)
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
-            const int dim = 32 * d + 8 * (e >> 2) + 4 * half + (e & 3);
-            const uint32_t w = s_v[v_off(r, dim >> 3) + (dim & 7)], x = (w & 0x7f80u) == 0x7f80u ? w << 16 : 0u;
-#pragma unroll
-            for (int n = 0; n < NB; ++n) acc[n][d][e] += __uint_as_float(x & see[n]);
-          }
+          const int dim = 32 * d + 8 * (e >> 2) + 4 * half + (e & 3);
+          const uint32_t w = s_v[v_off(r, dim >> 3) + (dim & 7)], x = (w & 0x7f80u) == 0x7f80u ? w << 16 : 0u;
+          acc[d][e] += __uint_as_float(x & see);
+        }
       }
       __syncthreads();
       for (int i = tid; i < C::TK * kD / 8; i += kThreads) {
@@ -554,104 +540,84 @@ __global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(con
             (__attribute__((address_space(3))) v4i16*)(lds + v_read[d] + at + C::TK * kD * 2 + (16 * i + 8 * e) * kD * 2));
       return __builtin_bit_cast(bf16x8, __builtin_shufflevector(w[0], w[1], 0, 1, 2, 3, 4, 5, 6, 7));
     };
-    // Scores of a piece: st[n][r] is token 8 (r / 4) + 4 half + r % 4 of it.  (`at`: its
+    // Scores of a piece: st[r] is token 8 (r / 4) + 4 half + r % 4 of it.  (`at`: its
     // place in LDS, in bytes; where that is a constant, it goes into the reads.)
-    auto scores = [&](int at, f32x16 (&st)[NB]) __attribute__((always_inline)) {
+    auto scores = [&](int at, f32x16& st) __attribute__((always_inline)) {
 #pragma unroll
-      for (int n = 0; n < NB; ++n)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) st[n][r] = 0.f;
+      for (int r = 0; r < 16; ++r) st[r] = 0.f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const bf16x8 a = key_part(at, i);
-#pragma unroll
-        for (int n = 0; n < NB; ++n) st[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[n][i], st[n], 0, 0, 0);
+        st = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[i], st, 0, 0, 0);
       }
     };
-    auto hide = [&](int t, int sub, f32x16 (&st)[NB]) __attribute__((always_inline)) {
+    auto hide = [&](int t, int sub, f32x16& st) __attribute__((always_inline)) {
       TP& P = *fresh(args);
+      const uint32_t bits = sees(P, mask, node, s.n, t * C::TK + place(sub) - s.context) >> (4 * half);
 #pragma unroll
-      for (int n = 0; n < NB; ++n) {
-        const uint32_t bits = sees(P, mask[n], node[n], s.n, t * C::TK + place(sub) - s.context) >> (4 * half);
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (!(bits >> (8 * (r >> 2) + (r & 3)) & 1u)) st[n][r] = kNegInf;
-      }
+      for (int r = 0; r < 16; ++r)
+        if (!(bits >> (8 * (r >> 2) + (r & 3)) & 1u)) st[r] = kNegInf;
     };
     // The reference m moves only where a score passes it by more than 2^8 (and at the
     // first score): sums keep their relative precision either way.
     const float scale = P.scale_log2;
-    auto tops = [&](const f32x16 (&st)[NB], float (&top)[NB]) __attribute__((always_inline)) {
+    auto tops = [&](const f32x16& st, float& top) __attribute__((always_inline)) {
+      top = st[0];
 #pragma unroll
-      for (int n = 0; n < NB; ++n) {
-        top[n] = st[n][0];
+      for (int r = 1; r < 16; ++r) top = fmaxf(top, st[r]);
+      top *= scale;
+    };
+    auto refer = [&](float top) __attribute__((always_inline)) {
+      if (__any(top > m + 8.f)) {
+        float a, c;
+        swap_rows32(top, a, c);
+        const float mn = fmaxf(m, fmaxf(a, c));
+        // (never 0: infinite sums stay so; the first reference finds no others)
+        const float f = m == kNegInf ? 1.f : fast_exp2(fmaxf(m - mn, -126.f));
+        m = mn;
+        l *= f;
 #pragma unroll
-        for (int r = 1; r < 16; ++r) top[n] = fmaxf(top[n], st[n][r]);
-        top[n] *= scale;
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) acc[d][r] *= f;
       }
     };
-    auto refer = [&](const float (&top)[NB]) __attribute__((always_inline)) {
-      bool over = false;
+    auto weights = [&](f32x16& st, bf16x8 (&p)[PARTS][2]) __attribute__((always_inline)) {
+      const float ref = m == kNegInf ? 0.f : m;
 #pragma unroll
-      for (int n = 0; n < NB; ++n) over |= top[n] > m[n] + 8.f;
-      if (__any(over)) {
-#pragma unroll
-        for (int n = 0; n < NB; ++n) {
-          float a, c;
-          swap_rows32(top[n], a, c);
-          const float mn = fmaxf(m[n], fmaxf(a, c));
-          // (never 0: infinite sums stay so; the first reference finds no others)
-          const float f = m[n] == kNegInf ? 1.f : fast_exp2(fmaxf(m[n] - mn, -126.f));
-          m[n] = mn;
-          l[n] *= f;
-#pragma unroll
-          for (int d = 0; d < 4; ++d)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) acc[n][d][r] *= f;
-        }
+      for (int r = 0; r < 16; ++r) {
+        st[r] = fast_exp2(fmaf(st[r], scale, -ref));
+        l += st[r];
       }
-    };
-    auto weights = [&](f32x16 (&st)[NB], bf16x8 (&p)[NB][PARTS][2]) __attribute__((always_inline)) {
 #pragma unroll
-      for (int n = 0; n < NB; ++n) {
-        const float ref = m[n] == kNegInf ? 0.f : m[n];
+      for (int k = 0; k < PARTS; ++k) {
+        uint32_t w[8];
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          st[n][r] = fast_exp2(fmaf(st[n][r], scale, -ref));
-          l[n] += st[n][r];
-        }
-#pragma unroll
-        for (int k = 0; k < PARTS; ++k) {
-          uint32_t w[8];
-#pragma unroll
-          for (int r = 0; r < 8; ++r) {
-            w[r] = pack_bf16(st[n][2 * r], st[n][2 * r + 1]);
-            if (k + 1 < PARTS) {
-              st[n][2 * r] -= bf_lo(w[r]);
-              st[n][2 * r + 1] -= bf_hi(w[r]);
-            }
+        for (int r = 0; r < 8; ++r) {
+          w[r] = pack_bf16(st[2 * r], st[2 * r + 1]);
+          if (k + 1 < PARTS) {
+            st[2 * r] -= bf_lo(w[r]);
+            st[2 * r + 1] -= bf_hi(w[r]);
           }
-          p[n][k][0] = __builtin_bit_cast(bf16x8, u32x4{w[0], w[1], w[2], w[3]});
-          p[n][k][1] = __builtin_bit_cast(bf16x8, u32x4{w[4], w[5], w[6], w[7]});
         }
+        p[k][0] = __builtin_bit_cast(bf16x8, u32x4{w[0], w[1], w[2], w[3]});
+        p[k][1] = __builtin_bit_cast(bf16x8, u32x4{w[4], w[5], w[6], w[7]});
       }
     };
-    auto products = [&](int at, const bf16x8 (&p)[NB][PARTS][2]) __attribute__((always_inline)) {
+    auto products = [&](int at, const bf16x8 (&p)[PARTS][2]) __attribute__((always_inline)) {
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int d = 0; d < 4; ++d) {
-          const bf16x8 a = value_part(at, i, d);
+        const bf16x8 a = value_part(at, i, d);
 #pragma unroll
-          for (int n = 0; n < NB; ++n)
-#pragma unroll
-            for (int j = 0; j < PARTS; ++j)
-              acc[n][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, p[n][j][i], acc[n][d], 0, 0, 0);
-        }
+        for (int j = 0; j < PARTS; ++j)
+          acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, p[j][i], acc[d], 0, 0, 0);
+      }
     };
 
-    auto weigh = [&](int at, f32x16 (&st)[NB]) __attribute__((always_inline)) {
-      bf16x8 p[NB][PARTS][2];
+    auto weigh = [&](int at, f32x16& st) __attribute__((always_inline)) {
+      bf16x8 p[PARTS][2];
       weights(st, p);
       products(at, p);
     };
@@ -668,8 +634,8 @@ __global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(con
       barrier();
       int t = t0;
       if (t + 8 < first_tail) {
-        f32x16 st[NB];
-        float top[NB];
+        f32x16 st;
+        float top;
         bf16x8 k_part[8];
         scores(0, st);
         tops(st, top);
@@ -683,7 +649,7 @@ __global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(con
           constexpr int kB = decltype(B)::value, kHere = kB * C::TILE_BYTES;
           constexpr int kNext = (kB + 1) % 4 * C::TILE_BYTES, kAfter = (kB + 2) % 4 * C::TILE_BYTES;
           uint8_t* const free_place = lds + kHere + wave * C::OWN * kD * 2;
-          f32x16 next_st[NB];
+          f32x16 next_st;
           refer(top);
           const int at = t + 4 - paged, here = __builtin_amdgcn_readlane(pages, at & 63);
           const int ahead = __builtin_amdgcn_readlane(more_pages, at & 63), page = at < kAhead ? here : ahead;
@@ -700,15 +666,11 @@ __global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(con
             // instruction of the scores, maxima, keys and loads behind those of the
             // products.  V is in registers by then, so the barrier comes between.
             bf16x8 v_part[8];
-            float ref[NB];
-            uint32_t w[NB][8];
+            uint32_t w[8];
             const uint8_t *k16 = nullptr, *v16 = nullptr;
+            const float ref = m == kNegInf ? 0.f : m;
 #pragma unroll
-            for (int n = 0; n < NB; ++n) {
-              ref[n] = m[n] == kNegInf ? 0.f : m[n];
-#pragma unroll
-              for (int r = 0; r < 16; ++r) next_st[n][r] = 0.f;
-            }
+            for (int r = 0; r < 16; ++r) next_st[r] = 0.f;
             __builtin_amdgcn_s_setprio(1);
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -717,33 +679,25 @@ __global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(con
               if (i == 2) v16 = v_head + page * v_page;
               if (i == 3) k16 += (uint64_t)(first & slots) * k_tok;
               if (i == 4) v16 += (uint64_t)(first & slots) * v_tok;
-#pragma unroll
-              for (int n = 0; n < NB; ++n)
-                next_st[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_part[i], qf[n][i], next_st[n], 0, 0, 0);
+              next_st = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_part[i], qf[i], next_st, 0, 0, 0);
               v_part[i] = value_part(kHere, i >> 2, i & 3);
-#pragma unroll
-              for (int n = 0; n < NB; ++n) {
-                const float x = fast_exp2(fmaf(st[n][2 * i], scale, -ref[n]));
-                const float y = fast_exp2(fmaf(st[n][2 * i + 1], scale, -ref[n]));
-                l[n] += x;
-                l[n] += y;
-                w[n][i] = pack_bf16(x, y);
-              }
+              const float x = fast_exp2(fmaf(st[2 * i], scale, -ref));
+              const float y = fast_exp2(fmaf(st[2 * i + 1], scale, -ref));
+              l += x;
+              l += y;
+              w[i] = pack_bf16(x, y);
               __builtin_amdgcn_sched_barrier(0);
             }
             wait_loads<2 * C::LOADS>();
             barrier();
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-#pragma unroll
-              for (int n = 0; n < NB; ++n) {
-                const uint32_t* const u = w[n] + (i >> 2) * 4;
-                acc[n][i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                    v_part[i], __builtin_bit_cast(bf16x8, u32x4{u[0], u[1], u[2], u[3]}), acc[n][i & 3], 0, 0, 0);
-                if (i == 0) top[n] = next_st[n][0];
-                top[n] = fmaxf(fmaxf(top[n], next_st[n][2 * i]), next_st[n][2 * i + 1]);
-                if (i == 7) top[n] *= scale;
-              }
+              const uint32_t* const u = w + (i >> 2) * 4;
+              acc[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                  v_part[i], __builtin_bit_cast(bf16x8, u32x4{u[0], u[1], u[2], u[3]}), acc[i & 3], 0, 0, 0);
+              if (i == 0) top = next_st[0];
+              top = fmaxf(fmaxf(top, next_st[2 * i]), next_st[2 * i + 1]);
+              if (i == 7) top *= scale;
               if (i < 4) {
                 k_part[2 * i] = key_part(kAfter, 2 * i);
                 k_part[2 * i + 1] = key_part(kAfter, 2 * i + 1);
@@ -755,8 +709,7 @@ __global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(con
             }
             __builtin_amdgcn_s_setprio(0);
           }
-#pragma unroll
-          for (int n = 0; n < NB; ++n) st[n] = next_st[n];
+          st = next_st;
         };
 #pragma unroll 1
         for (; t + 8 < first_tail; t += 4) {
@@ -773,10 +726,10 @@ __global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(con
         const int buf = (t - t0) & 3;
         const bool tail = t >= first_tail;
         if (tail) clean(t, buf);
-        f32x16 st[NB];
+        f32x16 st;
         scores(buf * C::TILE_BYTES, st);
         if (tail) hide(t, 0, st);
-        float top[NB];
+        float top;
         tops(st, top);
         refer(top);
         weigh(buf * C::TILE_BYTES, st);
@@ -810,10 +763,10 @@ __global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(con
 #pragma unroll
         for (int sub = 0; sub < C::SUB; ++sub) {
           const int at = (t & 1) * C::TILE_BYTES + place(sub) * kD * 2;
-          f32x16 st[NB];
+          f32x16 st;
           scores(at, st);
           if (is_tail(t)) hide(t, sub, st);
-          float top[NB];
+          float top;
           tops(st, top);
           refer(top);
           weigh(at, st);
@@ -821,54 +774,49 @@ __global__ void __launch_bounds__(kThreads, RB > kWaves ? 1 : 2) tree_kernel(con
       }
     }
 
-    // ---- the wavefronts' records, joined: a block of each at a time ----
+    // ---- the wavefronts' records, joined ----
     TP& W = *fresh(args);
     float* const to = W.records + (2 * me + (begins ? 1 : 0)) * (C::kRows * (kD + 2));
     const int64_t row0 = (int64_t)(s.first + node0) * W.q_heads + kvh * W.group;
+    float l0, l1;
+    swap_rows32(l, l0, l1);
+    __syncthreads();
+    float* const rec = s_rec + wave * 32 * C::PITCH;
 #pragma unroll
-    for (int n = 0; n < NB; ++n) {
-      float l0, l1;
-      swap_rows32(l[n], l0, l1);
-      __syncthreads();
-      float* const rec = s_rec + wave * 32 * C::PITCH;
+    for (int d = 0; d < 4; ++d)
 #pragma unroll
-      for (int d = 0; d < 4; ++d)
+      for (int e = 0; e < 4; ++e)
+        *reinterpret_cast<f32x4*>(rec + lo * C::PITCH + 32 * d + 8 * e + 4 * half) =
+            f32x4{acc[d][4 * e], acc[d][4 * e + 1], acc[d][4 * e + 2], acc[d][4 * e + 3]};
+    if (half == 0) {
+      s_m[wave][lo] = m;
+      s_l[wave][lo] = l0 + l1;
+    }
+    __syncthreads();
+    for (int i = tid; i < M * (kD / 4); i += kThreads) {
+      const int r = i / (kD / 4), d = i % (kD / 4) * 4, w0 = r / 32 * C::TS, rr = r % 32;
+      float top = kNegInf;
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          *reinterpret_cast<f32x4*>(rec + lo * C::PITCH + 32 * d + 8 * e + 4 * half) =
-              f32x4{acc[n][d][4 * e], acc[n][d][4 * e + 1], acc[n][d][4 * e + 2], acc[n][d][4 * e + 3]};
-      if (half == 0) {
-        s_m[wave][lo] = m[n];
-        s_l[wave][lo] = l0 + l1;
+      for (int w = 0; w < C::TS; ++w) top = fmaxf(top, s_m[w0 + w][rr]);
+      f32x4 sum{0.f, 0.f, 0.f, 0.f};
+      float mass = 0.f;
+#pragma unroll
+      for (int w = 0; w < C::TS; ++w) {
+        const float f = factor(s_m[w0 + w][rr], top);
+        const f32x4 y = *reinterpret_cast<const f32x4*>(s_rec + (w0 + w) * 32 * C::PITCH + rr * C::PITCH + d);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sum[j] = fmaf(y[j], f, sum[j]);
+        mass = fmaf(s_l[w0 + w][rr], f, mass);
       }
-      __syncthreads();
-      for (int i = tid; i < C::kRows / NB * (kD / 4); i += kThreads) {
-        const int at_block = i / (kD / 4) / 32, rr = i / (kD / 4) % 32, d = i % (kD / 4) * 4, w0 = at_block * C::TS;
-        const int r = 32 * (at_block * NB + n) + rr;
-        if (r >= M) continue;
-        float top = kNegInf;
-#pragma unroll
-        for (int w = 0; w < C::TS; ++w) top = fmaxf(top, s_m[w0 + w][rr]);
-        f32x4 sum{0.f, 0.f, 0.f, 0.f};
-        float mass = 0.f;
-#pragma unroll
-        for (int w = 0; w < C::TS; ++w) {
-          const float f = factor(s_m[w0 + w][rr], top);
-          const f32x4 y = *reinterpret_cast<const f32x4*>(s_rec + (w0 + w) * 32 * C::PITCH + rr * C::PITCH + d);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) sum[j] = fmaf(y[j], f, sum[j]);
-          mass = fmaf(s_l[w0 + w][rr], f, mass);
-        }
-        if (whole) {
-          const int64_t at_row = row0 + (int64_t)(r / W.group) * W.q_heads + r % W.group;
-          write4(W, at_row, d, over(sum, mass));
-          if (d == 0) W.lse[at_row] = mass == 0.f ? kNegInf : ln_of(top, mass);
-        } else {
-          *reinterpret_cast<f32x4*>(to + r * kD + d) = sum;
-          if (d == 0) {
-            to[C::kRows * kD + r] = top;
-            to[C::kRows * kD + C::kRows + r] = mass;
-          }
+      if (whole) {
+        const int64_t at_row = row0 + (int64_t)(r / W.group) * W.q_heads + r % W.group;
+        write4(W, at_row, d, over(sum, mass));
+        if (d == 0) W.lse[at_row] = mass == 0.f ? kNegInf : ln_of(top, mass);
+      } else {
+        *reinterpret_cast<f32x4*>(to + r * kD + d) = sum;
+        if (d == 0) {
+          to[C::kRows * kD + r] = top;
+          to[C::kRows * kD + C::kRows + r] = mass;
         }
       }
     }
@@ -954,13 +902,12 @@ art_status plan_tree(const art_decode_shape* s, const art_tree_opts* o, TreePlan
     return ART_ERR_UNSUPPORTED;
   // a row tile that holds a sequence's rows, on average
   const int64_t rows = s->batch > 0 ? ((int64_t)o->rows + s->batch - 1) / s->batch * g : 0;
-  p->rb = rows <= 32 && g <= 32 ? 1 : rows <= 64 && g <= 64 ? 2 : true ? 4 : 8;
+  p->rb = rows <= 32 && g <= 32 ? 1 : rows <= 64 && g <= 64 ? 2 : 4;
   p->nodes = rows_of(p->rb) / g;
   const int tk = p->rb == 1 ? 128 : p->rb == 2 ? 64 : 32;
-  const int64_t most = p->rb > kWaves ? kMaxWorkers / 2 : kMaxWorkers;                // one to a CU, or two
   const int64_t units = (int64_t)s->num_kv_heads * (o->rows / p->nodes + s->batch);   // at most
-  const int64_t tiles = units < most ? units * ((cap + tk - 1) / tk) : units;
-  p->workers = (int)(tiles < most ? (tiles < 1 ? 1 : tiles) : most);
+  const int64_t tiles = units < kMaxWorkers ? units * ((cap + tk - 1) / tk) : units;
+  p->workers = (int)(tiles < kMaxWorkers ? (tiles < 1 ? 1 : tiles) : kMaxWorkers);
   p->slots = (int)(units < p->workers ? units : p->workers);
   if (p->slots < 1) p->slots = 1;
   p->records_off = ((size_t)p->slots * sizeof(int4) + 255) / 256 * 256;
@@ -1052,8 +999,7 @@ art_status art_tree_attention(const art_decode_shape* shape, const art_tree_opts
   p.records = reinterpret_cast<float*>(static_cast<char*>(workspace) + plan.records_off);
   if (plan.rb == 1) launch<1>(plan, p, stream);
   else if (plan.rb == 2) launch<2>(plan, p, stream);
-  else if (plan.rb == 4) launch<4>(plan, p, stream);
-  else launch<8>(plan, p, stream);
+  else launch<4>(plan, p, stream);
   return hipGetLastError() == hipSuccess ? ART_OK : ART_ERR_HIP;
 }
 
