@@ -8,7 +8,7 @@
 // The rows of a sequence's nodes that share a KV head lie together: a row tile is
 // as many whole nodes as fit kRows rows.  Row tiles of all sequences and heads are
 // the units of work; a unit has a tile of 64 or 128 tokens after the other to go
-// through.  The tiles of all units, kLead places for each unit's set-up in front
+// through.  The tiles of all units, LEAD places for each unit's set-up in front
 // of them, form one line, and every workgroup takes an equal, contiguous part of
 // it, however ragged the batch is.  A unit that lies in one workgroup is written
 // there; of the others each workgroup leaves a record (o, m, l) in the workspace
@@ -38,8 +38,6 @@ typedef short v4i16 __attribute__((ext_vector_type(4)));
 
 constexpr int kD = kHeadDim;
 constexpr int kMaxWorkers = 512;   // two workgroups for each of 256 CUs
-constexpr int kLead = 4;           // places of a unit's set-up and end
-constexpr int kLeast = 3;          // places of a workgroup
 
 // RB: blocks of 32 rows of a row tile
 template <int RB>
@@ -51,6 +49,8 @@ struct Tree {
   static constexpr bool WIDE = RB == kWaves;
   static constexpr int TK = RB == 1 ? 128 : WIDE ? 32 : 64;  // tokens of a tile
   static constexpr int SUB = TK / 32 / TS;          // 32-token pieces of a wavefront
+  static constexpr int LEAD = RB == 1 ? 2 : 4;      // places on the line of a unit's set-up and end
+  static constexpr int LEAST = RB == 1 ? 1 : 2;     // ... of a workgroup
   static constexpr int OWN = TK / kWaves;           // tokens of a tile that a wavefront loads
   static constexpr int LOADS = OWN / 4;             // its load instructions for K (and for V)
   static constexpr int BUFS = WIDE ? 4 : 2;         // tiles in LDS
@@ -140,7 +140,7 @@ __device__ __forceinline__ int64_t floor_sum(uint32_t n, uint32_t m, uint32_t a,
 // Places of a head's first `k` row tiles on the line.
 template <int RB>
 __device__ __forceinline__ int64_t places(TP& P, const Seq& s, int k) {
-  constexpr int TK = Tree<RB>::TK;
+  constexpr int TK = Tree<RB>::TK, kLead = Tree<RB>::LEAD;
   if (k == 0) return 0;                            // (a sequence of no nodes has no tiles)
   const int64_t all = (s.context + s.n + TK - 1) / TK;
   if (P.words || s.tiles == 1) return k * (kLead + all);
@@ -148,6 +148,25 @@ __device__ __forceinline__ int64_t places(TP& P, const Seq& s, int k) {
   const int64_t sum = floor_sum(min(k, s.tiles - 1), TK, P.nodes, s.context + P.nodes + TK - 1);
   return (int64_t)k * kLead + sum + (k == s.tiles ? all : 0);
 }
+
+// Sums of lanes 0 .. lane: within rows of 16 lanes, then over them.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int64_t add_lanes(int64_t x) {
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xf, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(x >> 32), CTRL, ROWS, 0xf, false);
+  return x + (int64_t)((uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ int64_t scan(int64_t x) {
+  x = add_lanes<0x111, 0xf>(x);   // row_shr:1, 2, 4, 8
+  x = add_lanes<0x112, 0xf>(x);
+  x = add_lanes<0x114, 0xf>(x);
+  x = add_lanes<0x118, 0xf>(x);
+  x = add_lanes<0x142, 0xa>(x);   // row_bcast:15 into rows 1 and 3
+  return add_lanes<0x143, 0xc>(x);  // row_bcast:31 into rows 2 and 3
+}
+// a / b for 0 <= a < 2^52, 0 < b: the quotient in fp64, rounded to nearest, reaches no
+// whole number that the exact one does not (which is at least 1 / b from it).
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) { return (int64_t)((double)a / (double)b); }
 
 __device__ __forceinline__ int64_t uniform(int64_t x) {
   const uint32_t lo = __builtin_amdgcn_readfirstlane((int)x), hi = __builtin_amdgcn_readfirstlane((int)(x >> 32));
@@ -202,8 +221,8 @@ __device__ __forceinline__ bool not_finite(uint32_t w) {
 }
 
 // Which of nodes j0 .. j0 + 31 row node i sees (bit k: node j0 + k; nodes below 0
-// are context).
-__device__ __forceinline__ uint32_t sees(TP& P, const uint64_t* mask, int i, int n, int j0) {
+// are context).  `word0`: the mask's first word.
+__device__ __forceinline__ uint32_t sees(TP& P, const uint64_t* mask, uint64_t word0, int i, int n, int j0) {
   if (j0 <= -32) return 0xffffffffu;
   uint64_t v;
   int count;                     // of the 32 that may be seen
@@ -213,10 +232,10 @@ __device__ __forceinline__ uint32_t sees(TP& P, const uint64_t* mask, int i, int
   } else {
     count = n - j0;
     if (j0 < 0) {
-      v = mask[0] << -j0 | ((1ull << -j0) - 1);
+      v = word0 << -j0 | ((1ull << -j0) - 1);
     } else {
       const int w = j0 >> 6, sh = j0 & 63;
-      v = w < P.words ? mask[w] >> sh : 0;
+      v = (w == 0 ? word0 : w < P.words ? mask[w] : 0) >> sh;
       if (sh > 32 && w + 1 < P.words) v |= mask[w + 1] << (64 - sh);
     }
   }
@@ -268,15 +287,7 @@ __global__ void __launch_bounds__(kThreads, 2) tree_kernel(const TreeParams) {
     own += P.kv_heads * places<RB>(P, s, s.tiles);
     mine += (int64_t)P.kv_heads * s.tiles;
   }
-  int64_t before = own, earlier = mine;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int64_t x = __shfl_up((long long)before, o), y = __shfl_up((long long)earlier, o);
-    if (lane >= o) {
-      before += x;
-      earlier += y;
-    }
-  }
+  int64_t before = scan(own), earlier = scan(mine);
   if (lane == 63) {
     s_scan[0][wave] = before;
     s_scan[1][wave] = earlier;
@@ -295,7 +306,7 @@ __global__ void __launch_bounds__(kThreads, 2) tree_kernel(const TreeParams) {
   before -= own;
   earlier -= mine;
   line = uniform(line);
-  const int64_t workers = min((int64_t)gridDim.x, max(line / kLeast, (int64_t)1));
+  const int64_t workers = min((int64_t)gridDim.x, max(line / C::LEAST, (int64_t)1));
   // Workgroups go to the eight XCDs in turn: each XCD gets one stretch of the line, so
   // that row tiles of the same keys meet in its L2.
   const int64_t me = gridDim.x % 8 ? blockIdx.x : blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8;
@@ -308,7 +319,7 @@ __global__ void __launch_bounds__(kThreads, 2) tree_kernel(const TreeParams) {
     }
   }
   if (me >= workers) return;
-  const int64_t begin = uniform(me * line / workers), end = uniform((me + 1) * line / workers);
+  const int64_t begin = uniform(quotient(me * line, workers)), end = uniform(quotient((me + 1) * line, workers));
   if (begin >= end) return;
   if (before <= begin && begin < before + own) {
     int b = b0;
@@ -382,7 +393,7 @@ __global__ void __launch_bounds__(kThreads, 2) tree_kernel(const TreeParams) {
     s.n = uniform(s.n);
     s.context = uniform(s.context);
     s.tiles = uniform(s.tiles);
-    const int kvh = uniform((int)((x - base) / each));
+    const int kvh = uniform((int)quotient(x - base, each));
     const int64_t at = x - base - kvh * each;
     int rt = 0, rt_end = s.tiles;                      // the last row tile whose places begin at or before
     while (rt_end - rt > 1) {
@@ -393,8 +404,8 @@ __global__ void __launch_bounds__(kThreads, 2) tree_kernel(const TreeParams) {
     rt = uniform(rt);
     const int64_t start = base + kvh * each + uniform(places<RB>(P, s, rt));
     const int seen = uniform(tokens_of(P, s, rt)), all = (seen + C::TK - 1) / C::TK;
-    const int64_t next = min(end, start + kLead + all);
-    const int t0 = uniform(max((int)(x - start) - kLead, 0)), t1 = uniform((int)(next - start) - kLead);
+    const int64_t next = min(end, start + C::LEAD + all);
+    const int t0 = uniform(max((int)(x - start) - C::LEAD, 0)), t1 = uniform((int)(next - start) - C::LEAD);
     if (C::WIDE && !rest && x == begin && start < begin && next < end) {
       put_off = true;
       x = next;
@@ -403,7 +414,7 @@ __global__ void __launch_bounds__(kThreads, 2) tree_kernel(const TreeParams) {
     x = rest ? end : next;
     if (t1 <= t0) continue;                            // only places before its tiles
     const bool begins = t0 == 0, whole = begins && t1 == all;
-    const int64_t last = ((start + kLead + all) * workers - 1) / line;   // who holds its last place
+    const int64_t last = quotient((start + C::LEAD + all) * workers - 1, line);   // who holds its last place
 
     const int node0 = rt * P.nodes, M = min(P.nodes, s.n - node0) * P.group;
     bf16x8 qf[8];
@@ -419,12 +430,9 @@ __global__ void __launch_bounds__(kThreads, 2) tree_kernel(const TreeParams) {
       }
       qf[i] = __builtin_bit_cast(bf16x8, w);
     }
+    const uint64_t mask0 = P.words ? mask[0] : 0;
     f32x16 acc[4];
-    float m = kNegInf, l = 0.f;
-#pragma unroll
-    for (int d = 0; d < 4; ++d)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) acc[d][r] = 0.f;
+    float m, l;
 
     // Pages: lane i has that of the wavefront's 16-token group i from tile `paged` on,
     // and of 64 more, asked for that much ahead.
@@ -437,6 +445,7 @@ __global__ void __launch_bounds__(kThreads, 2) tree_kernel(const TreeParams) {
       return min(max(page, 0), P.num_pages - 1);
     };
     int paged = t0, pages = pages_from(t0), more_pages = t0 + kAhead < t1 ? pages_from(t0 + kAhead) : 0;
+    const int pages0 = pages, more_pages0 = more_pages;
     const uint8_t* const k_head = reinterpret_cast<const uint8_t*>(P.k + kvh * P.ks_head);
     const uint8_t* const v_head = reinterpret_cast<const uint8_t*>(P.v + kvh * P.vs_head);
     const int64_t k_page = P.ks_page * 2, v_page = P.vs_page * 2;
@@ -487,9 +496,10 @@ __global__ void __launch_bounds__(kThreads, 2) tree_kernel(const TreeParams) {
     const int open = P.words ? s.context : s.context + node0 + 1;
     auto is_tail = [&](int t) { return (t + 1) * C::TK > open; };
 
-    // Infinities and NaN among the nodes' values: 0 times them is no 0, and a row that
-    // does not see them must not get them.  Rows that do get them added, then they
-    // leave the tile.
+    // Infinities and NaN among the values: a row that does not see them must not get
+    // them, but 0 times them is no 0 (and a probability's lower parts may be 0).  Sums
+    // that are not finite are therefore made again, with care: rows that see such a
+    // value get it added, and it leaves the tile.
     auto clean = [&](int t, int buf) __attribute__((always_inline)) {
       __syncthreads();     // (a wavefront may have waited for its own tokens only)
       uint16_t* const s_v = reinterpret_cast<uint16_t*>(lds + buf * C::TILE_BYTES) + C::TK * kD;
@@ -505,7 +515,7 @@ __global__ void __launch_bounds__(kThreads, 2) tree_kernel(const TreeParams) {
         const int r = place(0) + k, tok = t * C::TK + r;
         // (-1 where the row sees the token: no branch for each of the sums)
         uint32_t see;
-        see = tok < seen && (sees(P, mask, node, s.n, tok - s.context) & 1u) ? ~0u : 0u;
+        see = tok < seen && (sees(P, mask, mask0, node, s.n, tok - s.context) & 1u) ? ~0u : 0u;
 #pragma unroll
         for (int d = 0; d < 4; ++d)
 #pragma unroll
@@ -553,7 +563,7 @@ __global__ void __launch_bounds__(kThreads, 2) tree_kernel(const TreeParams) {
     };
     auto hide = [&](int t, int sub, f32x16& st) __attribute__((always_inline)) {
       TP& P = *fresh(args);
-      const uint32_t bits = sees(P, mask, node, s.n, t * C::TK + place(sub) - s.context) >> (4 * half);
+      const uint32_t bits = sees(P, mask, mask0, node, s.n, t * C::TK + place(sub) - s.context) >> (4 * half);
 #pragma unroll
       for (int r = 0; r < 16; ++r)
         if (!(bits >> (8 * (r >> 2) + (r & 3)) & 1u)) st[r] = kNegInf;
@@ -622,156 +632,175 @@ __global__ void __launch_bounds__(kThreads, 2) tree_kernel(const TreeParams) {
       products(at, p);
     };
 
-    __syncthreads();       // the segment before has left LDS
-    if constexpr (C::WIDE) {
-      // Four tiles in LDS: one whose probabilities are in work, the next with its
-      // scores, and two on their way.
-      const int first_tail = max(min(open / C::TK, t1), t0);
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (t0 + i < t1) load_tile(t0 + i, i);
-      wait_loads<0>();
-      barrier();
-      int t = t0;
-      if (t + 8 < first_tail) {
-        f32x16 st;
-        float top;
-        bf16x8 k_part[8];
-        scores(0, st);
-        tops(st, top);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) k_part[i] = key_part(C::TILE_BYTES, i);
-        // One tile, in buffer B, and the next one's scores, whose keys are in registers;
-        // then that buffer is free for the tile four further, and the keys two further
-        // are there.  (All of it is before the tail: every row of a tile exists.)  No
-        // branch but the reference's.
-        auto step = [&](auto B, int t) __attribute__((always_inline)) {
-          constexpr int kB = decltype(B)::value, kHere = kB * C::TILE_BYTES;
-          constexpr int kNext = (kB + 1) % 4 * C::TILE_BYTES, kAfter = (kB + 2) % 4 * C::TILE_BYTES;
-          uint8_t* const free_place = lds + kHere + wave * C::OWN * kD * 2;
-          f32x16 next_st;
-          refer(top);
-          const int at = t + 4 - paged, here = __builtin_amdgcn_readlane(pages, at & 63);
-          const int ahead = __builtin_amdgcn_readlane(more_pages, at & 63), page = at < kAhead ? here : ahead;
-          const int first = (t + 4) * C::TK + wave * C::OWN;
-          if constexpr (PARTS > 1) {
-            scores(kNext, next_st);
-            weigh(kHere, st);
-            wait_loads<2 * C::LOADS>();
-            barrier();
-            load_rows(first, page, free_place);
-            tops(next_st, top);
-          } else {
-            // In this order: two probabilities and a piece of V behind every matrix
-            // instruction of the scores, maxima, keys and loads behind those of the
-            // products.  V is in registers by then, so the barrier comes between.
-            bf16x8 v_part[8];
-            uint32_t w[8];
-            const uint8_t *k16 = nullptr, *v16 = nullptr;
-            const float ref = m == kNegInf ? 0.f : m;
-#pragma unroll
-            for (int r = 0; r < 16; ++r) next_st[r] = 0.f;
-            __builtin_amdgcn_s_setprio(1);
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              if (i == 1) k16 = k_head + page * k_page;
-              if (i == 2) v16 = v_head + page * v_page;
-              if (i == 3) k16 += (uint64_t)(first & slots) * k_tok;
-              if (i == 4) v16 += (uint64_t)(first & slots) * v_tok;
-              next_st = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_part[i], qf[i], next_st, 0, 0, 0);
-              v_part[i] = value_part(kHere, i >> 2, i & 3);
-              const float x = fast_exp2(fmaf(st[2 * i], scale, -ref));
-              const float y = fast_exp2(fmaf(st[2 * i + 1], scale, -ref));
-              l += x;
-              l += y;
-              w[i] = pack_bf16(x, y);
-              __builtin_amdgcn_sched_barrier(0);
-            }
-            wait_loads<2 * C::LOADS>();
-            barrier();
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const uint32_t* const u = w + (i >> 2) * 4;
-              acc[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                  v_part[i], __builtin_bit_cast(bf16x8, u32x4{u[0], u[1], u[2], u[3]}), acc[i & 3], 0, 0, 0);
-              if (i == 0) top = next_st[0];
-              top = fmaxf(fmaxf(top, next_st[2 * i]), next_st[2 * i + 1]);
-              if (i == 7) top *= scale;
-              if (i < 4) {
-                k_part[2 * i] = key_part(kAfter, 2 * i);
-                k_part[2 * i + 1] = key_part(kAfter, 2 * i + 1);
-              } else if (i - 4 < kRows / 4) {
-                load_lds(k16 + (uint64_t)(4 * (i - 4) * k_tok), k_lane[i - 4], free_place + 4 * (i - 4) * kD * 2);
-                load_lds(v16 + (uint64_t)(4 * (i - 4) * v_tok), v_lane, free_place + C::TK * kD * 2 + 4 * (i - 4) * kD * 2);
-              }
-              __builtin_amdgcn_sched_barrier(0);
-            }
-            __builtin_amdgcn_s_setprio(0);
-          }
-          st = next_st;
-        };
 #pragma unroll 1
-        for (; t + 8 < first_tail; t += 4) {
-          if (t + 4 >= paged + kAhead) next_pages();
-          step(std::integral_constant<int, 0>{}, t);
-          step(std::integral_constant<int, 1>{}, t + 1);
-          step(std::integral_constant<int, 2>{}, t + 2);
-          step(std::integral_constant<int, 3>{}, t + 3);
-        }
-      }
-      // (behind the steps: the tile of the pending scores again, from its keys)
-#pragma unroll 1
-      for (; t < t1; ++t) {
-        const int buf = (t - t0) & 3;
-        const bool tail = t >= first_tail;
-        if (tail) clean(t, buf);
-        f32x16 st;
-        scores(buf * C::TILE_BYTES, st);
-        if (tail) hide(t, 0, st);
-        float top;
-        tops(st, top);
-        refer(top);
-        weigh(buf * C::TILE_BYTES, st);
-        if (t + 1 < t1) {
-          // the next tile is there, and this one has been used up
-          if (t + 3 < t1) wait_loads<4 * C::LOADS>();
-          else wait_loads<0>();
-          barrier();
-          if (t + 4 < t1) load_tile(t + 4, buf);
-        }
-      }
-    } else {
-      load_tile(t0, t0 & 1);
-#pragma unroll 1
-      for (int t = t0; t < t1; ++t) {
-        if constexpr (C::TS == kWaves) {
-          // a wavefront works on the tokens that it loads itself: no other's are waited for
-          end_reads();
-          if (t + 1 < t1) {
-            load_tile(t + 1, (t + 1) & 1);
-            wait_loads<2 * C::LOADS>();
-          } else {
-            wait_loads<0>();
-          }
-        } else {
-          wait_loads<0>();
-          barrier();       // the tile is there, and the one before it has been read
-          if (t + 1 < t1) load_tile(t + 1, (t + 1) & 1);
-        }
-        if (is_tail(t)) clean(t, t & 1);
+    for (bool careful = false;; careful = true) {
+      m = kNegInf;
+      l = 0.f;
 #pragma unroll
-        for (int sub = 0; sub < C::SUB; ++sub) {
-          const int at = (t & 1) * C::TILE_BYTES + place(sub) * kD * 2;
+      for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[d][r] = 0.f;
+      __syncthreads();     // the segment before has left LDS
+      if constexpr (C::WIDE) {
+        // Four tiles in LDS: one whose probabilities are in work, the next with its
+        // scores, and two on their way.
+        const int first_tail = max(min(open / C::TK, t1), t0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (t0 + i < t1) load_tile(t0 + i, i);
+        wait_loads<0>();
+        barrier();
+        int t = t0;
+        if (!careful && t + 8 < first_tail) {
           f32x16 st;
-          scores(at, st);
-          if (is_tail(t)) hide(t, sub, st);
+          float top;
+          bf16x8 k_part[8];
+          scores(0, st);
+          tops(st, top);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) k_part[i] = key_part(C::TILE_BYTES, i);
+          // One tile, in buffer B, and the next one's scores, whose keys are in registers;
+          // then that buffer is free for the tile four further, and the keys two further
+          // are there.  (All of it is before the tail: every row of a tile exists.)  No
+          // branch but the reference's.
+          auto step = [&](auto B, int t) __attribute__((always_inline)) {
+            constexpr int kB = decltype(B)::value, kHere = kB * C::TILE_BYTES;
+            constexpr int kNext = (kB + 1) % 4 * C::TILE_BYTES, kAfter = (kB + 2) % 4 * C::TILE_BYTES;
+            uint8_t* const free_place = lds + kHere + wave * C::OWN * kD * 2;
+            f32x16 next_st;
+            refer(top);
+            const int at = t + 4 - paged, here = __builtin_amdgcn_readlane(pages, at & 63);
+            const int ahead = __builtin_amdgcn_readlane(more_pages, at & 63), page = at < kAhead ? here : ahead;
+            const int first = (t + 4) * C::TK + wave * C::OWN;
+            if constexpr (PARTS > 1) {
+              scores(kNext, next_st);
+              weigh(kHere, st);
+              wait_loads<2 * C::LOADS>();
+              barrier();
+              load_rows(first, page, free_place);
+              tops(next_st, top);
+            } else {
+              // In this order: two probabilities and a piece of V behind every matrix
+              // instruction of the scores, maxima, keys and loads behind those of the
+              // products.  V is in registers by then, so the barrier comes between.
+              bf16x8 v_part[8];
+              uint32_t w[8];
+              const uint8_t *k16 = nullptr, *v16 = nullptr;
+              const float ref = m == kNegInf ? 0.f : m;
+#pragma unroll
+              for (int r = 0; r < 16; ++r) next_st[r] = 0.f;
+              __builtin_amdgcn_s_setprio(1);
+              __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                if (i == 1) k16 = k_head + page * k_page;
+                if (i == 2) v16 = v_head + page * v_page;
+                if (i == 3) k16 += (uint64_t)(first & slots) * k_tok;
+                if (i == 4) v16 += (uint64_t)(first & slots) * v_tok;
+                next_st = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_part[i], qf[i], next_st, 0, 0, 0);
+                v_part[i] = value_part(kHere, i >> 2, i & 3);
+                const float x = fast_exp2(fmaf(st[2 * i], scale, -ref));
+                const float y = fast_exp2(fmaf(st[2 * i + 1], scale, -ref));
+                l += x;
+                l += y;
+                w[i] = pack_bf16(x, y);
+                __builtin_amdgcn_sched_barrier(0);
+              }
+              wait_loads<2 * C::LOADS>();
+              barrier();
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                const uint32_t* const u = w + (i >> 2) * 4;
+                acc[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                    v_part[i], __builtin_bit_cast(bf16x8, u32x4{u[0], u[1], u[2], u[3]}), acc[i & 3], 0, 0, 0);
+                if (i == 0) top = next_st[0];
+                top = fmaxf(fmaxf(top, next_st[2 * i]), next_st[2 * i + 1]);
+                if (i == 7) top *= scale;
+                if (i < 4) {
+                  k_part[2 * i] = key_part(kAfter, 2 * i);
+                  k_part[2 * i + 1] = key_part(kAfter, 2 * i + 1);
+                } else if (i - 4 < kRows / 4) {
+                  load_lds(k16 + (uint64_t)(4 * (i - 4) * k_tok), k_lane[i - 4], free_place + 4 * (i - 4) * kD * 2);
+                  load_lds(v16 + (uint64_t)(4 * (i - 4) * v_tok), v_lane, free_place + C::TK * kD * 2 + 4 * (i - 4) * kD * 2);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+              }
+              __builtin_amdgcn_s_setprio(0);
+            }
+            st = next_st;
+          };
+#pragma unroll 1
+          for (; t + 8 < first_tail; t += 4) {
+            if (t + 4 >= paged + kAhead) next_pages();
+            step(std::integral_constant<int, 0>{}, t);
+            step(std::integral_constant<int, 1>{}, t + 1);
+            step(std::integral_constant<int, 2>{}, t + 2);
+            step(std::integral_constant<int, 3>{}, t + 3);
+          }
+        }
+        // (behind the steps: the tile of the pending scores again, from its keys)
+#pragma unroll 1
+        for (; t < t1; ++t) {
+          const int buf = (t - t0) & 3;
+          const bool tail = t >= first_tail;
+          if (careful) clean(t, buf);
+          f32x16 st;
+          scores(buf * C::TILE_BYTES, st);
+          if (tail) hide(t, 0, st);
           float top;
           tops(st, top);
           refer(top);
-          weigh(at, st);
+          weigh(buf * C::TILE_BYTES, st);
+          if (t + 1 < t1) {
+            // the next tile is there, and this one has been used up
+            if (t + 3 < t1) wait_loads<4 * C::LOADS>();
+            else wait_loads<0>();
+            barrier();
+            if (t + 4 < t1) load_tile(t + 4, buf);
+          }
+        }
+      } else {
+        load_tile(t0, t0 & 1);
+#pragma unroll 1
+        for (int t = t0; t < t1; ++t) {
+          if constexpr (C::TS == kWaves) {
+            // a wavefront works on the tokens that it loads itself: no other's are waited for
+            end_reads();
+            if (t + 1 < t1) {
+              load_tile(t + 1, (t + 1) & 1);
+              wait_loads<2 * C::LOADS>();
+            } else {
+              wait_loads<0>();
+            }
+          } else {
+            wait_loads<0>();
+            barrier();       // the tile is there, and the one before it has been read
+            if (t + 1 < t1) load_tile(t + 1, (t + 1) & 1);
+          }
+          if (careful) clean(t, t & 1);
+#pragma unroll
+          for (int sub = 0; sub < C::SUB; ++sub) {
+            const int at = (t & 1) * C::TILE_BYTES + place(sub) * kD * 2;
+            f32x16 st;
+            scores(at, st);
+            if (is_tail(t)) hide(t, sub, st);
+            float top;
+            tops(st, top);
+            refer(top);
+            weigh(at, st);
+          }
         }
       }
+      float all_finite = 0.f;
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) all_finite = fmaf(acc[d][r], 0.f, all_finite);
+      // (the tiles have been read, too)
+      if (!__syncthreads_or(!(all_finite == 0.f)) || careful) break;
+      paged = t0;
+      pages = pages0;
+      more_pages = more_pages0;
     }
 
     // ---- the wavefronts' records, joined ----
@@ -780,7 +809,6 @@ __global__ void __launch_bounds__(kThreads, 2) tree_kernel(const TreeParams) {
     const int64_t row0 = (int64_t)(s.first + node0) * W.q_heads + kvh * W.group;
     float l0, l1;
     swap_rows32(l, l0, l1);
-    __syncthreads();
     float* const rec = s_rec + wave * 32 * C::PITCH;
 #pragma unroll
     for (int d = 0; d < 4; ++d)
@@ -906,6 +934,8 @@ art_status plan_tree(const art_decode_shape* s, const art_tree_opts* o, TreePlan
   p->nodes = rows_of(p->rb) / g;
   const int tk = p->rb == 1 ? 128 : p->rb == 2 ? 64 : 32;
   const int64_t units = (int64_t)s->num_kv_heads * (o->rows / p->nodes + s->batch);   // at most
+  // places on the line, by 512 workgroups, are counted in 52 bits
+  if (units >= (int64_t(1) << 40) / ((cap + tk - 1) / tk + 4)) return ART_ERR_UNSUPPORTED;
   const int64_t tiles = units < kMaxWorkers ? units * ((cap + tk - 1) / tk) : units;
   p->workers = (int)(tiles < kMaxWorkers ? (tiles < 1 ? 1 : tiles) : kMaxWorkers);
   p->slots = (int)(units < p->workers ? units : p->workers);
