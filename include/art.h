@@ -573,7 +573,8 @@ art_status art_rope_append(const art_decode_shape* shape, const art_rope* rope, 
  *   positions  int32 [rows], out, or NULL: context_lens[b] plus the node's depth
  *              (node 0 has depth 0).
  * A parent that is not an earlier node (-1 among them) ends the walk.  1 <=
- * mask_words <= 16; sequences of more than ART_MAX_NODES nodes are passed over.
+ * mask_words <= 16; sequences of more than ART_MAX_NODES nodes are passed over
+ * (without row_offsets the call is refused).
  */
 #define ART_MAX_NODES 1024
 art_status art_tree_layout(int32_t batch, int32_t rows, const int32_t* parents,
@@ -595,12 +596,14 @@ art_status art_tree_layout(int32_t batch, int32_t rows, const int32_t* parents,
  *          sum_j p_j v_j / sum_j p_j, p_j = exp(softmax_scale q.k_j)
  *   lse    fp32 [rows][num_q_heads]: ln of sum_j p_j
  * A row that sees nothing gets zeros and -inf (scores of -inf count as unseen).
+ * An infinite value that a row sees makes that dim of its output infinite, two of
+ * both signs or a NaN make it NaN; the other dims are as without it.
  * Values of V within 2^118 over the number of tokens cannot overflow the sums,
  * which are held in fp32.  With an fp32 output probabilities carry 24 bits, with
  * a bf16 output 8 (as the output itself).
  * Shape fields used: those of art_decode_attention but block_size and the list's;
- * num_q_heads / num_kv_heads is any whole number up to 128, and token strides are
- * less than 2^27 elements.
+ * num_q_heads / num_kv_heads is any whole number up to 128, token strides are less
+ * than 2^27 elements, and max_pages_per_seq * page_size less than 2^31 - 2^16.
  */
 typedef struct {
     float softmax_scale;
@@ -649,7 +652,7 @@ art_status art_tree_attention(const art_decode_shape* shape, const art_tree_opts
  *   counts       int32 [batch], out: their number
  *   next_tokens  int32 [batch], out
  * A sequence of no nodes, or of more than ART_MAX_NODES, gets 0, -1 and a row of
- * -1.  target and draft have the same type; row strides in elements, any that are
+ * -1 (without row_offsets the latter is refused).  target and draft have the same type; row strides in elements, any that are
  * >= vocab, and any alignment to the type.  vocab < 2^24.
  */
 typedef struct {

@@ -552,6 +552,7 @@ art_status art_tree_layout(int32_t batch, int32_t rows, const int32_t* parents, 
   if (batch < 0 || rows < 0 || mask_words < 1) return ART_ERR_INVALID_ARG;
   if (!row_offsets && batch > 0 && rows % batch) return ART_ERR_INVALID_ARG;
   if (mask_words > 16 || batch >= (1 << 24)) return ART_ERR_UNSUPPORTED;   // a launch has less than 2^32 threads
+  if (!row_offsets && batch > 0 && rows / batch > ART_MAX_NODES) return ART_ERR_UNSUPPORTED;
   if (batch == 0 || rows == 0) return ART_OK;
   if (!parents || !mask || (positions && !context_lens) || (uintptr_t)mask % 8) return ART_ERR_INVALID_ARG;
   LayoutParams p;
@@ -587,6 +588,7 @@ art_status art_verify_drafts(const art_verify_opts* opts, const void* target, co
   if (status != ART_OK) return (art_status)status;
   if (draft && opts->draft_stride < opts->vocab) return ART_ERR_INVALID_ARG;
   if (!row_offsets && opts->batch > 0 && opts->rows % opts->batch) return ART_ERR_INVALID_ARG;
+  if (!row_offsets && opts->batch > 0 && opts->rows / opts->batch > ART_MAX_NODES) return ART_ERR_UNSUPPORTED;
   if (opts->batch == 0) return ART_OK;
   if (!accepted || !counts || !next_tokens || !last_uniforms ||
       (opts->rows > 0 && (!target || !tokens || !parents || !uniforms)))

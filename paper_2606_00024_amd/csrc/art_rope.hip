@@ -110,13 +110,16 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const RopeParams P) {
   const int half = P.rot >> 1;
   float c = 1.f, sn = 0.f;
   if (lane < half) {
-    // turns: 1 / 2 pi in fp64 costs 2^-53 of them, and what is left after the
-    // nearest integer is rounded to fp32 (2^-26 of a turn)
-    double t = (double)position * (P.freqs[lane] * 0.15915494309189535);
-    t -= rint(t);
-    sincospif((float)(2.0 * t), &sn, &c);
-    c *= P.scale;
-    sn *= P.scale;
+    // half turns: 1 / pi in fp64 costs 2^-53 of them.  What is left after the nearest
+    // whole turn goes to the functions as fp32, and what that leaves of it (2^-25) in
+    // by the first order.
+    double t = (double)position * (P.freqs[lane] * 0.3183098861837907);
+    t -= 2.0 * rint(0.5 * t);
+    const float near = (float)t, rest = (float)((t - near) * 3.141592653589793);
+    float s0, c0;
+    sincospif(near, &s0, &c0);
+    c = fmaf(-rest, s0, c0) * P.scale;
+    sn = fmaf(rest, c0, s0) * P.scale;
   }
   s_turn[wave][lane] = make_float2(c, sn);
   __builtin_amdgcn_wave_barrier();

@@ -69,7 +69,7 @@ struct TreeParams {
   int32_t slots;               // entries of `units`
   int32_t by_unit;             // entries are units (else workgroups)
   int32_t out_bf16, negate;    // negate: a negative scale
-  float scale_log2;            // its magnitude
+  float scale_log2, scale_rest;  // its magnitude: rounded down to fp32, and what that leaves
   int64_t qs_row, qs_head;
   int64_t ks_page, ks_head, ks_tok, vs_page, vs_head, vs_tok;
   const int32_t* offsets;
@@ -570,7 +570,7 @@ __global__ void __launch_bounds__(kThreads, 2) tree_kernel(const TreeParams) {
     };
     // The reference m moves only where a score passes it by more than 2^8 (and at the
     // first score): sums keep their relative precision either way.
-    const float scale = P.scale_log2;
+    const float scale = P.scale_log2, scale_rest = P.scale_rest;
     auto tops = [&](const f32x16& st, float& top) __attribute__((always_inline)) {
       top = st[0];
 #pragma unroll
@@ -596,7 +596,10 @@ __global__ void __launch_bounds__(kThreads, 2) tree_kernel(const TreeParams) {
       const float ref = m == kNegInf ? 0.f : m;
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        st[r] = fast_exp2(fmaf(st[r], scale, -ref));
+        // (where fp32 is kept, the scale's own rounding would move large scores by more
+        // than their own does)
+        const float x = PARTS > 1 ? fmaf(st[r], scale_rest, -ref) : -ref;
+        st[r] = fast_exp2(fmaf(st[r], scale, x));
         l += st[r];
       }
 #pragma unroll
@@ -925,7 +928,7 @@ art_status plan_tree(const art_decode_shape* s, const art_tree_opts* o, TreePlan
     return ART_ERR_INVALID_ARG;
   const int g = s->num_q_heads / s->num_kv_heads;
   const int64_t cap = (int64_t)s->max_pages_per_seq * s->page_size;
-  if (g > 128 || s->num_kv_heads >= (1 << 20) || o->rows >= (1 << 24) || s->batch >= (1 << 20) || cap >= (1ll << 31) - 256 ||
+  if (g > 128 || s->num_kv_heads >= (1 << 20) || o->rows >= (1 << 24) || s->batch >= (1 << 20) || cap >= (1ll << 31) - (1 << 16) ||
       (o->q_stride_row | o->q_stride_head) % 8 || s->k_stride_token >= (1 << 27) || s->v_stride_token >= (1 << 27))
     return ART_ERR_UNSUPPORTED;
   // a row tile that holds a sequence's rows, on average
@@ -1006,8 +1009,13 @@ art_status art_tree_attention(const art_decode_shape* shape, const art_tree_opts
   p.out_bf16 = opts->out_dtype == ART_OUT_BF16;
   p.negate = opts->softmax_scale < 0.f;
   // (a scale of 0 weighs all tokens alike; hidden scores of -inf times 0 would not be -inf)
-  p.scale_log2 = (float)(fabs((double)opts->softmax_scale) * 1.4426950408889634);
+  const double scale_log2 = fabs((double)opts->softmax_scale) * 1.4426950408889634;
+  // (both above 0: a hidden score of -inf stays one under either)
+  p.scale_log2 = (float)scale_log2;
+  if (p.scale_log2 > scale_log2) p.scale_log2 = nextafterf(p.scale_log2, 0.f);
+  p.scale_rest = (float)(scale_log2 - p.scale_log2);
   if (p.scale_log2 < 1e-37f) p.scale_log2 = 1e-37f;
+  if (p.scale_rest < 1e-37f) p.scale_rest = 1e-37f;
   p.qs_row = opts->q_stride_row;
   p.qs_head = opts->q_stride_head;
   p.ks_page = shape->k_stride_page;

@@ -147,7 +147,7 @@ def test_layout_refusals():
     assert call(batch=-1) == BAD and call(rows=-1) == BAD and call(rows=5) == BAD and call(words=0) == BAD
     assert call(words=17) == NO and call(parents=0) == BAD and call(mask=0) == BAD and call(mask=PTR + 4) == BAD
     assert call(context=0) == BAD
-    assert call(rows=0, mask=0) == OK and call(batch=0) == OK
+    assert call(rows=2050) == NO and call(rows=0, mask=0) == OK and call(batch=0) == OK
 
 
 def test_tree_refusals():
@@ -158,7 +158,7 @@ def test_tree_refusals():
     assert _tree(opts=_tree_opts(q_stride_head=4)) == NO and _tree(opts=_tree_opts(rows=1 << 24)) == NO
     assert _tree(_shape(num_q_heads=7)) == BAD and _tree(_shape(num_q_heads=0)) == BAD
     assert _tree(_shape(num_q_heads=258)) == NO
-    assert _tree(_shape(max_pages_per_seq=1 << 25)) == NO
+    assert _tree(_shape(max_pages_per_seq=1 << 25)) == NO and _tree(_shape(max_pages_per_seq=(1 << 25) - 1024)) == NO
     for name in ("q", "k", "v", "page_table", "context_lens", "out", "lse"):
         assert _tree(**{name: 0}) == BAD, name
     for name in ("q", "k", "v", "out"):
@@ -186,7 +186,7 @@ def test_verify_refusals():
     for name in ("target", "tokens", "parents", "uniforms", "last_uniforms", "accepted", "counts", "next_tokens"):
         assert _verify(**{name: 0}) == BAD, name
     assert _verify(target=PTR + 2) == BAD and _verify(draft=PTR + 1) == BAD and _verify(workspace=PTR + 4) == BAD
-    assert _verify(workspace=0) == SMALL
+    assert _verify(_verify_opts(rows=2050)) == NO and _verify(workspace=0) == SMALL
     assert _verify(workspace_bytes=_lib.verify_workspace_bytes(_verify_opts()) - 1) == SMALL
     assert _verify(_verify_opts(batch=0)) == OK
 

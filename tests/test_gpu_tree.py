@@ -178,6 +178,32 @@ def test_a_value_of_the_context_reaches_all():
     assert bool((live[..., 7] == math.inf).all()) and bool(torch.isfinite(live[..., :7]).all())
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("held, new, heads", [(300, 5, (4, 2)), (700, 30, (2, 1)), (1500, 40, (8, 1)), (9000, 3, (2, 1))], ids=str)
+def test_infinities_that_are_seen(held, new, heads, dtype):
+    """Infinities and NaN in the context, far from the nodes and near: their dims are
+    infinite or NaN in every row, the other dims as the definition has them."""
+    p = Problem([held], [new], heads, seed=25)
+    odd = {7: (3, math.inf), 64: (held // 2, -math.inf), 65: (held - 1, math.nan), 127: (held // 3, math.inf)}
+    cache = p.cache.to(DEV)
+    for dim, (t, x) in odd.items():
+        p.cache.v[p.cache.table[0, t // 16].long(), :, t % 16, dim] = 0
+        cache.v[cache.table[0, t // 16].long(), :, t % 16, dim] = x
+    # both signs in one dim
+    for t, x in ((5, math.inf), (held - 2, -math.inf)):
+        p.cache.v[p.cache.table[0, t // 16].long(), :, t % 16, 100] = 0
+        cache.v[cache.table[0, t // 16].long(), :, t % 16, 100] = x
+    out, lse = (x.double().cpu()[p.lead: -p.lead] for x in p.run(dtype, cache=cache))
+    for dim, (_, x) in odd.items():
+        assert bool((out[..., dim].isnan() if math.isnan(x) else out[..., dim] == x).all()), dim
+    assert bool(out[..., 100].isnan().all())
+    ref = R.attend(p.q, p.cache.k, p.cache.v, p.cache.table, p.context, p.offsets, p.mask, p.scale)
+    far, far_lse = (x[p.lead: -p.lead] for x in R.attend_bounds(*ref, dtype is torch.bfloat16))
+    plain = [d for d in range(128) if d not in odd and d != 100]
+    assert bool(((out - ref[0][p.lead: -p.lead]).abs() <= far)[..., plain].all())
+    assert bool(((lse - ref[1][p.lead: -p.lead]).abs() <= far_lse).all())
+
+
 @pytest.mark.parametrize("scale", [0.0, -0.1, 3.0, 1e-30])
 def test_scales(scale):
     p = Problem([300], [9], (4, 2), seed=17)
