@@ -48,9 +48,12 @@ struct Tree {
   // with one's probabilities, so it has to be there before that one has been used up
   static constexpr bool WIDE = RB == kWaves;
   static constexpr int TK = RB == 1 ? 128 : WIDE ? 32 : 64;  // tokens of a tile
-  static constexpr int SUB = TK / 32 / TS;          // 32-token pieces of a wavefront
-  static constexpr int LEAD = RB == 1 ? 2 : 4;      // places on the line of a unit's set-up and end
-  static constexpr int LEAST = RB == 1 ? 1 : 2;     // ... of a workgroup
+  static_assert(TK == 32 * TS);                     // a piece of 32 tokens to a wavefront
+  // Places on the line of a unit's set-up and end (16 sequences of up to 2K tokens and
+  // 16 nodes 37 us, without them 51), and of a workgroup, at least (one of 4K tokens, 4
+  // heads to each of 2 KV heads 17 us, with four times as many 21).
+  static constexpr int LEAD = RB == 1 ? 2 : 4;
+  static constexpr int LEAST = RB == 1 ? 1 : 2;
   static constexpr int OWN = TK / kWaves;           // tokens of a tile that a wavefront loads
   static constexpr int LOADS = OWN / 4;             // its load instructions for K (and for V)
   static constexpr int BUFS = WIDE ? 4 : 2;         // tiles in LDS
@@ -490,8 +493,7 @@ __global__ void __launch_bounds__(kThreads, 2) tree_kernel(const TreeParams) {
         }
       }
     };
-    // the piece's first token of the tile
-    auto place = [&](int sub) { return 32 * (ts * C::SUB + sub); };
+    const int place = 32 * ts;     // the piece's first token of the tile
     // Tokens that every row of the tile sees; only behind them are rows told apart.
     const int open = P.words ? s.context : s.context + node0 + 1;
     auto is_tail = [&](int t) { return (t + 1) * C::TK > open; };
@@ -511,8 +513,8 @@ __global__ void __launch_bounds__(kThreads, 2) tree_kernel(const TreeParams) {
       }
       if (!__syncthreads_or(bad)) return;
 #pragma unroll 1
-      for (int k = 0; k < 32 * C::SUB; ++k) {
-        const int r = place(0) + k, tok = t * C::TK + r;
+      for (int k = 0; k < 32; ++k) {
+        const int r = place + k, tok = t * C::TK + r;
         // (-1 where the row sees the token: no branch for each of the sums)
         uint32_t see;
         see = tok < seen && (sees(P, mask, mask0, node, s.n, tok - s.context) & 1u) ? ~0u : 0u;
@@ -561,9 +563,9 @@ __global__ void __launch_bounds__(kThreads, 2) tree_kernel(const TreeParams) {
         st = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[i], st, 0, 0, 0);
       }
     };
-    auto hide = [&](int t, int sub, f32x16& st) __attribute__((always_inline)) {
+    auto hide = [&](int t, f32x16& st) __attribute__((always_inline)) {
       TP& P = *fresh(args);
-      const uint32_t bits = sees(P, mask, mask0, node, s.n, t * C::TK + place(sub) - s.context) >> (4 * half);
+      const uint32_t bits = sees(P, mask, mask0, node, s.n, t * C::TK + place - s.context) >> (4 * half);
 #pragma unroll
       for (int r = 0; r < 16; ++r)
         if (!(bits >> (8 * (r >> 2) + (r & 3)) & 1u)) st[r] = kNegInf;
@@ -749,7 +751,7 @@ __global__ void __launch_bounds__(kThreads, 2) tree_kernel(const TreeParams) {
           if (careful) clean(t, buf);
           f32x16 st;
           scores(buf * C::TILE_BYTES, st);
-          if (tail) hide(t, 0, st);
+          if (tail) hide(t, st);
           float top;
           tops(st, top);
           refer(top);
@@ -781,17 +783,14 @@ __global__ void __launch_bounds__(kThreads, 2) tree_kernel(const TreeParams) {
             if (t + 1 < t1) load_tile(t + 1, (t + 1) & 1);
           }
           if (careful) clean(t, t & 1);
-#pragma unroll
-          for (int sub = 0; sub < C::SUB; ++sub) {
-            const int at = (t & 1) * C::TILE_BYTES + place(sub) * kD * 2;
-            f32x16 st;
-            scores(at, st);
-            if (is_tail(t)) hide(t, sub, st);
-            float top;
-            tops(st, top);
-            refer(top);
-            weigh(at, st);
-          }
+          const int at = (t & 1) * C::TILE_BYTES + place * kD * 2;
+          f32x16 st;
+          scores(at, st);
+          if (is_tail(t)) hide(t, st);
+          float top;
+          tops(st, top);
+          refer(top);
+          weigh(at, st);
         }
       }
       float all_finite = 0.f;
@@ -931,16 +930,26 @@ art_status plan_tree(const art_decode_shape* s, const art_tree_opts* o, TreePlan
   if (g > 128 || s->num_kv_heads >= (1 << 20) || o->rows >= (1 << 24) || s->batch >= (1 << 20) || cap >= (1ll << 31) - (1 << 16) ||
       (o->q_stride_row | o->q_stride_head) % 8 || s->k_stride_token >= (1 << 27) || s->v_stride_token >= (1 << 27))
     return ART_ERR_UNSUPPORTED;
-  // a row tile that holds a sequence's rows, on average
+  // A row tile that holds a sequence's rows, on average.  32 rows at most: tiles of 128
+  // tokens, each wavefront for itself, one workgroup to a CU, read fastest (8 x 32K
+  // tokens, 32/8 heads, one node each: 192 us, 200 by tiles of 64 rows; one of 128K,
+  // one KV head, 30 and 39), but where units are many or all of them short, two
+  // workgroups to a CU end sooner (200 sequences of 50 to 150 tokens 46 us and 58; one of
+  // 4K tokens, 8 KV heads, 21 and 22).  Tiles of 64 rows serve 48 and 64 rows in 203 and
+  // 205 us where 128 rows take 227 and 228, and 96 and 128 rows in 266 and 270 where those
+  // take 232 and 235.
   const int64_t rows = s->batch > 0 ? ((int64_t)o->rows + s->batch - 1) / s->batch * g : 0;
-  p->rb = rows <= 32 && g <= 32 ? 1 : rows <= 64 && g <= 64 ? 2 : 4;
+  const int64_t groups = (int64_t)s->batch * s->num_kv_heads;
+  const bool few = rows <= 32 && g <= 32 && groups <= kMaxWorkers && groups * ((cap + 127) / 128) >= kMaxWorkers;
+  p->rb = few ? 1 : rows <= 64 && g <= 64 ? 2 : 4;
   p->nodes = rows_of(p->rb) / g;
   const int tk = p->rb == 1 ? 128 : p->rb == 2 ? 64 : 32;
+  const int64_t most = p->rb == 1 ? kMaxWorkers / 2 : kMaxWorkers;   // one or two to a CU
   const int64_t units = (int64_t)s->num_kv_heads * (o->rows / p->nodes + s->batch);   // at most
   // places on the line, by 512 workgroups, are counted in 52 bits
   if (units >= (int64_t(1) << 40) / ((cap + tk - 1) / tk + 4)) return ART_ERR_UNSUPPORTED;
-  const int64_t tiles = units < kMaxWorkers ? units * ((cap + tk - 1) / tk) : units;
-  p->workers = (int)(tiles < kMaxWorkers ? (tiles < 1 ? 1 : tiles) : kMaxWorkers);
+  const int64_t tiles = units < most ? units * ((cap + tk - 1) / tk) : units;
+  p->workers = (int)(tiles < most ? (tiles < 1 ? 1 : tiles) : most);
   p->slots = (int)(units < p->workers ? units : p->workers);
   if (p->slots < 1) p->slots = 1;
   p->records_off = ((size_t)p->slots * sizeof(int4) + 255) / 256 * 256;
@@ -951,8 +960,9 @@ art_status plan_tree(const art_decode_shape* s, const art_tree_opts* o, TreePlan
 template <int RB, int PARTS>
 void launch(const TreePlan& plan, const TreeParams& p, hipStream_t stream) {
   hipLaunchKernelGGL((tree_kernel<RB, PARTS>), dim3((unsigned)plan.workers), dim3(kThreads), 0, stream, p);
-  // a row to a workgroup where a unit may have a record in each of many workgroups,
-  // else eight
+  // a row to a workgroup where a unit may have a record in each of many workgroups
+  // (one sequence of 128K tokens, one KV head: 46 us, 102 with eight), else eight (45 of
+  // 400 to 1000 tokens: 44 us, 50 with one)
   if (plan.workers > 32 * plan.slots)
     hipLaunchKernelGGL((tree_join_kernel<RB, 1>), dim3((unsigned)(plan.slots * rows_of(RB))), dim3(kThreads), 0, stream, p);
   else
