@@ -219,10 +219,6 @@ __device__ __forceinline__ void load_lds(const uint8_t* from, uint8_t* to) {
                        : : "s"(at), "v"(from) : "memory");
 }
 
-__device__ __forceinline__ bool not_finite(uint32_t w) {
-  return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
-}
-
 // Which of nodes j0 .. j0 + 31 row node i sees (bit k: node j0 + k; nodes below 0
 // are context).  `word0`: the mask's first word.
 __device__ __forceinline__ uint32_t sees(TP& P, const uint64_t* mask, uint64_t word0, int i, int n, int j0) {
@@ -500,42 +496,19 @@ __global__ void __launch_bounds__(kThreads, 2) tree_kernel(const TreeParams) {
 
     // Infinities and NaN among the values: a row that does not see them must not get
     // them, but 0 times them is no 0 (and a probability's lower parts may be 0).  Sums
-    // that are not finite are therefore made again, with care: rows that see such a
-    // value get it added, and it leaves the tile.
-    auto clean = [&](int t, int buf) __attribute__((always_inline)) {
+    // that are not finite are therefore made again, with care: such values leave the
+    // tile, and are added to the rows that see them in the end.
+    auto clean = [&](int buf) __attribute__((always_inline)) {
+      uint8_t* const tile = lds + buf * C::TILE_BYTES + C::TK * kD * 2;
       __syncthreads();     // (a wavefront may have waited for its own tokens only)
-      uint16_t* const s_v = reinterpret_cast<uint16_t*>(lds + buf * C::TILE_BYTES) + C::TK * kD;
-      bool bad = false;
       for (int i = tid; i < C::TK * kD / 8; i += kThreads) {
-        const u32x4 w = *reinterpret_cast<const u32x4*>(s_v + 8 * i);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) bad |= not_finite(w[j]);
-      }
-      if (!__syncthreads_or(bad)) return;
-#pragma unroll 1
-      for (int k = 0; k < 32; ++k) {
-        const int r = place + k, tok = t * C::TK + r;
-        // (-1 where the row sees the token: no branch for each of the sums)
-        uint32_t see;
-        see = tok < seen && (sees(P, mask, mask0, node, s.n, tok - s.context) & 1u) ? ~0u : 0u;
-#pragma unroll
-        for (int d = 0; d < 4; ++d)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-          const int dim = 32 * d + 8 * (e >> 2) + 4 * half + (e & 3);
-          const uint32_t w = s_v[v_off(r, dim >> 3) + (dim & 7)], x = (w & 0x7f80u) == 0x7f80u ? w << 16 : 0u;
-          acc[d][e] += __uint_as_float(x & see);
-        }
-      }
-      __syncthreads();
-      for (int i = tid; i < C::TK * kD / 8; i += kThreads) {
-        u32x4 w = *reinterpret_cast<const u32x4*>(s_v + 8 * i);
+        u32x4 w = *reinterpret_cast<const u32x4*>(tile + 16 * i);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           if ((w[j] & 0x7f80u) == 0x7f80u) w[j] &= 0xffff0000u;
           if ((w[j] & 0x7f800000u) == 0x7f800000u) w[j] &= 0xffffu;
         }
-        *reinterpret_cast<u32x4*>(s_v + 8 * i) = w;
+        *reinterpret_cast<u32x4*>(tile + 16 * i) = w;
       }
       __syncthreads();
     };
@@ -637,8 +610,9 @@ __global__ void __launch_bounds__(kThreads, 2) tree_kernel(const TreeParams) {
       products(at, p);
     };
 
+    bool careful = false;
 #pragma unroll 1
-    for (bool careful = false;; careful = true) {
+    for (;; careful = true) {
       m = kNegInf;
       l = 0.f;
 #pragma unroll
@@ -748,7 +722,7 @@ __global__ void __launch_bounds__(kThreads, 2) tree_kernel(const TreeParams) {
         for (; t < t1; ++t) {
           const int buf = (t - t0) & 3;
           const bool tail = t >= first_tail;
-          if (careful) clean(t, buf);
+          if (careful) clean(buf);
           f32x16 st;
           scores(buf * C::TILE_BYTES, st);
           if (tail) hide(t, st);
@@ -782,7 +756,7 @@ __global__ void __launch_bounds__(kThreads, 2) tree_kernel(const TreeParams) {
             barrier();       // the tile is there, and the one before it has been read
             if (t + 1 < t1) load_tile(t + 1, (t + 1) & 1);
           }
-          if (careful) clean(t, t & 1);
+          if (careful) clean(t & 1);
           const int at = (t & 1) * C::TILE_BYTES + place * kD * 2;
           f32x16 st;
           scores(at, st);
@@ -847,6 +821,45 @@ __global__ void __launch_bounds__(kThreads, 2) tree_kernel(const TreeParams) {
         if (d == 0) {
           to[C::kRows * kD + r] = top;
           to[C::kRows * kD + C::kRows + r] = mass;
+        }
+      }
+    }
+    if (careful) {
+      // The values that are not finite, added to what has just been written: thread d
+      // takes dim d of eight tokens at a time.
+      __syncthreads();
+      const int until = min(t1 * C::TK, seen);
+      for (int tok = t0 * C::TK; tid < kD && tok < until; tok += 8) {
+        uint32_t x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int at = min(tok + i, until - 1);
+          const int page = min(max(W.table[(int64_t)b * W.max_pages + (at >> W.page_shift)], 0), W.num_pages - 1);
+          x[i] = W.v[page * W.vs_page + kvh * W.vs_head + (at & ((1 << W.page_shift) - 1)) * W.vs_tok + tid];
+        }
+#pragma unroll 1
+        for (int i = 0; i < 8; ++i) {
+          uint32_t v = x[0];
+#pragma unroll
+          for (int j = 1; j < 8; ++j) v = i == j ? x[j] : v;
+          if ((v & 0x7f80u) != 0x7f80u || tok + i >= until) continue;
+          for (int r = 0; r < M; ++r) {
+            const int of = node0 + r / W.group;
+            const uint64_t* const bits = W.mask + (int64_t)(s.first + of) * W.words;
+            if (!(sees(W, bits, W.words ? bits[0] : 0, of, s.n, tok + i - s.context) & 1u)) continue;
+            const float y = __uint_as_float(v << 16);
+            if (whole) {
+              const int64_t i_out = (row0 + (int64_t)(r / W.group) * W.q_heads + r % W.group) * kD + tid;
+              if (W.out_bf16) {
+                uint16_t* const o = static_cast<uint16_t*>(W.out) + i_out;
+                *o = (uint16_t)f32_to_bf16_bits(bf_lo(*o) + y);
+              } else {
+                static_cast<float*>(W.out)[i_out] += y;
+              }
+            } else {
+              to[r * kD + tid] += y;
+            }
+          }
         }
       }
     }
