@@ -683,7 +683,7 @@ def tree_layout(parents: torch.Tensor, context_lens: torch.Tensor, *, mask_words
     if token_offsets is not None:
         _check(token_offsets, "token_offsets", torch.int32, dev, (B + 1,))
     mask = torch.empty((rows, int(mask_words)), dtype=torch.int64, device=parents.device)
-    positions = torch.empty(rows, dtype=torch.int32, device=parents.device)
+    positions = torch.empty_like(parents)
     st = _on_device(dev, _lib.tree_layout, B, rows, parents.data_ptr(), _ptr(token_offsets),
                     context_lens.data_ptr(), int(mask_words), mask.data_ptr(), positions.data_ptr())
     if st != _lib.OK:
@@ -732,7 +732,9 @@ def tree_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor
         _check(token_offsets, "token_offsets", torch.int32, dev, (B + 1,))
     words = 0
     if mask is not None:
-        words = mask.shape[-1]
+        words = mask.shape[-1] if mask.dim() else 0
+        if words < 1:
+            raise ValueError("mask must be [rows][words] with a word at least")
         _check(mask, "mask", torch.int64, dev, (rows, words))
     if out_dtype not in (torch.float32, torch.bfloat16):
         raise ValueError("out_dtype must be float32 or bfloat16")
@@ -806,8 +808,7 @@ def verify_drafts(target: torch.Tensor, tokens: torch.Tensor, parents: torch.Ten
                for t in (target, target if draft is None else draft)]
     opts = _lib.VerifyOpts(B, rows, vocab, int(max_path), kind, *strides)
     ws = _call_workspace(workspace, _lib.verify_workspace_bytes(opts), dev, target.device)
-    accepted = torch.empty((B, int(max_path)), dtype=torch.int32, device=target.device)
-    counts, following = (torch.empty(B, dtype=torch.int32, device=target.device) for _ in range(2))
+    accepted, counts, following = tokens.new_empty((B, int(max_path))), tokens.new_empty(B), tokens.new_empty(B)
     st = _on_device(dev, _lib.verify_drafts, opts, target.data_ptr(), _ptr(draft), tokens.data_ptr(),
                     parents.data_ptr(), _ptr(token_offsets), uniforms.data_ptr(),
                     last_uniforms.data_ptr(), accepted.data_ptr(), counts.data_ptr(),

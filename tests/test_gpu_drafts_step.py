@@ -126,3 +126,51 @@ def test_steps(captured):
                 where = int(table[b, t // page]), slice(None), t % page
                 assert torch.equal(pools[0][where].cpu(), key) and torch.equal(pools[1][where].cpu(), value)
     assert max(held) > 6
+
+
+def test_far_offsets():
+    """Pages 2^28 elements apart: bytes and elements pass 32 bits."""
+    gen = torch.Generator().manual_seed(2)
+    H, page, n, held = 2, 16, 5, 40
+    near = R.Cache(gen, [held + n], H, page, spare=6)
+    pages, stride = near.k.shape[0], 1 << 28
+    far = object.__new__(R.Cache)
+    for name in ("k", "v"):
+        base = torch.empty((pages - 1) * stride + H * page * 128, dtype=torch.bfloat16, device=DEV)
+        setattr(far, name, base.as_strided(near.k.shape, (stride, page * 128, 128, 1)))
+        getattr(far, name).copy_(getattr(near, name))
+    near, far.table = near.to(DEV), near.table.to(DEV)
+    context = torch.tensor([held], dtype=torch.int32, device=DEV)
+    x = torch.randn(n, H, 128, generator=gen).bfloat16().to(DEV)
+    q = torch.randn(n, 4, 128, generator=gen).bfloat16().to(DEV)
+    rope = api.rope_frequencies(128)
+    accepted, counts = torch.tensor([[0, 2, 4]], dtype=torch.int32, device=DEV), torch.tensor([3], dtype=torch.int32, device=DEV)
+    results = []
+    for c in (near, far):
+        turned = api.rope_append(c.k, c.v, x, x, c.table, context, rope=rope, q=q)
+        out, lse = api.tree_attention(turned, c.k, c.v, c.table, context)
+        api.keep_accepted(c.k, c.v, c.table, context, accepted, counts)
+        results.append((turned, out, lse, c.k.contiguous().view(torch.int16), c.v.contiguous().view(torch.int16)))
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
+
+
+def test_nothing_to_do():
+    """No rows, no sequences, sequences without nodes."""
+    c = R.Cache(torch.Generator().manual_seed(3), [20], 2, 16).to(DEV)
+    none = torch.zeros(0, dtype=torch.int32, device=DEV)
+    one, offsets = torch.tensor([4], dtype=torch.int32, device=DEV), torch.zeros(2, dtype=torch.int32, device=DEV)
+    rows, q = torch.zeros(0, 2, 128, dtype=torch.bfloat16, device=DEV), torch.zeros(0, 4, 128, dtype=torch.bfloat16, device=DEV)
+    was = c.k.clone().view(torch.int16)
+    for kw in ({}, {"token_offsets": offsets}):
+        assert api.rope_append(c.k, c.v, rows, rows, c.table, one, q=q, **kw).shape == (0, 4, 128)
+        assert api.tree_attention(q, c.k, c.v, c.table, one, **kw)[0].shape == (0, 4, 128)
+        assert api.tree_layout(none, one, **kw)[0].shape == (0, 1)
+        accepted, counts, following = api.verify_drafts(
+            torch.zeros(0, 10, device=DEV), none, none, torch.zeros(0, device=DEV), torch.zeros(1, device=DEV), max_path=2, **kw)
+        assert accepted.tolist() == [[-1, -1]] and counts.tolist() == [0] and following.tolist() == [-1]
+        api.keep_accepted(c.k, c.v, c.table, one, accepted, counts)
+    assert api.rope_rows(rows, none, api.rope_frequencies(64)).shape == (0, 2, 128)
+    assert torch.equal(c.k.view(torch.int16), was)
+    with pytest.raises(ValueError):
+        api.tree_attention(q, c.k, c.v, c.table, one, mask=torch.zeros(0, 0, dtype=torch.int64, device=DEV))
