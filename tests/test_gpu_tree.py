@@ -27,13 +27,14 @@ def _gpu_tensor(t):
 
 
 class Problem:
-    def __init__(self, held, new, heads, *, page=16, tree=True, seed=0, offsets="ragged", pad=0, words=None, sharp=1.0):
+    def __init__(self, held, new, heads, *, page=16, tree=True, seed=0, offsets="ragged", pad=0, words=None, sharp=1.0,
+                 extra_width=0):
         gen = torch.Generator().manual_seed(seed)
         self.gen = gen
         Hq, H = heads
         self.lead = 3 if offsets == "ragged" else 0
         rows = sum(new) + 2 * self.lead
-        self.cache = R.Cache(gen, [a + b for a, b in zip(held, new)], H, page, pad=pad)
+        self.cache = R.Cache(gen, [a + b for a, b in zip(held, new)], H, page, pad=pad, extra_width=extra_width)
         self.q = (torch.randn(rows, Hq, 128, generator=gen) * sharp).bfloat16()
         self.context = torch.tensor(held, dtype=torch.int32)
         self.offsets = None
@@ -74,6 +75,33 @@ class Problem:
 
 
 DTYPES = [torch.float32, torch.bfloat16]
+# Columns of the page table behind the sequences' own: with room for long contexts, and
+# up to 32 rows a sequence, the row tiles are of 32 rows (of 64 without).
+LONG = 4096
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("tree", [True, False])
+@pytest.mark.parametrize("heads", [(1, 1), (4, 1), (8, 2), (5, 1), (32, 1), (9, 3)])
+def test_row_tiles_of_32_rows(heads, tree, dtype):
+    for i, (held, new) in enumerate((([0], [1]), ([1], [5]), ([127], [2]), ([128], [1]), ([129], [3]), ([700, 0, 33], [4, 1, 0]),
+                                     ([5000], [3]), ([20, 300] * 6, [1, 2] * 6), ([64, 20], [11, 1]))):
+        Problem(held, new, heads, tree=tree, seed=i, extra_width=LONG).check(dtype)
+
+
+def test_hidden_values_in_row_tiles_of_32_rows():
+    for new, heads in ((6, (4, 2)), (2, (16, 1))):
+        for k_bad, v_bad in ((math.nan, math.nan), (0.0, math.inf)):
+            p = Problem([150], [new], heads, seed=26, extra_width=LONG)
+            others = torch.tensor([i for i in range(new) if i != new - 1]) + p.lead
+            p.mask[others] &= ~(1 << (new - 1))
+            clean = p.run(torch.float32)
+            cache = p.cache.to(DEV)
+            t = 150 + new - 1
+            cache.k[cache.table[0, t // 16].long(), :, t % 16] = k_bad
+            cache.v[cache.table[0, t // 16].long(), :, t % 16] = v_bad
+            out, lse = p.run(torch.float32, cache=cache)
+            assert torch.equal(out[others], clean[0][others]) and torch.equal(lse[others], clean[1][others])
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
@@ -128,6 +156,14 @@ def test_long_contexts_are_split_and_joined():
     Problem([4000], [70], (2, 1), page=64, seed=11, tree=False).check()
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_more_units_than_workgroups(dtype):
+    """Parts of the line that begin inside a unit and go on behind it (wide row tiles
+    put that rest off), and whole units between."""
+    held = [20 + 37 * b % 400 for b in range(70)]
+    Problem(held, [2] * 70, (264, 8), tree=dtype is torch.float32, seed=27).check(dtype)
+
+
 def test_masks_that_leave_rows_empty():
     """No context and no bits; and bits that no node, word or row has."""
     p = Problem([0, 0, 40], [6, 3, 5], (4, 2), seed=12)
@@ -179,11 +215,12 @@ def test_a_value_of_the_context_reaches_all():
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("extra", [0, LONG])
 @pytest.mark.parametrize("held, new, heads", [(300, 5, (4, 2)), (700, 30, (2, 1)), (1500, 40, (8, 1)), (9000, 3, (2, 1))], ids=str)
-def test_infinities_that_are_seen(held, new, heads, dtype):
+def test_infinities_that_are_seen(held, new, heads, extra, dtype):
     """Infinities and NaN in the context, far from the nodes and near: their dims are
     infinite or NaN in every row, the other dims as the definition has them."""
-    p = Problem([held], [new], heads, seed=25)
+    p = Problem([held], [new], heads, seed=25, extra_width=extra)
     odd = {7: (3, math.inf), 64: (held // 2, -math.inf), 65: (held - 1, math.nan), 127: (held // 3, math.inf)}
     cache = p.cache.to(DEV)
     for dim, (t, x) in odd.items():
@@ -300,3 +337,24 @@ def test_graphs_streams_and_a_shared_workspace():
         live = slice(p.lead, -p.lead)
         for out, lse in outs:
             assert torch.equal(out[live], eager[0][live]) and torch.equal(lse[live], eager[1][live])
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_random_shapes(seed):
+    """Batches, heads, pages, contexts and masks at random, every row tile's height
+    among them; bits of the masks at random too, not only trees."""
+    gen = torch.Generator().manual_seed(1000 + seed)
+    pick = lambda *xs: xs[int(torch.randint(0, len(xs), (1,), generator=gen))]  # noqa: E731
+    number = lambda lo, hi: int(torch.randint(lo, hi + 1, (1,), generator=gen))  # noqa: E731
+    H, g = pick((1, 1), (2, 3), (1, 7), (4, 2), (1, 16), (2, 5), (1, 33), (1, 100))
+    B = pick(1, 2, 5, 13)
+    top = pick(20, 300, 1500 if B < 5 else 200)
+    nodes = max(1, pick(3, 30, 150) // (1 + g * B // 20))
+    held, new = [number(0, top) for _ in range(B)], [number(0, nodes) for _ in range(B)]
+    new[0] = max(new[0], 1)
+    p = Problem(held, new, (H * g, H), page=pick(16, 32, 128), tree=pick(True, False), seed=seed, pad=pick(0, 1),
+                sharp=pick(0.3, 1.0, 4.0), extra_width=pick(0, LONG))
+    if p.mask is not None and pick(True, False):
+        p.mask = torch.randint(-2 ** 63, 2 ** 63 - 1, p.mask.shape, generator=gen)
+    p.scale = pick(1 / math.sqrt(128), -0.05, 0.2)
+    p.check(pick(*DTYPES))
