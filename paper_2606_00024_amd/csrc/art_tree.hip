@@ -581,14 +581,18 @@ __global__ void __launch_bounds__(kThreads, 2) tree_kernel(const TreeParams) {
     };
     auto weights = [&](f32x16& st, bf16x8 (&p)[PARTS][2]) __attribute__((always_inline)) {
       const float ref = m == kNegInf ? 0.f : m;
+      // (a tile's sum first: many small probabilities, added one by one to the large sum
+      // that a few high scores have made, would round away)
+      float sum = 0.f;
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         // (where fp32 is kept, the scale's own rounding would move large scores by more
         // than their own does)
         const float x = PARTS > 1 ? fmaf(st[r], scale_rest, -ref) : -ref;
         st[r] = fast_exp2(fmaf(st[r], scale, x));
-        l += st[r];
+        sum += st[r];
       }
+      l += sum;
 #pragma unroll
       for (int k = 0; k < PARTS; ++k) {
         uint32_t w[8];
@@ -678,6 +682,7 @@ __global__ void __launch_bounds__(kThreads, 2) tree_kernel(const TreeParams) {
               uint32_t w[8];
               const uint8_t *k16 = nullptr, *v16 = nullptr;
               const float ref = m == kNegInf ? 0.f : m;
+              float sum = 0.f;
 #pragma unroll
               for (int r = 0; r < 16; ++r) next_st[r] = 0.f;
               __builtin_amdgcn_s_setprio(1);
@@ -692,11 +697,12 @@ __global__ void __launch_bounds__(kThreads, 2) tree_kernel(const TreeParams) {
                 v_part[i] = value_part(kHere, i >> 2, i & 3);
                 const float x = fast_exp2(fmaf(st[2 * i], scale, -ref));
                 const float y = fast_exp2(fmaf(st[2 * i + 1], scale, -ref));
-                l += x;
-                l += y;
+                sum += x;
+                sum += y;
                 w[i] = pack_bf16(x, y);
                 __builtin_amdgcn_sched_barrier(0);
               }
+              l += sum;
               wait_loads<2 * C::LOADS>();
               barrier();
 #pragma unroll

@@ -358,3 +358,28 @@ def test_random_shapes(seed):
         p.mask = torch.randint(-2 ** 63, 2 ** 63 - 1, p.mask.shape, generator=gen)
     p.scale = pick(1 / math.sqrt(128), -0.05, 0.2)
     p.check(pick(*DTYPES))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("batch,nodes,group", [(256, 1, 8), (512, 8, 8), (512, 16, 8)])
+def test_small_probabilities_behind_large_ones(batch, nodes, group, dtype):
+    """128 tokens of weight 1 come first, and 16K of 2^-20.5, each of them below half
+    a step of a sum that holds the first ones (16 of them or more): together they are
+    8.6e-5 of it.  Scores are exact: 0 and -16 * 8.  A sum may add a tile's part at a
+    time, of 32 tokens or more, and within it up to 16, each addition and the few that
+    join the parts off by 2^-24 of the sum, and the logarithm is off by two steps."""
+    context, page, scale = 16384, 128, 0.1109375
+    pages = context // page + 1
+    k = torch.zeros(pages, 1, page, 128, dtype=torch.bfloat16, device=DEV)
+    k[1:, :, :, 0] = -8.0
+    v = torch.ones_like(k)
+    q = torch.zeros(batch * nodes, group, 128, dtype=torch.bfloat16, device=DEV)
+    q[:, :, 0] = 16.0
+    table = torch.arange(pages, dtype=torch.int32, device=DEV).expand(batch, pages).contiguous()
+    held = torch.full((batch,), context, dtype=torch.int32, device=DEV)
+    _, lse = api.tree_attention(q, k, v, table, held, softmax_scale=scale, out_dtype=dtype)
+    small = context - 128 + 1 + torch.arange(nodes, dtype=torch.float64)
+    ref = torch.log(128 + small * math.exp(-128 * scale))
+    tol = (context / 32 + 24) * 2.0 ** -24 + 2 * 5 * 2.0 ** -23
+    err = (lse.cpu().double().view(batch, nodes, group) - ref[:, None]).abs().max().item()
+    assert err <= tol, (err, tol)
