@@ -488,7 +488,8 @@ __global__ void __launch_bounds__(kThreads) keep_kernel(const KeepParams P) {
   if (side > 1) return;
   uint16_t* const pool = P.pool[side] + head * P.sh[side] + 8 * piece;
   const int slots = 1 << P.page_shift;
-  auto where = [&](int token) -> uint16_t* {
+  // (tokens in 64 bits: a context near 2^31 and a node's number pass it)
+  auto where = [&](int64_t token) -> uint16_t* {
     const int page = P.table[(int64_t)b * P.max_pages + (token >> P.page_shift)];
     if (page < 0 || page >= P.num_pages) return nullptr;
     return pool + page * P.sp[side] + (token & (slots - 1)) * P.st[side];
@@ -501,9 +502,9 @@ __global__ void __launch_bounds__(kThreads) keep_kernel(const KeepParams P) {
       const int j = j0 + i;
       to[i] = nullptr;
       if (j >= n || nodes[j] == j) continue;
-      const uint16_t* from = where(context + nodes[j]);
+      const uint16_t* from = where((int64_t)context + nodes[j]);
       if (!from) continue;
-      to[i] = where(context + j);
+      to[i] = where((int64_t)context + j);
       x[i] = *reinterpret_cast<const u32x4*>(from);
     }
 #pragma unroll

@@ -1,0 +1,54 @@
+"""Calls on drafted tokens where a sequence's slots pass 2^31, in tables that have
+room for them (needs a gfx950 GPU)."""
+from __future__ import annotations
+
+import pytest
+import torch
+
+from paper_2606_00024_amd import _lib, api
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+PAGE = 1 << 16
+FAR = 2 ** 31
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    _lib.load()
+    yield
+
+
+class FarCache:
+    """Two sequences whose table goes a few pages past slot 2^31; the pages around it
+    exist, all others are marked as missing."""
+
+    def __init__(self, seed):
+        gen = torch.Generator(device=DEV).manual_seed(seed)
+        self.k, self.v = (torch.randn(4, 2, PAGE, 128, generator=gen, device=DEV, dtype=torch.bfloat16) for _ in range(2))
+        self.table = torch.full((2, FAR // PAGE + 3), -1, dtype=torch.int32, device=DEV)
+        for b in range(2):
+            self.table[b, FAR // PAGE - 1], self.table[b, FAR // PAGE] = 2 * b + 1, 2 * b
+
+    def rows(self, pool, b, slots):
+        """The rows [slots][heads][128] of a pool."""
+        return torch.stack([pool[int(self.table[b, t // PAGE]), :, t % PAGE] for t in slots])
+
+
+def test_accepted_nodes_move_across_2_to_the_31():
+    c = FarCache(1)
+    was = {name: getattr(c, name).clone() for name in "kv"}
+    paths = [[0, 2, 4, 5], [1, 3, 4]]
+    held = [FAR - 3, FAR - 1]
+    accepted = torch.tensor([p + [-1] * (4 - len(p)) for p in paths], dtype=torch.int32, device=DEV)
+    counts = torch.tensor([len(p) for p in paths], dtype=torch.int32, device=DEV)
+    api.keep_accepted(c.k, c.v, c.table, torch.tensor(held, dtype=torch.int32, device=DEV), accepted, counts)
+    for name in "kv":
+        want = was[name].clone()
+        for b, path in enumerate(paths):
+            for j, node in enumerate(path):
+                to = held[b] + j
+                want[int(c.table[b, to // PAGE]), :, to % PAGE] = c.rows(was[name], b, [held[b] + node])[0]
+        assert torch.equal(getattr(c, name), want)
