@@ -95,7 +95,8 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const RopeParams P) {
   if (row >= P.rows) return;
 
   // where the row lies, and its position
-  int page = -1, slot = 0, position = 0;
+  int page = -1, slot = 0;
+  double position = 0.0;
   if (P.k.heads || !P.row_positions) {
     const SpanTable table = span_table(P, lane);
     const Span s = span_of(P, table, row, lane);
@@ -104,7 +105,7 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const RopeParams P) {
     const int64_t token = s.pos + (row - s.first);
     page = page_of(P, s.b, token);
     slot = (int)(token & ((1 << P.page_shift) - 1));
-    position = (int)token;
+    position = (double)(uint32_t)token;   // (a context near 2^31 and its rows pass that, but no 2^32)
   }
   if (P.row_positions) position = P.row_positions[row];
 
@@ -114,7 +115,7 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const RopeParams P) {
     // half turns: 1 / pi in fp64 costs 2^-53 of them.  What is left after the nearest
     // whole turn goes to the functions as fp32, and what that leaves of it (2^-25) in
     // by the first order.
-    double t = (double)position * (P.freqs[lane] * 0.3183098861837907);
+    double t = position * (P.freqs[lane] * 0.3183098861837907);
     t -= 2.0 * rint(0.5 * t);
     const float near = (float)t, rest = (float)((t - near) * 3.141592653589793);
     float s0, c0;

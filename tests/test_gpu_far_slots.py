@@ -52,3 +52,25 @@ def test_accepted_nodes_move_across_2_to_the_31():
                 to = held[b] + j
                 want[int(c.table[b, to // PAGE]), :, to % PAGE] = c.rows(was[name], b, [held[b] + node])[0]
         assert torch.equal(getattr(c, name), want)
+
+
+def test_appended_keys_turn_by_positions_past_2_to_the_31():
+    """Without row_positions a row's position is its slot: 2^31 and further are no
+    negative numbers.  A frequency of 2^-34 turns slot 2^31 by 1/8 rad (and -2^31 by
+    -1/8).  Bound: 2^-21 of |x| + |y| in fp32, and a rounding to bf16 of 2^-8."""
+    c = FarCache(2)
+    freqs = torch.full((64,), 2.0 ** -34, dtype=torch.float64, device=DEV)
+    x = torch.randn(10, 2, 128, generator=torch.Generator().manual_seed(3))
+    held = [FAR - 2, FAR - 3]
+    rows = x.to(DEV)
+    q = api.rope_append(c.k, c.v, rows, rows, c.table, torch.tensor(held, dtype=torch.int32, device=DEV),
+                        rope=api.Rope(freqs), q=rows)
+    for b in range(2):
+        slots = [held[b] + i for i in range(5)]
+        at, y = torch.tensor(slots, dtype=torch.float64)[:, None, None] * 2.0 ** -34, x[5 * b: 5 * b + 5].double()
+        lo, hi = y[..., :64], y[..., 64:]
+        want = torch.cat([lo * at.cos() - hi * at.sin(), hi * at.cos() + lo * at.sin()], -1)
+        size = (lo.abs() + hi.abs()).repeat(1, 1, 2)
+        for got in (c.rows(c.k, b, slots), q[5 * b: 5 * b + 5]):
+            assert bool(((got.cpu().double() - want).abs() <= (2.0 ** -8 + 2.0 ** -20) * size).all())
+        assert torch.equal(c.rows(c.v, b, slots), rows[5 * b: 5 * b + 5].bfloat16())
