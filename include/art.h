@@ -574,7 +574,8 @@ art_status art_rope_append(const art_decode_shape* shape, const art_rope* rope, 
  *              (node 0 has depth 0).
  * A parent that is not an earlier node (-1 among them) ends the walk.  1 <=
  * mask_words <= 16; sequences of more than ART_MAX_NODES nodes are passed over
- * (without row_offsets the call is refused).
+ * (without row_offsets the call is refused), and so are, with positions, those of
+ * context + nodes > 2^31.
  */
 #define ART_MAX_NODES 1024
 art_status art_tree_layout(int32_t batch, int32_t rows, const int32_t* parents,

@@ -41,6 +41,7 @@ __global__ void __launch_bounds__(kThreads) layout_kernel(const LayoutParams P) 
   const int2 span = rows_of(P, b);
   const int n = span.y - span.x, context = P.positions ? P.positions[b] : 0;
   if (n == 0 || n > ART_MAX_NODES || context < 0) return;
+  if (P.out && context > INT32_MAX - (n - 1)) return;   // a chain's positions would not be held by 32 bits
   for (int i = threadIdx.x; i < n; i += kThreads) {
     const int p = P.parents[span.x + i];
     s_parent[i] = p >= 0 && p < i ? p : -1;

@@ -74,3 +74,18 @@ def test_appended_keys_turn_by_positions_past_2_to_the_31():
         for got in (c.rows(c.k, b, slots), q[5 * b: 5 * b + 5]):
             assert bool(((got.cpu().double() - want).abs() <= (2.0 ** -8 + 2.0 ** -20) * size).all())
         assert torch.equal(c.rows(c.v, b, slots), rows[5 * b: 5 * b + 5].bfloat16())
+
+
+def test_layouts_whose_positions_32_bits_do_not_hold_are_passed_over():
+    parents = torch.tensor([-1, 0, 1, 2] * 3, dtype=torch.int32, device=DEV)
+    context = torch.tensor([FAR - 4, FAR - 3, FAR - 1], dtype=torch.int32, device=DEV)
+    mask = torch.full((12, 1), 9, dtype=torch.int64, device=DEV)
+    positions = torch.full((12,), 9, dtype=torch.int32, device=DEV)
+    stream = torch.cuda.current_stream().cuda_stream
+    args = (3, 12, parents.data_ptr(), 0, context.data_ptr(), 1, mask.data_ptr())
+    assert _lib.tree_layout(*args, positions.data_ptr(), stream) == _lib.OK
+    assert positions.tolist() == [FAR - 4, FAR - 3, FAR - 2, FAR - 1] + [9] * 8
+    assert mask[:, 0].tolist() == [1, 3, 7, 15] + [9] * 8
+    # bits alone have no such bound
+    assert _lib.tree_layout(*args, 0, stream) == _lib.OK
+    assert mask[:, 0].tolist() == [1, 3, 7, 15] * 3
