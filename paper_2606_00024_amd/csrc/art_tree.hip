@@ -508,11 +508,25 @@ __global__ void __launch_bounds__(kThreads, 2) tree_kernel(const TreeParams) {
 
     // Infinities and NaN among the values: a row that does not see them must not get
     // them, but 0 times them is no 0 (and a probability's lower parts may be 0).  Sums
-    // that are not finite are therefore made again, with care: such values leave the
-    // tile, and are added to the rows that see them in the end.
+    // that are not finite are therefore made again, with care: such values are added to
+    // the rows that see them, those with a score above -inf, and leave the tile before
+    // its products.
+    auto wild = [&](int buf) __attribute__((always_inline)) {
+      const uint8_t* const tile = lds + buf * C::TILE_BYTES + C::TK * kD * 2;
+      bool found = false;
+      int at = tid;
+      __asm__ __volatile__("" : "+v"(at));   // (addresses made here, not held throughout)
+      __syncthreads();     // (a wavefront may have waited for its own tokens only)
+      for (int i = at; i < C::TK * kD / 8; i += kThreads) {
+        const u32x4 w = *reinterpret_cast<const u32x4*>(tile + 16 * i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) found |= (w[j] & 0x7f80u) == 0x7f80u || (w[j] & 0x7f800000u) == 0x7f800000u;
+      }
+      return __syncthreads_or(found) != 0;
+    };
     auto clean = [&](int buf) __attribute__((always_inline)) {
       uint8_t* const tile = lds + buf * C::TILE_BYTES + C::TK * kD * 2;
-      __syncthreads();     // (a wavefront may have waited for its own tokens only)
+      __syncthreads();     // (the wavefronts have added what is there)
       for (int i = tid; i < C::TK * kD / 8; i += kThreads) {
         u32x4 w = *reinterpret_cast<const u32x4*>(tile + 16 * i);
 #pragma unroll
@@ -620,6 +634,34 @@ __global__ void __launch_bounds__(kThreads, 2) tree_kernel(const TreeParams) {
       }
     };
 
+    // A piece's values that are not finite, to the rows that see them.  (The reference is
+    // above -inf where there is one, so no later factor is 0.)
+    auto add_wild = [&](int at, const f32x16& st) __attribute__((always_inline)) {
+      uint32_t bits = 0;   // the piece's tokens that the lane's row sees
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (!(st[r] * scale == kNegInf)) bits |= 1u << (8 * (r >> 2) + 4 * half + (r & 3));
+      const auto both = __builtin_amdgcn_permlane32_swap(bits, bits, false, false);
+      bits = both[0] | both[1];
+#pragma unroll 1
+      for (int tok = 0; tok < 32; ++tok) {
+        const bool seen_here = bits >> tok & 1u;
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+          const uint8_t* const from = lds + at + C::TK * kD * 2 + 2 * v_off(tok, 4 * d) + 8 * half;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {      // (16-byte pieces 4 d .. 4 d + 3 of a row lie in order)
+            const u32x2 w = *reinterpret_cast<const u32x2*>(from + 16 * e);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const float y = j & 1 ? bf_hi(w[j >> 1]) : bf_lo(w[j >> 1]);
+              if (seen_here && !(fabsf(y) < __builtin_inff())) acc[d][4 * e + j] += y;
+            }
+            __builtin_amdgcn_sched_barrier(0);   // (few registers are left)
+          }
+        }
+      }
+    };
     auto weigh = [&](int at, f32x16& st) __attribute__((always_inline)) {
       bf16x8 p[PARTS][2];
       weights(st, p);
@@ -740,13 +782,16 @@ __global__ void __launch_bounds__(kThreads, 2) tree_kernel(const TreeParams) {
         for (; t < t1; ++t) {
           const int buf = (t - t0) & 3;
           const bool tail = t >= first_tail;
-          if (careful) clean(buf);
           f32x16 st;
           scores(buf * C::TILE_BYTES, st);
           if (tail) hide(t, st);
           float top;
           tops(st, top);
           refer(top);
+          if (careful && wild(buf)) {
+            add_wild(buf * C::TILE_BYTES, st);
+            clean(buf);
+          }
           weigh(buf * C::TILE_BYTES, st);
           if (t + 1 < t1) {
             // the next tile is there, and this one has been used up
@@ -774,7 +819,6 @@ __global__ void __launch_bounds__(kThreads, 2) tree_kernel(const TreeParams) {
             barrier();       // the tile is there, and the one before it has been read
             if (t + 1 < t1) load_tile(t + 1, (t + 1) & 1);
           }
-          if (careful) clean(t & 1);
           const int at = (t & 1) * C::TILE_BYTES + place * kD * 2;
           f32x16 st;
           scores(at, st);
@@ -782,6 +826,10 @@ __global__ void __launch_bounds__(kThreads, 2) tree_kernel(const TreeParams) {
           float top;
           tops(st, top);
           refer(top);
+          if (careful && wild(t & 1)) {
+            add_wild(at, st);
+            clean(t & 1);
+          }
           weigh(at, st);
         }
       }
@@ -839,45 +887,6 @@ __global__ void __launch_bounds__(kThreads, 2) tree_kernel(const TreeParams) {
         if (d == 0) {
           to[C::kRows * kD + r] = top;
           to[C::kRows * kD + C::kRows + r] = mass;
-        }
-      }
-    }
-    if (careful) {
-      // The values that are not finite, added to what has just been written: thread d
-      // takes dim d of eight tokens at a time.
-      __syncthreads();
-      const int until = min(t1 * C::TK, seen);
-      for (int tok = t0 * C::TK; tid < kD && tok < until; tok += 8) {
-        uint32_t x[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int at = min(tok + i, until - 1);
-          const int page = min(max(W.table[(int64_t)b * W.max_pages + (at >> W.page_shift)], 0), W.num_pages - 1);
-          x[i] = W.v[page * W.vs_page + kvh * W.vs_head + (at & ((1 << W.page_shift) - 1)) * W.vs_tok + tid];
-        }
-#pragma unroll 1
-        for (int i = 0; i < 8; ++i) {
-          uint32_t v = x[0];
-#pragma unroll
-          for (int j = 1; j < 8; ++j) v = i == j ? x[j] : v;
-          if ((v & 0x7f80u) != 0x7f80u || tok + i >= until) continue;
-          for (int r = 0; r < M; ++r) {
-            const int of = node0 + r / W.group;
-            const uint64_t* const bits = W.mask + (int64_t)(s.first + of) * W.words;
-            if (!(sees(W, bits, W.words ? bits[0] : 0, of, s.n, tok + i - s.context) & 1u)) continue;
-            const float y = __uint_as_float(v << 16);
-            if (whole) {
-              const int64_t i_out = (row0 + (int64_t)(r / W.group) * W.q_heads + r % W.group) * kD + tid;
-              if (W.out_bf16) {
-                uint16_t* const o = static_cast<uint16_t*>(W.out) + i_out;
-                *o = (uint16_t)f32_to_bf16_bits(bf_lo(*o) + y);
-              } else {
-                static_cast<float*>(W.out)[i_out] += y;
-              }
-            } else {
-              to[r * kD + tid] += y;
-            }
-          }
         }
       }
     }
