@@ -83,6 +83,7 @@ struct TreeParams {
   int32_t page_shift, num_pages, max_pages;
   int32_t slots;               // entries of `units`
   int32_t by_unit;             // entries are units (else workgroups)
+  int64_t most_units;          // that rows of distinct sequences can make
   int32_t out_bf16, negate;    // negate: a negative scale
   float scale_log2, scale_rest;  // its magnitude: rounded down to fp32, and what that leaves
   int64_t qs_row, qs_head;
@@ -316,6 +317,9 @@ __global__ void __launch_bounds__(kThreads, 2) tree_kernel(const TreeParams) {
   }
   before -= own;
   earlier -= mine;
+  // Offsets that decrease can claim rows for many sequences: more units than there are
+  // entries, and a line longer than its arithmetic holds.  Nothing is done for them.
+  if (n_units > P.most_units) line = n_units = 0;
   line = uniform(line);
   const int64_t workers = min((int64_t)gridDim.x, max(line / C::LEAST, (int64_t)1));
   // Workgroups go to the eight XCDs in turn: each XCD gets one stretch of the line, so
@@ -953,6 +957,7 @@ __global__ void __launch_bounds__(kThreads) tree_join_kernel(const TreeParams) {
 
 struct TreePlan {
   int rb, nodes, workers, slots;
+  int64_t units;
   size_t records_off, total;
 };
 
@@ -990,6 +995,7 @@ art_status plan_tree(const art_decode_shape* s, const art_tree_opts* o, TreePlan
   if (units >= (int64_t(1) << 40) / ((cap + tk - 1) / tk + 4)) return ART_ERR_UNSUPPORTED;
   const int64_t tiles = units < most ? units * ((cap + tk - 1) / tk) : units;
   p->workers = (int)(tiles < most ? (tiles < 1 ? 1 : tiles) : most);
+  p->units = units;
   p->slots = (int)(units < p->workers ? units : p->workers);
   if (p->slots < 1) p->slots = 1;
   p->records_off = ((size_t)p->slots * sizeof(int4) + 255) / 256 * 256;
@@ -1056,6 +1062,7 @@ art_status art_tree_attention(const art_decode_shape* shape, const art_tree_opts
   p.max_pages = shape->max_pages_per_seq;
   p.slots = plan.slots;
   p.by_unit = plan.slots < plan.workers;
+  p.most_units = plan.units;
   p.out_bf16 = opts->out_dtype == ART_OUT_BF16;
   p.negate = opts->softmax_scale < 0.f;
   // (a scale of 0 weighs all tokens alike; hidden scores of -inf times 0 would not be -inf)

@@ -1,5 +1,5 @@
-"""Attention of drafted tokens: values that are not finite behind scores of -inf
-(needs a gfx950 GPU)."""
+"""Attention of drafted tokens: values that are not finite behind scores of -inf, and
+offsets that claim rows many times over (needs a gfx950 GPU)."""
 from __future__ import annotations
 
 import math
@@ -93,3 +93,19 @@ def test_a_value_that_some_rows_see(held, new, heads, extra, dtype):
     assert bool((out[odd][..., 77] == -math.inf).all())
     others = [d for d in range(128) if d != 77]
     assert torch.equal(out[odd][..., others], plain[0][odd][..., others])
+
+
+@pytest.mark.parametrize("heads, batch, rows, extra", [((128, 1), 40, 8, 300), ((256, 2), 100, 100, LONG), ((8, 1), 300, 600, 40)])
+def test_offsets_that_claim_rows_many_times(heads, batch, rows, extra):
+    """0, rows, 0, rows, ...: half of the sequences claim every row, more units of work
+    than any offsets that do not decrease can make.  Nothing is written, and the next
+    call over the same workspace is as ever."""
+    p = Problem([20] * batch, [rows // batch or 1] * batch, heads, seed=34, extra_width=extra, tree=False, offsets=None)
+    p.q = p.q[:rows]
+    p.offsets = torch.tensor([rows * (b % 2) for b in range(batch + 1)], dtype=torch.int32)
+    workspace = torch.empty(128 << 20, dtype=torch.uint8, device=DEV)
+    out, lse = p.run(torch.float32, workspace=workspace)
+    assert bool((out == 77).all()) and bool((lse == 77).all())
+    fine = Problem([700, 30], [9, 3], (8, 2), seed=35)
+    want, got = fine.run(torch.float32), fine.run(torch.float32, workspace=workspace)
+    assert torch.equal(want[0], got[0]) and torch.equal(want[1], got[1])
