@@ -223,13 +223,13 @@ __device__ __forceinline__ void barrier() {
 __device__ __forceinline__ void load_lds(const uint8_t* base, uint32_t offset, uint8_t* to) {
   const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)to);
   __asm__ __volatile__("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
-                       : : "s"(at), "v"(offset), "s"(base) : "memory");
+                       : : "s"(at), "v"(offset), "s"(base) : "m0", "memory");
 }
 // ... of a lane's own address
 __device__ __forceinline__ void load_lds(const uint8_t* from, uint8_t* to) {
   const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)to);
   __asm__ __volatile__("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
-                       : : "s"(at), "v"(from) : "memory");
+                       : : "s"(at), "v"(from) : "m0", "memory");
 }
 
 // Which of nodes j0 .. j0 + 31 row node i sees (bit k: node j0 + k; nodes below 0
