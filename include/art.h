@@ -509,8 +509,8 @@ art_status art_quant_read(const art_decode_shape* shape, const art_quant_cache* 
  */
 
 /* Packed rows [rows][heads][128] of a type: strides in elements of it, multiples
- * of 16 bytes (>= 0), row strides less than 256 MiB, arrays 16-byte aligned;
- * head_dim is contiguous. */
+ * of 16 bytes (>= 0), row strides less than 256 MiB, less than 2^28 heads, arrays
+ * 16-byte aligned; head_dim is contiguous. */
 typedef struct {
     int32_t dtype;                 /* art_rows_dtype */
     int32_t heads;

@@ -237,6 +237,8 @@ art_status check_rows(const art_rows* r) {
   if (!r || r->dtype < ART_ROWS_BF16 || r->dtype > ART_ROWS_F32 || r->heads <= 0 || r->stride_row < 0 || r->stride_head < 0)
     return ART_ERR_INVALID_ARG;
   const int64_t size = size_of(r->dtype);
+  // heads of q, k and v together, and a step past them, are counted in 32 bits
+  if (r->heads >= (1 << 28)) return ART_ERR_UNSUPPORTED;
   // (each by itself: a product could leave 64 bits)
   if (r->stride_row >= (1 << 28) || r->stride_row * size >= (1 << 28) || r->stride_head >= (int64_t(1) << 40) ||
       r->stride_row * size % 16 || r->stride_head * size % 16)
