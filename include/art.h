@@ -601,7 +601,9 @@ art_status art_tree_layout(int32_t batch, int32_t rows, const int32_t* parents,
  * both signs or a NaN make it NaN; the other dims are as without it.
  * Values of V within 2^118 over the number of tokens cannot overflow the sums,
  * which are held in fp32.  With an fp32 output probabilities carry 24 bits, with
- * a bf16 output 8 (as the output itself).
+ * a bf16 output 16, or 8 (as the output itself) where a KV head has, on average,
+ * more than 64 rows of queries of a sequence (rows / batch, rounded up, times
+ * num_q_heads / num_kv_heads): wide trees, chunks of prompts.
  * Shape fields used: those of art_decode_attention but block_size and the list's;
  * num_q_heads / num_kv_heads is any whole number up to 128, token strides are less
  * than 2^27 elements, and max_pages_per_seq * page_size less than 2^31 - 2^16.

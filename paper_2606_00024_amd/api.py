@@ -716,9 +716,12 @@ def tree_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor
     [rows][words], as from ``tree_layout``) has a bit for; without a mask node i sees
     nodes 0 .. i (a chain of drafts, a chunk of a prompt).  Returns (out
     [rows][Hq][128] out_dtype, lse [rows][Hq] fp32); a row that sees nothing gets 0
-    and -inf, and rows of no sequence are not written.  ``workspace`` (uint8 of
-    ``tree_workspace_bytes``, needs no initialisation) defaults to one of the call's
-    own.
+    and -inf, and rows of no sequence are not written.  Sums are held in fp32 and
+    probabilities with 24 bits; with ``out_dtype`` bfloat16 these have 16, or 8 (as the
+    output itself) where a KV head has, on average, more than 64 rows of queries of a
+    sequence (rows / B, rounded up, times Hq / Hkv).  ``workspace`` (uint8 of
+    ``_lib.tree_workspace_bytes``, needs no initialisation) defaults to one of the
+    call's own.
     """
     dev, H, B, fields = _bf16_pools(k_cache, v_cache, page_table)
     if q.dim() != 3 or q.dtype is not torch.bfloat16 or q.get_device() != dev:

@@ -273,8 +273,13 @@ __device__ __forceinline__ f32x4 over(const f32x4& o, float l) {
   return f32x4{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
 }
 
-// PARTS: bf16 parts that a probability is multiplied in: one (8 bits) for bf16
-// outputs, three (24) for fp32.
+// PARTS: bf16 parts that a probability is multiplied in: three (24 bits) for fp32
+// outputs.  For bf16 outputs two (16 bits, so that the output's own rounding is all that
+// shows: 1.67e-3 of the output in the relative 2-norm, 1.88e-3 with one) in row tiles of
+// up to 64 rows, where memory is the bound (8 x 32K tokens, 16 nodes: 204 us, 202 with
+// one and 208 with three); one (8 bits, as the output has itself) in those of 128 rows,
+// which the matrix cores bound (4096 prompt tokens each behind 16K: 2.16 ms, 3.14 with
+// two and 4.32 with three).
 template <int RB, int PARTS>
 __global__ void __launch_bounds__(kThreads, 2) tree_kernel(const TreeParams) {
   TP* const args = (TP*)__builtin_amdgcn_kernarg_segment_ptr();
@@ -1016,7 +1021,7 @@ void launch(const TreePlan& plan, const TreeParams& p, hipStream_t stream) {
 }
 template <int RB>
 void launch(const TreePlan& plan, const TreeParams& p, hipStream_t stream) {
-  if (p.out_bf16) launch<RB, 1>(plan, p, stream);
+  if (p.out_bf16) launch<RB, RB == 4 ? 1 : 2>(plan, p, stream);
   else launch<RB, 3>(plan, p, stream);
 }
 

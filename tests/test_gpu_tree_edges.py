@@ -1,5 +1,6 @@
-"""Attention of drafted tokens: values that are not finite behind scores of -inf, and
-offsets that claim rows many times over (needs a gfx950 GPU)."""
+"""Attention of drafted tokens: values that are not finite behind scores of -inf,
+offsets that claim rows many times over, and what a bf16 output rounds (needs a
+gfx950 GPU)."""
 from __future__ import annotations
 
 import math
@@ -109,3 +110,20 @@ def test_offsets_that_claim_rows_many_times(heads, batch, rows, extra):
     fine = Problem([700, 30], [9, 3], (8, 2), seed=35)
     want, got = fine.run(torch.float32), fine.run(torch.float32, workspace=workspace)
     assert torch.equal(want[0], got[0]) and torch.equal(want[1], got[1])
+
+
+@pytest.mark.parametrize("tree", [True, False])
+@pytest.mark.parametrize("held, new, heads, extra", [([300], [3], (4, 2), LONG), ([900, 40], [2, 4], (8, 2), LONG),
+                                                     ([300], [9], (4, 2), 0), ([700, 33], [5, 5], (8, 1), 0)], ids=str)
+def test_bf16_outputs_of_few_rows_are_rounded_once(held, new, heads, extra, tree):
+    """Up to 64 rows to a KV head (the packed rows, unused ones too, over the batch, times
+    the group: 18, 24, 30 and 64 here): probabilities carry 16 bits (two roundings
+    to bf16 of what the one before leaves: 2^-16), so that outputs near 0, where values
+    cancel, are as close as the output's own rounding (2^-8) lets them be."""
+    p = Problem(held, new, heads, seed=36, extra_width=extra, tree=tree)
+    out, _ = p.run(torch.bfloat16)
+    ref, ref_lse, size, work, count = R.attend(p.q, p.cache.k, p.cache.v, p.cache.table, p.context, p.offsets, p.mask, p.scale)
+    far = R.attend_bounds(ref, ref_lse, size, work, count, False)[0] + 2.0 ** -16 * size
+    far = far + 2.0 ** -8 * (ref.abs() + far)
+    live = slice(p.lead, -p.lead)
+    assert bool(((out.double().cpu() - ref).abs() <= far)[live].all())
