@@ -219,17 +219,16 @@ __device__ __forceinline__ void barrier() {
 // 16 bytes for every lane straight into LDS, lane after lane from `to` on: `base`
 // uniform, `offset` the lane's.  In assembly, as the compiler would have every later
 // read of LDS wait for all loads on their way; wait_loads says when they are there.
-// (It has no output register, so nothing can be taken for loaded too early.)
+// (It has no output register, so nothing can be taken for loaded too early; m0 is an
+// operand, set by the compiler, which so knows what it holds.)
 __device__ __forceinline__ void load_lds(const uint8_t* base, uint32_t offset, uint8_t* to) {
   const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)to);
-  __asm__ __volatile__("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
-                       : : "s"(at), "v"(offset), "s"(base) : "m0", "memory");
+  __asm__ __volatile__("s_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "{m0}"(at), "v"(offset), "s"(base) : "memory");
 }
 // ... of a lane's own address
 __device__ __forceinline__ void load_lds(const uint8_t* from, uint8_t* to) {
   const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)to);
-  __asm__ __volatile__("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
-                       : : "s"(at), "v"(from) : "m0", "memory");
+  __asm__ __volatile__("s_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "{m0}"(at), "v"(from) : "memory");
 }
 
 // Which of nodes j0 .. j0 + 31 row node i sees (bit k: node j0 + k; nodes below 0

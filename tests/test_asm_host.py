@@ -11,10 +11,12 @@ from paper_2606_00024_amd import build
 
 
 @pytest.mark.parametrize("path", sorted(glob.glob(os.path.join(build.CSRC, "*"))), ids=os.path.basename)
-def test_assembly_that_writes_m0_says_so(path):
-    """A statement that sets m0 declares it: the compiler may keep values there."""
+def test_m0_is_the_compilers(path):
+    """Loads into LDS take their place in m0 as an operand, and no statement writes m0
+    itself: the compiler may keep values there."""
     with open(path) as f:
         statements = re.findall(r"__asm__[^;]*;", f.read())
     for s in statements:
-        if re.search(r"\bs_\w+ m0,", s):
-            assert re.search(r':[^:]*"m0"[^:]*\);$', s), s
+        assert not re.search(r"\bs_\w+ m0,", s), s
+        if "load_lds" in s:
+            assert '"{m0}"(' in s, s
