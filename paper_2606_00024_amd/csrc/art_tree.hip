@@ -280,7 +280,7 @@ __device__ __forceinline__ f32x4 over(const f32x4& o, float l) {
 // which the matrix cores bound (4096 prompt tokens each behind 16K: 2.16 ms, 3.14 with
 // two and 4.32 with three).
 template <int RB, int PARTS>
-__global__ void __launch_bounds__(kThreads, 2) tree_kernel(const TreeParams) {
+__global__ void __launch_bounds__(kThreads, RB == 1 ? 1 : 2) tree_kernel(const TreeParams) {
   TP* const args = (TP*)__builtin_amdgcn_kernarg_segment_ptr();
   TP& P = *args;
   using C = Tree<RB>;
