@@ -518,7 +518,8 @@ __global__ void __launch_bounds__(kThreads, RB == 1 ? 1 : 2) tree_kernel(const T
     // them, but 0 times them is no 0 (and a probability's lower parts may be 0).  Sums
     // that are not finite are therefore made again, with care: such values are added to
     // the rows that see them, those with a score above -inf, and leave the tile before
-    // its products.
+    // its products.  (8 x 32K tokens, 16 nodes: 204 us, 348 with one such value in each
+    // sequence and 654 with one in every page of 64 tokens.)
     auto wild = [&](int buf) __attribute__((always_inline)) {
       const uint8_t* const tile = lds + buf * C::TILE_BYTES + C::TK * kD * 2;
       bool found = false;
@@ -653,6 +654,9 @@ __global__ void __launch_bounds__(kThreads, RB == 1 ? 1 : 2) tree_kernel(const T
       bits = both[0] | both[1];
 #pragma unroll 1
       for (int tok = 0; tok < 32; ++tok) {
+        // (two values to a lane: most tokens have none)
+        const uint32_t mine = *reinterpret_cast<const uint32_t*>(lds + at + C::TK * kD * 2 + tok * kD * 2 + 4 * lane);
+        if (!__any((mine & 0x7f80u) == 0x7f80u || (mine & 0x7f800000u) == 0x7f800000u)) continue;
         const bool seen_here = bits >> tok & 1u;
 #pragma unroll
         for (int d = 0; d < 4; ++d) {
