@@ -672,7 +672,8 @@ def tree_layout(parents: torch.Tensor, context_lens: torch.Tensor, *, mask_words
     ``parents`` int32 [rows]: the parent's number within the sequence, -1 for node
     0.  Returns (mask int64 [rows][mask_words], positions int32 [rows]): bit j % 64
     of word j / 64 is set for the node and its ancestors j; a node's position is
-    its sequence's context plus its depth.  Rows of no sequence are not written.
+    its sequence's context plus its depth.  Rows of no sequence are not written, nor
+    those of sequences of more than 1024 nodes or of context + nodes > 2^31.
     """
     dev, B = parents.get_device(), context_lens.shape[0]
     rows = parents.shape[0]

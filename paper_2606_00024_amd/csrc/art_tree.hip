@@ -21,8 +21,8 @@
 //
 // Up to 64 rows of a sequence share a KV head's keys (eight nodes of eight heads):
 // the memory is the bound, and a tile is loaded into LDS while the one before is in
-// work.  8 x 32K tokens, 32/8 heads, 16 nodes each: 196 us, 5.5 TB/s of 6.1 that a
-// plain read reaches; 32 ragged sequences of 8K to 64K, 64/8 heads, 8 nodes: 752 us,
+// work.  8 x 32K tokens, 32/8 heads, 16 nodes each: 200 us, 5.4 TB/s of 6.1 that a
+// plain read reaches; 32 ragged sequences of 8K to 64K, 64/8 heads, 8 nodes: 759 us,
 // 5.8 TB/s.  From 128 rows on the matrix cores are: 4096 prompt tokens each behind
 // 16K, 32/8 heads, run at 1.05 PFLOP/s, where a large matrix product runs at 1.62.
 // There a wavefront's matrix and vector instructions are interleaved by hand (the
@@ -62,8 +62,8 @@ struct Tree {
   static constexpr int TK = RB == 1 ? 128 : WIDE ? 32 : 64;  // tokens of a tile
   static_assert(TK == 32 * TS);                     // a piece of 32 tokens to a wavefront
   // Places on the line of a unit's set-up and end (16 sequences of up to 2K tokens and
-  // 16 nodes 37 us, without them 51), and of a workgroup, at least (one of 4K tokens, 4
-  // heads to each of 2 KV heads 17 us, with four times as many 21).
+  // 16 nodes 35 us, without them 48), and of a workgroup, at least (one of 4K tokens, 4
+  // heads to each of 2 KV heads 15 us, with four times as many 24).
   static constexpr int LEAD = RB == 1 ? 2 : 4;
   static constexpr int LEAST = RB == 1 ? 1 : 2;
   static constexpr int OWN = TK / kWaves;           // tokens of a tile that a wavefront loads
@@ -985,12 +985,13 @@ art_status plan_tree(const art_decode_shape* s, const art_tree_opts* o, TreePlan
     return ART_ERR_UNSUPPORTED;
   // A row tile that holds a sequence's rows, on average.  32 rows at most: tiles of 128
   // tokens, each wavefront for itself, one workgroup to a CU, read fastest (8 x 32K
-  // tokens, 32/8 heads, one node each: 192 us, 200 by tiles of 64 rows; one of 128K,
-  // one KV head, 30 and 39), but where units are many or all of them short, two
-  // workgroups to a CU end sooner (200 sequences of 50 to 150 tokens 46 us and 58; one of
-  // 4K tokens, 8 KV heads, 21 and 22).  Tiles of 64 rows serve 48 and 64 rows in 203 and
-  // 205 us where 128 rows take 227 and 228, and 96 and 128 rows in 266 and 270 where those
-  // take 232 and 235.
+  // tokens, 32/8 heads, one node each: 190 us, 195 by tiles of 64 rows; one of 128K,
+  // one KV head, 30 and 38), but where units are many or all of them short, two
+  // workgroups to a CU end sooner (200 sequences of 50 to 150 tokens 44 us and 58; one of
+  // 4K tokens, 8 KV heads, 19 and 21).  Tiles of 64 rows serve 48 and 64 rows in 203 and
+  // 201 us where 128 rows take 228 both times, and 96 and 128 rows in 286 and 291 where
+  // those take 231 and 235.  (A table 32 times as wide as
+  // the sequences need slows none of these batches, long or short, by more than 1 %.)
   const int64_t rows = s->batch > 0 ? ((int64_t)o->rows + s->batch - 1) / s->batch * g : 0;
   const int64_t groups = (int64_t)s->batch * s->num_kv_heads;
   const bool few = rows <= 32 && g <= 32 && groups <= kMaxWorkers && groups * ((cap + 127) / 128) >= kMaxWorkers;
@@ -1015,8 +1016,8 @@ template <int RB, int PARTS>
 void launch(const TreePlan& plan, const TreeParams& p, hipStream_t stream) {
   hipLaunchKernelGGL((tree_kernel<RB, PARTS>), dim3((unsigned)plan.workers), dim3(kThreads), 0, stream, p);
   // a row to a workgroup where a unit may have a record in each of many workgroups
-  // (one sequence of 128K tokens, one KV head: 46 us, 102 with eight), else eight (45 of
-  // 400 to 1000 tokens: 44 us, 50 with one)
+  // (one sequence of 128K tokens, one KV head: 30 us, 59 with eight), else eight (45 of
+  // 400 to 1000 tokens: 37 us, 39 with one; 200 of 50 to 150 44 and 50)
   if (plan.workers > 32 * plan.slots)
     hipLaunchKernelGGL((tree_join_kernel<RB, 1>), dim3((unsigned)(plan.slots * rows_of(RB))), dim3(kThreads), 0, stream, p);
   else
